@@ -184,7 +184,7 @@ def _prepare_verify(case, g):
     u = torch.rand(drafts, generator=g, device=DEV)
     e = (-torch.log1p(-torch.rand((n, vocab), generator=g, device=DEV))).clamp(min=1e-30)  # exponential, above 0
     s = {"case": case, "p": p, "q": q, "draft": x.to(torch.int32), "u": u, "e": e, "row_start": _int32(row_start),
-         "seqs": n, "drafts": k}
+         "draft_start": _int32([a - b for b, a in enumerate(row_start)]), "seqs": n, "drafts": k}
     if own:
         from paper_2609_15039_gb300 import spl
         s["workspace"] = spl.workspace(spl.spl_verify_drafts_workspace_bytes(n), DEV)
@@ -204,7 +204,7 @@ def _run_own(s):
         accepted = torch.empty(n, dtype=torch.int32, device=DEV)
         token = torch.empty(n, dtype=torch.int32, device=DEV)
         spl.spl_verify_drafts(accepted, token, s["p"], s["q"], s["draft"], s["u"], s["e"], s["row_start"],
-                              workspace=s["workspace"])
+                              s["draft_start"], workspace=s["workspace"])
         return {"accepted": accepted, "token": token}
     hq, hk, d = s["heads"]
     if kind == "attention":
@@ -306,7 +306,7 @@ def _verify_plain(s):
     count = start[1:] - start[:-1] - 1  # drafts of each sequence
     i = torch.arange(k, device=DEV)
     there = i[None, :] < count[:, None]
-    first = start[:-1] - torch.arange(n, device=DEV)  # first draft of each sequence
+    first = s["draft_start"][:-1].long()  # first draft of each sequence
     at = torch.where(there, first[:, None] + i, torch.zeros_like(there, dtype=torch.long))
     x = s["draft"][at].long()
     target = s["p"][torch.where(there, start[:-1, None] + i, start[:-1, None]), x]
