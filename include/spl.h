@@ -575,10 +575,120 @@ spl_status spl_test_tc_swap_product(float* Y, const float* Xt, const spl_weight*
                                     size_t workspace_bytes, cudaStream_t stream);
 size_t spl_test_tc_swap_workspace_bytes(int64_t M, int64_t K, int64_t N, int tile_tokens, int ctas);
 
+/* ---- serving: a paged KV cache, attention over it, verification of drafts ---
+ * The steps between the Q|K|V product and the O product, and after the LM head,
+ * for configurations that keep them on this device (the paper's "GPU" runs, or
+ * an enclave that spans it; in the split configuration they belong to the
+ * trusted party, Sec. 5.1).  Array contents on the device are not read by the
+ * host: a length, page id or token id outside its range is skipped by the
+ * kernels, never followed, and reported by the next spl_get_device_status as
+ * SPL_EINVAL. */
+
+/* Format of a cache's vectors.
+ *  F16 -- fp16(x), rounded to nearest, values beyond +-65504 saturated.
+ *  I8  -- a scale for each token and head, s = fl32(max|x| / 127), and the codes
+ *         rint(fl32(x / s)) in [-127, 127]; read back as fl32(code s).  A zero
+ *         vector has s = 0; one that holds an infinity or NaN has s = NaN and
+ *         reads back as NaN. */
+typedef enum spl_kv_format { SPL_KV_F16 = 0, SPL_KV_I8 = 1 } spl_kv_format;
+
+/* One layer's cache: `pages` pages of page_size tokens (16, 32, 64, 128 or 256).
+ * k, v [pages, kv_heads, page_size, head_dim] binary16 or int8; k_scale, v_scale
+ * [pages, kv_heads, page_size] fp32 for I8 (not read for F16).  head_dim 64 or
+ * 128, kv_heads up to 1024.  Device pointers owned by the caller, 16-byte
+ * aligned. */
+typedef struct spl_kv_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t pages, kv_heads, page_size, head_dim;
+  spl_kv_format format;
+} spl_kv_cache;
+
+/* A ragged batch of up to 4096 sequences, device arrays (4-byte aligned).  Rows row_start[b] ..
+ * row_start[b + 1] - 1 are the new tokens of sequence b, in order, its last
+ * ones: kv_len[b] counts them, and row i of n stands at position
+ * kv_len[b] - n + i.  Token j of sequence b is in page
+ * page_table[b, j / page_size] at place j % page_size.  max_rows: the most rows
+ * of any sequence, or more (only the choice of kernel goes by it). */
+typedef struct spl_kv_batch {
+  const int32_t* row_start;  /* [seqs + 1] */
+  const int32_t* kv_len;     /* [seqs] */
+  const int32_t* page_table; /* [seqs, max_pages] */
+  int64_t seqs, max_pages, max_rows;
+} spl_kv_batch;
+
+/* Writes the rows' keys and values to the cache: K, V [rows, kv_heads head_dim]
+ * fp32, rows ldk / ldv elements apart (multiples of 4; e.g. columns of the fused
+ * Q|K|V output).  Rows of no sequence, or at negative positions, are skipped.
+ * Errors: EINVAL for NULL or negative arguments, an unknown format or rows
+ * closer than they are wide; ESHAPE for a page size, head_dim, kv_heads or seqs
+ * outside the above; EALIGN. */
+spl_status spl_kv_append(const spl_kv_cache* cache, const spl_kv_batch* batch, const float* K, int64_t ldk,
+                         const float* V, int64_t ldv, int64_t rows, cudaStream_t stream);
+
+/* Reads sequences back: row out_start[b] + j of K and V [out_rows, kv_heads
+ * head_dim] fp32 receives token j of sequence b, for j < kv_len[b] and rows
+ * below out_start[b + 1] (out_start [seqs + 1] on the device, ascending) and
+ * below out_rows; other rows are left as they are.  batch->row_start is not
+ * used (but not NULL).  Errors as spl_kv_append. */
+spl_status spl_kv_read(float* K, float* V, const spl_kv_cache* cache, const spl_kv_batch* batch,
+                       const int32_t* out_start, int64_t out_rows, cudaStream_t stream);
+
+/* Attention of the batch's rows over the cache (which holds their own keys and
+ * values already: append first).  Q, out [rows, q_heads head_dim] fp32, rows
+ * ldq / ldo elements apart (multiples of 4); query head h reads key head
+ * h / (q_heads / kv_heads).  A row at position p sees the keys j <= p of its
+ * sequence and, if window > 0, j > p - window:
+ *   out = sum_j softmax_j(scale q . k_j) v_j,
+ * and zeros if it sees none; rows of no sequence are left as they are.  What a
+ * row does not see (stale slots, later tokens) does not reach it, NaN or not; of
+ * one that sees a NaN or infinity the outputs concerned, or all, are NaN.
+ * fp32 accuracy from the stored values: query rows and probabilities enter the
+ * tensor cores as two binary16 terms (hi + lo, scaled by powers of two), the
+ * softmax is held in fp32.
+ * Workspace: spl_paged_attention_workspace_bytes, zero-filled before its first
+ * use; its first 64 KiB (arrival counters) are zero again after every call that
+ * completes, so the product workspace can be shared.  Errors: as spl_kv_append,
+ * EINVAL for q_heads not a multiple of kv_heads, a scale that is not finite or a
+ * negative window, ESHAPE for q_heads > 1024 kv_heads, EUNSUPPORTED on a device
+ * without tcgen05, EWORKSPACE. */
+size_t spl_paged_attention_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows,
+                                           int64_t q_heads);
+spl_status spl_paged_attention(float* out, int64_t ldo, const float* Q, int64_t ldq, const spl_kv_cache* cache,
+                               const spl_kv_batch* batch, int64_t rows, int64_t q_heads, float scale,
+                               int64_t window, void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* Decides on drafted tokens, from given random numbers.  Sequence b has the
+ * drafts draft[draft_start[b]] .. draft[draft_start[b + 1] - 1], the rows of Q
+ * [drafts, vocab] are the distributions they were sampled from, and P [rows,
+ * vocab] has from row_start[b] on the target's distribution at each draft and
+ * one more, after the last (fewer rows: fewer drafts are looked at).  With u
+ * [drafts] uniform in [0, 1) and e [seqs, vocab] exponential (> 0):
+ *   accepted[b] = the drafts before the first i with not u_i q_i(x_i) < p_i(x_i),
+ *   token[b] = argmax_v w(v) / e[b, v], the lowest v of equal ones,
+ * w = max(p_i - q_i, 0) at that i (or p_i, if that is zero everywhere), or the
+ * row after the last draft if all are accepted.  Each operation is one fp32
+ * rounding.  A draft outside the vocabulary is rejected.  A sequence without
+ * rows gets 0 and -1.  Rows are ldp / ldq / lde elements apart.
+ * Workspace: spl_verify_drafts_workspace_bytes, zero-filled before its first
+ * use, zero again after every call (inside the counters' 64 KiB of a shared
+ * workspace).  Errors: EINVAL for NULL or negative arguments, vocab = 0 or rows
+ * closer than vocab; ESHAPE for seqs > 4096 or sizes beyond int32; EALIGN for
+ * pointers not 4-byte aligned; EWORKSPACE. */
+size_t spl_verify_drafts_workspace_bytes(int64_t seqs);
+spl_status spl_verify_drafts(int32_t* accepted, int32_t* token, const float* P, int64_t ldp, const float* Q,
+                             int64_t ldq, const int32_t* draft, const float* u, const float* e, int64_t lde,
+                             const int32_t* row_start, const int32_t* draft_start, int64_t rows, int64_t drafts,
+                             int64_t seqs, int64_t vocab, void* workspace, size_t workspace_bytes,
+                             cudaStream_t stream);
+
 /* ---- status -------------------------------------------------------------
  * Synchronises `stream`, returns SPL_ETIMEOUT if any kernel since the last
- * call gave up a bounded wait (and clears the flag), else SPL_ECUDA if the
- * stream reports an error, else SPL_OK. */
+ * call gave up a bounded wait (and clears the flag), else SPL_EINVAL if one met
+ * a length, page id or token id outside its range (cleared likewise), else
+ * SPL_ECUDA if the stream reports an error, else SPL_OK. */
 spl_status spl_get_device_status(cudaStream_t stream);
 
 /* Number of kernels this library has launched in this process so far

@@ -48,6 +48,7 @@
 #include "common.cuh"
 #include "fp64.cuh"
 #include "noise.cuh"  // packed fp32 pairs
+#include "paged.cuh"  // device_status_word
 
 namespace spl {
 
@@ -61,6 +62,11 @@ cudaError_t read_clear_device_status(unsigned int* word) {
     e = cudaMemcpyToSymbol(g_device_status, &zero, sizeof(zero));
   }
   return e;
+}
+
+unsigned int* device_status_word() {
+  void* p = nullptr;
+  return cudaGetSymbolAddress(&p, g_device_status) == cudaSuccess ? static_cast<unsigned int*>(p) : nullptr;
 }
 
 namespace {

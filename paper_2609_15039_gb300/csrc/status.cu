@@ -2,7 +2,7 @@
 
 #include <atomic>
 
-#include "common.cuh"
+#include "paged.cuh"
 
 namespace spl {
 
@@ -49,6 +49,7 @@ extern "C" spl_status spl_get_device_status(cudaStream_t stream) {
   unsigned int word = 0;
   if (spl::read_clear_device_status(&word) != cudaSuccess) return SPL_ECUDA;
   if (word & spl::kStatusTimeout) return SPL_ETIMEOUT;
+  if (word & spl::kStatusIndex) return SPL_EINVAL;
   return cudaGetLastError() == cudaSuccess ? SPL_OK : SPL_ECUDA;
 }
 

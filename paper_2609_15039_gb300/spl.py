@@ -22,6 +22,8 @@ SPL_PATH_AUTO, SPL_PATH_TF32X3, SPL_PATH_FP32, SPL_PATH_FP16X3 = 0, 1, 2, 3
 MECHS = {"laplace": SPL_MECH_LAPLACE, "gaussian": SPL_MECH_GAUSSIAN}
 PATHS = {"auto": SPL_PATH_AUTO, "tf32x3": SPL_PATH_TF32X3, "fp32": SPL_PATH_FP32, "fp16x3": SPL_PATH_FP16X3}
 PATH_NAMES = {v: k for k, v in PATHS.items()}
+SPL_KV_F16, SPL_KV_I8 = 0, 1
+KV_FORMATS = {"f16": SPL_KV_F16, "i8": SPL_KV_I8}
 
 
 class SplError(RuntimeError):
@@ -40,8 +42,21 @@ class spl_weight(ctypes.Structure):
                 ("f16_hi", ctypes.c_void_p), ("f16_lo", ctypes.c_void_p), ("f16_exp", ctypes.c_void_p)]
 
 
+class spl_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int64),
+                ("page_size", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("format", ctypes.c_int)]
+
+
+class spl_kv_batch(ctypes.Structure):
+    _fields_ = [("row_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("max_rows", ctypes.c_int64)]
+
+
 _P = ctypes.c_void_p
 _PW = ctypes.POINTER(spl_weight)
+_PC = ctypes.POINTER(spl_kv_cache)
+_PB = ctypes.POINTER(spl_kv_batch)
 _I64 = ctypes.c_int64
 _D = ctypes.c_double
 _I = ctypes.c_int
@@ -97,6 +112,13 @@ _SIGS = {
     "spl_test_tc_shape": (_I, [_I64, _I64, _I64, _I64, ctypes.POINTER(ctypes.c_int64)]),
     "spl_test_tc_product": (_I, [_P, _P, _PW, _P, _I64, _I64, _I64, _I, _I, _I, _I, _I64, _I, _I, _P, _SZ, _P]),
     "spl_test_tc_swap_product": (_I, [_P, _P, _PW, _P, _I64, _I64, _I64, _I, _I, _P, _SZ, _P]),
+    "spl_kv_append": (_I, [_PC, _PB, _P, _I64, _P, _I64, _I64, _P]),
+    "spl_kv_read": (_I, [_P, _P, _PC, _PB, _P, _I64, _P]),
+    "spl_paged_attention_workspace_bytes": (_SZ, [_PC, _PB, _I64, _I64]),
+    "spl_paged_attention": (_I, [_P, _I64, _P, _I64, _PC, _PB, _I64, _I64, ctypes.c_float, _I64, _P, _SZ, _P]),
+    "spl_verify_drafts_workspace_bytes": (_SZ, [_I64]),
+    "spl_verify_drafts": (_I, [_P, _P, _P, _I64, _P, _I64, _P, _P, _P, _I64, _P, _P, _I64, _I64, _I64, _I64, _P, _SZ,
+                               _P]),
     "spl_get_device_status": (_I, [_P]),
     "spl_launch_count": (ctypes.c_uint64, []),
     "spl_status_string": (ctypes.c_char_p, [_I]),
@@ -634,6 +656,142 @@ def spl_choose_path(X, Nz, W, stream=None):
                                  N, _dev(ws, "workspace"), nbytes, _stream(stream)), "spl_choose_path")
     stats = {name: _stats_dict(st[9 * i:9 * (i + 1)]) for i, name in enumerate(("fp32", "tf32x3", "fp16x3"))}
     return PATH_NAMES.get(chosen.value, str(chosen.value)), stats
+
+
+def _scratch(nbytes, device, stream):
+    """A workspace for one call on ``stream``: its memory goes back to that stream."""
+    if stream is None:
+        return workspace(nbytes, device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))):
+        return workspace(nbytes, device)
+
+
+def _rows_view(t, name, width):
+    """(pointer, row stride) of a CUDA fp32 matrix [rows, width] whose rows are contiguous, at any distance."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != torch.float32:
+        raise TypeError(f"{name} must be {torch.float32}")
+    if t.dim() != 2 or (width is not None and t.shape[1] != width) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [rows, {width or 'columns'}] with contiguous rows")
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+class KVCache:
+    """One layer's paged cache (spl_kv_cache): k, v [pages, kv_heads, page_size, head_dim] float16, or int8
+    with k_scale, v_scale [pages, kv_heads, page_size] fp32."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        self.format = {torch.float16: "f16", torch.int8: "i8"}.get(k.dtype)
+        if self.format is None or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("KVCache: k and v are [pages, kv_heads, page_size, head_dim], both float16 or both int8")
+        i8 = self.format == "i8"
+        for t in (k_scale, v_scale):
+            if (t is not None) != i8 or (i8 and t.shape != k.shape[:3]):
+                raise ValueError("KVCache: int8 caches, and no others, have scales [pages, kv_heads, page_size]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self._c = spl_kv_cache(_dev(k, "k", k.dtype), _dev(v, "v", k.dtype), _dev(k_scale, "k_scale"),
+                               _dev(v_scale, "v_scale"), *k.shape, KV_FORMATS[self.format])
+
+    @classmethod
+    def empty(cls, pages, kv_heads, head_dim, page_size=64, format="f16", device="cuda"):
+        """A cache of unwritten pages."""
+        shape = (pages, kv_heads, page_size, head_dim)
+        dtype = torch.int8 if format == "i8" else torch.float16
+        scales = [torch.empty(shape[:3], device=device) for _ in range(2)] if format == "i8" else [None, None]
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device),
+                   *scales)
+
+    def c_struct(self):
+        return self._c
+
+
+class KVBatch:
+    """A ragged batch over a paged cache (spl_kv_batch): int32 CUDA tensors row_start [seqs + 1], kv_len [seqs]
+    and page_table [seqs, max_pages]; ``rows`` new tokens in all, at most ``max_rows`` of a sequence (default:
+    rows).  The tensors' contents may change between calls; the tensors are kept."""
+
+    def __init__(self, row_start, kv_len, page_table, rows, max_rows=None):
+        seqs = kv_len.numel()
+        if row_start.numel() != seqs + 1 or page_table.dim() != 2 or page_table.shape[0] != seqs:
+            raise ValueError("KVBatch: row_start [seqs + 1], kv_len [seqs], page_table [seqs, max_pages]")
+        self.row_start, self.kv_len, self.page_table = row_start, kv_len, page_table
+        self.seqs, self.rows = seqs, int(rows)
+        self._c = spl_kv_batch(_dev(row_start, "row_start", torch.int32), _dev(kv_len, "kv_len", torch.int32),
+                               _dev(page_table, "page_table", torch.int32), seqs, page_table.shape[1],
+                               self.rows if max_rows is None else int(max_rows))
+
+    def c_struct(self):
+        return self._c
+
+
+def spl_kv_append(cache, batch, K, V, stream=None):
+    """Writes the batch's rows K, V [rows, kv_heads head_dim] fp32 (rows at any distance) to the cache."""
+    width = cache.kv_heads * cache.head_dim
+    (kp, ldk), (vp, ldv) = _rows_view(K, "K", width), _rows_view(V, "V", width)
+    if K.shape[0] != batch.rows or V.shape[0] != batch.rows:
+        raise ValueError("spl_kv_append: shape mismatch")
+    _check(lib().spl_kv_append(ctypes.byref(cache.c_struct()), ctypes.byref(batch.c_struct()), kp, ldk, vp, ldv,
+                               batch.rows, _stream(stream)), "spl_kv_append")
+
+
+def spl_kv_read(K, V, cache, batch, out_start, stream=None):
+    """Reads every sequence back: rows out_start[b] + j of K and V [out_rows, kv_heads head_dim] fp32."""
+    width = cache.kv_heads * cache.head_dim
+    if K.dim() != 2 or K.shape[1] != width or V.shape != K.shape or out_start.numel() != batch.seqs + 1:
+        raise ValueError("spl_kv_read: shape mismatch")
+    _check(lib().spl_kv_read(_dev(K, "K"), _dev(V, "V"), ctypes.byref(cache.c_struct()),
+                             ctypes.byref(batch.c_struct()), _dev(out_start, "out_start", torch.int32), K.shape[0],
+                             _stream(stream)), "spl_kv_read")
+
+
+def spl_paged_attention_workspace_bytes(cache, batch, q_heads):
+    return int(lib().spl_paged_attention_workspace_bytes(ctypes.byref(cache.c_struct()),
+                                                         ctypes.byref(batch.c_struct()), batch.rows, int(q_heads)))
+
+
+def spl_paged_attention(out, Q, cache, batch, q_heads, scale=None, window=0, workspace=None, stream=None):
+    """out = attention of the batch's rows Q [rows, q_heads head_dim] fp32 (rows at any distance) over the cache,
+    causal; scale: 1 / sqrt(head_dim) by default; window: the keys a row sees (0: all up to its own)."""
+    width = int(q_heads) * cache.head_dim
+    (op, ldo), (qp, ldq) = _rows_view(out, "out", width), _rows_view(Q, "Q", width)
+    if out.shape[0] != batch.rows or Q.shape[0] != batch.rows:
+        raise ValueError("spl_paged_attention: shape mismatch")
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.head_dim)
+    if workspace is None:
+        workspace = _scratch(spl_paged_attention_workspace_bytes(cache, batch, q_heads), Q.device, stream)
+    wsp, wsb = _ws(workspace)
+    _check(lib().spl_paged_attention(op, ldo, qp, ldq, ctypes.byref(cache.c_struct()),
+                                     ctypes.byref(batch.c_struct()), batch.rows, int(q_heads), float(scale),
+                                     int(window), wsp, wsb, _stream(stream)), "spl_paged_attention")
+
+
+def spl_verify_drafts_workspace_bytes(seqs):
+    return int(lib().spl_verify_drafts_workspace_bytes(int(seqs)))
+
+
+def spl_verify_drafts(accepted, token, P, Q, draft, u, e, row_start, draft_start, workspace=None, stream=None):
+    """Accepted drafts and next token of each sequence (int32 [seqs]): P [rows, vocab] the target's probabilities,
+    Q [drafts, vocab] the draft's, draft [drafts] int32, u [drafts] uniform, e [seqs, vocab] exponential;
+    sequence b's rows start at row_start[b], its drafts at draft_start[b] (int32 [seqs + 1])."""
+    seqs = accepted.numel()
+    (pp, ldp), (qp, ldq), (ep, lde) = (_rows_view(P, "P", None), _rows_view(Q, "Q", P.shape[-1]),
+                                       _rows_view(e, "e", P.shape[-1]))
+    drafts = draft.numel()
+    if (token.numel() != seqs or Q.shape[0] != drafts or u.numel() != drafts or e.shape[0] != seqs
+            or row_start.numel() != seqs + 1 or draft_start.numel() != seqs + 1):
+        raise ValueError("spl_verify_drafts: shape mismatch")
+    if workspace is None:
+        workspace = _scratch(spl_verify_drafts_workspace_bytes(seqs), P.device, stream)
+    wsp, wsb = _ws(workspace)
+    i32 = torch.int32
+    _check(lib().spl_verify_drafts(_dev(accepted, "accepted", i32), _dev(token, "token", i32), pp, ldp, qp, ldq,
+                                   _dev(draft, "draft", i32), _dev(u, "u"), ep, lde,
+                                   _dev(row_start, "row_start", i32), _dev(draft_start, "draft_start", i32),
+                                   P.shape[0], drafts, seqs, P.shape[1], wsp, wsb, _stream(stream)),
+           "spl_verify_drafts")
 
 
 def spl_test_tc_wait_timeout(out, A, W, workspace=None, stream=None):

@@ -1,0 +1,426 @@
+"""The paged cache, attention over it and the verification of drafts, on the GPU against 64 bits."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def spl():
+    from paper_2609_15039_gb300 import spl as binding
+    assert torch.cuda.is_available(), "GPU tests need CUDA"
+    binding.lib()
+    return binding
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+class Case:
+    """A batch of sequences (new rows, length) on shuffled pages, every slot outside the tokens poisoned with NaN."""
+
+    def __init__(self, spl, seqs, heads, fmt, page, seed, std=1.0, spare=2):
+        self.spl, self.seqs, self.fmt, self.page = spl, seqs, fmt, page
+        self.hq, self.hk, self.d = heads
+        g = np.random.default_rng(seed)
+        need = [-(-n // page) for _, n in seqs]
+        pages = sum(need) + spare
+        order = g.permutation(pages)[:sum(need)]
+        self.table = np.full((len(seqs), max(need + [1]) + 1), pages + 7, dtype=np.int32)  # ids past the pool
+        at = 0
+        for b, m in enumerate(need):
+            self.table[b, :m] = order[at:at + m]
+            at += m
+        self.rows = sum(r for r, _ in seqs)
+        self.start = np.concatenate([[0], np.cumsum([r for r, _ in seqs])]).astype(np.int32)
+        self.k = [g.standard_normal((n, self.hk, self.d)).astype(np.float32) * std for _, n in seqs]
+        self.v = [(g.standard_normal((n, self.hk, self.d)) + 0.25).astype(np.float32) for _, n in seqs]
+        self.q = g.standard_normal((self.rows, self.hq, self.d)).astype(np.float32) * std
+        self.cache = spl.KVCache.empty(pages, self.hk, self.d, page, fmt)
+        self.poison()
+
+    def poison(self):
+        if self.fmt == "f16":
+            self.cache.k.fill_(float("nan"))
+            self.cache.v.fill_(float("nan"))
+        else:
+            self.cache.k.fill_(-128)
+            self.cache.v.fill_(127)
+            self.cache.k_scale.fill_(float("nan"))
+            self.cache.v_scale.fill_(float("inf"))
+
+    def batch(self, all_rows=False):
+        """The batch of the new rows, or of every token as a new row."""
+        lens = [n for _, n in self.seqs]
+        start = np.concatenate([[0], np.cumsum(lens)]) if all_rows else self.start
+        rows = sum(lens) if all_rows else self.rows
+        most = max([r for r, _ in self.seqs] + [1])
+        return self.spl.KVBatch(i32(start.tolist()), i32(lens), torch.as_tensor(self.table).to(DEV), rows,
+                                max(lens) if all_rows else most)
+
+    def fill(self):
+        cat = lambda parts: torch.as_tensor(np.concatenate(parts).reshape(-1, self.hk * self.d)).to(DEV)  # noqa: E731
+        self.spl.spl_kv_append(self.cache, self.batch(True), cat(self.k), cat(self.v))
+
+    def stored(self, which, b):
+        """fp32 values that the cache holds of sequence b, from the definition."""
+        x = (self.k if which == "k" else self.v)[b]
+        if self.fmt == "f16":
+            return serving.quantize_f16(x).astype(np.float32)
+        code, scale = serving.quantize_i8(x)
+        return (code.astype(np.float32) * scale[..., None]).astype(np.float32)
+
+    def attend(self, window=0, scale=None, workspace=None, q=None):
+        out = torch.full((self.rows, self.hq * self.d), float("nan"), device=DEV)
+        q = torch.as_tensor(self.q.reshape(self.rows, -1)).to(DEV) if q is None else q
+        self.spl.spl_paged_attention(out, q, self.cache, self.batch(), self.hq, scale=scale, window=window,
+                                     workspace=workspace)
+        torch.cuda.synchronize()
+        return out.cpu().numpy().reshape(self.rows, self.hq, self.d)
+
+    def check(self, window=0, scale=None, **kw):
+        got = self.attend(window, scale, **kw)
+        s = 1.0 / np.sqrt(self.d) if scale is None else scale
+        num = den = 0.0
+        for b, (r, n) in enumerate(self.seqs):
+            k, v = self.stored("k", b), self.stored("v", b)
+            q = self.q[self.start[b]:self.start[b + 1]]
+            ref, mass = serving.attention(q, k, v, n, self.hq // self.hk, s, window)
+            mine = got[self.start[b]:self.start[b + 1]]
+            tol = tolerance(q, k, s, n, self.hq // self.hk, mass)
+            err = np.abs(mine.astype(np.float64) - ref)
+            assert not np.isnan(mine).any(), f"sequence {b}: NaN"
+            assert np.all(err <= tol), f"sequence {b} {r, n}: worst err/tol {np.max(err / np.maximum(tol, 1e-300)):.3g}"
+            num += float(np.sum((mine - ref) ** 2))
+            den += float(np.sum(ref ** 2))
+        assert num <= (1e-5 ** 2) * den, f"relative error {np.sqrt(num / max(den, 1e-300)):.3g}"
+        assert self.spl.spl_get_device_status() == self.spl.SPL_OK
+        return got
+
+
+def tolerance(q, k, scale, n, group, mass):
+    """Elementwise bound.  A score is a sum of `dim` terms of which q's split loses 2^-22 and each of the dim / 16
+    accumulations (twice, for the two halves) at most 2^-23 of the sum of sizes S: its error is at most
+    (2^-22 + (dim / 8) 2^-23) S, and a few ulp from the scaling.  That, an exp of 2^-21, a probability's split of 2^-22
+    and the accumulation of the n / 16 key steps (2^-23 each, twice) are relative to sum_j p_j |v_j|; the total has
+    the same, and three roundings follow."""
+    if n == 0 or q.shape[0] == 0:
+        return np.zeros_like(mass)
+    dim = q.shape[-1]
+    size = abs(scale) * np.max(np.einsum("ihd,jhd->ihj", np.abs(q).astype(np.float64),
+                                         np.repeat(np.abs(k).astype(np.float64), group, axis=1)), axis=2)
+    score = (2.0 ** -22 + dim / 8 * 2.0 ** -23 + 4 * U) * size
+    rel = 2 * (score + 2.0 ** -21) + 2.0 ** -22 + (n / 8 + 16) * 2.0 ** -23 + 4 * U
+    return rel[..., None] * mass + 1e-30
+
+
+HEADS = [(24, 8, 128), (8, 2, 64), (3, 3, 128), (7, 1, 64), (16, 1, 128)]
+BATCHES = {
+    "one": [(1, 1)], "two": [(1, 2)], "page": [(1, 64)], "past_page": [(1, 65)], "odd": [(1, 299)],
+    "ragged": [(1, 5), (1, 1000), (0, 17), (1, 128), (0, 0), (1, 1)],
+    "drafts": [(5, 261), (3, 3), (1, 700), (4, 64)],
+    "chunks": [(37, 37), (130, 333), (1, 90), (64, 64)],
+}
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("heads", HEADS, ids=str)
+@pytest.mark.parametrize("name", BATCHES)
+def test_attention(spl, name, heads, fmt):
+    c = Case(spl, BATCHES[name], heads, fmt, 16 if name == "ragged" else 64, seed=len(name))
+    c.fill()
+    c.check()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_attention_page_sizes(spl, page, fmt):
+    c = Case(spl, [(3, 300), (20, 257), (1, page), (150, 150 + page)], (6, 2, 128), fmt, page, seed=page)
+    c.fill()
+    c.check()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("window", [1, 2, 63, 64, 129, 1000])
+def test_attention_window(spl, window, fmt):
+    c = Case(spl, [(1, 500), (9, 300), (140, 400), (70, 70)], (4, 2, 64), fmt, 32, seed=window)
+    c.fill()
+    c.check(window=window)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+def test_rows_without_keys_are_zero(spl, fmt):
+    """A sequence shorter than its rows: the first stand before position 0 and see nothing."""
+    c = Case(spl, [(6, 2), (1, 0), (140, 3)], (4, 2, 128), fmt, 16, seed=3)
+    c.fill()  # writes the tokens that exist
+    got = c.check()
+    assert np.all(got[:4] == 0) and np.all(got[6] == 0) and np.all(got[7:7 + 137] == 0)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attention_sharp_and_flat(spl, rows, fmt):
+    """Scores that single out one key, and scores that are all equal; other scales, a negative one among them."""
+    for std, scale in ((6.0, None), (1.0, 0.0), (1.0, -0.3), (2.0, 1.0)):
+        c = Case(spl, [(rows, 777)], (4, 1, 64), fmt, 64, seed=rows, std=std)
+        c.fill()
+        c.check(scale=scale)
+
+
+@pytest.mark.parametrize("rows", [2, 5, 48, 200])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_nan_reaches_only_rows_that_see_it(spl, which, rows):
+    """A NaN in a later token of the chunk: earlier rows are as without it, later ones are NaN."""
+    for fmt in ("f16", "i8"):
+        c = Case(spl, [(rows, 100 + rows)], (4, 2, 64), fmt, 16, seed=rows)
+        c.fill()
+        clean = c.check()
+        at = rows // 2
+        x = getattr(c, which)[0]
+        x[100 + at, 1, 3] = np.nan
+        c.fill()
+        got = c.attend()
+        assert np.array_equal(got[:at], clean[:at])
+        assert np.array_equal(got[:, :2], clean[:, :2])  # the other key head's rows
+        assert np.isnan(got[at:, 2:]).any(axis=2).all()
+
+
+def test_attention_reads_and_writes_strided_rows(spl):
+    c = Case(spl, [(3, 50), (60, 61)], (6, 2, 64), "f16", 16, seed=8)
+    c.fill()
+    want = c.check()
+    wide = torch.full((c.rows, 1000), 7.0, device=DEV)
+    wide[:, 8:8 + 384] = torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV)
+    out = torch.full((c.rows, 516), 5.0, device=DEV)
+    spl.spl_paged_attention(out[:, 64:448], wide[:, 8:392], c.cache, c.batch(), 6)
+    assert np.array_equal(out[:, 64:448].cpu().numpy().reshape(want.shape), want)
+    assert bool((out[:, :64] == 5).all()) and bool((out[:, 448:] == 5).all())
+
+
+@pytest.mark.parametrize("rows", [1, 60])
+def test_attention_is_deterministic_and_leaves_the_workspace_clean(spl, rows):
+    """Same bits again on one workspace, shared with other shapes; the arrival counters end at zero."""
+    a = Case(spl, [(rows, 3000), (rows, 100)], (8, 2, 128), "f16", 64, seed=1)
+    b = Case(spl, [(1, 40)], (4, 4, 64), "i8", 16, seed=2)
+    for c in (a, b):
+        c.fill()
+    ws = spl.workspace(max(spl.spl_paged_attention_workspace_bytes(c.cache, c.batch(), c.hq) for c in (a, b)))
+    first = a.attend(workspace=ws)
+    for _ in range(3):
+        b.check(workspace=ws)
+        assert np.array_equal(a.attend(workspace=ws), first)
+    assert int(ws[:65536].count_nonzero()) == 0
+
+
+def test_attention_in_a_graph_follows_the_lengths(spl):
+    """A captured decode step is replayed as its sequences grow: lengths and tables are read on the device."""
+    c = Case(spl, [(1, 90), (1, 31)], (4, 2, 64), "f16", 16, seed=5)
+    c.fill()
+    batch = c.batch()
+    q = torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV)
+    out = torch.zeros((c.rows, 4 * 64), device=DEV)
+    ws = spl.workspace(spl.spl_paged_attention_workspace_bytes(c.cache, batch, 4))
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        spl.spl_paged_attention(out, q, c.cache, batch, 4, workspace=ws)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        spl.spl_paged_attention(out, q, c.cache, batch, 4, workspace=ws)
+    for lens in ([90, 31], [40, 1], [90, 0]):
+        batch.kv_len.copy_(i32(lens))
+        graph.replay()
+        torch.cuda.synchronize()
+        for b, n in enumerate(lens):
+            ref, _ = serving.attention(c.q[b:b + 1], c.stored("k", b)[:n], c.stored("v", b)[:n], n, 2, 0.125)
+            assert np.allclose(out[b].cpu().numpy().reshape(4, 64), ref[0], rtol=0, atol=1e-5)
+
+
+def test_ids_outside_the_pool_are_reported_and_not_followed(spl):
+    for rows in (1, 40):
+        c = Case(spl, [(rows, 200), (rows, 64)], (4, 2, 64), "f16", 16, seed=4)
+        c.fill()
+        good = c.check()
+        keep = c.table.copy()
+        c.table[0, 3] = -5
+        c.table[0, 6] = 1 << 30
+        bad = c.attend()
+        assert spl.spl_get_device_status() == spl.SPL_EINVAL
+        assert spl.spl_get_device_status() == spl.SPL_OK
+        assert np.array_equal(bad[rows:], good[rows:]) and np.isfinite(bad).all()
+        c.table = keep
+        batch = c.batch()
+        batch.kv_len.copy_(i32([1 << 30, 64]))  # past the table: its tokens end where the table does
+        x = torch.zeros((c.rows, 2 * 64), device=DEV)
+        spl.spl_kv_append(c.cache, batch, x, x)
+        assert spl.spl_get_device_status() == spl.SPL_EINVAL
+
+
+# ---------------------------------------------------------------------------------- the cache itself
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("heads", [(8, 8, 128), (2, 2, 64), (1, 1, 128), (9, 9, 64), (20, 20, 128)], ids=str)
+def test_append_and_read_back_exactly(spl, heads, fmt):
+    c = Case(spl, [(1, 1), (0, 40), (17, 200), (64, 64), (0, 0), (1, 33)], heads, fmt, 16, seed=11)
+    for x in c.k + c.v:
+        if x.size:
+            x[0, 0] = 0.0  # a zero vector
+            x[-1, -1] *= 1e30 if fmt == "i8" else 1e6
+    c.fill()
+    lens = [n for _, n in c.seqs]
+    start = np.concatenate([[0], np.cumsum(lens)])
+    width = c.hk * c.d
+    K = torch.full((int(start[-1]) + 3, width), 3.0, device=DEV)
+    V = torch.full_like(K, 3.0)
+    spl.spl_kv_read(K, V, c.cache, c.batch(), i32(start.tolist()))
+    for got, which in ((K, "k"), (V, "v")):
+        want = np.concatenate([c.stored(which, b) for b in range(len(lens))]).reshape(-1, width)
+        assert np.array_equal(got[:-3].cpu().numpy(), want)
+        assert bool((got[-3:] == 3.0).all())  # rows of no token
+    assert spl.spl_get_device_status() == spl.SPL_OK
+    # untouched: the pages of no sequence
+    used = set(int(p) for b, n in enumerate(lens) for p in c.table[b, :-(-n // 16)])
+    free = [p for p in range(c.cache.pages) if p not in used]
+    x = c.cache.k[free].float()
+    assert bool((x.isnan() if fmt == "f16" else x == -128).all())
+
+
+def test_append_writes_only_the_new_rows(spl):
+    c = Case(spl, [(2, 50), (1, 7)], (2, 2, 64), "i8", 16, seed=12)
+    rows = torch.randn((c.rows, 300), device=DEV)
+    spl.spl_kv_append(c.cache, c.batch(), rows[:, 4:132], rows[:, 136:264])
+    code, scale = serving.quantize_i8(rows[:, 4:132].cpu().numpy().reshape(-1, 2, 64))
+    want = np.full(tuple(c.cache.k.shape), -128, dtype=np.int8)
+    for r, (b, pos) in enumerate([(0, 48), (0, 49), (1, 6)]):
+        want[c.table[b, pos // 16], :, pos % 16] = code[r]
+    assert np.array_equal(c.cache.k.cpu().numpy(), want)
+    assert int(c.cache.k_scale.isfinite().sum()) == 3 * 2
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_special_values_in_the_cache(spl, bad):
+    for fmt in ("f16", "i8"):
+        c = Case(spl, [(1, 3)], (2, 2, 64), fmt, 16, seed=13)
+        c.k[0][1, 1, 5] = bad
+        c.fill()
+        K, V = torch.zeros((3, 128), device=DEV), torch.zeros((3, 128), device=DEV)
+        spl.spl_kv_read(K, V, c.cache, c.batch(), i32([0, 3]))
+        got = K.cpu().numpy().reshape(3, 2, 64)
+        want = c.stored("k", 0)
+        assert np.array_equal(got, want, equal_nan=True)
+        if fmt == "i8":
+            assert np.isnan(got[1, 1]).all()
+        else:
+            assert np.isnan(got[1, 1, 5]) if np.isnan(bad) else got[1, 1, 5] == np.sign(bad) * 65504
+
+
+# ---------------------------------------------------------------------------------- drafts
+def draws(seed, counts, vocab, sharp=2.5):
+    g = np.random.default_rng(seed)
+    soft = lambda z: (np.exp(z) / np.exp(z).sum(-1, keepdims=True)).astype(np.float32)  # noqa: E731
+    rows, drafts = sum(k + 1 for k in counts), sum(counts)
+    p = soft(g.standard_normal((rows, vocab)) * sharp)
+    q = soft(g.standard_normal((max(drafts, 1), vocab)) * sharp)[:drafts]
+    x = np.array([g.choice(vocab, p=r.astype(np.float64) / r.sum(dtype=np.float64)) for r in q], dtype=np.int32)
+    return p, q, x, g.random(drafts, dtype=np.float32), g.exponential(size=(len(counts), vocab)).astype(np.float32)
+
+
+def run_verify(spl, p, q, x, u, e, counts, pad=0):
+    dev = lambda t: torch.as_tensor(np.ascontiguousarray(t)).to(DEV)  # noqa: E731
+
+    def rows(t):
+        wide = torch.full((t.shape[0], t.shape[1] + pad), 9.0, device=DEV)
+        wide[:, :t.shape[1]] = dev(t)
+        return wide[:, :t.shape[1]]
+
+    n = len(counts)
+    accepted, token = torch.full((n,), -9, dtype=torch.int32, device=DEV), i32([-9] * n)
+    start = np.concatenate([[0], np.cumsum([k + 1 for k in counts])])
+    dstart = np.concatenate([[0], np.cumsum(counts)])
+    ws = spl.workspace(spl.spl_verify_drafts_workspace_bytes(n))
+    for _ in range(2):
+        spl.spl_verify_drafts(accepted, token, rows(p), rows(q), dev(x), dev(u), rows(e), i32(start.tolist()),
+                              i32(dstart.tolist()), workspace=ws)
+    assert int(ws.count_nonzero()) == 0
+    return accepted.cpu().tolist(), token.cpu().tolist()
+
+
+def expected(p, q, x, u, e, counts):
+    out, r, d = [], 0, 0
+    for b, k in enumerate(counts):
+        out.append(serving.verify(p[r:r + k + 1], q[d:d + k], x[d:d + k], u[d:d + k], e[b]))
+        r, d = r + k + 1, d + k
+    return [a for a, _ in out], [t for _, t in out]
+
+
+@pytest.mark.parametrize("vocab,pad", [(1, 0), (5, 3), (1000, 0), (1001, 0), (4099, 5), (32768, 4)])
+@pytest.mark.parametrize("counts", [[0], [1], [3, 0, 8, 1], [40, 2]], ids=str)
+def test_verify(spl, counts, vocab, pad):
+    args = draws(vocab + len(counts), counts, vocab)
+    if vocab == 1000:  # a target that the drafts follow: whole runs are accepted
+        p, q, x, u, e = args
+        r = d = 0
+        for k in counts:
+            q[d:d + k] = p[r:r + k]
+            r, d = r + k + 1, d + k
+        q = q.copy()
+        x = np.array([int(np.argmax(row)) for row in q], dtype=np.int32)
+        args = (p, q, x, u, e)
+    assert run_verify(spl, *args, counts, pad) == expected(*args, counts)
+
+
+def test_verify_edges(spl):
+    vocab, counts = 64, [2, 2, 2, 2]
+    p, q, x, u, e = draws(7, counts, vocab)
+    q[0], x[0], u[0] = p[0], 5, 1.0 - 2.0 ** -24  # equal rows and u just below 1: accepted
+    q[1], x[1], u[1] = p[1], 6, 0.5
+    p[3, 9], x[2] = 0.0, 9                         # p = 0 at the draft: rejected
+    q[4], u[4], x[4] = p[6] * 3, 0.999, 11         # p nowhere above q: the draw is from p
+    p[9] = 0.25
+    e[3] = 1.0
+    x[6], q[6], u[6] = 1, p[9], 0.0                # then a draft outside the vocabulary
+    x[7] = vocab
+    p[10] = 0.0
+    p[10, 40:50] = 0.1                             # ties: the lowest index
+    q[7] = 0.0
+    got = run_verify(spl, p, q, x, u, e, counts)
+    assert got == expected(p, q, x, u, e, counts)
+    assert got[0][0] == 2 and got[0][1] == 0 and got[0][2] == 0 and got[0][3] == 1
+    assert got[1][3] == 40
+    assert spl.spl_get_device_status() == spl.SPL_EINVAL  # the draft outside the vocabulary
+
+
+def test_verify_sequences_without_rows(spl):
+    p, q, x, u, e = draws(3, [2], 100)
+    dev = lambda t: torch.as_tensor(t).to(DEV)  # noqa: E731
+    accepted, token = i32([-9, -9, -9]), i32([-9, -9, -9])
+    e3 = np.repeat(e, 3, axis=0)
+    spl.spl_verify_drafts(accepted, token, dev(p), dev(q), dev(x), dev(u), dev(e3), i32([0, 0, 3, 3]),
+                          i32([0, 0, 2, 2]))
+    n, t = serving.verify(p, q, x, u, e[0])
+    assert accepted.cpu().tolist() == [0, n, 0] and token.cpu().tolist() == [-1, t, -1]
+
+
+def test_verify_draws_follow_the_target(spl):
+    """The token after no drafts is a draw from p: frequencies of 4096 races within 5 standard deviations."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    n, vocab = 4096, 8
+    p = torch.softmax(torch.arange(vocab, device=DEV) * 0.4, 0)[None].repeat(n, 1).contiguous()
+    e = -torch.log1p(-torch.rand((n, vocab), generator=g, device=DEV)).clamp(max=-1e-30)
+    e = e.clamp(min=1e-30)
+    accepted, token = torch.empty(n, dtype=torch.int32, device=DEV), torch.empty(n, dtype=torch.int32, device=DEV)
+    start = torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    zero = torch.zeros(n + 1, dtype=torch.int32, device=DEV)
+    empty = torch.empty((0, vocab), device=DEV)
+    spl.spl_verify_drafts(accepted, token, p, empty, torch.empty(0, dtype=torch.int32, device=DEV),
+                          torch.empty(0, device=DEV), e, start, zero)
+    freq = torch.bincount(token.long(), minlength=vocab).double().cpu() / n
+    want = p[0].double().cpu()
+    assert bool((freq - want).abs().le(5 * (want * (1 - want) / n).sqrt()).all())
