@@ -646,14 +646,14 @@ spl_status spl_kv_read(float* K, float* V, const spl_kv_cache* cache, const spl_
  * row does not see (stale slots, later tokens) does not reach it, NaN or not; of
  * one that sees a NaN or infinity the outputs concerned, or all, are NaN.
  * fp32 accuracy from the stored values: query rows and probabilities enter the
- * tensor cores as two binary16 terms (hi + lo, scaled by powers of two), the
+ * tensor cores as two binary16 terms (hi + lo, scaled by powers of two; a
+ * probability far below its row's largest keeps an absolute 2^-38 of it), the
  * softmax is held in fp32.
  * Workspace: spl_paged_attention_workspace_bytes, zero-filled before its first
  * use; its first 64 KiB (arrival counters) are zero again after every call that
  * completes, so the product workspace can be shared.  Errors: as spl_kv_append,
  * EINVAL for q_heads not a multiple of kv_heads, a scale that is not finite or a
- * negative window, ESHAPE for q_heads > 1024 kv_heads, EUNSUPPORTED on a device
- * without tcgen05, EWORKSPACE. */
+ * negative window, ESHAPE for q_heads > 1024 kv_heads, EWORKSPACE. */
 size_t spl_paged_attention_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows,
                                            int64_t q_heads);
 spl_status spl_paged_attention(float* out, int64_t ldo, const float* Q, int64_t ldq, const spl_kv_cache* cache,

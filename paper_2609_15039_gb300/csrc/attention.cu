@@ -450,8 +450,9 @@ spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, int bloc
 namespace {
 
 struct Shape {
+  bool few;
   int blocks;
-  size_t slot_bytes;  // of a block
+  size_t bytes;  // of the workspace
 };
 
 spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows, int64_t q_heads, PagedCache* c,
@@ -463,11 +464,25 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
   return paged_batch_view(b, batch, rows);
 }
 
-Shape shape_of(const spl_kv_cache* cache) {
-  const int d = (int)cache->head_dim;
+// The few-row kernel where every sequence's rows of a key head fit its tile, or where the units (64 keys of a tile) that
+// the batch can have, by its longest chunk and its page table, are few: the tensor-core kernel costs 15 us more at the
+// start and a tenth as much per unit.  Measured with 24 query heads on 8 (few rows, tensor cores): 16 rows over 2048 keys
+// 24, 27 us, over 8192 50, 39; 64 rows over 512 25, 35, over 2048 47, 42; 16 sequences of 8 rows over 128 22, 32, over
+// 512 41, 40.
+constexpr int64_t kFewUnits = 3000;
+Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_heads) {
+  const int d = (int)cache->head_dim, sms = device_sm_count();
   Shape s;
-  s.blocks = attention_rows_blocks(d, cache->format == SPL_KV_I8, device_sm_count());
-  s.slot_bytes = (size_t)2 * kRowsTile * (d + kSlotStats) * sizeof(float);
+  const int64_t tiles = ceil_div(std::max<int64_t>(batch->max_rows, 1) * (q_heads / cache->kv_heads), kRowsTile);
+  const int64_t units = ceil_div(batch->max_pages * cache->page_size, kUnit);
+  s.few = tiles == 1 || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;
+  if (s.few) {
+    s.blocks = attention_rows_blocks(d, cache->format == SPL_KV_I8, sms);
+    s.bytes = kCounterBytes + (size_t)s.blocks * 2 * kRowsTile * (d + kSlotStats) * sizeof(float);
+  } else {
+    s.blocks = sms;
+    s.bytes = kCounterBytes + attention_tc_bytes(d, sms);
+  }
   return s;
 }
 
@@ -481,8 +496,7 @@ extern "C" size_t spl_paged_attention_workspace_bytes(const spl_kv_cache* cache,
   PagedCache c;
   PagedBatch b;
   if (check(cache, batch, rows, q_heads, &c, &b) != SPL_OK || rows == 0 || b.seqs == 0) return 0;
-  const Shape s = shape_of(cache);
-  return kCounterBytes + s.blocks * s.slot_bytes;
+  return shape_of(cache, batch, q_heads).bytes;
 }
 
 extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* Q, int64_t ldq,
@@ -498,8 +512,8 @@ extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* 
   if (!out || !Q) return SPL_EINVAL;
   if (rows > 1 && (ldo < width || ldq < width)) return SPL_EINVAL;
   if (!aligned16(out) || !aligned16(Q) || (rows > 1 && (ldo % 4 != 0 || ldq % 4 != 0))) return SPL_EALIGN;
-  const Shape s = shape_of(cache);
-  if (!workspace || workspace_bytes < kCounterBytes + s.blocks * s.slot_bytes) return SPL_EWORKSPACE;
+  const Shape s = shape_of(cache, batch, q_heads);
+  if (!workspace || workspace_bytes < s.bytes) return SPL_EWORKSPACE;
   if (!aligned16(workspace)) return SPL_EALIGN;
   if (!(a.batch.status = device_status_word())) return SPL_ECUDA;
   a.out = out;
@@ -512,5 +526,7 @@ extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* 
   a.counters = static_cast<unsigned int*>(workspace);
   a.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
   a.min_units = 2;
-  return run_attention_rows(a, (int)cache->head_dim, cache->format == SPL_KV_I8, s.blocks, stream);
+  const int d = (int)cache->head_dim;
+  const bool i8 = cache->format == SPL_KV_I8;
+  return s.few ? run_attention_rows(a, d, i8, s.blocks, stream) : run_attention_tc(a, d, i8, s.blocks, stream);
 }

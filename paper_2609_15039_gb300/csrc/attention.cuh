@@ -204,7 +204,9 @@ __device__ __forceinline__ uint32_t i8_pair(uint32_t bytes, uint32_t select) {
 
 constexpr int kSlotStats = 2;  // per row: maximum (in units of log2) and total
 
-// Entry side (attention.cu).
+// The two kernels' launches and the workspace behind the counters.
+spl_status run_attention_tc(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
+size_t attention_tc_bytes(int head_dim, int blocks);
 spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
 int attention_rows_blocks(int head_dim, bool i8, int sms);
 constexpr int kRowsTile = 8;

@@ -164,7 +164,7 @@ spl_status paged_cache_view(PagedCache* out, const spl_kv_cache* c) {
 }
 
 spl_status paged_batch_view(PagedBatch* out, const spl_kv_batch* b, int64_t rows) {
-  if (!b || b->seqs < 0 || b->max_pages < 0 || rows < 0) return SPL_EINVAL;
+  if (!b || b->seqs < 0 || b->max_pages < 0 || b->max_rows < 0 || rows < 0) return SPL_EINVAL;
   if (b->seqs > kMaxSeqs || rows > INT32_MAX || b->max_pages > (int64_t(1) << 26)) return SPL_ESHAPE;
   if (b->seqs > 0 && (!b->row_start || !b->kv_len || (b->max_pages > 0 && !b->page_table))) return SPL_EINVAL;
   if (!aligned4(b->row_start) || !aligned4(b->kv_len) || !aligned4(b->page_table)) return SPL_EALIGN;
