@@ -4,46 +4,46 @@
 // For few rows the pass is bound by reading the cache once.  A tile has 8 rows (for one new token, the query heads of
 // a key head); its products run on mma.m16n8k16 with the 8 rows' high and low halves as the 16 rows of A, so that one
 // instruction makes both terms of q = hi + lo, or of p = hi + lo, for which the stored binary16 (or int8) values are
-// exact: fp32 accuracy at no further cost.  Keys and values go from global memory to the B fragments' registers
-// directly, 16 bytes a lane, without shared memory: the order of the dimensions in a product is free, so a lane takes
-// neighbouring ones (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys are byte permutes).
-// A warp takes 16 keys at a time, of one page, and holds the values' loads in flight while it makes the scores, the
-// next keys' while it makes the sums.
+// exact: fp32 accuracy at no further cost.
+// A block has an SM.  One warp copies units of 128 or 256 keys (some 64 KB of keys and values) into a ring by bulk copies
+// of whole runs of a page, so that some 190 KB are on their way on an SM, across the ends of tiles and sequences; 8 warps
+// make the sums, each of its 16 or 32 keys of a unit.  The order of the dimensions in a product is free, so a lane reads
+// 16 neighbouring bytes for its B fragments (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys
+// are byte permutes).
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 
 #include <cuda_fp16.h>
 
 #include "attention.cuh"
+#include "ptx.cuh"
 
 namespace spl {
 namespace {
 
-constexpr int kThreads = 128, kWarps = 4;
-constexpr int kRT = kRowsTile, kUnit = 64;
+constexpr int kWarps = 8, kThreads = 32 * (kWarps + 4);  // and a warpgroup of which one warp copies
+constexpr int kRT = kRowsTile;
 // p is held as 2^kShift p, at most 2^13, so that its low half keeps an absolute 2^-38 of the largest.
 constexpr float kShift = 13.0f;
 constexpr int kMinExp = -100, kMaxExp = 126;  // of the values' scales
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint4 ldg_stream(const void* p) {
-  uint4 r;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
-               : "l"(p));
-  return r;
+// size bytes (a multiple of 16, both addresses too) from global to shared memory, counted on the barrier; read once.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t size, uint32_t bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
+          dst),
+      "l"(src), "r"(size), "r"(bar), "l"(policy)
+      : "memory");
 }
-__device__ __forceinline__ uint2 ldg_stream8(const void* p) {
-  uint2 r;
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
-  return r;
+template <class T>
+__device__ __forceinline__ T lds(const uint8_t* p) {
+  return *reinterpret_cast<const T*>(p);
 }
 // Whether a pair of binary16 holds an infinity or NaN.
 __device__ __forceinline__ bool f16_special(uint32_t h) {
@@ -65,21 +65,116 @@ struct Frag {
     constexpr int per = E / 4;  // steps a chunk
     return (s / per) * 4 * E + t * E + 4 * (s % per);
   }
+  // A ring stage, of BLOCKS blocks of 16 keys a warp: keys, values, and the scales of both.
+  static constexpr int ESZ = I8 ? 1 : 2, BLOCKS = D * ESZ == 256 ? 1 : 2, UNIT = 16 * kWarps * BLOCKS;
+  static constexpr uint32_t K = 0, V = UNIT * D * ESZ, KS = 2 * V, VS = KS + (I8 ? UNIT * 4 : 0);
+  static constexpr uint32_t STAGE = VS + (I8 ? UNIT * 4 : 0);
+  static constexpr int STAGES = 3 * 65536 / (2 * V) < 4 ? 3 * 65536 / (2 * V) : 4;
+  static constexpr uint32_t RING = STAGES * STAGE;
+  // shared memory: the ring (the prefix sums before it), sums of four warps, maxima and totals, barriers (full, empty) and
+  // the mask of a stage's blocks that hold keys
+  static constexpr uint32_t SO = RING, SM = SO + 4 * kRT * D * 4, SL = SM + kWarps * kRT * 4;
+  static constexpr uint32_t BARS = SL + kWarps * kRT * 4, MASK = BARS + 16 * STAGES, LAST = MASK + 4 * STAGES;
+  static constexpr uint32_t SMEM = LAST + 8;
+  static_assert(SMEM <= 232448 && kMaxSeqs * 8 <= RING, "fits");
   // dim of column n of n-block nb
   static __device__ __forceinline__ int v_dim(int nb, int n) { return (nb / VE) * 8 * VE + n * VE + nb % VE; }
 };
 
+// The copying warp: unit after unit of the block's run into the ring's stages in turn.
 template <int D, bool I8>
-__global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_kernel(const AttnArgs a) {
+__device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8_t* smem) {
   using F = Frag<D, I8>;
-  constexpr int ESZ = I8 ? 1 : 2;
+  constexpr int BLOCKS = F::UNIT / 16;
+  const PagedCache& cache = run.a.cache;
+  const int lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(smem), bars = base + F::BARS;
+  const uint64_t policy = l2_evict_first();
+  const int per_page = min(BLOCKS, 1 << (cache.page_shift - 4));  // blocks of a unit that lie side by side
+  volatile int* abort = reinterpret_cast<volatile int*>(smem + F::LAST + 4);
+  int it = 0;
+  bool ok = true;
+  for (; ok && run.busy(); run.next()) {
+    const AttnTile& x = run.x;
+    const int last = run.last();
+    int64_t slot = -1;  // of the first key of the lane's block of 16, -1 where no row sees any
+    auto look_up = [&](int u) {
+      const int j = (x.unit0 + u) * F::UNIT + 16 * lane;
+      slot = -1;
+      if (lane < BLOCKS && u < last && j < x.key_hi && j + 16 > x.key_lo) {
+        const int page = paged_page(cache, run.a.batch, x.b, j);
+        if (page >= 0) slot = paged_slot(cache, page, x.h, j);
+      }
+    };
+    look_up(run.first);
+    for (int u = run.first; u < last; ++u, ++it) {
+      const int stage = it % F::STAGES;
+      const uint32_t at = base + stage * F::STAGE, full = bars + 8u * stage;
+      if (it >= F::STAGES) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (F::STAGES + stage), (uint32_t)(it / F::STAGES - 1) & 1u,
+                                               kWaitNs, abort));
+        if (!ok) break;
+      }
+      const uint32_t mask = __ballot_sync(0xffffffffu, slot >= 0);
+      // The first block of a run of them in a page copies the run.
+      const uint32_t page_mask = ((1u << per_page) - 1u) << (lane / per_page * per_page) & mask;
+      const bool leads = slot >= 0 && (page_mask & ((1u << lane) - 1u)) == 0;
+      const uint32_t keys = 16u * __popc(page_mask);
+      if (lane == 0) {
+        *reinterpret_cast<volatile uint32_t*>(smem + F::MASK + 4 * stage) = mask;
+        mbar_expect_tx(full, 16u * __popc(mask) * (2u * D * F::ESZ + (I8 ? 8u : 0u)));
+      }
+      __syncwarp();
+      if (leads) {
+        const uint32_t key0 = 16u * lane;
+        bulk_load(at + F::K + key0 * D * F::ESZ, static_cast<const char*>(cache.k) + slot * (D * F::ESZ),
+                  keys * D * F::ESZ, full, policy);
+        bulk_load(at + F::V + key0 * D * F::ESZ, static_cast<const char*>(cache.v) + slot * (D * F::ESZ),
+                  keys * D * F::ESZ, full, policy);
+        if constexpr (I8) {
+          bulk_load(at + F::KS + key0 * 4u, cache.k_scale + slot, keys * 4u, full, policy);
+          bulk_load(at + F::VS + key0 * 4u, cache.v_scale + slot, keys * 4u, full, policy);
+        }
+      }
+      look_up(u + 1);
+    }
+  }
+  if (!ok) {  // given up: what is on its way lands before the block leaves
+    *abort = 1;
+    if (lane == 0) atomicOr(run.a.batch.status, kStatusTimeout);
+    for (int t = max(0, it - F::STAGES); t < it; ++t)
+      mbar_wait(bars + 8u * (t % F::STAGES), (uint32_t)(t / F::STAGES) & 1u, kDrainNs, nullptr);
+  }
+}
+
+template <int D, bool I8>
+__global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __grid_constant__ AttnArgs a) {
+  using F = Frag<D, I8>;
+  constexpr int ESZ = F::ESZ, BLOCKS = F::BLOCKS;
   constexpr int SLOT = kRT * (D + kSlotStats);
-  extern __shared__ int64_t prefix[];
-  __shared__ float s_o[kWarps][kRT][D];
-  __shared__ float s_m[kWarps][kRT], s_l[kWarps][kRT];
-  __shared__ int s_last;
+  extern __shared__ __align__(128) uint8_t smem[];
+  auto s_o = reinterpret_cast<float(*)[kRT][D]>(smem + F::SO);
+  auto s_m = reinterpret_cast<float(*)[kRT]>(smem + F::SM);
+  auto s_l = reinterpret_cast<float(*)[kRT]>(smem + F::SL);
+  volatile int* s_last = reinterpret_cast<volatile int*>(smem + F::LAST);
+  volatile int* abort = s_last + 1;
+  if (threadIdx.x == 0) *abort = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  AttnRun<kRT, kUnit, kThreads> run(a, prefix);
+  const uint32_t bars = smem_u32(smem + F::BARS);
+  if (threadIdx.x < 2 * F::STAGES) mbar_init(bars + 8u * threadIdx.x, threadIdx.x < F::STAGES ? 1 : kWarps);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  AttnRun<kRT, F::UNIT, kThreads> run(a, reinterpret_cast<int64_t*>(smem));
+  fence_proxy_async_smem();
+  __syncthreads();  // the prefix sums have been read: their place is the ring's
+  // 168 registers a thread at the start; 3 x 168 = 2 x 232 + 40
+  if (warp >= kWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == kWarps) copy_units<D, I8>(run, smem);
+    return;
+  }
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+  auto sync = []() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); };  // the warps that sum
+  int it = 0;
   for (; run.busy(); run.next()) {
     const AttnTile& x = run.x;
     // ---- the tile's rows: q = (hi + lo) 2^-e ----
@@ -99,8 +194,8 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = fp16_row_exponent(top);
-      const float up = __int_as_float((e + 127) << 23);
-      row_scale = a.scale_log2 * __int_as_float((127 - e) << 23);
+      const float up = pow2f(e);
+      row_scale = a.scale_log2 * pow2f(-e);
 #pragma unroll
       for (int s = 0; s < F::STEPS; ++s) {
         split_f16(v[s].x * up, v[s].y * up, qa[s][0], qa[s][1]);
@@ -119,123 +214,108 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
     int ev = kMinExp;  // the sums are in units of 2^ev (int8: the exponent of the largest scale met)
 
     const int u_end = run.last();
-    const int64_t head_slot = (int64_t)x.h << a.cache.page_shift;
-    const int64_t page_slots = (int64_t)a.cache.heads << a.cache.page_shift;
-    const int in_page = (1 << a.cache.page_shift) - 1;
-    // the first slot of the 16 keys from j0 on, -1 if none of them is there
-    auto slot_of = [&](int u) -> int64_t {
-      const int j0 = (x.unit0 + u) * kUnit + warp * 16;
-      if (u >= u_end || j0 >= x.key_hi || j0 + 16 <= x.key_lo) return -1;
-      const int page = paged_page(a.cache, a.batch, x.b, j0);
-      return page < 0 ? -1 : page * page_slots + head_slot + (j0 & in_page);
-    };
-    uint4 kr[2][F::KB];
-    float ks[4];
-    auto load_k = [&](int64_t slot, int j0) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int j = j0 + 8 * c + g;
-        const bool there = slot >= 0 && j >= x.key_lo && j < x.key_hi;
-        const char* p = static_cast<const char*>(a.cache.k) + ((slot + 8 * c + g) * D + t * F::E) * ESZ;
-#pragma unroll
-        for (int i = 0; i < F::KB; ++i) kr[c][i] = there ? ldg_stream(p + i * 64) : make_uint4(0u, 0u, 0u, 0u);
-        if constexpr (I8) {
-          const float2 sc = slot >= 0 ? __ldg(reinterpret_cast<const float2*>(a.cache.k_scale + slot + 8 * c + 2 * t))
-                                      : make_float2(0.f, 0.f);
-          ks[2 * c] = sc.x;
-          ks[2 * c + 1] = sc.y;
-        }
+    for (int u = run.first; u < u_end; ++u, ++it) {
+      const int stage = it % F::STAGES;
+      const uint8_t* at = smem + stage * F::STAGE;
+      const bool there =
+          __all_sync(0xffffffffu, mbar_wait(bars + 8u * stage, (uint32_t)(it / F::STAGES) & 1u, kWaitNs, abort));
+      if (!there && lane == 0) {
+        *abort = 1;
+        atomicOr(a.batch.status, kStatusTimeout);
       }
-    };
-    int64_t slot = slot_of(run.first);
-    load_k(slot, (x.unit0 + run.first) * kUnit + warp * 16);
-    for (int u = run.first; u < u_end; ++u) {
-      const int j0 = (x.unit0 + u) * kUnit + warp * 16;
-      const int64_t next_slot = slot_of(u + 1);
-      if (slot >= 0) {
-        // ---- values in flight, scores meanwhile ----
-        uint32_t vr[4][F::VC * F::VW];
-        float vs[4];
+      const int b0 = warp * BLOCKS;  // the warp's blocks of the unit
+      const uint32_t mask = there ? *reinterpret_cast<volatile const uint32_t*>(smem + F::MASK + 4 * stage) >> b0 : 0u;
+      const int j0 = (x.unit0 + u) * F::UNIT + 16 * b0;
+      if (mask & ((1u << BLOCKS) - 1u)) {
+        // ---- scores of keys 2t, 2t + 1, 2t + 8, 2t + 9 of each block and row g ----
+        float s[4 * BLOCKS];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int dj = 8 * (c >> 1) + 2 * t + (c & 1), j = j0 + dj;
-          const bool there = j >= x.key_lo && j < x.key_hi;
-          const char* p = static_cast<const char*>(a.cache.v) + ((slot + dj) * D + g * F::VE) * ESZ;
-#pragma unroll
-          for (int i = 0; i < F::VC; ++i) {
-            if constexpr (F::VW == 4) {
-              const uint4 w = there ? ldg_stream(p + i * 8 * F::VE * ESZ) : make_uint4(0u, 0u, 0u, 0u);
-              vr[c][4 * i] = w.x, vr[c][4 * i + 1] = w.y, vr[c][4 * i + 2] = w.z, vr[c][4 * i + 3] = w.w;
-            } else {
-              const uint2 w = there ? ldg_stream8(p) : make_uint2(0u, 0u);
-              vr[c][0] = w.x, vr[c][1] = w.y;
-            }
-          }
-        }
-        if constexpr (I8) {
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const float2 sc = __ldg(reinterpret_cast<const float2*>(a.cache.v_scale + slot + 8 * c + 2 * t));
-            vs[2 * c] = sc.x;
-            vs[2 * c + 1] = sc.y;
-          }
-        }
-        float s[4];  // keys 2t, 2t + 1, 2t + 8, 2t + 9 of row g
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < 2 * BLOCKS; ++c) {
+          float acc[2][4] = {};  // two chains of products
 #pragma unroll
           for (int i = 0; i < F::KB; ++i) {
-            const uint32_t w[4] = {kr[c][i].x, kr[c][i].y, kr[c][i].z, kr[c][i].w};
+            const uint4 k16 = lds<uint4>(at + F::K + (16 * b0 + 8 * c + g) * (D * ESZ) + 64 * i + 16 * t);
+            const uint32_t w[4] = {k16.x, k16.y, k16.z, k16.w};
             if constexpr (I8) {
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const uint32_t biased = w[k] ^ 0x80808080u;
-                mma16816(acc, qa[4 * i + k], i8_pair(biased, 0x4140u), i8_pair(biased, 0x4342u));
+                mma16816(acc[k & 1], qa[4 * i + k], i8_pair(biased, 0x4140u), i8_pair(biased, 0x4342u));
               }
             } else {
-              mma16816(acc, qa[2 * i], w[0], w[1]);
-              mma16816(acc, qa[2 * i + 1], w[2], w[3]);
+              mma16816(acc[0], qa[2 * i], w[0], w[1]);
+              mma16816(acc[1], qa[2 * i + 1], w[2], w[3]);
             }
           }
-          s[2 * c] = (acc[0] + acc[2]) * row_scale;
-          s[2 * c + 1] = (acc[1] + acc[3]) * row_scale;
+          s[2 * c] = ((acc[0][0] + acc[1][0]) + (acc[0][2] + acc[1][2])) * row_scale;
+          s[2 * c + 1] = ((acc[0][1] + acc[1][1]) + (acc[0][3] + acc[1][3])) * row_scale;
           if constexpr (I8) {
-            s[2 * c] *= ks[2 * c];
-            s[2 * c + 1] *= ks[2 * c + 1];
+            const float2 sc = lds<float2>(at + F::KS + 4 * (16 * b0 + 8 * c + 2 * t));
+            s[2 * c] *= sc.x;
+            s[2 * c + 1] *= sc.y;
           }
         }
-        load_k(next_slot, j0 + kUnit);
-        // ---- softmax: a warp's edge blocks mask by row ----
-        const bool edge = j0 < x.all_lo || j0 + 16 > x.all_hi;
-        unsigned hidden = 0;
-        if (edge) {
-          bool bad[4] = {false, false, false, false};
-          if constexpr (!I8) {  // a value that only some rows see must not reach the others as 0 times NaN
+        float vs[4 * BLOCKS];
+        if constexpr (I8) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2 * BLOCKS; ++c) {
+            const float2 sc = lds<float2>(at + F::VS + 4 * (16 * b0 + 8 * c + 2 * t));
+            vs[2 * c] = sc.x;
+            vs[2 * c + 1] = sc.y;
+          }
+        }
+        // The values of keys 2t, 2t + 1, 2t + 8, 2t + 9 of a block.
+        auto values = [&](int blk, uint32_t (&vr)[4][F::VC * F::VW]) {
 #pragma unroll
-              for (int i = 0; i < F::VC * F::VW; ++i) bad[c] |= f16_special(vr[c][i]);
-              const unsigned who = __ballot_sync(0xffffffffu, bad[c]);
-              bad[c] = (who & (0x11111111u << t)) != 0;
-              if (bad[c]) {
+          for (int c = 0; c < 4; ++c) {
+            const uint8_t* p = at + F::V + (16 * (b0 + blk) + 8 * (c >> 1) + 2 * t + (c & 1)) * (D * ESZ) + g * F::VE * ESZ;
 #pragma unroll
-                for (int i = 0; i < F::VC * F::VW; ++i) vr[c][i] = 0u;
+            for (int i = 0; i < F::VC; ++i) {
+              if constexpr (F::VW == 4) {
+                const uint4 w = lds<uint4>(p + i * 8 * F::VE * ESZ);
+                vr[c][4 * i] = w.x, vr[c][4 * i + 1] = w.y, vr[c][4 * i + 2] = w.z, vr[c][4 * i + 3] = w.w;
+              } else {
+                const uint2 w = lds<uint2>(p);
+                vr[c][0] = w.x, vr[c][1] = w.y;
               }
             }
           }
+        };
+        // ---- softmax: blocks at an edge of what the rows see, and what no copy brought, mask by row ----
+        const bool edge = j0 < x.all_lo || j0 + 16 * BLOCKS > x.all_hi || (~mask & ((1u << BLOCKS) - 1u)) != 0;
+        uint32_t hidden = 0, zap = 0;  // bits: scores that the row does not see; keys whose values become zeros
+        if (edge) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int j = j0 + 8 * (c >> 1) + 2 * t + (c & 1);
-            if (j < row_lo || j >= row_hi) {
-              s[c] = -INFINITY;
-              hidden |= 1u << c;
-            } else if (bad[c]) {
-              s[c] = __int_as_float(0x7fc00000);
+          for (int blk = 0; blk < BLOCKS; ++blk) {
+            const bool copied = mask >> blk & 1u;
+            bool bad[4] = {false, false, false, false};
+            if constexpr (!I8) {  // a value that only some rows see must not reach the others as 0 times NaN
+              uint32_t vr[4][F::VC * F::VW];
+              values(blk, vr);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const int j = j0 + 16 * blk + 8 * (c >> 1) + 2 * t + (c & 1);
+#pragma unroll
+                for (int i = 0; i < F::VC * F::VW; ++i) bad[c] |= f16_special(vr[c][i]);
+                const unsigned who = __ballot_sync(0xffffffffu, bad[c]);
+                bad[c] = (who & (0x11111111u << t)) != 0;
+                if (bad[c] || !copied || j < x.key_lo || j >= x.key_hi) zap |= 1u << (4 * blk + c);
+              }
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const int j = j0 + 16 * blk + 8 * (c >> 1) + 2 * t + (c & 1);
+              if (!copied || j < row_lo || j >= row_hi) {
+                s[4 * blk + c] = -INFINITY;
+                hidden |= 1u << (4 * blk + c);
+              } else if (bad[c]) {
+                s[4 * blk + c] = __int_as_float(0x7fc00000);
+              }
             }
           }
         }
         float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        if constexpr (BLOCKS == 2) top = fmaxf(top, fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const float m_new = fmaxf(m, top);
@@ -243,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
         if constexpr (I8) {
           float big = 0.f;  // of the scales that the row sees
 #pragma unroll
-          for (int c = 0; c < 4; ++c) big = fmaxf(big, (hidden >> c & 1u) ? 0.f : vs[c]);
+          for (int c = 0; c < 4 * BLOCKS; ++c) big = fmaxf(big, (hidden >> c & 1u) ? 0.f : vs[c]);
           big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
           big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
           ev_new = max(ev, min(kMaxExp, ((__float_as_int(big) >> 23) & 255) - 127));
@@ -260,59 +340,80 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
           ev = ev_new;
         }
         const float base = kShift - (m == -INFINITY ? 0.f : m);
-        float p[4];
+        float p[4 * BLOCKS];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 4 * BLOCKS; ++c) {
           p[c] = exp2_approx(s[c] + base);
           l += p[c];
           if constexpr (I8) p[c] = (hidden >> c & 1u) ? 0.f : p[c] * (vs[c] * exp2_int(-ev));
         }
         // ---- sums ----
-        uint32_t pa[4];
-        split_f16(p[0], p[1], pa[0], pa[1]);
-        split_f16(p[2], p[3], pa[2], pa[3]);
 #pragma unroll
-        for (int w = 0; w < F::VC * F::VW; ++w) {
-          if constexpr (I8) {
-            const uint32_t k0 = vr[0][w] ^ 0x80808080u, k1 = vr[1][w] ^ 0x80808080u;
-            const uint32_t k2 = vr[2][w] ^ 0x80808080u, k3 = vr[3][w] ^ 0x80808080u;
-            const uint32_t lo0 = __byte_perm(k0, k1, 0x5140u), hi0 = __byte_perm(k0, k1, 0x7362u);
-            const uint32_t lo1 = __byte_perm(k2, k3, 0x5140u), hi1 = __byte_perm(k2, k3, 0x7362u);
-            mma16816(o[4 * w], pa, i8_pair(lo0, 0x4140u), i8_pair(lo1, 0x4140u));
-            mma16816(o[4 * w + 1], pa, i8_pair(lo0, 0x4342u), i8_pair(lo1, 0x4342u));
-            mma16816(o[4 * w + 2], pa, i8_pair(hi0, 0x4140u), i8_pair(hi1, 0x4140u));
-            mma16816(o[4 * w + 3], pa, i8_pair(hi0, 0x4342u), i8_pair(hi1, 0x4342u));
-          } else {
-            mma16816(o[2 * w], pa, __byte_perm(vr[0][w], vr[1][w], 0x5410u), __byte_perm(vr[2][w], vr[3][w], 0x5410u));
-            mma16816(o[2 * w + 1], pa, __byte_perm(vr[0][w], vr[1][w], 0x7632u),
-                     __byte_perm(vr[2][w], vr[3][w], 0x7632u));
+        for (int blk = 0; blk < BLOCKS; ++blk) {
+          uint32_t vr[4][F::VC * F::VW];
+          values(blk, vr);
+          if (!I8 && edge) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (zap >> (4 * blk + c) & 1u) {
+#pragma unroll
+                for (int i = 0; i < F::VC * F::VW; ++i) vr[c][i] = 0u;
+              }
+          }
+          uint32_t pa[4];
+          split_f16(p[4 * blk], p[4 * blk + 1], pa[0], pa[1]);
+          split_f16(p[4 * blk + 2], p[4 * blk + 3], pa[2], pa[3]);
+#pragma unroll
+          for (int w = 0; w < F::VC * F::VW; ++w) {
+            if constexpr (I8) {
+              const uint32_t k0 = vr[0][w] ^ 0x80808080u, k1 = vr[1][w] ^ 0x80808080u;
+              const uint32_t k2 = vr[2][w] ^ 0x80808080u, k3 = vr[3][w] ^ 0x80808080u;
+              const uint32_t lo0 = __byte_perm(k0, k1, 0x5140u), hi0 = __byte_perm(k0, k1, 0x7362u);
+              const uint32_t lo1 = __byte_perm(k2, k3, 0x5140u), hi1 = __byte_perm(k2, k3, 0x7362u);
+              mma16816(o[4 * w], pa, i8_pair(lo0, 0x4140u), i8_pair(lo1, 0x4140u));
+              mma16816(o[4 * w + 1], pa, i8_pair(lo0, 0x4342u), i8_pair(lo1, 0x4342u));
+              mma16816(o[4 * w + 2], pa, i8_pair(hi0, 0x4140u), i8_pair(hi1, 0x4140u));
+              mma16816(o[4 * w + 3], pa, i8_pair(hi0, 0x4342u), i8_pair(hi1, 0x4342u));
+            } else {
+              mma16816(o[2 * w], pa, __byte_perm(vr[0][w], vr[1][w], 0x5410u), __byte_perm(vr[2][w], vr[3][w], 0x5410u));
+              mma16816(o[2 * w + 1], pa, __byte_perm(vr[0][w], vr[1][w], 0x7632u),
+                       __byte_perm(vr[2][w], vr[3][w], 0x7632u));
+            }
           }
         }
-      } else {
-        load_k(next_slot, j0 + kUnit);
       }
-      slot = next_slot;
+      __syncwarp();  // every lane has read the stage
+      if (lane == 0) mbar_arrive(bars + 8u * (F::STAGES + stage));
     }
 
-    // ---- the warps' sums together, in their order ----
+    // ---- the warps' sums together: the upper four's to the lower four, then those in their order ----
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
-    __syncthreads();  // the shared arrays' last readers are done
+    sync();  // the shared arrays' last readers are done
     if (t == 0) {
       s_m[warp][g] = m;
       s_l[warp][g] = l;
     }
-    __syncthreads();
+    sync();
     float m_all = s_m[0][g];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) m_all = fmaxf(m_all, s_m[w][g]);
     const float f = (m == -INFINITY ? (l != l ? l : 0.f) : exp2_approx(m - m_all)) * (I8 ? exp2_int(ev) : 1.f);
 #pragma unroll
-    for (int nb = 0; nb < F::NB; ++nb) {
-      s_o[warp][g][F::v_dim(nb, 2 * t)] = (o[nb][0] + o[nb][2]) * f;
-      s_o[warp][g][F::v_dim(nb, 2 * t + 1)] = (o[nb][1] + o[nb][3]) * f;
+    for (int turn = 0; turn < 2; ++turn) {
+      if ((warp < 4) == (turn == 1)) {
+#pragma unroll
+        for (int nb = 0; nb < F::NB; ++nb) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float* dst = &s_o[warp & 3][g][F::v_dim(nb, 2 * t + i)];
+            const float v = (o[nb][i] + o[nb][2 + i]) * f;
+            *dst = turn == 0 ? v : v + *dst;
+          }
+        }
+      }
+      sync();
     }
-    __syncthreads();
     const bool whole = run.whole();
     float* slots = a.slots + (int64_t)blockIdx.x * 2 * SLOT;
     float* mine = slots + (run.first == 0 ? SLOT : 0);
@@ -323,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
           make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
     };
     constexpr int Q4 = D / 4;
-    for (int i = threadIdx.x; i < x.rows * Q4; i += kThreads) {
+    for (int i = threadIdx.x; i < x.rows * Q4; i += 32 * kWarps) {
       const int row = i / Q4, d = 4 * (i % Q4);
       float top = s_m[0][row];
 #pragma unroll
@@ -331,9 +432,12 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float total = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
+      for (int w = 0; w < 4; ++w) {
         const float4 part = *reinterpret_cast<const float4*>(&s_o[w][row][d]);
         v = make_float4(v.x + part.x, v.y + part.y, v.z + part.z, v.w + part.w);
+      }
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
         const float lw = s_l[w][row];
         total += s_m[w][row] == -INFINITY ? lw : lw * exp2_approx(s_m[w][row] - top);
       }
@@ -350,14 +454,14 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
     if (whole) continue;
     // ---- a divided tile: the last block joins the pieces ----
     const int c0 = run.first_block(), c1 = run.last_block();
-    __syncthreads();
+    sync();
     if (threadIdx.x == 0) {
       __threadfence();
-      s_last = atomicAdd(a.counters + c0, 1u) == (unsigned)(c1 - c0);
+      *s_last = atomicAdd(a.counters + c0, 1u) == (unsigned)(c1 - c0);
       __threadfence();
     }
-    __syncthreads();
-    if (!s_last) continue;
+    sync();
+    if (!*s_last) continue;
     auto piece = [&](int c) { return a.slots + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * SLOT; };
     // rows' maxima over the pieces
     for (int row = warp; row < x.rows; row += kWarps) {
@@ -367,8 +471,8 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
       for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
       if (lane == 0) s_m[0][row] = top;
     }
-    __syncthreads();
-    // each warp every kWarps-th piece, then the warps in order
+    sync();
+    // each warp every kWarps-th piece, then the warps together as above
     constexpr int ROWS = 32 / Q4 > 0 ? 32 / Q4 : 1;  // rows a warp covers at once (D = 64: 2)
     float4 acc[kRT / ROWS];
     float tot[kRT / ROWS];
@@ -393,24 +497,31 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
         }
       }
     }
-    __syncthreads();
+    sync();
 #pragma unroll
-    for (int i = 0; i < kRT / ROWS; ++i) {
-      const int row = i * ROWS + sub;
-      *reinterpret_cast<float4*>(&s_o[warp][row][d4]) = acc[i];
-      if (d4 == 0) s_l[warp][row] = tot[i];
+    for (int turn = 0; turn < 2; ++turn) {
+      if ((warp < 4) == (turn == 1)) {
+#pragma unroll
+        for (int i = 0; i < kRT / ROWS; ++i) {
+          float4* dst = reinterpret_cast<float4*>(&s_o[warp & 3][i * ROWS + sub][d4]);
+          const float4 v = turn == 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *dst;
+          *dst = make_float4(acc[i].x + v.x, acc[i].y + v.y, acc[i].z + v.z, acc[i].w + v.w);
+          if (d4 == 0) s_l[warp][i * ROWS + sub] = tot[i];
+        }
+      }
+      sync();
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < x.rows * Q4; i += kThreads) {
+    for (int i = threadIdx.x; i < x.rows * Q4; i += 32 * kWarps) {
       const int row = i / Q4, d = 4 * (i % Q4);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float total = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
+      for (int w = 0; w < 4; ++w) {
         const float4 part = *reinterpret_cast<const float4*>(&s_o[w][row][d]);
         v = make_float4(v.x + part.x, v.y + part.y, v.z + part.z, v.w + part.w);
-        total += s_l[w][row];
       }
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) total += s_l[w][row];
       store(row, d, v, total);
     }
     if (threadIdx.x == 0) a.counters[c0] = 0u;
@@ -418,33 +529,20 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) attention_rows_ker
 }
 
 template <int D, bool I8>
-int rows_blocks(int sms) {
-  static std::atomic<int> known{0};
-  int per_sm = known.load(std::memory_order_relaxed);
-  if (per_sm == 0) {
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, attention_rows_kernel<D, I8>, kThreads,
-                                                      kMaxSeqs * sizeof(int64_t)) != cudaSuccess ||
-        per_sm < 1)
-      return sms;
-    known.store(per_sm, std::memory_order_relaxed);
-  }
-  return per_sm * sms;
+spl_status launch_rows(const AttnArgs& a, int blocks, cudaStream_t stream) {
+  constexpr uint32_t smem = Frag<D, I8>::SMEM;
+  if (cudaFuncSetAttribute(attention_rows_kernel<D, I8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
+      cudaSuccess)
+    return SPL_ECUDA;
+  attention_rows_kernel<D, I8><<<blocks, kThreads, smem, stream>>>(a);
+  return launch_status();
 }
 
 }  // namespace
 
-int attention_rows_blocks(int head_dim, bool i8, int sms) {
-  if (head_dim == 128) return i8 ? rows_blocks<128, true>(sms) : rows_blocks<128, false>(sms);
-  return i8 ? rows_blocks<64, true>(sms) : rows_blocks<64, false>(sms);
-}
-
 spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream) {
-  auto launch = [&](auto kernel) {
-    kernel<<<blocks, kThreads, a.batch.seqs * sizeof(int64_t), stream>>>(a);
-    return launch_status();
-  };
-  if (head_dim == 128) return i8 ? launch(attention_rows_kernel<128, true>) : launch(attention_rows_kernel<128, false>);
-  return i8 ? launch(attention_rows_kernel<64, true>) : launch(attention_rows_kernel<64, false>);
+  if (head_dim == 128) return i8 ? launch_rows<128, true>(a, blocks, stream) : launch_rows<128, false>(a, blocks, stream);
+  return i8 ? launch_rows<64, true>(a, blocks, stream) : launch_rows<64, false>(a, blocks, stream);
 }
 
 namespace {
@@ -474,10 +572,10 @@ Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_h
   const int d = (int)cache->head_dim, sms = device_sm_count();
   Shape s;
   const int64_t tiles = ceil_div(std::max<int64_t>(batch->max_rows, 1) * (q_heads / cache->kv_heads), kRowsTile);
-  const int64_t units = ceil_div(batch->max_pages * cache->page_size, kUnit);
+  const int64_t units = ceil_div(batch->max_pages * cache->page_size, 64);
   s.few = tiles == 1 || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;
   if (s.few) {
-    s.blocks = attention_rows_blocks(d, cache->format == SPL_KV_I8, sms);
+    s.blocks = sms;
     s.bytes = kCounterBytes + (size_t)s.blocks * 2 * kRowsTile * (d + kSlotStats) * sizeof(float);
   } else {
     s.blocks = sms;
@@ -525,7 +623,7 @@ extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* 
   a.scale_log2 = (float)(scale * 1.4426950408889634);
   a.counters = static_cast<unsigned int*>(workspace);
   a.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
-  a.min_units = 2;
+  a.min_units = s.few ? 1 : 2;
   const int d = (int)cache->head_dim;
   const bool i8 = cache->format == SPL_KV_I8;
   return s.few ? run_attention_rows(a, d, i8, s.blocks, stream) : run_attention_tc(a, d, i8, s.blocks, stream);

@@ -27,6 +27,8 @@ struct AttnArgs {
   int min_units;     // units a block takes at least (fewer blocks for little work)
 };
 
+constexpr int kFewTiles = 4;  // tiles of a sequence that one thread counts
+
 struct AttnTile {
   int b, h, t;           // sequence, key head, tile
   PagedSeq s;
@@ -66,7 +68,21 @@ struct AttnRun {
   __device__ AttnRun(const AttnArgs& args, int64_t* prefix) : a(args) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int seqs = a.batch.seqs, heads = a.cache.heads;
+    // A thread a sequence, whose loads then run side by side; the few sequences of many tiles a warp each.
+    for (int b = threadIdx.x; b < seqs; b += THREADS) {
+      AttnTile y;
+      y.s = paged_seq(a.batch, a.cache.page_shift, b);
+      const int tiles = (y.s.n * a.group + RT - 1) / RT;
+      int64_t sum = 0;
+      for (y.t = 0; tiles <= kFewTiles && y.t < tiles; ++y.t) {
+        tile_span<RT, U>(y, a.group, a.window);
+        sum += y.units;
+      }
+      prefix[b] = tiles <= kFewTiles ? sum * heads : -1;
+    }
+    __syncthreads();
     for (int b = warp; b < seqs; b += THREADS / 32) {
+      if (prefix[b] >= 0) continue;
       AttnTile y;
       y.s = paged_seq(a.batch, a.cache.page_shift, b);
       const int tiles = (y.s.n * a.group + RT - 1) / RT;
@@ -77,6 +93,7 @@ struct AttnRun {
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      __syncwarp();
       if (lane == 0) prefix[b] = sum * heads;
     }
     __syncthreads();
@@ -208,7 +225,6 @@ constexpr int kSlotStats = 2;  // per row: maximum (in units of log2) and total
 spl_status run_attention_tc(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
 size_t attention_tc_bytes(int head_dim, int blocks);
 spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
-int attention_rows_blocks(int head_dim, bool i8, int sms);
 constexpr int kRowsTile = 8;
 
 }  // namespace spl
