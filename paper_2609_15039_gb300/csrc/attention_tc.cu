@@ -1,25 +1,24 @@
 // Attention of many rows over a paged cache on the 5th-generation tensor cores (chunks of new tokens, prefill).
 //
-// o = sum_j softmax_j(scale q . k_j) v_j over tiles of 256 rows (two halves, A and B, of 128) and 128 keys.  Each half:
+// o = sum_j softmax_j(scale q . k_j) v_j over tiles of 128 rows and 128 keys:
 //   S = q_hi K^T + q_lo K^T        q = (hi + lo) 2^-e in binary16, a row's largest entry in [2^14, 2^15)
 //   p = 2^(scale log2(e) S - m)    m the row's running maximum, l the running total, both fp32
 //   O = O 2^(m_old - m) + p_hi V + p_lo V
 // The stored keys and values are exact in binary16, so two products instead of one give fp32 accuracy, and the kernel
-// is bound by the tensor pipe: 4 products of 128 x 128 x dim a half and tile.  Two halves, so that the products of one
-// run while the softmax of the other does; they share the tiles of K and V in shared memory.
-//   warp 0      MMA issuer.
-//   warps 1-3   producer: K and V tiles from the pages in the 128-byte-swizzled layout that the MMAs read, by TMA (a
-//               box a page; warp 1), or, int8, through registers, widened.  Values of tiles at an edge of what the
-//               rows see are looked over: stale ones become zeros.
-//   warps 4-11  softmax of half A, 16 rows a warp and four threads a row (so that a half's softmax takes half as long as
-//               its products, which the other half's wait for); also q's split, the sums' rescaling and the output.
-//   warps 12-19 the same of half B.
-// Tensor memory: S of A and of B (128 columns each) and O of A and of B (dim columns each).  p overwrites S in place: a
-// chunk of 32 scores becomes 16 columns of p_hi and 16 of p_lo, the A operand of the second product.
-// p is held as 2^9 p: the low half keeps an absolute 2^-34 of the row's largest.  The running maximum is raised only
-// where it would let p pass 2^5, so that O is seldom rescaled.  O is folded into an fp32 sum in the workspace with
-// round-to-nearest every kChain tiles, since the tensor core truncates as it accumulates (an unbroken chain's bias grows
-// with its length).
+// is bound by the tensor pipe: 4 products of 128 x 128 x dim a tile.  S of the next tile is made before O of this one,
+// so that the softmax of a tile runs beside the products of its neighbours.  Roles:
+//   warp 0       MMA issuer.
+//   warp 1       hands out the block's pieces of tiles and loads K and V tiles from the pages, by TMA: binary16 in the
+//                128-byte-swizzled layout that the MMAs read, a box a page; int8 as it is stored, beside.
+//   warps 2-7    int8: widen the tiles to binary16, in that layout.  binary16: look over the values of tiles at an edge of
+//                what the rows see (stale ones become zeros).
+//   warps 8-11   the sums: O, out of tensor memory, a thread a row, into the workspace or the output.
+//   warps 12-19  softmax, 16 rows a warp and four threads a row; also q's split.
+// Tensor memory: two places of S and two of O.  p overwrites S: a chunk of 32 scores becomes 16 columns of p_hi and 16 of
+// p_lo, the A operand of the second product.  p is held as 2^9 p: the low half keeps an absolute 2^-33 of the row's
+// largest.  The running maximum is raised only where it would let p pass 2^5, so that O is seldom rescaled.  The tensor
+// core truncates as it accumulates, and an unbroken chain's bias grows with its length: after kChain tiles O goes on in
+// its other place while the sums' warps add the first to an fp32 sum in the workspace, rounding to nearest.
 // Divided tiles are joined by a second, small launch over all SMs.
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its copies and MMAs done.
 
@@ -35,18 +34,21 @@
 namespace spl {
 namespace {
 
-constexpr int kThreads = 20 * 32, kProducers = 3;
-constexpr int kRows = 256, kKeys = 128, kStages = 3;
-constexpr int kChain = 8;        // key tiles of an accumulation chain of O (1024 keys)
-constexpr float kShift = 9.0f;  // p is held as 2^kShift p
+constexpr int kHelpers = 6, kSoftmax = 8;  // warps
+constexpr int kThreads = 32 * (2 + kHelpers + 4 + kSoftmax);
+constexpr int kRows = 128, kKeys = 128;
+constexpr int kChain = 4;        // key tiles of an accumulation chain of O (512 keys)
+constexpr float kShift = 9.0f;   // p is held as 2^kShift p
 constexpr float kLazy = 5.0f;    // and may reach 2^(kShift + kLazy), times a scale below 2, before the maximum is raised
 constexpr int kMinExp = -100, kMaxExp = 126;
+constexpr int kSteps = 4;        // key tiles whose scales or marks have a place (see the barriers of the producer)
 
-// Barriers by index: kFull, kEmpty a stage; kScale the scales of K of two steps; kRaw the copies of V's edge tiles; the
-// others a half each, their phases counting its own key tiles (kQ: its pieces); kPieceFull, kPieceFree a piece's place.
+// Barriers by index: kFull, kEmpty a stage; kRawFull, kRawEmpty a stage of int8 tiles as stored; kScale a place of K's scales; kQ a piece's q; kSFull, kPFull a place of S and
+// the p in it (whose waiter may be a tile behind); kPv a tile's product with V; kOFull, kOFree, kMFull a place of O: its chain is complete, has been added up, its rows'
+// maxima are there; kEdge the copies of V's edge tiles; kPieceFull, kPieceFree a piece's place.
 enum {
-  kFull = 0, kEmpty = 3, kScale = 6, kQ = 8, kSFull = 10, kPFull = 12, kPv = 14, kDrain = 16, kRaw = 17,
-  kPieceFull = 18, kPieceFree = 20, kBars = 22
+  kFull = 0, kEmpty = 5, kScale = 10, kQ = 14, kSFull = 15, kPFull = 17, kPv = 19, kOFull = 20, kOFree = 22, kMFull = 24,
+  kDrain = 26, kEdge = 27, kPieceFull = 28, kPieceFree = 30, kRawFull = 32, kRawEmpty = 35, kBars = 38
 };
 
 // A block's piece of a tile, as warp 1 hands it to the others (two in shared memory, in turn).
@@ -64,28 +66,33 @@ struct Piece {
 };
 constexpr int kPieces = 2;
 
-// D columns of binary16 in panels of 64 (128 bytes, 128-byte swizzle): a panel of R rows is R x 128 bytes.
-template <int D>
+// D columns of binary16 in panels of 64 (128 bytes, 128-byte swizzle): a panel of 128 rows is 16 KB.
+template <int D, bool I8>
 struct Layout {
+  static constexpr int STAGES = I8 ? 3 : 5, RAW_STAGES = 3;
   static constexpr int PANELS = D / 64;
-  static constexpr uint32_t PANEL = 128 * 128;             // 128 rows
-  static constexpr uint32_t TILE = PANELS * PANEL;         // q_hi or q_lo of a half; a K or V tile
-  static constexpr uint32_t Q = 0, KV = 4 * TILE;          // [A hi, A lo, B hi, B lo], stages
-  static constexpr uint32_t AUX = KV + kStages * TILE;
-  // aux: scales of K and of V of two tiles, bits of bad values of two tiles, largest scales of two tiles, barriers
-  static constexpr uint32_t KS = AUX, VS = KS + 2 * kKeys * 4, BAD = VS + 2 * kKeys * 4, VMAX = BAD + 2 * 16;
-  static constexpr uint32_t BARS = VMAX + 2 * 16, MISC = BARS + 8 * kBars, PIECES = MISC + 16;
-  static constexpr uint32_t BYTES = PIECES + kPieces * sizeof(Piece);
-  static constexpr uint32_t SMEM = BYTES;                  // the base is aligned (checked by the kernel)
-  static_assert(SMEM <= 232448, "227 KB of dynamic shared memory per block");
-  static_assert(kMaxSeqs * 8 <= 4 * TILE + kStages * TILE, "the prefix sums fit where the tiles go");
-  static constexpr uint32_t S = 0, O = 256;                // tensor memory columns (+ 128 and + D for half B)
+  static constexpr uint32_t PANEL = 128 * 128;
+  static constexpr uint32_t TILE = PANELS * PANEL;         // q_hi or q_lo; a K or V tile
+  static constexpr uint32_t Q = 0, KV = 2 * TILE;          // [q_hi, q_lo], stages
+  // int8 tiles as stored, their scales and the mask of the blocks of 16 keys that were copied
+  static constexpr uint32_t RAW = KV + STAGES * TILE, RAW_SCALE = kKeys * D, RAW_MASK = RAW_SCALE + kKeys * 4;
+  static constexpr uint32_t RAW_STAGE = RAW_MASK + 16;
+  static constexpr uint32_t AUX = RAW + (I8 ? RAW_STAGES * RAW_STAGE : 0);
+  // rows' maxima and totals of two chains (int8: and exponents); int8: scales of K and V, largest of V's a warp; binary16:
+  // marks of bad values; each for kSteps tiles
+  static constexpr uint32_t M = AUX, LT = M + 2 * kRows * 4, EV = LT + 2 * kRows * 4, KS = EV + (I8 ? 2 * kRows * 4 : 0);
+  static constexpr uint32_t VS = KS + (I8 ? kSteps * kKeys * 4 : 0), VMAX = VS + (I8 ? kSteps * kKeys * 4 : 0);
+  static constexpr uint32_t BAD = VMAX + (I8 ? kSteps * 32 : 0), BARS = BAD + (I8 ? 0 : kSteps * 16);
+  static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
+  static_assert(BARS % 8 == 0 && PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
+  static_assert(kMaxSeqs * 8 <= AUX, "the prefix sums fit where the tiles go");
+  static constexpr uint32_t S = 0, O = 256;                // tensor memory columns (+ 128 and + D for the other place)
   static constexpr uint32_t IDESC_S = make_idesc(0, 128, kKeys);
   static constexpr uint32_t IDESC_O = make_idesc(0, 128, D) | (1u << 16);  // B: the values, dims contiguous
 };
 constexpr uint32_t kTmemCols = 512;
 
-// A workspace slot: sums as [dim / 4][256 rows][4], then the rows' maxima and totals.
+// A workspace slot: sums as [dim / 4][128 rows][4], then the rows' maxima and totals.
 template <int D>
 constexpr int64_t slot_floats() {
   return (int64_t)kRows * (D + kSlotStats);
@@ -132,11 +139,18 @@ __device__ __forceinline__ bool f16_special2(uint32_t h) {
   return (h & 0x7c00u) == 0x7c00u || (h & 0x7c000000u) == 0x7c000000u;
 }
 
+__device__ __forceinline__ void st_global32(float* p, float4 a, float4 b) {
+  asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w),
+               "f"(b.x), "f"(b.y), "f"(b.z), "f"(b.w)
+               : "memory");
+}
+
 using Run = AttnRun<kRows, kKeys, kThreads>;
 
 template <int D, bool I8>
 struct Kernel {
-  using L = Layout<D>;
+  using L = Layout<D, I8>;
+  static constexpr int STAGES = L::STAGES;
   const AttnArgs& a;
   const CUtensorMap &map_k, &map_v;  // F16: the stored vectors as [slots, D]
   uint32_t smem;                     // shared address of the aligned base
@@ -147,6 +161,11 @@ struct Kernel {
   __device__ uint32_t bar(int i) const { return smem + L::BARS + 8u * i; }
   __device__ bool wait(int i, uint32_t parity) const {
     return __all_sync(0xffffffffu, mbar_wait(bar(i), parity, kWaitNs, abort));
+  }
+  // One arrival for the warp, after all its lanes' work.
+  __device__ void arrive(int i) const {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar(i));
   }
   __device__ void give_up() const {
     *abort = 1;
@@ -159,10 +178,7 @@ struct Kernel {
     ok = ok && wait(kPieceFull + k % kPieces, (uint32_t)(k / kPieces) & 1u);
     return pieces + k % kPieces;
   }
-  __device__ void piece_done(int k) const {
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) mbar_arrive(bar(kPieceFree + k % kPieces));
-  }
+  __device__ void piece_done(int k) const { arrive(kPieceFree + k % kPieces); }
   // Warp 1: the k-th piece of the run (or its end) for all.
   __device__ bool hand_out(const Run& run, int k) const {
     if (k >= kPieces && !wait(kPieceFree + k % kPieces, (uint32_t)(k / kPieces - 1) & 1u)) return false;
@@ -180,16 +196,178 @@ struct Kernel {
     return true;
   }
 
-  // ---------------------------------------------------------------- producer
+  // ---------------------------------------------------------------- loads
+  // A piece's tiles are loaded in the order in which the MMAs take them: K0, K1, V0, K2, V1, ..., V(n-1).  Scales and marks
+  // of a tile lie in one of kSteps places: the place of step s is written again for step s + 4, whose tile goes into a
+  // stage that was freed by an MMA issued after p of step s had arrived, so its softmax has read them.
+
+  // The u-th of that order's 2 n tiles: true for V, and the step within the piece.
+  static __device__ bool in_order(int i, int n, int& u) {
+    const bool v = i == 2 * n - 1 || (i > 0 && (i & 1) == 0);
+    u = i == 0 ? 0 : (v ? (i == 2 * n - 1 ? n - 1 : i / 2 - 1) : (i + 1) / 2);
+    return v;
+  }
+  // The page of the first 16 keys from j on that some row sees of the `size` from there (in one page), -1 if there is none.
+  __device__ int page_of(const Piece& x, int j, int size) const {
+    const int from = max(j, x.key_lo & ~15);
+    return from < min(j + size, x.key_hi) ? paged_page(a.cache, a.batch, x.b, from) : -1;
+  }
+  static __device__ __forceinline__ void mbar_arrive_more(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+  }
+
+  struct Loads {                                 // so far, of the whole run
+    int tile = 0, step = 0;                      // tiles of K and V, of K
+    int edge_tile = -STAGES, edge_phase = 0;     // V's last edge tile; the parity of the next one's copy
+  };
+
+  // Warp 1.
+  __device__ void loader(Run& run) const {
+    bool ok = true;
+    Loads y;
+    for (int k = 0; ok; ++k) {
+      ok = hand_out(run, k);
+      if (run.busy()) run.next();
+      const Piece* place = piece(k, ok);
+      if (!ok) break;
+      const int n = place->tiles;
+      if (n == 0) break;
+      ok = I8 ? load_i8(*place, y) : load_f16(*place, y);
+      y.step += n;
+      piece_done(k);
+    }
+    if (!ok) {
+      if ((threadIdx.x & 31) == 0) give_up();
+      // no copy in flight when the block leaves
+      constexpr int first = I8 ? kRawFull : kFull, stages = I8 ? L::RAW_STAGES : STAGES;
+      for (int t = max(0, y.tile - stages); t <= y.tile; ++t)
+        mbar_wait(bar(first + t % stages), (uint32_t)(t / stages) & 1u, kDrainNs, nullptr);
+    }
+  }
+  __device__ bool load_f16(const Piece& x, Loads& y) const {
+    const int lane = threadIdx.x & 31, n = x.tiles, shift = a.cache.page_shift;
+    const uint64_t policy = l2_evict_last();  // other tiles of rows read the same keys
+    // Boxes of a page's tokens, at most 128, a lane each; where no row sees any key of it the box lies past the pool's
+    // end and the copy fills it with zeros.
+    const int box = min(kKeys, 1 << shift), boxes = kKeys / box;
+    auto row_of = [&](int u) {
+      const int j = x.j0 + u * kKeys + lane * box;
+      const int page = lane < boxes && u < n ? page_of(x, j, box) : -1;
+      return page >= 0 ? (int)((((int64_t)page * a.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1)))
+                       : (int)((int64_t)a.cache.pages * a.cache.heads << shift);
+    };
+    int row[4] = {row_of(0), row_of(1), row_of(2), 0};  // of step u at u % 4
+    bool ok = true;
+    for (int i = 0; ok && i < 2 * n; ++i, ++y.tile) {
+      int u;
+      const bool v = in_order(i, n, u), edge = v && edge_of(x, x.j0 + u * kKeys);
+      const int stage = y.tile % STAGES, to = edge ? kEdge : kFull + stage;
+      // No second copy on kEdge while a warp may still wait for the first (those that freed its stage do not).
+      if (edge && y.tile - y.edge_tile < STAGES)
+        ok = wait(kFull + y.edge_tile % STAGES, (uint32_t)(y.edge_tile / STAGES) & 1u);
+      if (edge) y.edge_tile = y.tile;
+      if (ok && y.tile >= STAGES) ok = wait(kEmpty + stage, (uint32_t)(y.tile / STAGES - 1) & 1u);
+      if (!ok) break;
+      if (lane == 0) {
+        mbar_expect_tx(bar(to), L::TILE);
+        if (!edge) mbar_arrive_more(bar(to), kHelpers - 1);
+      }
+      __syncwarp();
+      const int at = (u & 3) == 0 ? row[0] : (u & 3) == 1 ? row[1] : (u & 3) == 2 ? row[2] : row[3];
+      if (lane < boxes) {
+        const uint32_t dst = smem + L::KV + (uint32_t)stage * L::TILE + (uint32_t)(lane * box) * 128u;
+#pragma unroll
+        for (int p = 0; p < L::PANELS; ++p)
+          tma_load_2d(dst + p * L::PANEL, v ? &map_v : &map_k, bar(to), 64 * p, at, policy);
+      }
+      __syncwarp();
+      if (v) {  // two steps ahead of the next K
+        const int next = row_of(u + 3);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (((u + 3) & 3) == q) row[q] = next;
+      }
+    }
+    return ok;
+  }
+  __device__ bool load_i8(const Piece& x, Loads& y) const {
+    const int lane = threadIdx.x & 31, n = x.tiles, shift = a.cache.page_shift;
+    const uint64_t policy = l2_evict_last();
+    const int box = min(kKeys, 1 << shift), boxes = kKeys / box;  // of a page's tokens, a lane each
+    auto slot_of = [&](int u) -> int64_t {
+      const int j = x.j0 + u * kKeys + lane * box;
+      const int page = lane < boxes && u < n ? page_of(x, j, box) : -1;
+      return page >= 0 ? ((((int64_t)page * a.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : -1;
+    };
+    int64_t slot[2] = {slot_of(0), slot_of(1)};  // of step u at u % 2
+    bool ok = true;
+    for (int i = 0; ok && i < 2 * n; ++i, ++y.tile) {
+      int u;
+      const bool v = in_order(i, n, u);
+      const int stage = y.tile % L::RAW_STAGES;
+      if (y.tile >= L::RAW_STAGES) ok = wait(kRawEmpty + stage, (uint32_t)(y.tile / L::RAW_STAGES - 1) & 1u);
+      if (!ok) break;
+      const int64_t at = (u & 1) ? slot[1] : slot[0];
+      const uint32_t raw = smem + L::RAW + (uint32_t)stage * L::RAW_STAGE, full = bar(kRawFull + stage);
+      const uint32_t mask = __ballot_sync(0xffffffffu, at >= 0);  // of boxes
+      if (lane == 0) {
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(raw + L::RAW_MASK), "r"(mask) : "memory");
+        mbar_expect_tx(full, (uint32_t)(__popc(mask) * box * (D + 4)));
+      }
+      __syncwarp();
+      if (at >= 0) {
+        bulk_load(raw + (uint32_t)(lane * box) * D, static_cast<const char*>(v ? a.cache.v : a.cache.k) + at * D,
+                  (uint32_t)box * D, full, policy);
+        bulk_load(raw + L::RAW_SCALE + (uint32_t)(lane * box) * 4u, (v ? a.cache.v_scale : a.cache.k_scale) + at,
+                  (uint32_t)box * 4u, full, policy);
+      }
+      __syncwarp();
+      if (v) {  // two steps ahead; the next K's is there
+        const int64_t next = slot_of(u + 2);
+        if (u & 1) slot[1] = next;
+        else slot[0] = next;
+      }
+    }
+    return ok;
+  }
+
+  // Warps 2-7.
+  __device__ void helper() const {
+    bool ok = true;
+    Loads y;
+    for (int k = 0; ok; ++k) {
+      const Piece* place = piece(k, ok);
+      if (!ok) break;
+      const Piece& x = *place;
+      const int n = x.tiles;
+      if (n == 0) break;
+      for (int i = 0; ok && i < 2 * n; ++i, ++y.tile) {
+        int u;
+        const bool v = in_order(i, n, u);
+        if constexpr (I8) {
+          ok = widen(y.tile, y.step + u, v);
+        } else if (v && edge_of(x, x.j0 + u * kKeys)) {
+          ok = wait(kEdge, (uint32_t)y.edge_phase);
+          if (!ok) break;
+          y.edge_phase ^= 1;
+          look_over(x, x.j0 + u * kKeys, smem + L::KV + (uint32_t)(y.tile % STAGES) * L::TILE, y.step + u);
+          arrive(kFull + y.tile % STAGES);
+        }
+      }
+      y.step += n;
+      piece_done(k);
+    }
+    if (!ok && (threadIdx.x & 31) == 0) give_up();
+  }
   // Values of an edge tile, a lane a key: those that no row sees become zeros; an infinity or NaN in one that only
   // some rows see becomes 0 and is marked.
   __device__ void look_over(const Piece& x, int j0, uint32_t base, int step) const {
-    const int lane = threadIdx.x & 31;
-    for (int word = (threadIdx.x >> 5) - 1; word < kKeys / 32; word += kProducers) {
+    const int lane = threadIdx.x & 31, word = (threadIdx.x >> 5) - 2;
+    if (word < kKeys / 32) {
       const int key = 32 * word + lane, j = j0 + key;
       const bool seen = j >= x.key_lo && j < x.key_hi;
       bool bad = false;
-#pragma unroll 4
+#pragma unroll 8
       for (int c = 0; c < D / 8; ++c) {
         const uint32_t at = base + (c >> 3) * L::PANEL + key * 128 + (((c & 7) ^ (key & 7)) << 4);
         const uint4 v = ld_shared16(at);
@@ -199,171 +377,64 @@ struct Kernel {
       }
       const unsigned marks = __ballot_sync(0xffffffffu, bad && seen);
       if (lane == 0)
-        asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem + L::BAD + 16u * (step & 1) + 4u * word), "r"(marks)
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem + L::BAD + 16u * (step % kSteps) + 4u * word), "r"(marks)
                      : "memory");
+      fence_proxy_async_smem();
+    }
+  }
+  // A tile of int8 to binary16 in the MMAs' layout, and its scales (0 for keys that were not copied).
+  __device__ bool widen(int tile, int step, bool v) const {
+    constexpr int THREADS = 32 * kHelpers, PARTS = D / 16, TOTAL = kKeys * PARTS;  // chunks of 16 values
+    const int i = threadIdx.x - 64, lane = i & 31, stage = tile % STAGES, raw_stage = tile % L::RAW_STAGES;
+    const uint32_t raw = smem + L::RAW + (uint32_t)raw_stage * L::RAW_STAGE;
+    const uint32_t base = smem + L::KV + (uint32_t)stage * L::TILE;
+    bool ok = wait(kRawFull + raw_stage, (uint32_t)(tile / L::RAW_STAGES) & 1u);
+    if (ok && tile >= STAGES) ok = wait(kEmpty + stage, (uint32_t)(tile / STAGES - 1) & 1u);
+    if (!ok) return false;
+#pragma unroll 3
+    for (int c = i; c < TOTAL; c += THREADS) {
+      const int key = c / PARTS, part = c % PARTS, c0 = (2 * part) & 7;  // two chunks of 8
+      const uint4 q = ld_shared16(raw + 16u * c);
+      const uint32_t row = base + (uint32_t)(part >> 2) * L::PANEL + key * 128;
+      const uint32_t w[4] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u, q.z ^ 0x80808080u, q.w ^ 0x80808080u};
+      st_shared16(row + ((c0 ^ (key & 7)) << 4), make_uint4(i8_pair(w[0], 0x4140u), i8_pair(w[0], 0x4342u),
+                                                            i8_pair(w[1], 0x4140u), i8_pair(w[1], 0x4342u)));
+      st_shared16(row + (((c0 + 1) ^ (key & 7)) << 4), make_uint4(i8_pair(w[2], 0x4140u), i8_pair(w[2], 0x4342u),
+                                                                  i8_pair(w[3], 0x4140u), i8_pair(w[3], 0x4342u)));
+    }
+    if (i < kKeys) {
+      uint32_t mask;
+      float scale;
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(mask) : "r"(raw + L::RAW_MASK));
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(raw + L::RAW_SCALE + 4u * i));
+      if (!(mask >> (i >> a.cache.page_shift) & 1u)) scale = 0.f;
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + (v ? L::VS : L::KS) + (uint32_t)(step % kSteps) * (kKeys * 4) +
+                                                   4u * i),
+                   "f"(scale)
+                   : "memory");
+      if (v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) scale = fmaxf(scale, __shfl_xor_sync(0xffffffffu, scale, o));
+        if (lane == 0)
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + L::VMAX + 32u * (step % kSteps) + 4u * (i >> 5)),
+                       "f"(scale)
+                       : "memory");
+      }
     }
     fence_proxy_async_smem();
-    __syncwarp();
-  }
-  static __device__ __forceinline__ void mbar_arrive_more(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-  }
-  __device__ void producer(Run& run) const {
-    const int i = threadIdx.x - 32, warp = i >> 5, lane = i & 31;
-    const uint64_t policy = l2_evict_last();  // other tiles of rows read the same keys
-    const int heads = a.cache.heads, shift = a.cache.page_shift, in_page = (1 << shift) - 1;
-    int tile = 0, step = 0;  // tiles issued, pairs of them
-    bool ok = true;
-    // F16: barriers of the copies in flight (a bit a stage: kRaw instead of kFull) and phases, for leaving early
-    uint32_t raw_phase = 0u;
-    for (int k = 0; ok; ++k) {
-      if (warp == 0) {
-        ok = hand_out(run, k);
-        if (run.busy()) run.next();
-      }
-      const Piece* place = piece(k, ok);
-      if (!ok) break;
-      const Piece x = *place;
-      if (warp > 0) piece_done(k);
-      if (x.tiles == 0) break;
-      // page of the keys 16 lane .. of the u-th tile, -1 where no row sees any of them (lanes 0-7)
-      auto pages_of = [&](int u) {
-        const int j = x.j0 + u * kKeys + 16 * lane;
-        if (lane >= kKeys / 16 || u >= x.tiles || j >= x.key_hi || j + 16 <= x.key_lo) return -1;
-        return paged_page(a.cache, a.batch, x.b, j);
-      };
-      int page = pages_of(0);
-      if constexpr (!I8) {
-        // Boxes of a page's tokens, at most 128, a lane each; where no row sees any key of it the box lies past the
-        // pool's end and the copy fills it with zeros.
-        const int box = min(kKeys, 1 << shift), boxes = kKeys / box;
-        for (int u = 0; ok && u < x.tiles; ++u, ++step) {
-          const int j0 = x.j0 + u * kKeys;
-          const int pg = __shfl_sync(0xffffffffu, page, (lane * box / 16) & 7);
-          const int row = pg >= 0 ? (int)((((int64_t)pg * heads + x.h) << shift) + ((j0 + lane * box) & in_page))
-                                  : (int)((int64_t)a.cache.pages * heads << shift);
-          const bool edge = edge_of(x, j0);
-          for (int which = 0; ok && which < 2; ++which, ++tile) {
-            const int stage = tile % kStages;
-            if (warp == 0) {
-              if (tile >= kStages) ok = wait(kEmpty + stage, (uint32_t)(tile / kStages - 1) & 1u);
-              if (!ok) break;
-              const bool raw = which && edge;  // values that are looked over before they are handed on
-              if (lane == 0) {
-                mbar_expect_tx(bar(raw ? kRaw : kFull + stage), L::TILE);
-                if (!raw) mbar_arrive_more(bar(kFull + stage), kProducers - 1);
-              }
-              __syncwarp();
-              if (lane < boxes) {
-                const uint32_t dst = smem + L::KV + (uint32_t)stage * L::TILE + (uint32_t)(lane * box) * 128u;
-#pragma unroll
-                for (int p = 0; p < L::PANELS; ++p)
-                  tma_load_2d(dst + p * L::PANEL, which ? &map_v : &map_k, bar(raw ? kRaw : kFull + stage), 64 * p, row,
-                              policy);
-              }
-              __syncwarp();
-            }
-            if (which && edge) {
-              ok = wait(kRaw, raw_phase);
-              if (!ok) break;
-              raw_phase ^= 1u;
-              look_over(x, j0, smem + L::KV + (uint32_t)stage * L::TILE, step);
-              if (lane == 0) mbar_arrive(bar(kFull + stage));
-            }
-          }
-          if (!ok) break;
-          page = pages_of(u + 1);
-        }
-      } else {
-        constexpr int PARTS = D / 16, KEY_STEP = 32 * kProducers / PARTS, PER = (kKeys + KEY_STEP - 1) / KEY_STEP;
-        uint4 regs[PER];  // the next tile's 16-byte chunks, on their way
-        float scale[2];
-        auto load = [&](int u, int which) {
-          const int j0 = x.j0 + u * kKeys;
-          const char* src = static_cast<const char*>(which ? a.cache.v : a.cache.k);
-          const int part = i % PARTS, key0 = i / PARTS;
-#pragma unroll
-          for (int k = 0; k < PER; ++k) {
-            const int key = key0 + KEY_STEP * k, j = j0 + key;
-            const int pg = __shfl_sync(0xffffffffu, page, (key >> 4) & 7);
-            const bool there = key < kKeys && pg >= 0 && j >= x.key_lo && j < x.key_hi;
-            const int64_t slot = there ? ((((int64_t)pg * heads + x.h) << shift) + (j & in_page)) : 0;
-            regs[k] = there ? __ldg(reinterpret_cast<const uint4*>(src + slot * D + part * 16))
-                            : make_uint4(0u, 0u, 0u, 0u);
-          }
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int key = i + 32 * kProducers * k, j = j0 + key;
-            const int pg = __shfl_sync(0xffffffffu, page, (key >> 4) & 7);
-            const bool there = key < kKeys && pg >= 0 && j >= x.key_lo && j < x.key_hi;
-            const int64_t slot = there ? ((((int64_t)pg * heads + x.h) << shift) + (j & in_page)) : 0;
-            scale[k] = there ? __ldg((which ? a.cache.v_scale : a.cache.k_scale) + slot) : 0.f;
-          }
-        };
-        auto put = [&](int which) {
-          const int stage = tile % kStages;
-          if (tile >= kStages) ok = wait(kEmpty + stage, (uint32_t)(tile / kStages - 1) & 1u);
-          if (!ok) return;
-          const uint32_t base = smem + L::KV + (uint32_t)stage * L::TILE;
-          const int part = i % PARTS, key0 = i / PARTS;  // two chunks of 8 values
-          const uint32_t panel = base + (uint32_t)(part >> 2) * L::PANEL;
-#pragma unroll
-          for (int k = 0; k < PER; ++k) {
-            const int key = key0 + KEY_STEP * k;
-            if (key >= kKeys) break;
-            const uint4 c = regs[k];
-            const uint32_t w[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
-            const int c0 = (2 * part) & 7;
-            st_shared16(panel + key * 128 + ((c0 ^ (key & 7)) << 4),
-                        make_uint4(i8_pair(w[0], 0x4140u), i8_pair(w[0], 0x4342u), i8_pair(w[1], 0x4140u),
-                                   i8_pair(w[1], 0x4342u)));
-            st_shared16(panel + key * 128 + (((c0 + 1) ^ (key & 7)) << 4),
-                        make_uint4(i8_pair(w[2], 0x4140u), i8_pair(w[2], 0x4342u), i8_pair(w[3], 0x4140u),
-                                   i8_pair(w[3], 0x4342u)));
-          }
-          const uint32_t sc = smem + (which ? L::VS : L::KS) + (uint32_t)(step & 1) * (kKeys * 4) + 4u * i;
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc), "f"(scale[0]) : "memory");
-          if (i < kKeys - 32 * kProducers)
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc + 4u * 32 * kProducers), "f"(scale[1]) : "memory");
-          if (which) {
-            float top = fmaxf(scale[0], scale[1]);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            if (lane == 0)
-              asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + L::VMAX + 16u * (step & 1) + 4u * warp), "f"(top)
-                           : "memory");
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(bar(kFull + stage));
-            if (!which) mbar_arrive(bar(kScale + (step & 1)));
-          }
-          ++tile;
-        };
-        load(0, 0);
-        for (int u = 0; ok && u < x.tiles; ++u, ++step) {
-          put(0);
-          load(u, 1);
-          page = pages_of(u + 1);
-          if (ok) put(1);
-          if (u + 1 < x.tiles) load(u + 1, 0);
-        }
-      }
+    arrive(kFull + stage);
+    if (lane == 0) {
+      mbar_arrive(bar(kRawEmpty + raw_stage));
+      if (!v) mbar_arrive(bar(kScale + step % kSteps));
     }
-    if constexpr (!I8) {  // no copy in flight when the block leaves early
-      if (!ok && warp == 0)
-        for (int t = max(0, tile - kStages); t <= tile; ++t)
-          mbar_wait(bar(kFull + t % kStages), (uint32_t)(t / kStages) & 1u, kDrainNs, nullptr);
-    }
-    if (!ok && lane == 0) give_up();
+    return true;
   }
 
   // ---------------------------------------------------------------- MMA issuer
-  __device__ void issue_s(int half, int tile, uint32_t leader) const {
-    const uint32_t q = sdesc_lo(smem + L::Q + (uint32_t)half * 2 * L::TILE);
-    const uint32_t k = sdesc_lo(smem + L::KV + (uint32_t)(tile % kStages) * L::TILE);
-    const uint32_t d = tmem + L::S + 128u * half;
+  __device__ void issue_s(int place, int tile, uint32_t leader) const {
+    const uint32_t q = sdesc_lo(smem + L::Q);
+    const uint32_t k = sdesc_lo(smem + L::KV + (uint32_t)(tile % STAGES) * L::TILE);
+    const uint32_t d = tmem + L::S + 128u * place;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
       const uint32_t off = ((uint32_t)(s / 4) * L::PANEL + (uint32_t)(s % 4) * 32u) >> 4;
@@ -371,9 +442,9 @@ struct Kernel {
       mma_ss(d, q + off + (L::TILE >> 4), k + off, kSdescHi128, L::IDESC_S, 1u, leader);
     }
   }
-  __device__ void issue_pv(int half, int tile, bool fresh, uint32_t leader) const {
-    const uint32_t v = sdesc_lo_mn(smem + L::KV + (uint32_t)(tile % kStages) * L::TILE);
-    const uint32_t p = tmem + L::S + 128u * half, d = tmem + L::O + (uint32_t)D * half;
+  __device__ void issue_pv(int place, int o, int tile, bool fresh, uint32_t leader) const {
+    const uint32_t v = sdesc_lo_mn(smem + L::KV + (uint32_t)(tile % STAGES) * L::TILE);
+    const uint32_t p = tmem + L::S + 128u * place, d = tmem + L::O + (uint32_t)D * o;
 #pragma unroll
     for (int s = 0; s < kKeys / 16; ++s) {
       const uint32_t at = p + 32u * (s / 2) + 8u * (s % 2), off = (uint32_t)(s * 16 * 128) >> 4;
@@ -384,53 +455,51 @@ struct Kernel {
   __device__ void issuer() const {
     const uint32_t leader = elect_one();
     bool ok = true;
-    int tile = 0;
-    uint32_t p_phase = 0u, q_phase = 0u;  // a bit each half
+    int tile = 0, step = 0, chain = 0;
     auto commit = [&](int i) {
       if (leader) mma_commit(bar(i));
       __syncwarp();
     };
     auto full = [&](int t) {
-      ok = ok && wait(kFull + t % kStages, (uint32_t)(t / kStages) & 1u);
+      ok = ok && wait(kFull + t % STAGES, (uint32_t)(t / STAGES) & 1u);
       tc_fence_after();
     };
-    // The loops' bounds come through shuffles: the compiler then knows them, and all that the descriptors are made of,
-    // to be the same in every lane.
+    // Loop bounds come through shuffles: the compiler then knows them, and all that the descriptors are made of, to be
+    // the same in every lane.
     for (int k = 0; ok; ++k) {
       const Piece* x = piece(k, ok);
       if (!ok) break;
-      const int halves = __shfl_sync(0xffffffffu, x->rows > 128 ? 2 : 1, 0);
       const int n = __shfl_sync(0xffffffffu, x->tiles, 0);
       piece_done(k);
       if (n == 0) break;
+      ok = wait(kQ, (uint32_t)k & 1u);
       full(tile);
-      for (int h = 0; ok && h < halves; ++h) {
-        ok = wait(kQ + h, q_phase >> h & 1u);
-        if (!ok) break;
-        q_phase ^= 1u << h;
-        tc_fence_after();
-        issue_s(h, tile, leader);
-        commit(kSFull + h);
-      }
       if (!ok) break;
-      commit(kEmpty + tile % kStages);
-      for (int j = 0; ok && j < n; ++j, tile += 2) {
-        for (int h = 0; ok && h < halves; ++h) {
-          ok = wait(kPFull + h, p_phase >> h & 1u);
-          if (ok && h == 0) full(tile + 1);
+      issue_s(step & 1, tile, leader);
+      commit(kSFull + (step & 1));
+      commit(kEmpty + tile % STAGES);
+      ++tile;
+      for (int j = 0; j < n; ++j, ++step) {
+        if (j + 1 < n) {
+          full(tile);
           if (!ok) break;
-          p_phase ^= 1u << h;
-          tc_fence_after();
-          issue_pv(h, tile + 1, j % kChain == 0, leader);
-          commit(kPv + h);
-          if (h == halves - 1) commit(kEmpty + (tile + 1) % kStages);
-          if (j + 1 < n) {
-            if (h == 0) full(tile + 2);
-            if (!ok) break;
-            issue_s(h, tile + 2, leader);
-            commit(kSFull + h);
-            if (h == halves - 1) commit(kEmpty + (tile + 2) % kStages);
-          }
+          issue_s((step + 1) & 1, tile, leader);
+          commit(kSFull + ((step + 1) & 1));
+          commit(kEmpty + tile % STAGES);
+          ++tile;
+        }
+        const bool fresh = j % kChain == 0;
+        if (fresh && chain >= 2) ok = wait(kOFree + (chain & 1), (uint32_t)(chain / 2 - 1) & 1u);
+        ok = ok && wait(kPFull + (step & 1), (uint32_t)(step >> 1) & 1u);
+        full(tile);
+        if (!ok) break;
+        issue_pv(step & 1, chain & 1, tile, fresh, leader);
+        commit(kPv);
+        commit(kEmpty + tile % STAGES);
+        ++tile;
+        if (j % kChain == kChain - 1 || j == n - 1) {
+          commit(kOFull + (chain & 1));
+          ++chain;
         }
       }
     }
@@ -439,49 +508,132 @@ struct Kernel {
     mbar_wait(bar(kDrain), 0u, kDrainNs, nullptr);
   }
 
-  // ---------------------------------------------------------------- softmax of one half
-  // A warp has 16 rows of its half, a thread (g, t) = (lane / 4, lane % 4) of rows g and g + 8 the columns 8 b + 2 t + {0, 1}.
+  // ---------------------------------------------------------------- the sums
+  // O of a chain, a thread a row, plus the sums so far: into the slot, or at the end of a whole tile out.
+  __device__ void sums(Divided* divided) const {
+    const int own = 32 * ((threadIdx.x >> 5) & 3) + (threadIdx.x & 31);
+    const uint32_t lanes = (uint32_t)(own & 96) << 16;
+    const bool wide = a.ldo % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
+    bool ok = true;
+    int chain = 0;
+    for (int k = 0; ok; ++k) {
+      const Piece* place = piece(k, ok);
+      if (!ok) break;
+      const Piece& x = *place;
+      const int n = x.tiles;
+      if (n == 0) break;
+      float* slot = a.slots + ((int64_t)blockIdx.x * 2 + (x.first == 0 ? 1 : 0)) * slot_floats<D>();
+      float4* slot4 = reinterpret_cast<float4*>(slot) + own;  // + 128 for each four dims
+      const int chains = (n + kChain - 1) / kChain;
+      float m_slot = -INFINITY;
+      int ev_slot = kMinExp;
+      for (int c = 0; c < chains; ++c, ++chain) {
+        const int o = chain & 1;
+        const uint32_t parity = (uint32_t)(chain >> 1) & 1u;
+        ok = wait(kMFull + o, parity) && wait(kOFull + o, parity);
+        if (!ok) break;
+        tc_fence_after();
+        const bool last = c == chains - 1, out = last && x.whole != 0;
+        float m, l = 0.f;
+        int ev = 0;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(m) : "r"(smem + L::M + 4u * (o * kRows + own)));
+        if (last) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(l) : "r"(smem + L::LT + 4u * (o * kRows + own)));
+        if constexpr (I8) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(ev) : "r"(smem + L::EV + 4u * (o * kRows + own)));
+        const float keep = m_slot == -INFINITY ? 1.f : exp2_approx(m_slot - m) * (I8 ? exp2_int(ev_slot - ev) : 1.f);
+        const float unit = last && I8 ? exp2_int(ev) : 1.f;
+        const float f = out ? (l == 0.f ? 0.f : 1.0f / l) * unit : unit;
+        const bool add = !last && c > 0 && __all_sync(0xffffffffu, keep == 1.f);
+        float* dst = nullptr;
+        if (own < x.rows) {
+          const int fr = x.r0 + own;
+          dst = a.out + (int64_t)(x.row0 + fr / a.group) * a.ldo + (int64_t)(x.h * a.group + fr % a.group) * D;
+        }
+        const uint32_t from = tmem + lanes + L::O + (uint32_t)D * o;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 32) {
+          float v[32];
+          tmem_ld_32x32(from + d, v);
+          float4 before = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float4* at = slot4 + (d / 4 + i) * kRows;
+            float4 w = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            if (add) {  // the units have not changed: added where it lies, without waiting
+              asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1,%2,%3,%4};" ::"l"(at), "f"(w.x), "f"(w.y),
+                           "f"(w.z), "f"(w.w)
+                           : "memory");
+              continue;
+            }
+            if (c > 0) {
+              const float4 s = __ldcg(at);
+              w = make_float4(fmaf(s.x, keep, w.x), fmaf(s.y, keep, w.y), fmaf(s.z, keep, w.z), fmaf(s.w, keep, w.w));
+            }
+            w = make_float4(w.x * f, w.y * f, w.z * f, w.w * f);
+            if (!out) *at = w;
+            else if (dst && !wide) *reinterpret_cast<float4*>(dst + d + 4 * i) = w;
+            if (i & 1) {  // whole 32-byte sectors
+              if (out && dst && wide) st_global32(dst + d + 4 * (i - 1), before, w);
+            }
+            before = w;
+          }
+        }
+        tc_fence_before();
+        arrive(kOFree + o);
+        if (last && !out) {
+          slot[(int64_t)kRows * D + own] = m;
+          slot[(int64_t)kRows * D + kRows + own] = l;
+        }
+        m_slot = m;
+        ev_slot = ev;
+      }
+      if (ok && x.whole == 0 && x.first == 0 && own == 0)
+        *divided = {x.last_block, x.h, x.row0, x.n, x.r0, x.rows};
+      piece_done(k);
+    }
+    if (!ok && (threadIdx.x & 31) == 0) give_up();
+  }
+
+  // ---------------------------------------------------------------- softmax
+  // A warp has 16 rows, a thread (g, t) = (lane / 4, lane % 4) of rows g and g + 8 the columns 8 b + 2 t + {0, 1}.
 
   // q's rows as hi + lo into shared memory; the scales of the thread's two rows.
-  __device__ void split_q(const Piece& x, int half, int row0, float (&row_scale)[2]) const {
+  __device__ void split_q(const Piece& x, int row0, float (&row_scale)[2]) const {
     const int lane = threadIdx.x & 31;
-    constexpr int LANES = D / 4, PER = 32 / LANES, BATCH = 8;  // lanes of a row, rows at a time
+    constexpr int LANES = D / 4, PER = 32 / LANES, BATCH = 16 / PER;  // lanes of a row, rows at a time
     const int sub = lane / LANES, at = lane % LANES;
     const float sign = a.scale_log2 < 0.f ? -1.f : 1.f;  // the scale's sign goes into q
     float mine = 0.f;                                    // scale of row `lane` of the 16
-    const uint32_t hi = smem + L::Q + (uint32_t)half * 2 * L::TILE + (uint32_t)(at >> 4) * L::PANEL;
+    const uint32_t hi = smem + L::Q + (uint32_t)(at >> 4) * L::PANEL;
     int64_t own = -1;  // where row `lane` begins
-    if (lane < 16 && 128 * half + row0 + lane < x.rows) {
-      const int fr = x.r0 + 128 * half + row0 + lane, token = fr / a.group;
+    if (lane < 16 && row0 + lane < x.rows) {
+      const int fr = x.r0 + row0 + lane, token = fr / a.group;
       own = (int64_t)(x.row0 + token) * a.ldq + (int64_t)(x.h * a.group + fr % a.group) * D;
     }
-    for (int r0 = 0; r0 < 16; r0 += BATCH * PER) {
-      float4 v[BATCH];
+    float4 v[BATCH];
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int64_t from = __shfl_sync(0xffffffffu, own, r0 + i * PER + sub);
-        v[i] = from >= 0 ? __ldg(reinterpret_cast<const float4*>(a.q + from) + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < BATCH; ++i) {
+      const int64_t from = __shfl_sync(0xffffffffu, own, i * PER + sub);
+      v[i] = from >= 0 ? __ldg(reinterpret_cast<const float4*>(a.q + from) + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      float top = fmaxf(fmaxf(fabsf(v[i].x), fabsf(v[i].y)), fmaxf(fabsf(v[i].z), fabsf(v[i].w)));
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const int e = fp16_row_exponent(top);
+      const float up = sign * pow2f(e);
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int ep = __shfl_sync(0xffffffffu, e, p * LANES);
+        if (lane == i * PER + p) mine = fabsf(a.scale_log2) * pow2f(-ep);
       }
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        float top = fmaxf(fmaxf(fabsf(v[i].x), fabsf(v[i].y)), fmaxf(fabsf(v[i].z), fabsf(v[i].w)));
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const int e = fp16_row_exponent(top);
-        const float up = sign * pow2f(e);
-#pragma unroll
-        for (int p = 0; p < PER; ++p) {
-          const int ep = __shfl_sync(0xffffffffu, e, p * LANES);
-          if (lane == r0 + i * PER + p) mine = fabsf(a.scale_log2) * pow2f(-ep);
-        }
-        uint32_t h0, l0, h1, l1;
-        split_f16(v[i].x * up, v[i].y * up, h0, l0);
-        split_f16(v[i].z * up, v[i].w * up, h1, l1);
-        const int r = row0 + r0 + i * PER + sub;  // of the half
-        const uint32_t addr = hi + (uint32_t)r * 128 + (((uint32_t)(at & 15) / 2 ^ (r & 7)) << 4) + 8u * (at & 1);
-        asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(addr), "r"(h0), "r"(h1) : "memory");
-        asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(addr + L::TILE), "r"(l0), "r"(l1) : "memory");
-      }
+      uint32_t h0, l0, h1, l1;
+      split_f16(v[i].x * up, v[i].y * up, h0, l0);
+      split_f16(v[i].z * up, v[i].w * up, h1, l1);
+      const int r = row0 + i * PER + sub;  // of the tile
+      const uint32_t addr = hi + (uint32_t)r * 128 + (((uint32_t)(at & 15) / 2 ^ (r & 7)) << 4) + 8u * (at & 1);
+      asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(addr), "r"(h0), "r"(h1) : "memory");
+      asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(addr + L::TILE), "r"(l0), "r"(l1) : "memory");
     }
     row_scale[0] = __shfl_sync(0xffffffffu, mine, lane >> 2);
     row_scale[1] = __shfl_sync(0xffffffffu, mine, (lane >> 2) + 8);
@@ -539,17 +691,22 @@ struct Kernel {
           }
         }
       }
+      // of the thread's keys, 8 b + {0, 1} from 64 c + 2 t on, a row sees [lo, hi)
+      const int lo[2] = {x.lo[0] - 64 * c - 2 * t, x.lo[1] - 64 * c - 2 * t};
+      const int hi[2] = {x.hi[0] - 64 * c - 2 * t, x.hi[1] - 64 * c - 2 * t};
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const int r = i >> 1 & 1, j = 8 * (i >> 2) + (i & 1);  // of the thread's keys, from 64 c + 2 t on
-        if (j < x.lo[r] - 64 * c - 2 * t || j >= x.hi[r] - 64 * c - 2 * t) s[i] = 0xff800000u;
+      for (int i = 0; i < 32; ++i)
+        if (8 * (i >> 2) + (i & 1) >= hi[i >> 1 & 1]) s[i] = 0xff800000u;
+      if (__any_sync(0xffffffffu, lo[0] > -2 || lo[1] > -2)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (8 * (i >> 2) + (i & 1) < lo[i >> 1 & 1]) s[i] = 0xff800000u;
       }
     }
   }
   // Scores to probabilities, in place in tensor memory.  Where a row's scores pass its maximum by more than kLazy it is
   // raised, and what was made with the old one is rescaled.  p = 2^(row_scale s + base); of a chunk of 32 columns the
-  // high halves (times the values' scales) take the first 16, the low ones the others.  The scores of 64 keys are in
-  // registers at a time, the first for the second time: all 128 beside p would be more than there are.
+  // high halves (times the values' scales) take the first 16, the low ones the others.  The high half is p cut to 11 bits.
   template <bool EDGE, class Rescale>
   static __device__ __forceinline__ bool make_p(const Scores& x, float (&m)[2], float (&l)[2], const float (&down)[2],
                                                 Rescale rescale_o) {
@@ -596,7 +753,8 @@ struct Kernel {
       sum[r] = p2(0.f, 0.f);
     }
     const unsigned long long minus1 = p2(-1.f, -1.f), zero2 = p2(-0.f, -0.f);
-    auto put = [&](int c, uint32_t (&s)[32]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
 #pragma unroll
       for (int b0 = 0; b0 < 8; b0 += 4) {
         uint32_t hi[8], lo[8];
@@ -606,7 +764,7 @@ struct Kernel {
           if constexpr (I8) w = ld_shared8(x.vs + 256u * c + 32u * b + 8u * t);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const float s0 = __uint_as_float(s[4 * b + 2 * r]), s1 = __uint_as_float(s[4 * b + 2 * r + 1]);
+            const float s0 = __uint_as_float(s[c][4 * b + 2 * r]), s1 = __uint_as_float(s[c][4 * b + 2 * r + 1]);
             float t0, t1;
             up2(fma2(p2(s0, s1), scale2[r], base2[r]), t0, t1);
             if constexpr (EDGE) {  // -inf times a scale of 0
@@ -618,29 +776,24 @@ struct Kernel {
             if constexpr (I8) {
               p = fma2(p, fma2(p2(__uint_as_float(w.x), __uint_as_float(w.y)), p2(down[r], down[r]), zero2), zero2);
               if constexpr (EDGE) {  // a hidden value's scale may be anything
-                float a, b;
-                up2(p, a, b);
-                p = p2(s0 == -INFINITY ? 0.f : a, s1 == -INFINITY ? 0.f : b);
+                float p0, p1;
+                up2(p, p0, p1);
+                p = p2(s0 == -INFINITY ? 0.f : p0, s1 == -INFINITY ? 0.f : p1);
               }
             }
             float p0, p1, r0, r1;
             up2(p, p0, p1);
-            const uint32_t h16 = pack_f16(p0, p1);
-            const float2 h = unpack_f16(h16);
-            up2(fma2(p2(h.x, h.y), minus1, p), r0, r1);
-            hi[2 * (b - b0) + r] = h16;
+            const float h0 = __uint_as_float(__float_as_uint(p0) & 0xffffe000u);
+            const float h1 = __uint_as_float(__float_as_uint(p1) & 0xffffe000u);
+            up2(fma2(p2(h0, h1), minus1, p), r0, r1);
+            hi[2 * (b - b0) + r] = pack_f16(h0, h1);
             lo[2 * (b - b0) + r] = pack_f16(r0, r1);
           }
         }
         tmem_st_16x16(x.ts + 64u * c + 8u * b0, hi);
         tmem_st_16x16(x.ts + 64u * c + 8u * b0 + 16u, lo);
       }
-    };
-    put(1, s[1]);
-    tmem_ld_16x64(x.ts, s[0]);
-    tmem_ld_wait(s[0]);
-    prepare<EDGE>(x, 0, s[0]);
-    put(0, s[0]);
+    }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       float p0, p1;
@@ -651,199 +804,125 @@ struct Kernel {
     return true;
   }
 
-  __device__ void softmax(int half, Divided* divided) const {
+  __device__ void softmax() const {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int row0 = 32 * (warp & 3) + 16 * ((warp - 4) >> 2 & 1);  // the warp's rows of the half (its tensor memory lanes)
+    const int row0 = 32 * (warp & 3) + 16 * (warp >> 2 & 1);  // the warp's rows (its tensor memory lanes)
     const uint32_t lanes = (uint32_t)row0 << 16;
-    const uint32_t ts = tmem + lanes + L::S + 128u * half, to = tmem + lanes + L::O + (uint32_t)D * half;
     bool ok = true;
-    int step = 0;        // tiles of K so far
-    uint32_t phase = 0;  // of this half's barriers: they complete once a key tile of a piece that has the half
+    int step = 0, tile0 = 0, chain = 0;  // tiles of K, of K and V before the piece, chains of O so far
     for (int k = 0; ok; ++k) {
       const Piece* place = piece(k, ok);
       if (!ok) break;
       const Piece& x = *place;
       const int n = x.tiles;
       if (n == 0) break;
-      const bool whole = x.whole != 0;
-      float* slot = a.slots + ((int64_t)blockIdx.x * 2 + (x.first == 0 ? 1 : 0)) * slot_floats<D>();
+      Scores sc;
+      split_q(x, row0, sc.row_scale);
+      fence_proxy_async_smem();
+      arrive(kQ);
+      const int own0 = row0 + g;  // the thread's rows of the tile: own0, own0 + 8
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-      if (x.rows > 128 * half) {
-        Scores sc;
-        split_q(x, half, row0, sc.row_scale);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(kQ + half));
-        const int own0 = 128 * half + row0 + g;  // the thread's rows of the tile: own0, own0 + 8
-        int ev[2] = {kMinExp, kMinExp}, ev_slot[2] = {kMinExp, kMinExp};
-        float m_slot[2] = {-INFINITY, -INFINITY};
-        bool has_slot = false;
-        // O, plus the slot's sums (if any) brought into its units: into the slot, or at the end of a whole tile out.
-        auto fold = [&](bool final) {
-          const bool out = final && whole;
-          float keep[2], f[2];
-          float* dst[2];
+      int ev[2] = {kMinExp, kMinExp};
+      for (int j = 0; j < n; ++j, ++step) {
+        const int j0 = x.j0 + j * kKeys, s4 = step % kSteps;
+        const bool edge = edge_of(x, j0), fresh = j % kChain == 0;
+        ok = wait(kSFull + (step & 1), (uint32_t)(step >> 1) & 1u);
+        if (ok && I8) ok = wait(kScale + s4, (uint32_t)(step / kSteps) & 1u);
+        if (ok && (I8 || edge)) {  // V's scales, or marks
+          const int tv = tile0 + (j < n - 1 ? 2 * j + 2 : 2 * j + 1);
+          ok = wait(kFull + tv % STAGES, (uint32_t)(tv / STAGES) & 1u);
+        }
+        if (!ok) break;
+        tc_fence_after();
+        sc.ts = tmem + lanes + L::S + 128u * (step & 1);
+        sc.ks = smem + L::KS + (uint32_t)s4 * (kKeys * 4);
+        sc.vs = smem + L::VS + (uint32_t)s4 * (kKeys * 4);
+        sc.bad = smem + L::BAD + 16u * s4;
+        if (edge) {
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            keep[r] = m_slot[r] == -INFINITY ? 1.f
-                                             : exp2_approx(m_slot[r] - m[r]) * (I8 ? exp2_int(ev_slot[r] - ev[r]) : 1.f);
-            const float unit = final && I8 ? exp2_int(ev[r]) : 1.f;
-            f[r] = out ? (l[r] == 0.f ? 0.f : 1.0f / l[r]) * unit : unit;
-            const int fr = x.r0 + own0 + 8 * r;
-            dst[r] = own0 + 8 * r < x.rows ? a.out + (int64_t)(x.row0 + fr / a.group) * a.ldo +
-                                                 (int64_t)(x.h * a.group + fr % a.group) * D + 2 * t
-                                           : nullptr;
+          for (int r = 0; r < 2; ++r) {  // (rows past the last see all: nothing reads them)
+            int lo = j0, hi = j0 + kKeys;
+            if (own0 + 8 * r < x.rows) row_keys({0, x.n, x.len}, a.window, (x.r0 + own0 + 8 * r) / a.group, lo, hi);
+            sc.lo[r] = lo - j0;
+            sc.hi[r] = hi - j0;
           }
-          const bool add = !final && has_slot && __all_sync(0xffffffffu, keep[0] == 1.f && keep[1] == 1.f);
-          // dims 8 b + 2 t, + 1 of a row in the slot
-          auto at = [&](int b, int r) { return slot + ((2 * b + (t >> 1)) * kRows + own0 + 8 * r) * 4 + 2 * (t & 1); };
+        }
+        auto rescale_o = [&](float f0, float f1) {
+          if (fresh || !__any_sync(0xffffffffu, f0 != 1.f || f1 != 1.f)) return true;  // (or O starts anew)
+          if (!wait(kPv, (uint32_t)(step - 1) & 1u)) return false;
+          tc_fence_after();
+          const uint32_t to = tmem + lanes + L::O + (uint32_t)D * (chain & 1);
 #pragma unroll 1
           for (int c = 0; c < D / 64; ++c) {
             uint32_t v[32];
             tmem_ld_16x64(to + 64u * c, v);
             tmem_ld_wait(v);
 #pragma unroll
-            for (int h = 0; h < 8; h += 4) {
-              float2 s[8];
-              if (has_slot && !add) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  s[i] = __ldcg(reinterpret_cast<const float2*>(at(8 * c + h + (i >> 1), i & 1)));
-              }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int b = h + (i >> 1), r = i & 1;
-                float2 w = make_float2(__uint_as_float(v[4 * b + 2 * r]), __uint_as_float(v[4 * b + 2 * r + 1]));
-                if (add) {  // the units have not changed: added where it lies, without waiting
-                  asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1,%2};" ::"l"(at(8 * c + b, r)), "f"(w.x),
-                               "f"(w.y)
-                               : "memory");
-                  continue;
-                }
-                if (has_slot) w = make_float2(fmaf(s[i].x, keep[r], w.x), fmaf(s[i].y, keep[r], w.y));
-                w = make_float2(w.x * f[r], w.y * f[r]);
-                if (!out) *reinterpret_cast<float2*>(at(8 * c + b, r)) = w;
-                else if (dst[r]) *reinterpret_cast<float2*>(dst[r] + 64 * c + 8 * b) = w;
-              }
-            }
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * (i & 2 ? f1 : f0));
+            tmem_st_16x64(to + 64u * c, v);
           }
-          has_slot = true;
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            m_slot[r] = m[r];
-            ev_slot[r] = ev[r];
-          }
+          return true;
         };
-        for (int j = 0; j < n; ++j, ++step, phase ^= 1u) {
-          const int j0 = x.j0 + j * kKeys;
-          const bool edge = edge_of(x, j0);
-          ok = wait(kSFull + half, phase);
-          if (!ok) break;
-          tc_fence_after();
-          // The scales, or the marks, of this step's tiles.  A stage of V is not filled again before this half's p is
-          // there; one of K may be, so its scales have barriers of their own.
-          if (I8) ok = wait(kScale + (step & 1), (uint32_t)(step >> 1) & 1u);
-          if (ok && (I8 || edge)) {
-            const int tv = 2 * step + 1;
-            ok = wait(kFull + tv % kStages, (uint32_t)(tv / kStages) & 1u);
-          }
-          if (!ok) break;
-          sc.ts = ts;
-          sc.ks = smem + L::KS + (uint32_t)(step & 1) * (kKeys * 4);
-          sc.vs = smem + L::VS + (uint32_t)(step & 1) * (kKeys * 4);
-          sc.bad = smem + L::BAD + 16u * (step & 1);
+        float down[2] = {1.f, 1.f};
+        if constexpr (I8) {  // the largest value scale that a row sees sets its sums' units
+          float big[2] = {0.f, 0.f};
           if (edge) {
+            for (int i = 2 * t; i < kKeys; i += 8) {
+              const uint2 w = ld_shared8(sc.vs + 4u * i);
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {  // (rows past the last see all: nothing reads them)
-              int lo = j0, hi = j0 + kKeys;
-              if (own0 + 8 * r < x.rows)
-                row_keys({0, x.n, x.len}, a.window, (x.r0 + own0 + 8 * r) / a.group, lo, hi);
-              sc.lo[r] = lo - j0;
-              sc.hi[r] = hi - j0;
-            }
-          }
-          const bool fresh = j % kChain == 0;
-          if (fresh && j > 0) {  // a chain is complete: O into the slot
-            ok = wait(kPv + half, phase ^ 1u);
-            if (!ok) break;
-            tc_fence_after();
-            fold(false);
-          }
-          auto rescale_o = [&](float f0, float f1) {
-            if (fresh || !__any_sync(0xffffffffu, f0 != 1.f || f1 != 1.f)) return true;  // (or O starts anew)
-            if (!wait(kPv + half, phase ^ 1u)) return false;
-            tc_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < D / 64; ++c) {
-              uint32_t v[32];
-              tmem_ld_16x64(to + 64u * c, v);
-              tmem_ld_wait(v);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * (i & 2 ? f1 : f0));
-              tmem_st_16x64(to + 64u * c, v);
-            }
-            return true;
-          };
-          float down[2] = {1.f, 1.f};
-          if constexpr (I8) {  // the largest value scale that a row sees sets its sums' units
-            float big[2] = {0.f, 0.f};
-            if (edge) {
-              for (int i = 2 * t; i < kKeys; i += 8) {
-                const uint2 w = ld_shared8(sc.vs + 4u * i);
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                  if (i >= sc.lo[r] && i < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.x));
-                  if (i + 1 >= sc.lo[r] && i + 1 < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.y));
-                }
+              for (int r = 0; r < 2; ++r) {
+                if (i >= sc.lo[r] && i < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.x));
+                if (i + 1 >= sc.lo[r] && i + 1 < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.y));
               }
-              big[0] = quad_max(big[0]);
-              big[1] = quad_max(big[1]);
-            } else {
-              const uint4 w = ld_shared16(smem + L::VMAX + 16u * (step & 1));
-              big[0] = big[1] = max3(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z));
             }
-            float f[2];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-              const int e = max(ev[r], min(kMaxExp, ((__float_as_int(big[r]) >> 23) & 255) - 127));
-              f[r] = exp2_int(ev[r] - e);
-              ev[r] = e;
-              down[r] = exp2_int(-e);
-            }
-            ok = rescale_o(f[0], f[1]);
-            if (!ok) break;
+            big[0] = quad_max(big[0]);
+            big[1] = quad_max(big[1]);
+          } else {
+            const uint4 w = ld_shared16(smem + L::VMAX + 32u * s4);
+            big[0] = big[1] = fmaxf(max3(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z)),
+                                    __uint_as_float(w.w));
           }
-          ok = edge ? make_p<true>(sc, m, l, down, rescale_o) : make_p<false>(sc, m, l, down, rescale_o);
-          if (!ok) break;
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(kPFull + half));
-        }
-        if (ok) {
+          float f[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+            const int e = max(ev[r], min(kMaxExp, ((__float_as_int(big[r]) >> 23) & 255) - 127));
+            f[r] = exp2_int(ev[r] - e);
+            ev[r] = e;
+            down[r] = exp2_int(-e);
           }
-          ok = wait(kPv + half, phase ^ 1u);
+          ok = rescale_o(f[0], f[1]);
+          if (!ok) break;
         }
-        if (ok) {
-          tc_fence_after();
-          fold(true);
-          tc_fence_before();
-          if (!whole && t == 0) {
+        ok = edge ? make_p<true>(sc, m, l, down, rescale_o) : make_p<false>(sc, m, l, down, rescale_o);
+        if (!ok) break;
+        tc_fence_before();
+        arrive(kPFull + (step & 1));
+        const bool last = j == n - 1;
+        if (j % kChain == kChain - 1 || last) {  // the chain's units for the sums, in the place of the one before last
+          const int o = chain & 1;
+          if (last) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              slot[(int64_t)kRows * D + own0 + 8 * r] = m[r];
-              slot[(int64_t)kRows * D + kRows + own0 + 8 * r] = l[r];
+              l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+              l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
             }
           }
+          if (chain >= 2) ok = wait(kOFree + o, (uint32_t)(chain / 2 - 1) & 1u);
+          if (!ok) break;
+          if (t == 0) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const uint32_t at = 4u * (o * kRows + own0 + 8 * r);
+              asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + L::M + at), "f"(m[r]) : "memory");
+              if (last) asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + L::LT + at), "f"(l[r]) : "memory");
+              if constexpr (I8) asm volatile("st.shared.b32 [%0], %1;" ::"r"(smem + L::EV + at), "r"(ev[r]) : "memory");
+            }
+          }
+          arrive(kMFull + o);
+          ++chain;
         }
-      } else {
-        step += n;
       }
-      if (ok && !whole && x.first == 0 && warp == 4 && lane == 0)
-        *divided = {x.last_block, x.h, x.row0, x.n, x.r0, x.rows};
+      tile0 += 2 * n;
       piece_done(k);
     }
     if (!ok && lane == 0) give_up();
@@ -854,7 +933,7 @@ template <int D, bool I8>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v, Divided* divided) {
-  using L = Layout<D>;
+  using L = Layout<D, I8>;
   extern __shared__ __align__(1024) uint8_t base[];
   const uint32_t smem = smem_u32(base);
   volatile int* abort = reinterpret_cast<volatile int*>(base + L::MISC);
@@ -866,22 +945,28 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     return;
   }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(smem + L::BARS + 8u * (kFull + s), kProducers);  // a warp each
-      mbar_init(smem + L::BARS + 8u * (kEmpty + s), 1);  // the MMAs
+    auto init = [&](int i, int count) { mbar_init(smem + L::BARS + 8u * i, count); };
+    for (int s = 0; s < L::STAGES; ++s) {
+      init(kFull + s, kHelpers);
+      init(kEmpty + s, 1);
     }
-    for (int h = 0; h < 2; ++h) {
-      mbar_init(smem + L::BARS + 8u * (kScale + h), kProducers);
-      mbar_init(smem + L::BARS + 8u * (kQ + h), 8);      // a softmax warp each
-      mbar_init(smem + L::BARS + 8u * (kSFull + h), 1);
-      mbar_init(smem + L::BARS + 8u * (kPFull + h), 8);
-      mbar_init(smem + L::BARS + 8u * (kPv + h), 1);
+    for (int s = 0; s < kSteps; ++s) init(kScale + s, kHelpers);
+    init(kQ, kSoftmax);
+    init(kPv, 1);
+    for (int i = 0; i < 2; ++i) {
+      init(kSFull + i, 1);
+      init(kPFull + i, kSoftmax);
+      init(kOFull + i, 1);
+      init(kOFree + i, 4);
+      init(kMFull + i, kSoftmax);
+      init(kPieceFull + i, 1);
+      init(kPieceFree + i, kThreads / 32);
     }
-    mbar_init(smem + L::BARS + 8u * kDrain, 1);
-    mbar_init(smem + L::BARS + 8u * kRaw, 1);
-    for (int i = 0; i < kPieces; ++i) {
-      mbar_init(smem + L::BARS + 8u * (kPieceFull + i), 1);
-      mbar_init(smem + L::BARS + 8u * (kPieceFree + i), kThreads / 32 - 1);  // every warp but warp 1
+    init(kDrain, 1);
+    init(kEdge, 1);
+    for (int s = 0; s < L::RAW_STAGES; ++s) {
+      init(kRawFull + s, 1);
+      init(kRawEmpty + s, kHelpers);
     }
     *abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -893,10 +978,18 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
   __syncthreads();
   tc_fence_after();
   const Kernel<D, I8> k{a, map_k, map_v, smem, __shfl_sync(0xffffffffu, *tmem_slot, 0), abort,
-                         reinterpret_cast<Piece*>(base + L::PIECES)};
-  if (warp == 0) k.issuer();
-  else if (warp < 4) k.producer(run);
-  else k.softmax((warp - 4) >> 3, divided + blockIdx.x);
+                        reinterpret_cast<Piece*>(base + L::PIECES)};
+  // 96 registers a thread at the start; 3 x 72 + 2 x 128 <= 5 x 96
+  if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 0) k.issuer();
+    else if (warp == 1) k.loader(run);
+    else if (warp < 8) k.helper();
+    else k.sums(divided + blockIdx.x);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+    k.softmax();
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 0) {
@@ -942,7 +1035,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Attn
 
 template <int D, bool I8>
 spl_status launch(const AttnArgs& a, int blocks, cudaStream_t stream) {
-  constexpr uint32_t smem = Layout<D>::SMEM;
+  constexpr uint32_t smem = Layout<D, I8>::SMEM;
   if (cudaFuncSetAttribute(attention_tc_kernel<D, I8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
       cudaSuccess)
     return SPL_ECUDA;
