@@ -666,67 +666,69 @@ struct Kernel {
     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
     return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
   }
-  // The scores of keys 64 c .. 64 c + 63: times the keys' scales, the hidden ones -inf, the bad ones NaN.
+  // The scores of keys 32 c .. 32 c + 31: times the keys' scales, the hidden ones -inf, the bad ones NaN.
   template <bool EDGE>
-  static __device__ __forceinline__ void prepare(const Scores& x, int c, uint32_t (&s)[32]) {
+  static __device__ __forceinline__ void prepare(const Scores& x, int c, uint32_t (&s)[16]) {
     const int t = threadIdx.x & 3;
     if constexpr (I8) {
 #pragma unroll
-      for (int b = 0; b < 8; ++b) {
-        const uint2 w = ld_shared8(x.ks + 256u * c + 32u * b + 8u * t);
+      for (int b = 0; b < 4; ++b) {
+        const uint2 w = ld_shared8(x.ks + 128u * c + 32u * b + 8u * t);
         mul2(s[4 * b], s[4 * b + 1], w.x, w.y);
         mul2(s[4 * b + 2], s[4 * b + 3], w.x, w.y);
       }
     }
     if constexpr (EDGE) {
       if constexpr (!I8) {
-        const uint2 bad = ld_shared8(x.bad + 8u * c);
-        if (bad.x | bad.y) {
+        uint32_t bad;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(bad) : "r"(x.bad + 4u * c));
+        if (bad) {
 #pragma unroll
-          for (int b = 0; b < 8; ++b) {
-            const uint32_t m = (b < 4 ? bad.x : bad.y) >> (8 * (b & 3) + 2 * t);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (m >> (i & 1) & 1u) s[4 * b + i] = 0x7fc00000u;
-          }
+          for (int i = 0; i < 16; ++i)
+            if (bad >> (8 * (i >> 2) + 2 * t + (i & 1)) & 1u) s[i] = 0x7fc00000u;
         }
       }
-      // of the thread's keys, 8 b + {0, 1} from 64 c + 2 t on, a row sees [lo, hi)
-      const int lo[2] = {x.lo[0] - 64 * c - 2 * t, x.lo[1] - 64 * c - 2 * t};
-      const int hi[2] = {x.hi[0] - 64 * c - 2 * t, x.hi[1] - 64 * c - 2 * t};
+      // of the thread's keys, 8 b + {0, 1} from 32 c + 2 t on, a row sees [lo, hi)
+      const int lo[2] = {x.lo[0] - 32 * c - 2 * t, x.lo[1] - 32 * c - 2 * t};
+      const int hi[2] = {x.hi[0] - 32 * c - 2 * t, x.hi[1] - 32 * c - 2 * t};
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (8 * (i >> 2) + (i & 1) >= hi[i >> 1 & 1]) s[i] = 0xff800000u;
-      if (__any_sync(0xffffffffu, lo[0] > -2 || lo[1] > -2)) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (8 * (i >> 2) + (i & 1) < lo[i >> 1 & 1]) s[i] = 0xff800000u;
+      for (int i = 0; i < 16; ++i) {
+        const int j = 8 * (i >> 2) + (i & 1), r = i >> 1 & 1;
+        if (j < lo[r] || j >= hi[r]) s[i] = 0xff800000u;
       }
     }
   }
+  // Over the chunks of 32 scores, the load of one beside the work on the one before it.  The loops are kept short: the
+  // roles' code together does not fit the instruction caches when this is unrolled over the whole tile.
+  template <class Take>
+  static __device__ __forceinline__ void over_chunks(uint32_t ts, Take take) {
+    uint32_t s[2][16];
+    tmem_ld_16x32(ts, s[0]);
+#pragma unroll 1
+    for (int c = 0; c < 4; c += 2) {
+      tmem_ld_wait(s[0]);
+      tmem_ld_16x32(ts + 32u * (c + 1), s[1]);
+      take(c, s[0]);
+      tmem_ld_wait(s[1]);
+      if (c == 0) tmem_ld_16x32(ts + 64u, s[0]);
+      take(c + 1, s[1]);
+    }
+  }
   // Scores to probabilities, in place in tensor memory.  Where a row's scores pass its maximum by more than kLazy it is
-  // raised, and what was made with the old one is rescaled.  p = 2^(row_scale s + base); of a chunk of 32 columns the
-  // high halves (times the values' scales) take the first 16, the low ones the others.  The high half is p cut to 11 bits.
+  // raised, and what was made with the old one is rescaled.  p = 2^(row_scale s + base), held in binary16 as hi + lo (times
+  // the values' scales); of a chunk of 32 columns the high halves take the first 16, the low ones the others.  The high
+  // half is p cut to 11 bits.
   template <bool EDGE, class Rescale>
   static __device__ __forceinline__ bool make_p(const Scores& x, float (&m)[2], float (&l)[2], const float (&down)[2],
                                                 Rescale rescale_o) {
     const int t = threadIdx.x & 3;
-    uint32_t s[2][32];
-    tmem_ld_16x64(x.ts, s[0]);
-    tmem_ld_16x64(x.ts + 64u, s[1]);
-    tmem_ld_wait(s[0]);
-    tmem_ld_wait(s[1]);
     float top[2] = {-INFINITY, -INFINITY};
+    over_chunks(x.ts, [&](int c, uint32_t (&s)[16]) {
+      prepare<EDGE>(x, c, s);
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      prepare<EDGE>(x, c, s[c]);
-      float u[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-      for (int i = 0; i < 32; i += 2)
-        u[i >> 1 & 1] = max3(u[i >> 1 & 1], __uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1]));
-      top[0] = fmaxf(top[0], u[0]);
-      top[1] = fmaxf(top[1], u[1]);
-    }
+      for (int i = 0; i < 16; i += 2)
+        top[i >> 1 & 1] = max3(top[i >> 1 & 1], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+    });
     bool raise[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -753,47 +755,44 @@ struct Kernel {
       sum[r] = p2(0.f, 0.f);
     }
     const unsigned long long minus1 = p2(-1.f, -1.f), zero2 = p2(-0.f, -0.f);
+    over_chunks(x.ts, [&](int c, uint32_t (&s)[16]) {
+      prepare<EDGE>(x, c, s);
+      uint32_t hi[8], lo[8];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+      for (int b = 0; b < 4; ++b) {
+        uint2 w = make_uint2(0u, 0u);
+        if constexpr (I8) w = ld_shared8(x.vs + 128u * c + 32u * b + 8u * t);
 #pragma unroll
-      for (int b0 = 0; b0 < 8; b0 += 4) {
-        uint32_t hi[8], lo[8];
-#pragma unroll
-        for (int b = b0; b < b0 + 4; ++b) {
-          uint2 w = make_uint2(0u, 0u);
-          if constexpr (I8) w = ld_shared8(x.vs + 256u * c + 32u * b + 8u * t);
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float s0 = __uint_as_float(s[c][4 * b + 2 * r]), s1 = __uint_as_float(s[c][4 * b + 2 * r + 1]);
-            float t0, t1;
-            up2(fma2(p2(s0, s1), scale2[r], base2[r]), t0, t1);
-            if constexpr (EDGE) {  // -inf times a scale of 0
-              t0 = s0 == -INFINITY ? s0 : t0;
-              t1 = s1 == -INFINITY ? s1 : t1;
-            }
-            unsigned long long p = p2(exp2_approx(t0), exp2_approx(t1));
-            sum[r] = add2(sum[r], p);
-            if constexpr (I8) {
-              p = fma2(p, fma2(p2(__uint_as_float(w.x), __uint_as_float(w.y)), p2(down[r], down[r]), zero2), zero2);
-              if constexpr (EDGE) {  // a hidden value's scale may be anything
-                float p0, p1;
-                up2(p, p0, p1);
-                p = p2(s0 == -INFINITY ? 0.f : p0, s1 == -INFINITY ? 0.f : p1);
-              }
-            }
-            float p0, p1, r0, r1;
-            up2(p, p0, p1);
-            const float h0 = __uint_as_float(__float_as_uint(p0) & 0xffffe000u);
-            const float h1 = __uint_as_float(__float_as_uint(p1) & 0xffffe000u);
-            up2(fma2(p2(h0, h1), minus1, p), r0, r1);
-            hi[2 * (b - b0) + r] = pack_f16(h0, h1);
-            lo[2 * (b - b0) + r] = pack_f16(r0, r1);
+        for (int r = 0; r < 2; ++r) {
+          const float s0 = __uint_as_float(s[4 * b + 2 * r]), s1 = __uint_as_float(s[4 * b + 2 * r + 1]);
+          float t0, t1;
+          up2(fma2(p2(s0, s1), scale2[r], base2[r]), t0, t1);
+          if constexpr (EDGE) {  // -inf times a scale of 0
+            t0 = s0 == -INFINITY ? s0 : t0;
+            t1 = s1 == -INFINITY ? s1 : t1;
           }
+          unsigned long long p = p2(exp2_approx(t0), exp2_approx(t1));
+          sum[r] = add2(sum[r], p);
+          if constexpr (I8) {
+            p = fma2(p, fma2(p2(__uint_as_float(w.x), __uint_as_float(w.y)), p2(down[r], down[r]), zero2), zero2);
+            if constexpr (EDGE) {  // a hidden value's scale may be anything
+              float p0, p1;
+              up2(p, p0, p1);
+              p = p2(s0 == -INFINITY ? 0.f : p0, s1 == -INFINITY ? 0.f : p1);
+            }
+          }
+          float p0, p1, r0, r1;
+          up2(p, p0, p1);
+          const float h0 = __uint_as_float(__float_as_uint(p0) & 0xffffe000u);
+          const float h1 = __uint_as_float(__float_as_uint(p1) & 0xffffe000u);
+          up2(fma2(p2(h0, h1), minus1, p), r0, r1);
+          hi[2 * b + r] = pack_f16(h0, h1);
+          lo[2 * b + r] = pack_f16(r0, r1);
         }
-        tmem_st_16x16(x.ts + 64u * c + 8u * b0, hi);
-        tmem_st_16x16(x.ts + 64u * c + 8u * b0 + 16u, lo);
       }
-    }
+      tmem_st_16x16(x.ts + 32u * c, hi);
+      tmem_st_16x16(x.ts + 32u * c + 16u, lo);
+    });
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       float p0, p1;
