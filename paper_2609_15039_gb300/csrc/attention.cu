@@ -103,7 +103,7 @@ __device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8
       const int stage = it % F::STAGES;
       const uint32_t at = base + stage * F::STAGE, full = bars + 8u * stage;
       if (it >= F::STAGES) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (F::STAGES + stage), (uint32_t)(it / F::STAGES - 1) & 1u,
+        ok = __all_sync(0xffffffffu, mbar_wait_soon(bars + 8u * (F::STAGES + stage), (uint32_t)(it / F::STAGES - 1) & 1u,
                                                kWaitNs, abort));
         if (!ok) break;
       }
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       const int stage = it % F::STAGES;
       const uint8_t* at = smem + stage * F::STAGE;
       const bool there =
-          __all_sync(0xffffffffu, mbar_wait(bars + 8u * stage, (uint32_t)(it / F::STAGES) & 1u, kWaitNs, abort));
+          __all_sync(0xffffffffu, mbar_wait_soon(bars + 8u * stage, (uint32_t)(it / F::STAGES) & 1u, kWaitNs, abort));
       if (!there && lane == 0) {
         *abort = 1;
         atomicOr(a.batch.status, kStatusTimeout);
@@ -523,9 +523,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
 template <int D, bool I8>
 spl_status launch_rows(const AttnArgs& a, int blocks, cudaStream_t stream) {
   constexpr uint32_t smem = Frag<D, I8>::SMEM;
-  if (cudaFuncSetAttribute(attention_rows_kernel<D, I8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
-      cudaSuccess)
-    return SPL_ECUDA;
+  static bool done[kMaxDevices] = {false};
+  if (!allow_shared(reinterpret_cast<const void*>(attention_rows_kernel<D, I8>), smem, done)) return SPL_ECUDA;
   attention_rows_kernel<D, I8><<<blocks, kThreads, smem, stream>>>(a);
   return launch_status();
 }

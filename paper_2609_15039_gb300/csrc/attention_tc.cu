@@ -160,7 +160,7 @@ struct Kernel {
 
   __device__ uint32_t bar(int i) const { return smem + L::BARS + 8u * i; }
   __device__ bool wait(int i, uint32_t parity) const {
-    return __all_sync(0xffffffffu, mbar_wait(bar(i), parity, kWaitNs, abort));
+    return __all_sync(0xffffffffu, mbar_wait_soon(bar(i), parity, kWaitNs, abort));
   }
   // One arrival for the warp, after all its lanes' work.
   __device__ void arrive(int i) const {
@@ -1035,9 +1035,8 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Attn
 template <int D, bool I8>
 spl_status launch(const AttnArgs& a, int blocks, cudaStream_t stream) {
   constexpr uint32_t smem = Layout<D, I8>::SMEM;
-  if (cudaFuncSetAttribute(attention_tc_kernel<D, I8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
-      cudaSuccess)
-    return SPL_ECUDA;
+  static bool done[kMaxDevices] = {false};
+  if (!allow_shared(reinterpret_cast<const void*>(attention_tc_kernel<D, I8>), smem, done)) return SPL_ECUDA;
   Divided* divided = reinterpret_cast<Divided*>(a.slots + (int64_t)blocks * 2 * slot_floats<D>());
   CUtensorMap map_k = {}, map_v = {};
   if (!I8) {

@@ -61,6 +61,11 @@ inline spl_status launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, si
   return e == cudaSuccess ? SPL_OK : SPL_ECUDA;
 }
 
+// Allows a kernel `bytes` of dynamic shared memory on the current device; asked of the driver once a device.  `done`: the
+// kernel's own, one flag a device.
+constexpr int kMaxDevices = 64;
+bool allow_shared(const void* kernel, size_t bytes, bool (&done)[kMaxDevices]);
+
 // Number of SMs of the current device (cached per device).
 int device_sm_count();
 // Compute capability major*10+minor of the current device.

@@ -80,6 +80,20 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, unsigne
     }
   }
 }
+// The same, for waits that are short and on the critical path: the clock is read only after 64 tries.
+__device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity, unsigned long long budget_ns,
+                                               volatile int* abort) {
+  unsigned long long deadline = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try(bar, parity)) return true;
+    if ((it & 63u) == 0u) {
+      if (abort && *abort) return false;
+      const unsigned long long now = now_ns();
+      if (deadline == 0) deadline = now + budget_ns;
+      if (now > deadline) return false;
+    }
+  }
+}
 // L2 eviction policies: a product's weight tiles are streamed (first out), its A tiles are re-read by every
 // output tile of the row block and the rows of C are wanted again in the epilogue (last out).
 __device__ __forceinline__ uint64_t l2_evict_first() {
@@ -215,6 +229,13 @@ __device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t (&r)[16])
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
                  "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_16x32(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::
+                   "r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+               "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[16]) {

@@ -8,7 +8,6 @@ namespace spl {
 
 namespace {
 std::atomic<uint64_t> g_launches{0};
-constexpr int kMaxDevices = 64;
 int g_sm_count[kMaxDevices] = {0};
 int g_cc[kMaxDevices] = {0};
 
@@ -20,6 +19,16 @@ int current_device() {
 }  // namespace
 
 void note_launches(uint64_t n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
+
+bool allow_shared(const void* kernel, size_t bytes, bool (&done)[kMaxDevices]) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
+  if (!done[dev]) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+    done[dev] = true;
+  }
+  return true;
+}
 
 int device_sm_count() {
   const int dev = current_device();
