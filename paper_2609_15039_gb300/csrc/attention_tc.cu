@@ -540,48 +540,60 @@ struct Kernel {
         if (last) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(l) : "r"(smem + L::LT + 4u * (o * kRows + own)));
         if constexpr (I8) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(ev) : "r"(smem + L::EV + 4u * (o * kRows + own)));
         const float keep = m_slot == -INFINITY ? 1.f : exp2_approx(m_slot - m) * (I8 ? exp2_int(ev_slot - ev) : 1.f);
-        const float unit = last && I8 ? exp2_int(ev) : 1.f;
-        const float f = out ? (l == 0.f ? 0.f : 1.0f / l) * unit : unit;
-        const bool add = !last && c > 0 && __all_sync(0xffffffffu, keep == 1.f);
-        float* dst = nullptr;
-        if (own < x.rows) {
-          const int fr = x.r0 + own;
-          dst = a.out + (int64_t)(x.row0 + fr / a.group) * a.ldo + (int64_t)(x.h * a.group + fr % a.group) * D;
-        }
-        const uint32_t from = tmem + lanes + L::O + (uint32_t)D * o;
-#pragma unroll 1
-        for (int d = 0; d < D; d += 32) {
-          float v[32];
-          tmem_ld_32x32(from + d, v);
-          float4 before = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float f = !out ? 1.f : (l == 0.f ? 0.f : 1.0f / l) * (I8 ? exp2_int(ev) : 1.f);
+        const bool mine = own < x.rows;  // the others' sums are nobody's
+        if (__any_sync(0xffffffffu, mine)) {
+          // The units have not changed: added where it lies, without waiting.  Else the slot's values are on their way
+          // while those before them are worked on.
+          const bool add = !out && c > 0 && __all_sync(0xffffffffu, keep == 1.f || !mine), fetch = c > 0 && !add && mine;
+          float* dst = a.out;
+          if (out && mine) {
+            const int fr = x.r0 + own;
+            dst += (int64_t)(x.row0 + fr / a.group) * a.ldo + (int64_t)(x.h * a.group + fr % a.group) * D;
+          }
+          const uint32_t from = tmem + lanes + L::O + (uint32_t)D * o;
+          const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+          float4 next[4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float4* at = slot4 + (d / 4 + i) * kRows;
-            float4 w = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            if (add) {  // the units have not changed: added where it lies, without waiting
-              asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1,%2,%3,%4};" ::"l"(at), "f"(w.x), "f"(w.y),
-                           "f"(w.z), "f"(w.w)
-                           : "memory");
-              continue;
+          for (int i = 0; i < 4; ++i) next[i] = fetch ? __ldcg(slot4 + i * kRows) : zero;
+#pragma unroll 1
+          for (int d = 0; d < D; d += 16) {
+            float v[16];
+            tmem_ld_32x16(from + d, v);
+            float4 w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              w[i] = make_float4(fmaf(next[i].x, keep, v[4 * i]), fmaf(next[i].y, keep, v[4 * i + 1]),
+                                 fmaf(next[i].z, keep, v[4 * i + 2]), fmaf(next[i].w, keep, v[4 * i + 3]));
+              next[i] = fetch && d + 16 < D ? __ldcg(slot4 + ((d + 16) / 4 + i) * kRows) : zero;
             }
-            if (c > 0) {
-              const float4 s = __ldcg(at);
-              w = make_float4(fmaf(s.x, keep, w.x), fmaf(s.y, keep, w.y), fmaf(s.z, keep, w.z), fmaf(s.w, keep, w.w));
+            if (!mine) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float4* at = slot4 + (d / 4 + i) * kRows;
+              if (add)
+                asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1,%2,%3,%4};" ::"l"(at), "f"(w[i].x), "f"(w[i].y),
+                             "f"(w[i].z), "f"(w[i].w)
+                             : "memory");
+              else if (!out)
+                *at = w[i];
+              else
+                w[i] = make_float4(w[i].x * f, w[i].y * f, w[i].z * f, w[i].w * f);
             }
-            w = make_float4(w.x * f, w.y * f, w.z * f, w.w * f);
-            if (!out) *at = w;
-            else if (dst && !wide) *reinterpret_cast<float4*>(dst + d + 4 * i) = w;
-            if (i & 1) {  // whole 32-byte sectors
-              if (out && dst && wide) st_global32(dst + d + 4 * (i - 1), before, w);
+            if (out && wide) {  // whole 32-byte sectors
+              st_global32(dst + d, w[0], w[1]);
+              st_global32(dst + d + 8, w[2], w[3]);
+            } else if (out) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(dst + d + 4 * i) = w[i];
             }
-            before = w;
           }
         }
         tc_fence_before();
         arrive(kOFree + o);
-        if (last && !out) {
-          slot[(int64_t)kRows * D + own] = m;
-          slot[(int64_t)kRows * D + kRows + own] = l;
+        if (last && !out) {  // the sums' exponent goes to the maximum
+          slot[(int64_t)kRows * D + own] = I8 ? m + (float)ev : m;
+          slot[(int64_t)kRows * D + kRows + own] = I8 ? l * exp2_int(-ev) : l;
         }
         m_slot = m;
         ev_slot = ev;
