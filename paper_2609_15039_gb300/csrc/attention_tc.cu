@@ -382,32 +382,40 @@ struct Kernel {
       fence_proxy_async_smem();
     }
   }
-  // A tile of int8 to binary16 in the MMAs' layout, and its scales (0 for keys that were not copied).
+  // A tile of int8 to binary16 in the MMAs' layout, and its scales (0 for keys that were not copied).  A thread has the
+  // same 16 dims of every KEY_STEP-th key; all its loads run side by side.
   __device__ bool widen(int tile, int step, bool v) const {
-    constexpr int THREADS = 32 * kHelpers, PARTS = D / 16, TOTAL = kKeys * PARTS;  // chunks of 16 values
+    constexpr int PARTS = D / 16, KEY_STEP = 32 * kHelpers / PARTS, PER = (kKeys + KEY_STEP - 1) / KEY_STEP;
     const int i = threadIdx.x - 64, lane = i & 31, stage = tile % STAGES, raw_stage = tile % L::RAW_STAGES;
     const uint32_t raw = smem + L::RAW + (uint32_t)raw_stage * L::RAW_STAGE;
-    const uint32_t base = smem + L::KV + (uint32_t)stage * L::TILE;
-    bool ok = wait(kRawFull + raw_stage, (uint32_t)(tile / L::RAW_STAGES) & 1u);
-    if (ok && tile >= STAGES) ok = wait(kEmpty + stage, (uint32_t)(tile / STAGES - 1) & 1u);
-    if (!ok) return false;
-#pragma unroll 3
-    for (int c = i; c < TOTAL; c += THREADS) {
-      const int key = c / PARTS, part = c % PARTS, c0 = (2 * part) & 7;  // two chunks of 8
-      const uint4 q = ld_shared16(raw + 16u * c);
-      const uint32_t row = base + (uint32_t)(part >> 2) * L::PANEL + key * 128;
-      const uint32_t w[4] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u, q.z ^ 0x80808080u, q.w ^ 0x80808080u};
+    const int part = i % PARTS, key0 = i / PARTS, c0 = (2 * part) & 7;  // two chunks of 8 values
+    const uint32_t panel = smem + L::KV + (uint32_t)stage * L::TILE + (uint32_t)(part >> 2) * L::PANEL;
+    if (!wait(kRawFull + raw_stage, (uint32_t)(tile / L::RAW_STAGES) & 1u)) return false;
+    uint4 q[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (key0 + KEY_STEP * k < kKeys) q[k] = ld_shared16(raw + (uint32_t)(key0 + KEY_STEP * k) * D + 16u * part);
+    float scale = 0.f;
+    uint32_t mask = 0u;
+    if (i < kKeys) {
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(mask) : "r"(raw + L::RAW_MASK));
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(raw + L::RAW_SCALE + 4u * i));
+      if (!(mask >> (i >> a.cache.page_shift) & 1u)) scale = 0.f;
+    }
+    arrive(kRawEmpty + raw_stage);
+    if (tile >= STAGES && !wait(kEmpty + stage, (uint32_t)(tile / STAGES - 1) & 1u)) return false;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int key = key0 + KEY_STEP * k;
+      if (key >= kKeys) break;
+      const uint32_t w[4] = {q[k].x ^ 0x80808080u, q[k].y ^ 0x80808080u, q[k].z ^ 0x80808080u, q[k].w ^ 0x80808080u};
+      const uint32_t row = panel + key * 128;
       st_shared16(row + ((c0 ^ (key & 7)) << 4), make_uint4(i8_pair(w[0], 0x4140u), i8_pair(w[0], 0x4342u),
                                                             i8_pair(w[1], 0x4140u), i8_pair(w[1], 0x4342u)));
       st_shared16(row + (((c0 + 1) ^ (key & 7)) << 4), make_uint4(i8_pair(w[2], 0x4140u), i8_pair(w[2], 0x4342u),
                                                                   i8_pair(w[3], 0x4140u), i8_pair(w[3], 0x4342u)));
     }
     if (i < kKeys) {
-      uint32_t mask;
-      float scale;
-      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(mask) : "r"(raw + L::RAW_MASK));
-      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(raw + L::RAW_SCALE + 4u * i));
-      if (!(mask >> (i >> a.cache.page_shift) & 1u)) scale = 0.f;
       asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + (v ? L::VS : L::KS) + (uint32_t)(step % kSteps) * (kKeys * 4) +
                                                    4u * i),
                    "f"(scale)
@@ -423,10 +431,7 @@ struct Kernel {
     }
     fence_proxy_async_smem();
     arrive(kFull + stage);
-    if (lane == 0) {
-      mbar_arrive(bar(kRawEmpty + raw_stage));
-      if (!v) mbar_arrive(bar(kScale + step % kSteps));
-    }
+    if (!v && lane == 0) mbar_arrive(bar(kScale + step % kSteps));
     return true;
   }
 
