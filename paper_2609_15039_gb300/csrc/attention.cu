@@ -558,7 +558,7 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
 // start and a tenth as much per unit.  Measured with 24 query heads on 8 (few rows, tensor cores): 16 rows over 2048 keys
 // 24, 27 us, over 8192 50, 39; 64 rows over 512 25, 35, over 2048 47, 42; 16 sequences of 8 rows over 128 22, 32, over
 // 512 41, 40.
-constexpr int64_t kFewUnits = 3000;
+constexpr int64_t kFewUnits = 1600;
 Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_heads) {
   const int d = (int)cache->head_dim, sms = device_sm_count();
   Shape s;

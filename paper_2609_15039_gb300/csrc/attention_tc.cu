@@ -993,6 +993,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();  // the join may be launched: it waits for this kernel's end
   const Kernel<D, I8> k{a, map_k, map_v, smem, __shfl_sync(0xffffffffu, *tmem_slot, 0), abort,
                         reinterpret_cast<Piece*>(base + L::PIECES)};
   // 96 registers a thread at the start; 3 x 72 + 2 x 128 <= 5 x 96
@@ -1019,6 +1020,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 constexpr int kJoinParts = 8, kJoinThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const AttnArgs a, const Divided* divided) {
+  pdl_wait();  // launched while the pieces are made
   const Divided x = divided[blockIdx.x];
   const int c0 = blockIdx.x, c1 = x.last_block;
   if (c1 <= c0) return;
@@ -1029,14 +1031,14 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Attn
     if (row >= x.rows) continue;
     auto slot = [&](int c) { return a.slots + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * slot_floats<D>(); };
     float m = -INFINITY;
-    for (int c = c0; c <= c1; ++c) m = fmaxf(m, __ldg(slot(c) + (int64_t)kRows * D + row));
+    for (int c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(slot(c) + (int64_t)kRows * D + row));
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll 4
     for (int c = c0; c <= c1; ++c) {
       const float* s = slot(c);
-      const float mc = __ldg(s + (int64_t)kRows * D + row), lc = __ldg(s + (int64_t)kRows * D + kRows + row);
-      const float4 p = __ldg(reinterpret_cast<const float4*>(s) + d4 * kRows + row);
+      const float mc = __ldcg(s + (int64_t)kRows * D + row), lc = __ldcg(s + (int64_t)kRows * D + kRows + row);
+      const float4 p = __ldcg(reinterpret_cast<const float4*>(s) + d4 * kRows + row);
       const float w = mc == -INFINITY ? 1.f : exp2_approx(mc - m);  // without keys: zeros, or NaN
       v = make_float4(fmaf(p.x, w, v.x), fmaf(p.y, w, v.y), fmaf(p.z, w, v.z), fmaf(p.w, w, v.w));
       l = fmaf(lc, w, l);
@@ -1066,8 +1068,8 @@ spl_status launch(const AttnArgs& a, int blocks, cudaStream_t stream) {
   attention_tc_kernel<D, I8><<<blocks, kThreads, smem, stream>>>(a, map_k, map_v, divided);
   const spl_status st = launch_status();
   if (st != SPL_OK) return st;
-  attention_join_kernel<D><<<dim3(blocks, kJoinParts), kJoinThreads, 0, stream>>>(a, divided);
-  return launch_status();
+  return launch_pdl(attention_join_kernel<D>, dim3(blocks, kJoinParts), dim3(kJoinThreads), 0, stream, a,
+                    static_cast<const Divided*>(divided));
 }
 
 }  // namespace
