@@ -68,7 +68,7 @@ struct Frag {
   static constexpr uint32_t SO = RING, SM = SO + 4 * kRT * D * 4, SL = SM + kWarps * kRT * 4;
   static constexpr uint32_t BARS = SL + kWarps * kRT * 4, MASK = BARS + 16 * STAGES, LAST = MASK + 4 * STAGES;
   static constexpr uint32_t SMEM = LAST + 8;
-  static_assert(SMEM <= 232448 && kMaxSeqs * 8 <= RING, "fits");
+  static_assert(SMEM <= 232448 && kMaxSeqs * kPrefixBytes <= RING, "fits");
   // dim of column n of n-block nb
   static __device__ __forceinline__ int v_dim(int nb, int n) { return (nb / VE) * 8 * VE + n * VE + nb % VE; }
 };
@@ -549,8 +549,9 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
   spl_status st = paged_cache_view(c, cache);
   if (st != SPL_OK) return st;
   if (q_heads < 1 || q_heads % cache->kv_heads != 0 || rows < 0) return SPL_EINVAL;
-  if (q_heads / cache->kv_heads > 1024 || rows * (q_heads / cache->kv_heads) > INT32_MAX / 2) return SPL_ESHAPE;
-  return paged_batch_view(b, batch, rows);
+  if (q_heads / cache->kv_heads > 1024 || rows > INT32_MAX / 2 / (q_heads / cache->kv_heads))
+    return SPL_ESHAPE;
+  return paged_batch_view(b, *c, batch, rows);
 }
 
 // The few-row kernel where every sequence's rows of a key head fit its tile, or where the units (64 keys of a tile) that
@@ -563,7 +564,7 @@ Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_h
   const int d = (int)cache->head_dim, sms = device_sm_count();
   Shape s;
   const int64_t tiles = ceil_div(std::max<int64_t>(batch->max_rows, 1) * (q_heads / cache->kv_heads), kRowsTile);
-  const int64_t units = ceil_div(batch->max_pages * cache->page_size, 64);
+  const int64_t units = cache->pages == 0 ? 0 : ceil_div(batch->max_pages * cache->page_size, 64);
   s.few = tiles == 1 || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;
   if (s.few) {
     s.blocks = sms;

@@ -55,8 +55,14 @@ __device__ __forceinline__ void tile_span(AttnTile& x, int group, int window) {
   x.units = max(1, (x.key_hi + U - 1) / U - x.unit0);
 }
 
-// A block's run of units.  `prefix` (shared, one entry a sequence) is filled by the constructor, which every thread of
+// a / b of numbers from 0 on, in 32 bits where they fit: a 64-bit division costs some hundred cycles.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// A block's run of units.  `prefix` (shared, kPrefixBytes a sequence) is filled by the constructor, which every thread of
 // the block calls; afterwards every thread walks the same tiles by itself.
+constexpr int kPrefixBytes = 8 + sizeof(PagedSeq);
 template <int RT, int U, int THREADS>
 struct AttnRun {
   AttnTile x;
@@ -65,6 +71,10 @@ struct AttnRun {
   int first;               // unit of the current tile at which the run stands
   const AttnArgs& a;
 
+  // The sequences, behind the prefix sums.
+  __device__ PagedSeq& kept(int64_t* prefix, int b) const {
+    return reinterpret_cast<PagedSeq*>(prefix + a.batch.seqs)[b];
+  }
   __device__ AttnRun(const AttnArgs& args, int64_t* prefix) : a(args) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int seqs = a.batch.seqs, heads = a.cache.heads;
@@ -72,6 +82,7 @@ struct AttnRun {
     for (int b = threadIdx.x; b < seqs; b += THREADS) {
       AttnTile y;
       y.s = paged_seq(a.batch, a.cache.page_shift, b);
+      kept(prefix, b) = y.s;
       const int tiles = (y.s.n * a.group + RT - 1) / RT;
       int64_t sum = 0;
       for (y.t = 0; tiles <= kFewTiles && y.t < tiles; ++y.t) {
@@ -84,7 +95,7 @@ struct AttnRun {
     for (int b = warp; b < seqs; b += THREADS / 32) {
       if (prefix[b] >= 0) continue;
       AttnTile y;
-      y.s = paged_seq(a.batch, a.cache.page_shift, b);
+      y.s = kept(prefix, b);
       const int tiles = (y.s.n * a.group + RT - 1) / RT;
       int64_t sum = 0;
       for (y.t = lane; y.t < tiles; y.t += 32) {
@@ -115,8 +126,8 @@ struct AttnRun {
     total = seqs > 0 ? prefix[seqs - 1] : 0;
     blocks = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
     const int c = blockIdx.x;
-    at = c < blocks ? total * c / blocks : 0;
-    end = c < blocks ? total * (c + 1) / blocks : 0;
+    at = c < blocks ? quotient(total * c, blocks) : 0;
+    end = c < blocks ? quotient(total * (c + 1), blocks) : 0;
     if (at >= end) return;
     int lo = 0, hi = seqs - 1;  // the first sequence whose prefix passes `at`
     while (lo < hi) {
@@ -126,10 +137,10 @@ struct AttnRun {
     }
     x.b = lo;
     const int64_t before = lo > 0 ? prefix[lo - 1] : 0;
-    const int64_t per_head = (prefix[lo] - before) / heads;
-    x.h = (int)((at - before) / per_head);
-    int64_t rest = (at - before) % per_head;
-    x.s = paged_seq(a.batch, a.cache.page_shift, x.b);
+    const int64_t per_head = quotient(prefix[lo] - before, heads);
+    x.h = (int)quotient(at - before, per_head);
+    int64_t rest = at - before - x.h * per_head;
+    x.s = kept(prefix, x.b);
     const int tiles = (x.s.n * a.group + RT - 1) / RT;
     for (int t0 = 0;; t0 += 32) {  // the tile that holds unit `rest`, 32 at a time
       AttnTile y;
@@ -163,7 +174,7 @@ struct AttnRun {
   // Units [first, last()) of the tile are the block's piece.
   __device__ int last() const { return (int)min((int64_t)x.units, first + (end - at)); }
   __device__ bool whole() const { return first == 0 && last() == x.units; }
-  __device__ int block_of(int64_t unit) const { return (int)(((unit + 1) * blocks - 1) / total); }
+  __device__ int block_of(int64_t unit) const { return (int)quotient((unit + 1) * blocks - 1, total); }
   __device__ int first_block() const { return block_of(at - first); }
   __device__ int last_block() const { return block_of(at - first + x.units - 1); }
 

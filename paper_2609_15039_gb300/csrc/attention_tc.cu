@@ -85,7 +85,7 @@ struct Layout {
   static constexpr uint32_t BAD = VMAX + (I8 ? kSteps * 32 : 0), BARS = BAD + (I8 ? 0 : kSteps * 16);
   static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
   static_assert(BARS % 8 == 0 && PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
-  static_assert(kMaxSeqs * 8 <= AUX, "the prefix sums fit where the tiles go");
+  static_assert(kMaxSeqs * kPrefixBytes <= AUX, "the prefix sums fit where the tiles go");
   static constexpr uint32_t S = 0, O = 256;                // tensor memory columns (+ 128 and + D for the other place)
   static constexpr uint32_t IDESC_S = make_idesc(0, 128, kKeys);
   static constexpr uint32_t IDESC_O = make_idesc(0, 128, D) | (1u << 16);  // B: the values, dims contiguous
@@ -244,19 +244,44 @@ struct Kernel {
         mbar_wait(bar(first + t % stages), (uint32_t)(t / stages) & 1u, kDrainNs, nullptr);
     }
   }
+  // The first slots of a piece's boxes (a page's tokens, at most 128), those of kAhead tiles in a lane each, -1 where no
+  // row sees any key of them; those of the next kAhead tiles are looked up meanwhile.
+  static constexpr int kAhead = 4;
+  struct Boxes {
+    const Kernel& k;
+    const Piece& x;
+    int box, per_tile, shift;
+    uint64_t policy = l2_evict_last();  // other tiles of rows read the same keys
+    int64_t now, next;
+    __device__ Boxes(const Kernel& kernel, const Piece& piece) : k(kernel), x(piece) {
+      shift = k.a.cache.page_shift;
+      box = min(kKeys, 1 << shift);
+      per_tile = kKeys / box;
+      now = look_up(0);
+      next = look_up(kAhead);
+    }
+    __device__ int64_t look_up(int u0) const {
+      const int lane = threadIdx.x & 31, u = u0 + lane / per_tile, j = x.j0 + u * kKeys + lane % per_tile * box;
+      const int page = lane < kAhead * per_tile && u < x.tiles ? k.page_of(x, j, box) : -1;
+      return page >= 0 ? ((((int64_t)page * k.a.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : -1;
+    }
+    // The slot of the lane's box of tile u, which is in the window.
+    __device__ int64_t of(int u) const {
+      const int lane = threadIdx.x & 31, at = u % kAhead * per_tile + lane;
+      const int64_t a = __shfl_sync(0xffffffffu, now, at & 31), b = __shfl_sync(0xffffffffu, next, at & 31);
+      return lane >= per_tile ? -1 : (u >= base + kAhead ? b : a);
+    }
+    int base = 0;
+    __device__ void advance() {  // past the last tile of the window's first half
+      base += kAhead;
+      now = next;
+      next = look_up(base + kAhead);
+    }
+  };
   __device__ bool load_f16(const Piece& x, Loads& y) const {
-    const int lane = threadIdx.x & 31, n = x.tiles, shift = a.cache.page_shift;
-    const uint64_t policy = l2_evict_last();  // other tiles of rows read the same keys
-    // Boxes of a page's tokens, at most 128, a lane each; where no row sees any key of it the box lies past the pool's
-    // end and the copy fills it with zeros.
-    const int box = min(kKeys, 1 << shift), boxes = kKeys / box;
-    auto row_of = [&](int u) {
-      const int j = x.j0 + u * kKeys + lane * box;
-      const int page = lane < boxes && u < n ? page_of(x, j, box) : -1;
-      return page >= 0 ? (int)((((int64_t)page * a.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1)))
-                       : (int)((int64_t)a.cache.pages * a.cache.heads << shift);
-    };
-    int row[4] = {row_of(0), row_of(1), row_of(2), 0};  // of step u at u % 4
+    const int lane = threadIdx.x & 31, n = x.tiles;
+    Boxes boxes(*this, x);
+    const int none = (int)((int64_t)a.cache.pages * a.cache.heads << boxes.shift);  // past the pool: filled with zeros
     bool ok = true;
     for (int i = 0; ok && i < 2 * n; ++i, ++y.tile) {
       int u;
@@ -272,34 +297,21 @@ struct Kernel {
         mbar_expect_tx(bar(to), L::TILE);
         if (!edge) mbar_arrive_more(bar(to), kHelpers - 1);
       }
-      __syncwarp();
-      const int at = (u & 3) == 0 ? row[0] : (u & 3) == 1 ? row[1] : (u & 3) == 2 ? row[2] : row[3];
-      if (lane < boxes) {
-        const uint32_t dst = smem + L::KV + (uint32_t)stage * L::TILE + (uint32_t)(lane * box) * 128u;
+      const int64_t slot = boxes.of(u);
+      if (lane < boxes.per_tile) {
+        const uint32_t dst = smem + L::KV + (uint32_t)stage * L::TILE + (uint32_t)(lane * boxes.box) * 128u;
 #pragma unroll
         for (int p = 0; p < L::PANELS; ++p)
-          tma_load_2d(dst + p * L::PANEL, v ? &map_v : &map_k, bar(to), 64 * p, at, policy);
+          tma_load_2d(dst + p * L::PANEL, v ? &map_v : &map_k, bar(to), 64 * p, slot >= 0 ? (int)slot : none, boxes.policy);
       }
       __syncwarp();
-      if (v) {  // two steps ahead of the next K
-        const int next = row_of(u + 3);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (((u + 3) & 3) == q) row[q] = next;
-      }
+      if (v && u % kAhead == kAhead - 1) boxes.advance();
     }
     return ok;
   }
   __device__ bool load_i8(const Piece& x, Loads& y) const {
-    const int lane = threadIdx.x & 31, n = x.tiles, shift = a.cache.page_shift;
-    const uint64_t policy = l2_evict_last();
-    const int box = min(kKeys, 1 << shift), boxes = kKeys / box;  // of a page's tokens, a lane each
-    auto slot_of = [&](int u) -> int64_t {
-      const int j = x.j0 + u * kKeys + lane * box;
-      const int page = lane < boxes && u < n ? page_of(x, j, box) : -1;
-      return page >= 0 ? ((((int64_t)page * a.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : -1;
-    };
-    int64_t slot[2] = {slot_of(0), slot_of(1)};  // of step u at u % 2
+    const int lane = threadIdx.x & 31, n = x.tiles;
+    Boxes boxes(*this, x);
     bool ok = true;
     for (int i = 0; ok && i < 2 * n; ++i, ++y.tile) {
       int u;
@@ -307,26 +319,22 @@ struct Kernel {
       const int stage = y.tile % L::RAW_STAGES;
       if (y.tile >= L::RAW_STAGES) ok = wait(kRawEmpty + stage, (uint32_t)(y.tile / L::RAW_STAGES - 1) & 1u);
       if (!ok) break;
-      const int64_t at = (u & 1) ? slot[1] : slot[0];
+      const int64_t slot = boxes.of(u);
       const uint32_t raw = smem + L::RAW + (uint32_t)stage * L::RAW_STAGE, full = bar(kRawFull + stage);
-      const uint32_t mask = __ballot_sync(0xffffffffu, at >= 0);  // of boxes
+      const uint32_t mask = __ballot_sync(0xffffffffu, slot >= 0);  // of boxes
       if (lane == 0) {
         asm volatile("st.shared.b32 [%0], %1;" ::"r"(raw + L::RAW_MASK), "r"(mask) : "memory");
-        mbar_expect_tx(full, (uint32_t)(__popc(mask) * box * (D + 4)));
+        mbar_expect_tx(full, (uint32_t)(__popc(mask) * boxes.box * (D + 4)));
       }
       __syncwarp();
-      if (at >= 0) {
-        bulk_load(raw + (uint32_t)(lane * box) * D, static_cast<const char*>(v ? a.cache.v : a.cache.k) + at * D,
-                  (uint32_t)box * D, full, policy);
-        bulk_load(raw + L::RAW_SCALE + (uint32_t)(lane * box) * 4u, (v ? a.cache.v_scale : a.cache.k_scale) + at,
-                  (uint32_t)box * 4u, full, policy);
+      if (slot >= 0) {
+        bulk_load(raw + (uint32_t)(lane * boxes.box) * D, static_cast<const char*>(v ? a.cache.v : a.cache.k) + slot * D,
+                  (uint32_t)boxes.box * D, full, boxes.policy);
+        bulk_load(raw + L::RAW_SCALE + (uint32_t)(lane * boxes.box) * 4u, (v ? a.cache.v_scale : a.cache.k_scale) + slot,
+                  (uint32_t)boxes.box * 4u, full, boxes.policy);
       }
       __syncwarp();
-      if (v) {  // two steps ahead; the next K's is there
-        const int64_t next = slot_of(u + 2);
-        if (u & 1) slot[1] = next;
-        else slot[0] = next;
-      }
+      if (v && u % kAhead == kAhead - 1) boxes.advance();
     }
     return ok;
   }
@@ -1061,7 +1069,6 @@ spl_status launch(const AttnArgs& a, int blocks, cudaStream_t stream) {
   if (!I8) {
     const int64_t slots = (int64_t)a.cache.pages * a.cache.heads << a.cache.page_shift;
     const int box = std::min(kKeys, 1 << a.cache.page_shift);
-    if (slots > INT32_MAX - kKeys) return SPL_ESHAPE;  // rows of a copy's coordinates
     if (!tma_panel_map(&map_k, a.cache.k, slots, D, box) || !tma_panel_map(&map_v, a.cache.v, slots, D, box))
       return SPL_ECUDA;
   }
