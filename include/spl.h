@@ -595,8 +595,8 @@ typedef enum spl_kv_format { SPL_KV_F16 = 0, SPL_KV_I8 = 1 } spl_kv_format;
 /* One layer's cache: `pages` pages of page_size tokens (16, 32, 64, 128 or 256).
  * k, v [pages, kv_heads, page_size, head_dim] binary16 or int8; k_scale, v_scale
  * [pages, kv_heads, page_size] fp32 for I8 (not read for F16).  head_dim 64 or
- * 128, kv_heads up to 1024.  Device pointers owned by the caller, 16-byte
- * aligned. */
+ * 128, kv_heads up to 1024, pages kv_heads page_size below 2^31 - 1024.  Device
+ * pointers owned by the caller, 16-byte aligned. */
 typedef struct spl_kv_cache {
   void* k;
   void* v;
@@ -606,9 +606,10 @@ typedef struct spl_kv_cache {
   spl_kv_format format;
 } spl_kv_cache;
 
-/* A ragged batch of up to 4096 sequences, device arrays (4-byte aligned).  Rows row_start[b] ..
- * row_start[b + 1] - 1 are the new tokens of sequence b, in order, its last
- * ones: kv_len[b] counts them, and row i of n stands at position
+/* A ragged batch of up to 4096 sequences of up to 2^30 tokens (max_pages
+ * page_size), device arrays (4-byte aligned).  Rows row_start[b] .. row_start[b
+ * + 1] - 1 are the new tokens of sequence b, in order, its last ones: kv_len[b]
+ * counts them, and row i of n stands at position
  * kv_len[b] - n + i.  Token j of sequence b is in page
  * page_table[b, j / page_size] at place j % page_size.  max_rows: the most rows
  * of any sequence, or more (only the choice of kernel goes by it). */

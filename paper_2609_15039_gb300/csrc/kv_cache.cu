@@ -155,6 +155,7 @@ spl_status paged_cache_view(PagedCache* out, const spl_kv_cache* c) {
   while (shift < 8 && (int64_t(1) << shift) != c->page_size) ++shift;
   if ((int64_t(1) << shift) != c->page_size) return SPL_ESHAPE;
   if (c->pages > INT32_MAX || c->kv_heads > 1024) return SPL_ESHAPE;
+  if (c->pages * c->kv_heads * c->page_size > INT32_MAX - 1024) return SPL_ESHAPE;  // rows of a copy's coordinates
   const bool i8 = c->format == SPL_KV_I8;
   if (c->pages > 0 && (!c->k || !c->v || (i8 && (!c->k_scale || !c->v_scale)))) return SPL_EINVAL;
   if (!aligned16(c->k) || !aligned16(c->v) || (i8 && (!aligned16(c->k_scale) || !aligned16(c->v_scale))))
@@ -163,9 +164,10 @@ spl_status paged_cache_view(PagedCache* out, const spl_kv_cache* c) {
   return SPL_OK;
 }
 
-spl_status paged_batch_view(PagedBatch* out, const spl_kv_batch* b, int64_t rows) {
+spl_status paged_batch_view(PagedBatch* out, const PagedCache& cache, const spl_kv_batch* b, int64_t rows) {
   if (!b || b->seqs < 0 || b->max_pages < 0 || b->max_rows < 0 || rows < 0) return SPL_EINVAL;
-  if (b->seqs > kMaxSeqs || rows > INT32_MAX || b->max_pages > (int64_t(1) << 26)) return SPL_ESHAPE;
+  if (b->seqs > kMaxSeqs || rows > INT32_MAX || b->max_pages > INT32_MAX) return SPL_ESHAPE;
+  if (b->max_pages << cache.page_shift > kMaxLength) return SPL_ESHAPE;
   if (b->seqs > 0 && (!b->row_start || !b->kv_len || (b->max_pages > 0 && !b->page_table))) return SPL_EINVAL;
   if (!aligned4(b->row_start) || !aligned4(b->kv_len) || !aligned4(b->page_table)) return SPL_EALIGN;
   *out = {b->row_start, b->kv_len, b->page_table, (int)b->seqs, b->max_pages, rows, nullptr};
@@ -187,7 +189,7 @@ extern "C" spl_status spl_kv_append(const spl_kv_cache* cache, const spl_kv_batc
   if (rows > 0 && batch->seqs > 0 && (!K || !V)) return SPL_EINVAL;
   if (rows > 1 && (ldk < width || ldv < width)) return SPL_EINVAL;
   if (!aligned16(K) || !aligned16(V) || (rows > 1 && (ldk % 4 != 0 || ldv % 4 != 0))) return SPL_EALIGN;
-  if ((st = paged_batch_view(&b, batch, rows)) != SPL_OK) return st;
+  if ((st = paged_batch_view(&b, c, batch, rows)) != SPL_OK) return st;
   if (rows == 0 || b.seqs == 0 || b.max_pages == 0 || c.pages == 0) return SPL_OK;
   if (!(b.status = device_status_word())) return SPL_ECUDA;
   auto launch = [&](auto kernel) {
@@ -209,7 +211,7 @@ extern "C" spl_status spl_kv_read(float* K, float* V, const spl_kv_cache* cache,
   if (out_rows > 0 && batch->seqs > 0 && (!K || !V || !out_start)) return SPL_EINVAL;
   if (out_rows > INT32_MAX) return SPL_ESHAPE;
   if (!aligned16(K) || !aligned16(V) || !aligned4(out_start)) return SPL_EALIGN;
-  if ((st = paged_batch_view(&b, batch, INT32_MAX)) != SPL_OK) return st;
+  if ((st = paged_batch_view(&b, c, batch, INT32_MAX)) != SPL_OK) return st;
   if (out_rows == 0 || b.seqs == 0 || b.max_pages == 0 || c.pages == 0) return SPL_OK;
   if (!(b.status = device_status_word())) return SPL_ECUDA;
   auto launch = [&](auto kernel) {

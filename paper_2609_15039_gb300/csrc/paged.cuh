@@ -76,8 +76,9 @@ __device__ __forceinline__ int paged_find(const int* start, int seqs, int64_t ro
 // Checks shared by the entries; fill the device's view of the cache and of the batch (but for its status word, which
 // an entry sets before it launches).
 spl_status paged_cache_view(PagedCache* out, const spl_kv_cache* cache);
-spl_status paged_batch_view(PagedBatch* out, const spl_kv_batch* batch, int64_t rows);
+spl_status paged_batch_view(PagedBatch* out, const PagedCache& cache, const spl_kv_batch* batch, int64_t rows);
 constexpr int kMaxSeqs = 4096;
+constexpr int64_t kMaxLength = int64_t(1) << 30;  // tokens of a sequence: positions and ends of tiles are 32-bit
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 }  // namespace spl

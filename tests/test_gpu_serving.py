@@ -424,3 +424,207 @@ def test_verify_draws_follow_the_target(spl):
     freq = torch.bincount(token.long(), minlength=vocab).double().cpu() / n
     want = p[0].double().cpu()
     assert bool((freq - want).abs().le(5 * (want * (1 - want) / n).sqrt()).all())
+
+
+# ---------------------------------------------------------------------------------- the kernel for many rows, at all sizes
+def many(c):
+    """The case with a bound on a chunk's rows that sends the call to the kernel for many rows, however few there are."""
+    batch = c.batch
+    c.batch = lambda all_rows=False: spl_batch_with_bound(c.spl, batch(all_rows))
+    return c
+
+
+def spl_batch_with_bound(spl, batch):
+    return spl.KVBatch(batch.row_start, batch.kv_len, batch.page_table, batch.rows, 1 << 24)
+
+
+def check_sample(c, samples, window=0, seed=0, scale=None):
+    """As Case.check, for some rows and heads; a probability's low half may lose an absolute 2^-33 of the row's largest
+    (hi rounded and lo rounded, each by 2^-25 of p's 2^9), which the n values that a row sees meet."""
+    got = c.attend(window, scale)
+    s = 1.0 / np.sqrt(c.d) if scale is None else scale
+    g = np.random.default_rng(seed)
+    group = c.hq // c.hk
+    num = den = 0.0
+    for b, (r, n) in enumerate(c.seqs):
+        if r == 0:
+            continue
+        k, v = c.stored("k", b), c.stored("v", b)
+        picks = {(0, 0), (r - 1, c.hq - 1)} | {(int(g.integers(r)), int(g.integers(c.hq))) for _ in range(samples)}
+        for i, h in picks:
+            kh = slice(h // group, h // group + 1)
+            q = c.q[c.start[b] + i:c.start[b] + i + 1, h:h + 1]
+            upto = max(0, min(n - r + i + 1, n))
+            ref, mass = serving.attention(q, k[:upto, kh], v[:upto, kh], upto, 1, s, window)
+            mine = got[c.start[b] + i, h]
+            if upto == 0:
+                assert np.all(mine == 0)
+                continue
+            tol = tolerance(q, k[:upto, kh], s, upto, 1, mass) + 2.0 ** -32 * upto * np.max(np.abs(v[:upto, kh]))
+            err = np.abs(mine.astype(np.float64) - ref[0, 0])
+            assert np.all(err <= tol[0, 0]), f"sequence {b} row {i} head {h}: {np.max(err / tol[0, 0]):.3g}"
+            num += float(np.sum((mine - ref[0, 0]) ** 2))
+            den += float(np.sum(ref ** 2))
+    assert not np.isnan(got).any() and num <= (1e-5 ** 2) * den
+    assert c.spl.spl_get_device_status() == c.spl.SPL_OK
+    return got
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("heads", HEADS, ids=str)
+@pytest.mark.parametrize("name", BATCHES)
+def test_many_rows(spl, name, heads, fmt):
+    c = many(Case(spl, BATCHES[name], heads, fmt, 16 if name == "ragged" else 256, seed=len(name)))
+    c.fill()
+    check_sample(c, 12)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("page", [16, 64, 128, 256])
+@pytest.mark.parametrize("window", [0, 1, 127, 128, 200, 1000])
+def test_many_rows_window(spl, window, page, fmt):
+    c = many(Case(spl, [(200, 900), (33, 1200), (130, 130), (150, 149 + page), (6, 2), (1, 0)], (4, 2, 64), fmt, page,
+                  seed=window))
+    c.fill()
+    check_sample(c, 16, window)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("heads,rows,keys", [((32, 8, 128), 512, 3000), ((16, 16, 64), 300, 7001), ((8, 8, 128), 129, 9000)],
+                         ids=str)
+@pytest.mark.parametrize("window", [0, 2500])
+def test_many_rows_long_pieces(spl, heads, rows, keys, window, fmt):
+    """Pieces of many accumulation chains, tiles divided among several blocks, int8 scales that grow along the keys."""
+    c = Case(spl, [(rows, keys), (2, 40)], heads, fmt, 64, seed=keys, std=2.0)
+    c.v[0] *= np.exp2(np.linspace(-6, 6, keys)).astype(np.float32)[:, None, None]
+    c.fill()
+    check_sample(c, 24, window)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("std,scale", [(6.0, None), (1.0, 0.0), (1.0, -0.3), (2.0, 1.0)])
+def test_many_rows_sharp_and_flat(spl, std, scale, fmt):
+    c = many(Case(spl, [(40, 777), (300, 1500)], (4, 1, 64), fmt, 64, seed=17, std=std))
+    c.fill()
+    check_sample(c, 30, scale=scale)
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("rows", [5, 48, 200, 400])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_many_rows_nan_reaches_only_rows_that_see_it(spl, which, rows, page):
+    for fmt in ("f16", "i8"):
+        for bad in (np.nan, np.inf):
+            c = many(Case(spl, [(rows, 100 + rows)], (4, 2, 64), fmt, page, seed=rows))
+            c.fill()
+            clean = check_sample(c, 4)
+            at = rows // 2
+            getattr(c, which)[0][100 + at, 1, 3] = bad
+            c.fill()
+            got = c.attend()
+            assert np.array_equal(got[:at], clean[:at])
+            assert np.array_equal(got[:, :2], clean[:, :2])
+            if fmt == "i8" or np.isnan(bad):  # (binary16 saturates an infinity)
+                assert np.isnan(got[at:, 2:]).any(axis=2).all()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+def test_many_rows_is_deterministic_and_leaves_the_workspace_clean(spl, fmt):
+    a = many(Case(spl, [(300, 3000), (20, 100), (129, 2000)], (8, 2, 128), fmt, 64, seed=1))
+    b = Case(spl, [(1, 40)], (4, 4, 64), "i8", 16, seed=2)
+    for c in (a, b):
+        c.fill()
+    ws = spl.workspace(max(spl.spl_paged_attention_workspace_bytes(c.cache, c.batch(), c.hq) for c in (a, b)))
+    first = a.attend(workspace=ws)
+    for _ in range(3):
+        b.check(workspace=ws)
+        assert np.array_equal(a.attend(workspace=ws), first)
+    assert int(ws[:65536].count_nonzero()) == 0
+    # strided rows give the same bits
+    wide = torch.full((a.rows, 8 * 128 + 12), 7.0, device=DEV)
+    wide[:, 8:-4] = torch.as_tensor(a.q.reshape(a.rows, -1)).to(DEV)
+    out = torch.full((a.rows, 8 * 128 + 4), 5.0, device=DEV)
+    spl.spl_paged_attention(out[:, 4:], wide[:, 8:-4], a.cache, a.batch(), 8, workspace=ws)
+    assert np.array_equal(out[:, 4:].cpu().numpy().reshape(first.shape), first) and bool((out[:, :4] == 5).all())
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("rows", [1, 5, 200])
+def test_offsets_past_32_bits(spl, rows, fmt):
+    """A pool whose elements and bytes pass 2^32: the sequences lie in its last pages."""
+    page, heads = 256, (16, 8, 128)
+    c = Case(spl, [(rows, 700), (rows, 300)], heads, fmt, page, seed=rows)
+    pages = (1 << 32) // (8 * page * 128) + 40
+    c.cache = spl.KVCache.empty(pages, 8, 128, page, fmt)
+    c.poison()
+    used = c.table < c.cache.pages - 40
+    c.table[used] += pages - 40
+    if rows == 200:
+        many(c)
+    c.fill()
+    check_sample(c, 10)
+    lens = [n for _, n in c.seqs]
+    K = torch.zeros((sum(lens), 8 * 128), device=DEV)
+    V = torch.zeros_like(K)
+    spl.spl_kv_read(K, V, c.cache, c.batch(), i32([0, lens[0], sum(lens)]))
+    for got, which in ((K, "k"), (V, "v")):
+        want = np.concatenate([c.stored(which, b) for b in range(2)]).reshape(-1, 8 * 128)
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("rows", [1, 60, 300])
+def test_calls_follow_the_stream_they_are_given(spl, rows):
+    """Queries, cache and lengths made on a stream that is still busy, by argument and as the current stream."""
+    c = Case(spl, [(rows, 600), (rows, 500)], (8, 2, 128), "i8", 64, seed=9)
+    c.fill()
+    if rows == 300:
+        many(c)
+    want = c.attend()
+    K, V = (torch.as_tensor(np.concatenate([x[n - r:] for x, (r, n) in zip(xs, c.seqs)]).reshape(c.rows, -1)).to(DEV)
+            for xs in (c.k, c.v))
+    q = torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV)
+    batch = c.batch()
+    good = batch.kv_len.clone()
+    torch.cuda.synchronize()
+    for given in (False, True):
+        s = torch.cuda.Stream()
+        out, late = torch.zeros_like(q), torch.zeros_like(q)
+        for b, (r, n) in enumerate(c.seqs):  # the new tokens' slots hold something else until the append
+            for pos in range(n - r, n):
+                c.cache.k[int(c.table[b, pos // 64]), :, pos % 64] = 0
+        batch.kv_len.fill_(3)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(20_000_000)
+            batch.kv_len.copy_(good)
+            late.copy_(q)
+            if not given:
+                spl.spl_kv_append(c.cache, batch, K, V)
+                spl.spl_paged_attention(out, late, c.cache, batch, c.hq)
+        if given:
+            spl.spl_kv_append(c.cache, batch, K, V, stream=s)
+            spl.spl_paged_attention(out, late, c.cache, batch, c.hq, stream=s)
+        s.synchronize()
+        assert np.array_equal(out.cpu().numpy().reshape(want.shape), want)
+
+
+def test_verify_on_another_stream_and_long_rows(spl):
+    """Rows whose offsets pass 2^31 elements; probabilities made on a stream that is still busy."""
+    vocab, rows = 151936, 14200
+    P = torch.zeros((rows, vocab), device=DEV)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    counts = [3, 2]
+    p, q, x, u, e = draws(5, counts, vocab)
+    dev = lambda t: torch.as_tensor(t).to(DEV)  # noqa: E731
+    dp, dq, dx, du, de = dev(p), dev(q), dev(x), dev(u), dev(e)
+    accepted, token = i32([-9, -9, -9]), i32([-9, -9, -9])
+    de = torch.cat([de[:1], de])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        P[rows - 7:].copy_(dp)
+        spl.spl_verify_drafts(accepted, token, P, dq, dx, du, de, i32([0, rows - 7, rows - 3, rows]), i32([0, 0, 3, 5]))
+    s.synchronize()
+    want = expected(p, q, x, u, np.concatenate([e[:1], e])[1:], counts)
+    assert accepted.cpu().tolist()[1:] == want[0] and token.cpu().tolist()[1:] == want[1]

@@ -1,0 +1,175 @@
+"""The serving operators' refusals and empty calls, which need no GPU, and the oracle against closed forms."""
+
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+from oracle import serving
+
+
+@pytest.fixture(scope="module")
+def spl():
+    from paper_2609_15039_gb300 import build, spl as binding
+    if not os.path.exists(binding.LIB_PATH):
+        build.build()
+    binding.lib()
+    return binding
+
+
+@pytest.fixture(scope="module")
+def base():
+    buf = (ctypes.c_float * 64)()
+    p = ctypes.cast(buf, ctypes.c_void_p).value
+    yield p + (16 - p % 16) % 16
+    del buf
+
+
+def cache_of(spl, base, **kw):
+    f = dict(k=base, v=base, k_scale=base, v_scale=base, pages=4, kv_heads=2, page_size=16, head_dim=64, format=1)
+    f.update(kw)
+    return spl.spl_kv_cache(*f.values())
+
+
+def batch_of(spl, base, **kw):
+    f = dict(row_start=base, kv_len=base, page_table=base, seqs=2, max_pages=2, max_rows=1)
+    f.update(kw)
+    return spl.spl_kv_batch(*f.values())
+
+
+CACHES = [({"format": 2}, "EINVAL"), ({"pages": -1}, "EINVAL"), ({"kv_heads": 0}, "EINVAL"), ({"k": None}, "EINVAL"),
+          ({"v_scale": None}, "EINVAL"), ({"head_dim": 96}, "ESHAPE"), ({"page_size": 48}, "ESHAPE"),
+          ({"page_size": 8}, "ESHAPE"), ({"page_size": 512}, "ESHAPE"), ({"kv_heads": 1025}, "ESHAPE"),
+          ({"pages": 1 << 26}, "ESHAPE"), ({"pages": 1 << 40}, "ESHAPE"), ({"k": 8}, "EALIGN"), ({"k_scale": 4}, "EALIGN")]
+BATCHES = [({"seqs": -1}, "EINVAL"), ({"max_rows": -1}, "EINVAL"), ({"row_start": None}, "EINVAL"),
+           ({"page_table": None}, "EINVAL"), ({"seqs": 4097}, "ESHAPE"), ({"max_pages": 1 << 27}, "ESHAPE"),
+           ({"max_pages": 1 << 60}, "ESHAPE"), ({"kv_len": 2}, "EALIGN")]
+
+
+def shifted(fields, base):
+    """Small numbers in place of pointers are offsets."""
+    pointers = ("k", "v", "k_scale", "v_scale", "row_start", "kv_len", "page_table")
+    return {n: base + v if n in pointers and v else v for n, v in fields.items()}
+
+
+def every(spl, cache, batch, p):
+    """The three operators' answers to one cache and batch."""
+    L = spl.lib()
+    c, b = (ctypes.byref(x) if x is not None else None for x in (cache, batch))
+    return (L.spl_kv_append(c, b, p, 128, p, 128, 2, None), L.spl_kv_read(p, p, c, b, p, 2, None),
+            L.spl_paged_attention(p, 256, p, 256, c, b, 2, 4, 1.0, 0, p, 1 << 40, None))
+
+
+@pytest.mark.parametrize("fields,error", CACHES, ids=str)
+def test_caches_that_are_refused(spl, base, fields, error):
+    want = getattr(spl, "SPL_" + error)
+    assert every(spl, cache_of(spl, base, **shifted(fields, base)), batch_of(spl, base), base) == (want,) * 3
+
+
+@pytest.mark.parametrize("fields,error", BATCHES, ids=str)
+def test_batches_that_are_refused(spl, base, fields, error):
+    want = getattr(spl, "SPL_" + error)
+    assert every(spl, cache_of(spl, base), batch_of(spl, base, **shifted(fields, base)), base) == (want,) * 3
+
+
+def test_null_structs_and_empty_calls(spl, base):
+    L, c, b = spl.lib(), cache_of(spl, base), batch_of(spl, base)
+    assert every(spl, None, b, base) == (spl.SPL_EINVAL,) * 3
+    assert every(spl, c, None, base) == (spl.SPL_EINVAL,) * 3
+    c, b, none = ctypes.byref(c), ctypes.byref(b), ctypes.byref(batch_of(spl, None, seqs=0, max_pages=0))
+    assert L.spl_kv_append(c, b, None, 0, None, 0, 0, None) == spl.SPL_OK
+    assert L.spl_kv_append(c, none, None, 0, None, 0, 0, None) == spl.SPL_OK
+    assert L.spl_kv_read(None, None, c, b, None, 0, None) == spl.SPL_OK
+    assert L.spl_paged_attention(None, 0, None, 0, c, b, 0, 4, 1.0, 0, None, 0, None) == spl.SPL_OK
+    assert L.spl_paged_attention(None, 0, None, 0, c, none, 0, 4, 1.0, 0, None, 0, None) == spl.SPL_OK
+    assert L.spl_verify_drafts(None, None, None, 0, None, 0, None, None, None, 0, None, None, 0, 0, 0, 9, None, 0,
+                               None) == spl.SPL_OK
+
+
+def test_rows_that_are_refused(spl, base):
+    L, c, b = spl.lib(), ctypes.byref(cache_of(spl, base)), ctypes.byref(batch_of(spl, base))
+    append = lambda k, ldk, v, ldv, rows: L.spl_kv_append(c, b, k, ldk, v, ldv, rows, None)  # noqa: E731
+    assert append(None, 128, base, 128, 2) == spl.SPL_EINVAL
+    assert append(base, 124, base, 128, 2) == spl.SPL_EINVAL
+    assert append(base, 128, base, 128, -1) == spl.SPL_EINVAL
+    assert append(base, 130, base, 128, 2) == spl.SPL_EALIGN
+    assert append(base, 128, base + 4, 128, 2) == spl.SPL_EALIGN
+    assert append(base, 128, base, 128, 1 << 33) == spl.SPL_ESHAPE
+    read = lambda k, start, rows: L.spl_kv_read(k, base, c, b, start, rows, None)  # noqa: E731
+    assert read(None, base, 2) == spl.SPL_EINVAL and read(base, None, 2) == spl.SPL_EINVAL
+    assert read(base, base, -2) == spl.SPL_EINVAL and read(base, base, 1 << 33) == spl.SPL_ESHAPE
+    assert read(base + 8, base, 2) == spl.SPL_EALIGN and read(base, base + 2, 2) == spl.SPL_EALIGN
+
+
+def test_attention_that_is_refused(spl, base):
+    L, c, b = spl.lib(), ctypes.byref(cache_of(spl, base)), ctypes.byref(batch_of(spl, base))
+    good = dict(out=base, ldo=256, Q=base, ldq=256, rows=2, heads=4, scale=1.0, window=0, ws=base, size=1 << 40)
+
+    def call(**kw):
+        a = {**good, **kw}
+        return L.spl_paged_attention(a["out"], a["ldo"], a["Q"], a["ldq"], c, b, a["rows"], a["heads"], a["scale"],
+                                     a["window"], a["ws"], a["size"], None)
+    for kw in ({"out": None}, {"Q": None}, {"ldo": 252}, {"ldq": -256}, {"rows": -1}, {"heads": 3}, {"heads": 0},
+               {"scale": float("nan")}, {"scale": float("inf")}, {"window": -1}):
+        assert call(**kw) == spl.SPL_EINVAL, kw
+    for kw in ({"rows": 1 << 60}, {"rows": 1 << 31}, {"heads": 2 * 1025}):
+        assert call(**kw) == spl.SPL_ESHAPE, kw
+    for kw in ({"out": base + 4}, {"Q": base + 8}, {"ldo": 258}, {"ldq": 257}, {"ws": base + 8}):
+        assert call(**kw) == spl.SPL_EALIGN, kw
+    need = L.spl_paged_attention_workspace_bytes(c, b, 2, 4)
+    assert need >= 65536
+    assert call(size=need - 1) == spl.SPL_EWORKSPACE and call(ws=None) == spl.SPL_EWORKSPACE
+    assert L.spl_paged_attention_workspace_bytes(c, b, 0, 4) == 0
+    assert L.spl_paged_attention_workspace_bytes(c, b, 2, 3) == 0
+
+
+def test_verification_that_is_refused(spl, base):
+    L = spl.lib()
+    names = "accepted token P ldp Q ldq draft u e lde row_start draft_start rows drafts seqs vocab ws size".split()
+    good = dict(zip(names, (base, base, base, 8, base, 8, base, base, base, 8, base, base, 3, 2, 2, 8, base, 64)))
+    call = lambda **kw: L.spl_verify_drafts(*{**good, **kw}.values(), None)  # noqa: E731
+    pointers = [n for n in names if good[n] == base and n != "ws"]
+    for n in pointers:
+        assert call(**{n: None}) == spl.SPL_EINVAL, n
+        assert call(**{n: base + 2}) == spl.SPL_EALIGN, n
+    for kw in ({"vocab": 0}, {"vocab": -1}, {"ldp": 7}, {"ldq": 7}, {"lde": 7}, {"rows": -1}, {"drafts": -1}, {"seqs": -1}):
+        assert call(**kw) == spl.SPL_EINVAL, kw
+    big = {"ldp": 1 << 32, "ldq": 1 << 32, "lde": 1 << 32}
+    for kw in ({"seqs": 4097}, {"rows": 1 << 31}, {"drafts": 1 << 31}, {"vocab": 1 << 31, **big}):
+        assert call(**kw) == spl.SPL_ESHAPE, kw
+    need = L.spl_verify_drafts_workspace_bytes(2)
+    assert call(size=need - 1) == spl.SPL_EWORKSPACE and call(ws=None) == spl.SPL_EWORKSPACE
+    assert call(ws=base + 8) == spl.SPL_EALIGN
+
+
+# ---------------------------------------------------------------------------------- the oracle
+def test_oracle_attention_closed_forms():
+    """Equal scores average the visible values; one key gives its value; a window and missing keys."""
+    v = np.arange(5.0)[:, None, None] * np.ones((1, 1, 4))
+    q, k = np.zeros((3, 1, 4)), np.ones((5, 1, 4))
+    out, mass = serving.attention(q, k, v, 5, 1, 1.0)
+    assert np.allclose(out[:, 0, 0], [1.0, 1.5, 2.0]) and np.allclose(mass, out)
+    out, _ = serving.attention(q, k, v, 5, 1, 1.0, window=2)
+    assert np.allclose(out[:, 0, 0], [1.5, 2.5, 3.5])
+    out, _ = serving.attention(q, k[:1], v[:1] + 7, 1, 1, 1.0)
+    assert np.allclose(out[:, 0, 0], [0, 0, 7])
+
+
+def test_oracle_quantisation():
+    x = np.array([[1.0, -2.0, 0.5], [0.0, 0.0, 0.0], [np.inf, 1.0, 2.0]], dtype=np.float32)
+    code, scale = serving.quantize_i8(x)
+    assert code[0].tolist() == [64, -127, 32] and scale[0] == np.float32(2.0) / np.float32(127.0)
+    assert scale[1] == 0 and not code[1].any() and np.isnan(scale[2])
+    assert serving.quantize_f16(np.float32([1e6, -1e6, 0.1])).tolist() == [65504.0, -65504.0, np.float16(0.1)]
+
+
+def test_oracle_verification_keeps_the_target_distribution():
+    """Exact: the token that follows a draft is distributed as p, whatever q (the race's choice by inversion)."""
+    g = np.random.default_rng(0)
+    p, q = g.dirichlet(np.ones(6)), g.dirichlet(np.ones(6))
+    accept = np.minimum(1.0, p / q)
+    rest = np.maximum(p - q, 0)
+    assert np.allclose(q * accept + (1 - q @ accept) * rest / rest.sum(), p)
+    n, token = serving.verify(np.stack([p, p]), q[None], [2], [0.0], 1 / np.arange(1.0, 7.0))
+    assert n == 1 and token == int(np.argmax(p * np.arange(1.0, 7.0)))
