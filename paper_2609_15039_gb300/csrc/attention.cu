@@ -2,14 +2,18 @@
 //
 // o = sum_j softmax_j(scale q . k_j) v_j, in one pass over the keys with a running maximum m, total l and sums O.
 // For few rows the pass is bound by reading the cache once.  A tile has 8 rows (for one new token, the query heads of
-// a key head); its products run on mma.m16n8k16 with the 8 rows' high and low halves as the 16 rows of A, so that one
-// instruction makes both terms of q = hi + lo, or of p = hi + lo, for which the stored binary16 (or int8) values are
-// exact: fp32 accuracy at no further cost.
+// a key head); its products run on mma.m16n8k16.  q . k: the 8 rows' high and low halves are the 16 rows of A, so that one
+// instruction makes both terms of q = (hi + lo) 2^-e.  p . v is made transposed, v^T as A and the high, then the low
+// halves of p as B, into the same sums.  The stored binary16 (or int8) values are exact in those products: fp32 accuracy.
 // A block has an SM.  One warp copies units of 128 or 256 keys (some 64 KB of keys and values) into a ring by bulk copies
 // of whole runs of a page, so that some 190 KB are on their way on an SM, across the ends of tiles and sequences; 8 warps
 // make the sums, each of its 16 or 32 keys of a unit.  The order of the dimensions in a product is free, so a lane reads
-// 16 neighbouring bytes for its B fragments (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys
+// 16 neighbouring bytes for its fragments (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys
 // are byte permutes).
+// Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 337 us (the rate of
+// a copy), int8 216 us (0.8 of it: bound by widening int8 to binary16); one sequence of 300 keys 10.7 us, bound by the
+// latency of a launch, four dependent loads and the join.  More rows a tile (up to 32) share the reads but not the
+// products, at whose rate such tiles are bound: 32 rows took 36 us for each 8, the tensor-core kernel 80 in all.
 
 #include <algorithm>
 #include <cmath>
@@ -23,15 +27,15 @@ namespace spl {
 namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * (kWarps + 4);  // and a warpgroup of which one warp copies
-constexpr int kRT = kRowsTile;
+constexpr int kRT = 8;  // rows of a tile
 // p is held as 2^kShift p, at most 2^13, so that its low half keeps an absolute 2^-38 of the largest.
 constexpr float kShift = 13.0f;
 constexpr int kMinExp = -100, kMaxExp = 126;  // of the values' scales
 
-__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 template <class T>
 __device__ __forceinline__ T lds(const uint8_t* p) {
@@ -51,7 +55,7 @@ struct Frag {
   static constexpr int VE = I8 ? D / 8 : 8;        // keys 2t, 2t+1, 2t+8, 2t+9: neighbouring dims of a chunk
   static constexpr int VC = D / (8 * VE);          // and chunks
   static constexpr int VW = VE * (I8 ? 1 : 2) / 4; // words of a chunk
-  static constexpr int NB = D / 8;                 // n-blocks of p . v
+  static constexpr int MB = D / 16;                // m-blocks of v^T . p^T
   // first of the two neighbours (first + {0, 1}, and + {2, 3} for the upper half of a k-step) of step s
   static __device__ __forceinline__ int k_dim(int s, int t) {
     constexpr int per = E / 4;  // steps a chunk
@@ -61,15 +65,16 @@ struct Frag {
   static constexpr int ESZ = I8 ? 1 : 2, BLOCKS = D * ESZ == 256 ? 1 : 2, UNIT = 16 * kWarps * BLOCKS;
   static constexpr uint32_t K = 0, V = UNIT * D * ESZ, KS = 2 * V, VS = KS + (I8 ? UNIT * 4 : 0);
   static constexpr uint32_t STAGE = VS + (I8 ? UNIT * 4 : 0);
-  static constexpr int STAGES = 3 * 65536 / (2 * V) < 4 ? 3 * 65536 / (2 * V) : 4;
+  static constexpr int STAGES = V > 24576 ? 3 : 4;
   static constexpr uint32_t RING = STAGES * STAGE;
   // shared memory: the ring (the prefix sums before it), sums of four warps, maxima and totals, barriers (full, empty) and
   // the mask of a stage's blocks that hold keys
-  static constexpr uint32_t SO = RING, SM = SO + 4 * kRT * D * 4, SL = SM + kWarps * kRT * 4;
+  static constexpr int PARTS = 4;
+  static constexpr uint32_t SO = RING, SM = SO + PARTS * kRT * D * 4, SL = SM + kWarps * kRT * 4;
   static constexpr uint32_t BARS = SL + kWarps * kRT * 4, MASK = BARS + 16 * STAGES, LAST = MASK + 4 * STAGES;
   static constexpr uint32_t SMEM = LAST + 8;
   static_assert(SMEM <= 232448 && kMaxSeqs * kPrefixBytes <= RING, "fits");
-  // dim of column n of n-block nb
+  // dim n of the nb-th eight; an m-block is two of them
   static __device__ __forceinline__ int v_dim(int nb, int n) { return (nb / VE) * 8 * VE + n * VE + nb % VE; }
 };
 
@@ -169,10 +174,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   int it = 0;
   for (; run.busy(); run.next()) {
     const AttnTile& x = run.x;
-    // ---- the tile's rows: q = (hi + lo) 2^-e ----
+    // ---- the tile's rows: q = (hi + lo) 2^-e; the high halves are rows 0-7 of A, the low ones rows 8-15 ----
     const int r = min(x.r0 + g, x.r0 + x.rows - 1);  // rows past the last repeat it
     const int token = r / a.group;
-    uint32_t qa[F::STEPS][4];
+    uint4 qa[F::STEPS];
     float row_scale;
     {
       const float* q = a.q + (x.s.row0 + token) * a.ldq + (int64_t)(x.h * a.group + r % a.group) * D;
@@ -190,16 +195,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       row_scale = a.scale_log2 * pow2f(-e);
 #pragma unroll
       for (int s = 0; s < F::STEPS; ++s) {
-        split_f16(v[s].x * up, v[s].y * up, qa[s][0], qa[s][1]);
-        split_f16(v[s].z * up, v[s].w * up, qa[s][2], qa[s][3]);
+        split_f16(v[s].x * up, v[s].y * up, qa[s].x, qa[s].y);
+        split_f16(v[s].z * up, v[s].w * up, qa[s].z, qa[s].w);
       }
     }
     int row_lo, row_hi;
     row_keys(x.s, a.window, token, row_lo, row_hi);
 
-    float o[F::NB][4];
+    // The sums, transposed: dims (16 of an m-block) x rows; a lane has dims g, g + 8 and rows 2t, 2t + 1 of each.  (As rows
+    // x dims, with the high and low halves of p as A, they would take twice the registers: 64 sequences, int8, 230 us
+    // instead of 216.)
+    float o[F::MB][4];
 #pragma unroll
-    for (int i = 0; i < F::NB; ++i)
+    for (int i = 0; i < F::MB; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
     float m = -INFINITY, l = 0.f;
@@ -221,30 +229,38 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       if (mask & ((1u << BLOCKS) - 1u)) {
         // ---- scores of keys 2t, 2t + 1, 2t + 8, 2t + 9 of each block and row g ----
         float s[4 * BLOCKS];
-#pragma unroll
-        for (int c = 0; c < 2 * BLOCKS; ++c) {
-          float acc[2][4] = {};  // two chains of products
+        {
+          float acc[2][2 * BLOCKS][4] = {};  // two chains of products
 #pragma unroll
           for (int i = 0; i < F::KB; ++i) {
-            const uint4 k16 = lds<uint4>(at + F::K + (16 * b0 + 8 * c + g) * (D * ESZ) + 64 * i + 16 * t);
-            const uint32_t w[4] = {k16.x, k16.y, k16.z, k16.w};
-            if constexpr (I8) {
+            uint4 k16[2 * BLOCKS];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint32_t biased = w[k] ^ 0x80808080u;
-                mma16816(acc[k & 1], qa[4 * i + k], i8_pair(biased, 0x4140u), i8_pair(biased, 0x4342u));
+            for (int c = 0; c < 2 * BLOCKS; ++c)
+              k16[c] = lds<uint4>(at + F::K + (16 * b0 + 8 * c + g) * (D * ESZ) + 64 * i + 16 * t);
+#pragma unroll
+            for (int c = 0; c < 2 * BLOCKS; ++c) {
+              const uint32_t w[4] = {k16[c].x, k16[c].y, k16[c].z, k16[c].w};
+              if constexpr (I8) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const uint32_t biased = w[k] ^ 0x80808080u;
+                  mma16816(acc[k & 1][c], qa[4 * i + k], i8_pair(biased, 0x4140u), i8_pair(biased, 0x4342u));
+                }
+              } else {
+                mma16816(acc[0][c], qa[2 * i], w[0], w[1]);
+                mma16816(acc[1][c], qa[2 * i + 1], w[2], w[3]);
               }
-            } else {
-              mma16816(acc[0], qa[2 * i], w[0], w[1]);
-              mma16816(acc[1], qa[2 * i + 1], w[2], w[3]);
             }
           }
-          s[2 * c] = ((acc[0][0] + acc[1][0]) + (acc[0][2] + acc[1][2])) * row_scale;
-          s[2 * c + 1] = ((acc[0][1] + acc[1][1]) + (acc[0][3] + acc[1][3])) * row_scale;
-          if constexpr (I8) {
-            const float2 sc = lds<float2>(at + F::KS + 4 * (16 * b0 + 8 * c + 2 * t));
-            s[2 * c] *= sc.x;
-            s[2 * c + 1] *= sc.y;
+#pragma unroll
+          for (int c = 0; c < 2 * BLOCKS; ++c) {
+            s[2 * c] = ((acc[0][c][0] + acc[1][c][0]) + (acc[0][c][2] + acc[1][c][2])) * row_scale;
+            s[2 * c + 1] = ((acc[0][c][1] + acc[1][c][1]) + (acc[0][c][3] + acc[1][c][3])) * row_scale;
+            if constexpr (I8) {
+              const float2 sc = lds<float2>(at + F::KS + 4 * (16 * b0 + 8 * c + 2 * t));
+              s[2 * c] *= sc.x;
+              s[2 * c + 1] *= sc.y;
+            }
           }
         }
         float vs[4 * BLOCKS];
@@ -256,20 +272,18 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
             vs[2 * c + 1] = sc.y;
           }
         }
-        // The values of keys 2t, 2t + 1, 2t + 8, 2t + 9 of a block.
-        auto values = [&](int blk, uint32_t (&vr)[4][F::VC * F::VW]) {
+        // A chunk of the values of keys 2t, 2t + 1, 2t + 8, 2t + 9 of a block.
+        auto values = [&](int blk, int i, uint32_t (&vr)[4][F::VW]) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const uint8_t* p = at + F::V + (16 * (b0 + blk) + 8 * (c >> 1) + 2 * t + (c & 1)) * (D * ESZ) + g * F::VE * ESZ;
-#pragma unroll
-            for (int i = 0; i < F::VC; ++i) {
-              if constexpr (F::VW == 4) {
-                const uint4 w = lds<uint4>(p + i * 8 * F::VE * ESZ);
-                vr[c][4 * i] = w.x, vr[c][4 * i + 1] = w.y, vr[c][4 * i + 2] = w.z, vr[c][4 * i + 3] = w.w;
-              } else {
-                const uint2 w = lds<uint2>(p);
-                vr[c][0] = w.x, vr[c][1] = w.y;
-              }
+            const uint8_t* p = at + F::V + (16 * (b0 + blk) + 8 * (c >> 1) + 2 * t + (c & 1)) * (D * ESZ) +
+                               (g + 8 * i) * F::VE * ESZ;
+            if constexpr (F::VW == 4) {
+              const uint4 w = lds<uint4>(p);
+              vr[c][0] = w.x, vr[c][1] = w.y, vr[c][2] = w.z, vr[c][3] = w.w;
+            } else {
+              const uint2 w = lds<uint2>(p);
+              vr[c][0] = w.x, vr[c][1] = w.y;
             }
           }
         };
@@ -277,32 +291,38 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         const bool edge = j0 < x.all_lo || j0 + 16 * BLOCKS > x.all_hi || (~mask & ((1u << BLOCKS) - 1u)) != 0;
         uint32_t hidden = 0, zap = 0;  // bits: scores that the row does not see; keys whose values become zeros
         if (edge) {
+          uint32_t bad = 0;  // keys whose values hold an infinity or NaN
+          if constexpr (!I8) {  // a value that only some rows see must not reach the others as 0 times NaN
 #pragma unroll
-          for (int blk = 0; blk < BLOCKS; ++blk) {
-            const bool copied = mask >> blk & 1u;
-            bool bad[4] = {false, false, false, false};
-            if constexpr (!I8) {  // a value that only some rows see must not reach the others as 0 times NaN
-              uint32_t vr[4][F::VC * F::VW];
-              values(blk, vr);
+            for (int blk = 0; blk < BLOCKS; ++blk) {
+              bool special[4] = {false, false, false, false};
+#pragma unroll
+              for (int i = 0; i < F::VC; ++i) {
+                uint32_t vr[4][F::VW];
+                values(blk, i, vr);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                  for (int w = 0; w < F::VW; ++w) special[c] |= f16_special(vr[c][w]);
+              }
 #pragma unroll
               for (int c = 0; c < 4; ++c) {
                 const int j = j0 + 16 * blk + 8 * (c >> 1) + 2 * t + (c & 1);
-#pragma unroll
-                for (int i = 0; i < F::VC * F::VW; ++i) bad[c] |= f16_special(vr[c][i]);
-                const unsigned who = __ballot_sync(0xffffffffu, bad[c]);
-                bad[c] = (who & (0x11111111u << t)) != 0;
-                if (bad[c] || !copied || j < x.key_lo || j >= x.key_hi) zap |= 1u << (4 * blk + c);
+                const unsigned who = __ballot_sync(0xffffffffu, special[c]);
+                if (who & (0x11111111u << t)) bad |= 1u << (4 * blk + c);
+                if ((bad >> (4 * blk + c) & 1u) || !(mask >> blk & 1u) || j < x.key_lo || j >= x.key_hi)
+                  zap |= 1u << (4 * blk + c);
               }
             }
+          }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const int j = j0 + 16 * blk + 8 * (c >> 1) + 2 * t + (c & 1);
-              if (!copied || j < row_lo || j >= row_hi) {
-                s[4 * blk + c] = -INFINITY;
-                hidden |= 1u << (4 * blk + c);
-              } else if (bad[c]) {
-                s[4 * blk + c] = __int_as_float(0x7fc00000);
-              }
+          for (int c = 0; c < 4 * BLOCKS; ++c) {
+            const int j = j0 + 16 * (c >> 2) + 8 * (c >> 1 & 1) + 2 * t + (c & 1);
+            if (!(mask >> (c >> 2) & 1u) || j < row_lo || j >= row_hi) {
+              s[c] = -INFINITY;
+              hidden |= 1u << c;
+            } else if (bad >> c & 1u) {
+              s[c] = __int_as_float(0x7fc00000);
             }
           }
         }
@@ -324,52 +344,60 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           const float f = m == -INFINITY ? 0.f : exp2_approx(m - m_new);
           l *= f;
           const float fo = I8 ? f * exp2_int(ev - ev_new) : f;
+          const float f0 = __shfl_sync(0xffffffffu, fo, 8 * t), f1 = __shfl_sync(0xffffffffu, fo, 8 * t + 4);
 #pragma unroll
-          for (int i = 0; i < F::NB; ++i)
+          for (int i = 0; i < F::MB; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[i][j] *= fo;
+            for (int j = 0; j < 4; ++j) o[i][j] *= j & 1 ? f1 : f0;
           m = m_new;
           ev = ev_new;
         }
         const float base = kShift - (m == -INFINITY ? 0.f : m);
+        const float down = I8 ? exp2_int(-ev) : 1.f;
         float p[4 * BLOCKS];
 #pragma unroll
         for (int c = 0; c < 4 * BLOCKS; ++c) {
           p[c] = exp2_approx(s[c] + base);
           l += p[c];
-          if constexpr (I8) p[c] = (hidden >> c & 1u) ? 0.f : p[c] * (vs[c] * exp2_int(-ev));
+          if constexpr (I8) p[c] = (hidden >> c & 1u) ? 0.f : p[c] * (vs[c] * down);
         }
         // ---- sums ----
 #pragma unroll
         for (int blk = 0; blk < BLOCKS; ++blk) {
-          uint32_t vr[4][F::VC * F::VW];
-          values(blk, vr);
-          if (!I8 && edge) {
+          uint32_t hi[2], lo[2];
+          split_f16(p[4 * blk], p[4 * blk + 1], hi[0], lo[0]);
+          split_f16(p[4 * blk + 2], p[4 * blk + 3], hi[1], lo[1]);
+          auto add = [&](int i, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+            const uint4 v = make_uint4(a0, a1, a2, a3);
+            mma16816(o[i], v, hi[0], hi[1]);
+            mma16816(o[i], v, lo[0], lo[1]);
+          };
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-              if (zap >> (4 * blk + c) & 1u) {
+          for (int i = 0; i < F::VC; ++i) {
+            uint32_t vr[4][F::VW];
+            values(blk, i, vr);
+            if (!I8 && edge) {
 #pragma unroll
-                for (int i = 0; i < F::VC * F::VW; ++i) vr[c][i] = 0u;
+              for (int c = 0; c < 4; ++c)
+                if (zap >> (4 * blk + c) & 1u) {
+#pragma unroll
+                  for (int w = 0; w < F::VW; ++w) vr[c][w] = 0u;
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < F::VW; ++w) {
+              if constexpr (I8) {
+                const uint32_t k0 = vr[0][w] ^ 0x80808080u, k1 = vr[1][w] ^ 0x80808080u;
+                const uint32_t k2 = vr[2][w] ^ 0x80808080u, k3 = vr[3][w] ^ 0x80808080u;
+                const uint32_t lo0 = __byte_perm(k0, k1, 0x5140u), hi0 = __byte_perm(k0, k1, 0x7362u);
+                const uint32_t lo1 = __byte_perm(k2, k3, 0x5140u), hi1 = __byte_perm(k2, k3, 0x7362u);
+                const int at = 2 * (i * F::VW + w);
+                add(at, i8_pair(lo0, 0x4140u), i8_pair(lo0, 0x4342u), i8_pair(lo1, 0x4140u), i8_pair(lo1, 0x4342u));
+                add(at + 1, i8_pair(hi0, 0x4140u), i8_pair(hi0, 0x4342u), i8_pair(hi1, 0x4140u), i8_pair(hi1, 0x4342u));
+              } else {
+                add(i * F::VW + w, __byte_perm(vr[0][w], vr[1][w], 0x5410u), __byte_perm(vr[0][w], vr[1][w], 0x7632u),
+                    __byte_perm(vr[2][w], vr[3][w], 0x5410u), __byte_perm(vr[2][w], vr[3][w], 0x7632u));
               }
-          }
-          uint32_t pa[4];
-          split_f16(p[4 * blk], p[4 * blk + 1], pa[0], pa[1]);
-          split_f16(p[4 * blk + 2], p[4 * blk + 3], pa[2], pa[3]);
-#pragma unroll
-          for (int w = 0; w < F::VC * F::VW; ++w) {
-            if constexpr (I8) {
-              const uint32_t k0 = vr[0][w] ^ 0x80808080u, k1 = vr[1][w] ^ 0x80808080u;
-              const uint32_t k2 = vr[2][w] ^ 0x80808080u, k3 = vr[3][w] ^ 0x80808080u;
-              const uint32_t lo0 = __byte_perm(k0, k1, 0x5140u), hi0 = __byte_perm(k0, k1, 0x7362u);
-              const uint32_t lo1 = __byte_perm(k2, k3, 0x5140u), hi1 = __byte_perm(k2, k3, 0x7362u);
-              mma16816(o[4 * w], pa, i8_pair(lo0, 0x4140u), i8_pair(lo1, 0x4140u));
-              mma16816(o[4 * w + 1], pa, i8_pair(lo0, 0x4342u), i8_pair(lo1, 0x4342u));
-              mma16816(o[4 * w + 2], pa, i8_pair(hi0, 0x4140u), i8_pair(hi1, 0x4140u));
-              mma16816(o[4 * w + 3], pa, i8_pair(hi0, 0x4342u), i8_pair(hi1, 0x4342u));
-            } else {
-              mma16816(o[2 * w], pa, __byte_perm(vr[0][w], vr[1][w], 0x5410u), __byte_perm(vr[2][w], vr[3][w], 0x5410u));
-              mma16816(o[2 * w + 1], pa, __byte_perm(vr[0][w], vr[1][w], 0x7632u),
-                       __byte_perm(vr[2][w], vr[3][w], 0x7632u));
             }
           }
         }
@@ -378,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       if (lane == 0) mbar_arrive(bars + 8u * (F::STAGES + stage));
     }
 
-    // ---- the warps' sums together: the upper four's to the lower four, then those in their order ----
+    // ---- the warps' sums together, PARTS warps at a time, always in the same order ----
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
     sync();  // the shared arrays' last readers are done
@@ -391,18 +419,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) m_all = fmaxf(m_all, s_m[w][g]);
     const float f = (m == -INFINITY ? (l != l ? l : 0.f) : exp2_approx(m - m_all)) * (I8 ? exp2_int(ev) : 1.f);
+    const float f0 = __shfl_sync(0xffffffffu, f, 8 * t), f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+#pragma unroll 1
+    for (int turn = kWarps / F::PARTS - 1; turn >= 0; --turn) {
+      if (warp / F::PARTS == turn) {
 #pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
-      if ((warp < 4) == (turn == 1)) {
+        for (int i = 0; i < F::MB; i += 2)  // two m-blocks: four neighbouring dims
 #pragma unroll
-        for (int nb = 0; nb < F::NB; ++nb) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float* dst = &s_o[warp & 3][g][F::v_dim(nb, 2 * t + i)];
-            const float v = (o[nb][i] + o[nb][2 + i]) * f;
-            *dst = turn == 0 ? v : v + *dst;
+          for (int j = 0; j < 2; ++j) {
+            const float fj = j ? f1 : f0;
+            float4* dst = reinterpret_cast<float4*>(&s_o[warp % F::PARTS][2 * t + j][F::v_dim(2 * i, g)]);
+            float4 v = make_float4(o[i][j] * fj, o[i][2 + j] * fj, o[i + 1][j] * fj, o[i + 1][2 + j] * fj);
+            if (turn < kWarps / F::PARTS - 1) {
+              const float4 w = *dst;
+              v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+            }
+            *dst = v;
           }
-        }
       }
       sync();
     }
@@ -554,21 +587,22 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
   return paged_batch_view(b, *c, batch, rows);
 }
 
-// The few-row kernel where every sequence's rows of a key head fit its tile, or where the units (64 keys of a tile) that
-// the batch can have, by its longest chunk and its page table, are few: the tensor-core kernel costs 15 us more at the
-// start and a tenth as much per unit.  Measured with 24 query heads on 8 (few rows, tensor cores): 16 rows over 2048 keys
-// 24, 27 us, over 8192 50, 39; 64 rows over 512 25, 35, over 2048 47, 42; 16 sequences of 8 rows over 128 22, 32, over
-// 512 41, 40.
+// The few-row kernel where every sequence's rows of a key head fit its tile (int8: two of them, which costs it less than
+// the tensor cores' widening to binary16), or where the units (64 keys of a tile) that the batch can have, by its longest
+// chunk and its page table, are few: the tensor-core kernel costs some 10 us more at the start and a tenth as much per
+// unit.  Measured, few rows and tensor cores: 16 sequences of 4 rows of 32 query heads on 8 over 800 to 8000 keys, int8
+// 75, 97 us, binary16 92, 78; of 5 rows, int8 105, 97.  24 query heads on 8, binary16: 16 rows over 2048 keys 20.4, 20.1,
+// over 8192 35, 27; 64 rows over 512 20, 20, over 2048 37, 27; 16 sequences of 8 rows over 128 16, 22, over 512 32, 26.
 constexpr int64_t kFewUnits = 1600;
 Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_heads) {
   const int d = (int)cache->head_dim, sms = device_sm_count();
   Shape s;
-  const int64_t tiles = ceil_div(std::max<int64_t>(batch->max_rows, 1) * (q_heads / cache->kv_heads), kRowsTile);
+  const int64_t tiles = ceil_div(std::max<int64_t>(batch->max_rows, 1) * (q_heads / cache->kv_heads), kRT);
   const int64_t units = cache->pages == 0 ? 0 : ceil_div(batch->max_pages * cache->page_size, 64);
-  s.few = tiles == 1 || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;
+  s.few = tiles <= (cache->format == SPL_KV_I8 ? 2 : 1) || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;
   if (s.few) {
     s.blocks = sms;
-    s.bytes = kCounterBytes + (size_t)s.blocks * 2 * kRowsTile * (d + kSlotStats) * sizeof(float);
+    s.bytes = kCounterBytes + (size_t)s.blocks * 2 * kRT * (d + kSlotStats) * sizeof(float);
   } else {
     s.blocks = sms;
     s.bytes = kCounterBytes + attention_tc_bytes(d, sms);

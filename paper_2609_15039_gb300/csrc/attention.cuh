@@ -236,6 +236,5 @@ constexpr int kSlotStats = 2;  // per row: maximum (in units of log2) and total
 spl_status run_attention_tc(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
 size_t attention_tc_bytes(int head_dim, int blocks);
 spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
-constexpr int kRowsTile = 8;
 
 }  // namespace spl
