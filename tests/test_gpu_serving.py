@@ -628,3 +628,50 @@ def test_verify_on_another_stream_and_long_rows(spl):
     s.synchronize()
     want = expected(p, q, x, u, np.concatenate([e[:1], e])[1:], counts)
     assert accepted.cpu().tolist()[1:] == want[0] and token.cpu().tolist()[1:] == want[1]
+
+
+@pytest.mark.parametrize("vocab,pad", [(997, 0), (4096, 0), (70001, 3)])
+@pytest.mark.parametrize("kind", ["near", "extreme"])
+def test_verify_chooses_the_rounded_quotient(spl, kind, vocab, pad):
+    """The draw is the largest fl32(w / e), the lowest index of equal ones: quotients that differ by few ulp or not at
+    all, and random numbers and weights at the ends of the range (zero, subnormal, infinite, NaN)."""
+    g = np.random.default_rng(vocab)
+    n = 24
+    if kind == "near":
+        e = (1.0 + g.integers(0, 64, (n, vocab)) * 2.0 ** -20).astype(np.float32)
+        p = (e * np.float32(0.37) * (1 + g.integers(-2, 3, (n, vocab)) * 2.0 ** -23)).astype(np.float32)
+    else:
+        ends = np.array([0.0, 1e-45, 1e-39, 1.2e-38, 1e-30, 1e-3, 0.5, 1.0, 3.0, 1e20, 1e37, 3e38, np.inf, np.nan], np.float32)
+        e = ends[g.integers(0, len(ends), (n, vocab))]
+        p = ends[g.integers(0, 9, (n, vocab))]
+        e[: n // 2] = np.where(e[: n // 2] < 1e-3, np.float32(1.0), e[: n // 2])  # without overflow and 0 / 0
+        p[: n // 4] *= np.float32(1e-38)
+    with np.errstate(all="ignore"):
+        r = (p / e).astype(np.float32)
+    want = np.argmax(np.where(r >= 0, r, -1), axis=1)
+    got = run_verify(spl, p, np.zeros((0, vocab), np.float32), np.zeros(0, np.int32), np.zeros(0, np.float32), e, [0] * n, pad)
+    assert got == ([0] * n, want.tolist())
+
+
+@pytest.mark.parametrize("heads", [(8, 8, 128), (3, 3, 64)], ids=str)
+def test_int8_codes_are_the_rounded_quotients(spl, heads):
+    """Values on and next to the middles of two codes, vectors at the ends of the range."""
+    c = Case(spl, [(1, 700)], heads, "i8", 16, seed=21)
+    g = np.random.default_rng(4)
+    n, (hk, d) = 700, (c.hk, c.d)
+    for x in (c.k[0], c.v[0]):
+        x[:] = (g.integers(-126, 126, (n, hk, d)) + 0.5) * (1 + g.integers(-3, 4, (n, hk, d)) * 2.0 ** -23)
+        x[..., 0] = 127.0  # the scale is 1: the quotients are x
+        x[100:] *= g.uniform(0.5, 2.0, (n - 100, hk, 1)).astype(np.float32)
+        x[300:330] *= np.float32(1e-38)
+        x[330:360] *= np.float32(1e-43)
+        x[360:390] = np.where(np.abs(x[360:390]) > 1, x[360:390] * np.float32(1e36), x[360:390])
+        x[390:400] = 0.0
+    c.fill()
+    for which in ("k", "v"):
+        code, scale = serving.quantize_i8(getattr(c, which)[0])
+        t = np.arange(n)
+        page = torch.as_tensor(c.table[0, t // 16].astype(np.int64)).to(DEV)
+        at = torch.as_tensor(t % 16).to(DEV)
+        assert np.array_equal(getattr(c.cache, which)[page, :, at].cpu().numpy(), code)
+        assert np.array_equal(getattr(c.cache, which + "_scale")[page, :, at].cpu().numpy(), scale)
