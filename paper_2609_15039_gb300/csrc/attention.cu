@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float total = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < F::PARTS; ++w) {
         const float4 part = *reinterpret_cast<const float4*>(&s_o[w][row][d]);
         v = make_float4(v.x + part.x, v.y + part.y, v.z + part.z, v.w + part.w);
       }
@@ -523,13 +523,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       }
     }
     sync();
-#pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
-      if ((warp < 4) == (turn == 1)) {
+#pragma unroll 1
+    for (int turn = kWarps / F::PARTS - 1; turn >= 0; --turn) {
+      if (warp / F::PARTS == turn) {
 #pragma unroll
         for (int i = 0; i < kRT / ROWS; ++i) {
-          float4* dst = reinterpret_cast<float4*>(&s_o[warp & 3][i * ROWS + sub][d4]);
-          const float4 v = turn == 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *dst;
+          float4* dst = reinterpret_cast<float4*>(&s_o[warp % F::PARTS][i * ROWS + sub][d4]);
+          const float4 v = turn == kWarps / F::PARTS - 1 ? make_float4(0.f, 0.f, 0.f, 0.f) : *dst;
           *dst = make_float4(acc[i].x + v.x, acc[i].y + v.y, acc[i].z + v.z, acc[i].w + v.w);
           if (d4 == 0) s_l[warp][i * ROWS + sub] = tot[i];
         }
@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float total = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < F::PARTS; ++w) {
         const float4 part = *reinterpret_cast<const float4*>(&s_o[w][row][d]);
         v = make_float4(v.x + part.x, v.y + part.y, v.z + part.z, v.w + part.w);
       }

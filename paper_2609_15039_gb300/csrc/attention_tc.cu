@@ -1034,8 +1034,8 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Attn
   if (c1 <= c0) return;
   const int lane = threadIdx.x & 31;
   const int warps = kJoinParts * (kJoinThreads / 32), first = blockIdx.y * (kJoinThreads / 32) + (threadIdx.x >> 5);
-  for (int task = first; task < (x.rows + 31) / 32 * (D / 4); task += warps) {
-    const int row = task / (D / 4) * 32 + lane, d4 = task % (D / 4);
+  for (int task = first; task < (x.rows + 3) / 4 * (D / 32); task += warps) {  // 4 rows of 32 dims a warp
+    const int row = task / (D / 32) * 4 + (lane & 3), d4 = task % (D / 32) * 8 + (lane >> 2);
     if (row >= x.rows) continue;
     auto slot = [&](int c) { return a.slots + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * slot_floats<D>(); };
     float m = -INFINITY;
