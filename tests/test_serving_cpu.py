@@ -173,3 +173,24 @@ def test_oracle_verification_keeps_the_target_distribution():
     assert np.allclose(q * accept + (1 - q @ accept) * rest / rest.sum(), p)
     n, token = serving.verify(np.stack([p, p]), q[None], [2], [0.0], 1 / np.arange(1.0, 7.0))
     assert n == 1 and token == int(np.argmax(p * np.arange(1.0, 7.0)))
+
+
+def test_pages_are_taken_and_given_back(monkeypatch):
+    import torch
+    from paper_2609_15039_gb300 import serving
+    made = []
+    monkeypatch.setattr(serving.spl, "KVBatch", lambda *a: made.append(a) or made[-1])
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self: self)
+    p = serving.Pages(pages=5, page_size=16, seqs=2, max_len=48)
+    start, lens, table, rows, most = p.grow([17, 16])
+    assert start.tolist() == [0, 17, 33] and lens.tolist() == [17, 16] and (rows, most) == (33, 17)
+    assert len(p.free) == 2 and len(set(p.own[0] + p.own[1])) == 3
+    assert table[0, :2].tolist() == p.own[0] and table[1, 0] == p.own[1][0]
+    p.grow([0, 1])
+    p.cut([16, 16])
+    assert p.lens == [16, 16] and len(p.free) == 3
+    with pytest.raises(ValueError):
+        p.grow([0, 33])  # past the table
+    p.grow([32, 0])
+    with pytest.raises(ValueError):
+        p.grow([0, 17])  # no page left
