@@ -39,6 +39,18 @@ kv_append_kernel(const PagedCache cache, const PagedBatch batch, const float* __
   const int lane = threadIdx.x & 31, part = lane / LANES, at = lane % LANES;
   const int64_t row = w >> 1;
   if (row >= batch.rows) return;
+  const bool is_v = w & 1;
+  const float* src = is_v ? V + row * ldv : K + row * ldk;
+  float4 x[kHeadsInFlight];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < kHeadsInFlight; ++u) {
+      const int h = h0 + u * PER_WARP + part;
+      x[u] = h < cache.heads ? __ldcs(reinterpret_cast<const float4*>(src + (int64_t)h * D) + at)
+                             : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  };
+  load(0);  // on its way while the row's place is looked up
   const int b = paged_find(batch.row_start, batch.seqs, row);
   const PagedSeq s = paged_seq(batch, cache.page_shift, b);
   const int64_t i = row - s.row0;
@@ -46,18 +58,10 @@ kv_append_kernel(const PagedCache cache, const PagedBatch batch, const float* __
   if (i < 0 || i >= s.n || pos < 0) return;  // no sequence's row, or before its first position
   const int page = paged_page(cache, batch, b, (int)pos);
   if (page < 0) return;
-  const bool is_v = w & 1;
-  const float* src = is_v ? V + row * ldv : K + row * ldk;
   void* dst = is_v ? cache.v : cache.k;
   float* scales = is_v ? cache.v_scale : cache.k_scale;
   for (int h0 = 0; h0 < cache.heads; h0 += kHeadsInFlight * PER_WARP) {
-    float4 x[kHeadsInFlight];
-#pragma unroll
-    for (int u = 0; u < kHeadsInFlight; ++u) {
-      const int h = h0 + u * PER_WARP + part;
-      x[u] = h < cache.heads ? __ldcs(reinterpret_cast<const float4*>(src + (int64_t)h * D) + at)
-                             : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+    if (h0 > 0) load(h0);
 #pragma unroll
     for (int u = 0; u < kHeadsInFlight; ++u) {
       const int h = h0 + u * PER_WARP + part;

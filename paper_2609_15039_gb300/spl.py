@@ -666,6 +666,17 @@ def _scratch(nbytes, device, stream):
         return workspace(nbytes, device)
 
 
+def _vector(t, name, dtype):
+    """(address, elements) of a contiguous CUDA tensor."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr(), t.numel()
+
+
 def _rows_view(t, name, width):
     """(address, row stride) of a CUDA fp32 matrix [rows, width] whose rows are contiguous, at any distance."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -781,22 +792,23 @@ def spl_verify_drafts(accepted, token, P, Q, draft, u, e, row_start, draft_start
     """Accepted drafts and next token of each sequence (int32 [seqs]): P [rows, vocab] the target's probabilities,
     Q [drafts, vocab] the draft's, draft [drafts] int32, u [drafts] uniform, e [seqs, vocab] exponential;
     sequence b's rows start at row_start[b], its drafts at draft_start[b] (int32 [seqs + 1])."""
-    seqs = accepted.numel()
-    (pp, ldp), (qp, ldq), (ep, lde) = (_rows_view(P, "P", None), _rows_view(Q, "Q", P.shape[-1]),
-                                       _rows_view(e, "e", P.shape[-1]))
-    drafts = draft.numel()
-    if (token.numel() != seqs or Q.shape[0] != drafts or u.numel() != drafts or e.shape[0] != seqs
-            or row_start.numel() != seqs + 1 or draft_start.numel() != seqs + 1):
+    (pp, ldp), (qp, ldq), (ep, lde) = (_rows_view(P, "P", None), _rows_view(Q, "Q", P.shape[1]),
+                                       _rows_view(e, "e", P.shape[1]))
+    i32 = torch.int32
+    ap, seqs = _vector(accepted, "accepted", i32)
+    tp, tokens = _vector(token, "token", i32)
+    xp, drafts = _vector(draft, "draft", i32)
+    up, randoms = _vector(u, "u", torch.float32)
+    rp, starts = _vector(row_start, "row_start", i32)
+    dp, draft_starts = _vector(draft_start, "draft_start", i32)
+    rows, vocab = P.shape
+    if not (tokens == e.shape[0] == seqs and Q.shape[0] == randoms == drafts and starts == draft_starts == seqs + 1):
         raise ValueError("spl_verify_drafts: shape mismatch")
     if workspace is None:
         workspace = _scratch(spl_verify_drafts_workspace_bytes(seqs), P.device, stream)
     wsp, wsb = _ws(workspace)
-    i32 = torch.int32
-    _check(lib().spl_verify_drafts(_dev(accepted, "accepted", i32), _dev(token, "token", i32), pp, ldp, qp, ldq,
-                                   _dev(draft, "draft", i32), _dev(u, "u"), ep, lde,
-                                   _dev(row_start, "row_start", i32), _dev(draft_start, "draft_start", i32),
-                                   P.shape[0], drafts, seqs, P.shape[1], wsp, wsb, _stream(stream)),
-           "spl_verify_drafts")
+    _check(lib().spl_verify_drafts(ap, tp, pp, ldp, qp, ldq, xp, up, ep, lde, rp, dp, rows, drafts, seqs, vocab, wsp,
+                                   wsb, _stream(stream)), "spl_verify_drafts")
 
 
 def spl_test_tc_wait_timeout(out, A, W, workspace=None, stream=None):
