@@ -73,7 +73,7 @@ struct Frag {
   static constexpr uint32_t SO = RING, SM = SO + PARTS * kRT * D * 4, SL = SM + kWarps * kRT * 4;
   static constexpr uint32_t BARS = SL + kWarps * kRT * 4, MASK = BARS + 16 * STAGES, LAST = MASK + 4 * STAGES;
   static constexpr uint32_t SMEM = LAST + 8;
-  static_assert(SMEM <= 232448 && kMaxSeqs * kPrefixBytes <= RING, "fits");
+  static_assert(SMEM <= 232448 && kMaxSeqs * kPrefixBytes + 8192 <= RING, "fits");
   // dim n of the nb-th eight; an m-block is two of them
   static __device__ __forceinline__ int v_dim(int nb, int n) { return (nb / VE) * 8 * VE + n * VE + nb % VE; }
 };
@@ -589,10 +589,11 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
 
 // The few-row kernel where every sequence's rows of a key head fit its tile (int8: two of them, which costs it less than
 // the tensor cores' widening to binary16), or where the units (64 keys of a tile) that the batch can have, by its longest
-// chunk and its page table, are few: the tensor-core kernel costs some 10 us more at the start and a tenth as much per
-// unit.  Measured, few rows and tensor cores: 16 sequences of 4 rows of 32 query heads on 8 over 800 to 8000 keys, int8
-// 75, 97 us, binary16 92, 78; of 5 rows, int8 105, 97.  24 query heads on 8, binary16: 16 rows over 2048 keys 20.4, 20.1,
-// over 8192 35, 27; 64 rows over 512 20, 20, over 2048 37, 27; 16 sequences of 8 rows over 128 16, 22, over 512 32, 26.
+// chunk and its page table, are few: the tensor-core kernel costs some 8 us more at the start and a tenth as much per
+// unit.  Measured, few rows and tensor cores, us: 16 sequences of 4 rows of 32 query heads on 8 over 800 to 8000 keys,
+// int8 75, 97, binary16 92, 78; of 5 rows, int8 105, 97; 64 of 4 rows over 1024, int8 77, 118.  24 query heads on 8,
+// binary16: 16 rows over 2048 keys 19, 22, over 8192 36, 28; 64 rows over 512 22, 21, over 2048 38, 28; 16 sequences of 8
+// rows over 128 17, 17, over 512 33, 20; 128 rows over 128 17, 17.
 constexpr int64_t kFewUnits = 1600;
 Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_heads) {
   const int d = (int)cache->head_dim, sms = device_sm_count();
@@ -649,7 +650,8 @@ extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* 
   a.scale_log2 = (float)(scale * 1.4426950408889634);
   a.counters = static_cast<unsigned int*>(workspace);
   a.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
-  a.min_units = s.few ? 1 : 2;
+  a.least = s.few ? 1 : 2;
+  a.slack = s.few ? 1 : 3;
   const int d = (int)cache->head_dim;
   const bool i8 = cache->format == SPL_KV_I8;
   return s.few ? run_attention_rows(a, d, i8, s.blocks, stream) : run_attention_tc(a, d, i8, s.blocks, stream);

@@ -7,6 +7,9 @@
 // a divided one go to the workspace as (sums, maximum, total) and the last block to arrive joins them in the order of
 // the blocks: the result does not depend on timing.  A block leaves at most one piece that begins inside a tile
 // (slot 0) and one that only ends inside one (slot 1).
+// A further piece costs a block as much as several units.  So where there are few tiles, each is cut into pieces of
+// `grain` units, the least of kGrains with which every piece has a block of its own, if that is little above the mean
+// (512 rows over themselves, 96 tiles of 1 to 4 units: 29 -> 23 us; 15 short sequences of one row 17.8 -> 16.5).
 #pragma once
 
 #include "paged.cuh"
@@ -24,10 +27,11 @@ struct AttnArgs {
   float scale_log2;  // scale log2(e): softmax in powers of two
   unsigned int* counters;
   float* slots;      // [blocks][2][slot floats]
-  int min_units;     // units a block takes at least (fewer blocks for little work)
+  int least, slack;  // units that a piece has at least, and that it may have above the mean for being a block's only one
 };
 
 constexpr int kFewTiles = 4;  // tiles of a sequence that one thread counts
+constexpr int kGrains = 8;    // 1 to 8 units
 
 struct AttnTile {
   int b, h, t;           // sequence, key head, tile
@@ -60,24 +64,30 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// A block's run of units.  `prefix` (shared, kPrefixBytes a sequence) is filled by the constructor, which every thread of
-// the block calls; afterwards every thread walks the same tiles by itself.
+// A block's run of units.  `prefix` (shared, kPrefixBytes a sequence and kGrains numbers for each of as many as there are
+// blocks) is filled by the constructor, which every thread of the block calls; afterwards every thread walks the same
+// tiles by itself.
 constexpr int kPrefixBytes = 8 + sizeof(PagedSeq);
 template <int RT, int U, int THREADS>
 struct AttnRun {
   AttnTile x;
-  int64_t total, at, end;  // units in all; the run [at, end)
+  int grain;               // units of a step
+  int64_t total, at, end;  // steps in all; the run [at, end)
   int blocks;              // blocks that have work
   int first;               // unit of the current tile at which the run stands
   const AttnArgs& a;
 
-  // The sequences, behind the prefix sums.
+  // The sequences, behind the prefix sums, and their steps of each grain.
   __device__ PagedSeq& kept(int64_t* prefix, int b) const {
     return reinterpret_cast<PagedSeq*>(prefix + a.batch.seqs)[b];
   }
-  __device__ AttnRun(const AttnArgs& args, int64_t* prefix) : a(args) {
+  __device__ int* steps(int64_t* prefix, int b) const {
+    return reinterpret_cast<int*>(&kept(prefix, a.batch.seqs)) + kGrains * b;
+  }
+  __device__ AttnRun(const AttnArgs& args, int64_t* prefix) : grain(1), a(args) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int seqs = a.batch.seqs, heads = a.cache.heads;
+    const bool few = seqs * heads <= (int)gridDim.x;  // a block for each piece is possible
     // A thread a sequence, whose loads then run side by side; the few sequences of many tiles a warp each.
     for (int b = threadIdx.x; b < seqs; b += THREADS) {
       AttnTile y;
@@ -85,11 +95,17 @@ struct AttnRun {
       kept(prefix, b) = y.s;
       const int tiles = (y.s.n * a.group + RT - 1) / RT;
       int64_t sum = 0;
+      int of[kGrains] = {};
       for (y.t = 0; tiles <= kFewTiles && y.t < tiles; ++y.t) {
         tile_span<RT, U>(y, a.group, a.window);
         sum += y.units;
+#pragma unroll
+        for (int k = 0; k < kGrains; ++k) of[k] += (int)((uint32_t)(y.units + k) / (uint32_t)(k + 1));
       }
       prefix[b] = tiles <= kFewTiles ? sum * heads : -1;
+      if (few)
+#pragma unroll
+        for (int k = 0; k < kGrains; ++k) steps(prefix, b)[k] = of[k];
     }
     __syncthreads();
     for (int b = warp; b < seqs; b += THREADS / 32) {
@@ -98,33 +114,50 @@ struct AttnRun {
       y.s = kept(prefix, b);
       const int tiles = (y.s.n * a.group + RT - 1) / RT;
       int64_t sum = 0;
+      int of[kGrains] = {};
       for (y.t = lane; y.t < tiles; y.t += 32) {
         tile_span<RT, U>(y, a.group, a.window);
         sum += y.units;
+        if (!few || tiles > (int)gridDim.x) continue;
+#pragma unroll
+        for (int k = 0; k < kGrains; ++k) of[k] += (int)((uint32_t)(y.units + k) / (uint32_t)(k + 1));
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (few) {
+#pragma unroll
+        for (int k = 0; k < kGrains; ++k) {
+          const int all = __reduce_add_sync(0xffffffffu, of[k]);
+          if (lane == k) steps(prefix, b)[k] = tiles > (int)gridDim.x ? (int)gridDim.x + 1 : all;
+        }
+      }
       __syncwarp();
       if (lane == 0) prefix[b] = sum * heads;
     }
     __syncthreads();
     if (warp == 0) {
-      int64_t carry = 0;
-      for (int b0 = 0; b0 < seqs; b0 += 32) {
-        int64_t v = b0 + lane < seqs ? prefix[b0 + lane] : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int64_t other = __shfl_up_sync(0xffffffffu, v, o);
-          if (lane >= o) v += other;
+      int64_t carry = scan(prefix, seqs);
+      if (few && carry > (a.least > 1 ? 0 : (int)gridDim.x) && carry <= (int64_t)kGrains * gridDim.x) {
+        const int mean = (int)(((uint32_t)carry + gridDim.x - 1) / gridDim.x);
+        for (int k = max(mean, a.least) - 1; k < min(mean + a.slack, kGrains); ++k) {
+          int sum = 0;
+          for (int b = lane; b < seqs; b += 32) sum += steps(prefix, b)[k];
+          sum = __reduce_add_sync(0xffffffffu, sum) * heads;
+          if (sum <= (int)gridDim.x) {
+            for (int b = lane; b < seqs; b += 32) prefix[b] = (int64_t)steps(prefix, b)[k] * heads;
+            __syncwarp();
+            scan(prefix, seqs);
+            grain = k + 1;
+            break;
+          }
         }
-        v += carry;
-        if (b0 + lane < seqs) prefix[b0 + lane] = v;
-        carry = __shfl_sync(0xffffffffu, v, 31);
       }
+      if (lane == 0) *steps(prefix, few ? seqs : 0) = grain;
     }
     __syncthreads();
+    grain = *steps(prefix, few ? seqs : 0);
     total = seqs > 0 ? prefix[seqs - 1] : 0;
-    blocks = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
+    blocks = (int)min((int64_t)gridDim.x, max((int64_t)1, total));
     const int c = blockIdx.x;
     at = c < blocks ? quotient(total * c, blocks) : 0;
     end = c < blocks ? quotient(total * (c + 1), blocks) : 0;
@@ -142,14 +175,14 @@ struct AttnRun {
     int64_t rest = at - before - x.h * per_head;
     x.s = kept(prefix, x.b);
     const int tiles = (x.s.n * a.group + RT - 1) / RT;
-    for (int t0 = 0;; t0 += 32) {  // the tile that holds unit `rest`, 32 at a time
+    for (int t0 = 0;; t0 += 32) {  // the tile that holds step `rest`, 32 at a time
       AttnTile y;
       y.s = x.s;
       y.t = t0 + lane;
       int64_t v = 0;
       if (y.t < tiles) {
         tile_span<RT, U>(y, a.group, a.window);
-        v = y.units;
+        v = steps_of(y.units);
       }
       const int64_t own = v;
 #pragma unroll
@@ -166,20 +199,38 @@ struct AttnRun {
       }
       rest -= __shfl_sync(0xffffffffu, v, 31);
     }
-    first = (int)rest;
+    first = (int)rest * grain;
     tile_span<RT, U>(x, a.group, a.window);
   }
+  // Sums up to each in place, by a warp; returns the last.
+  static __device__ int64_t scan(int64_t* prefix, int seqs) {
+    const int lane = threadIdx.x & 31;
+    int64_t carry = 0;
+    for (int b0 = 0; b0 < seqs; b0 += 32) {
+      int64_t v = b0 + lane < seqs ? prefix[b0 + lane] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t other = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += other;
+      }
+      v += carry;
+      if (b0 + lane < seqs) prefix[b0 + lane] = v;
+      carry = __shfl_sync(0xffffffffu, v, 31);
+    }
+    return carry;
+  }
+  __device__ int steps_of(int units) const { return grain == 1 ? units : (units + grain - 1) / grain; }
 
   __device__ bool busy() const { return at < end; }
   // Units [first, last()) of the tile are the block's piece.
-  __device__ int last() const { return (int)min((int64_t)x.units, first + (end - at)); }
+  __device__ int last() const { return (int)min((int64_t)x.units, first + (end - at) * grain); }
   __device__ bool whole() const { return first == 0 && last() == x.units; }
-  __device__ int block_of(int64_t unit) const { return (int)quotient((unit + 1) * blocks - 1, total); }
-  __device__ int first_block() const { return block_of(at - first); }
-  __device__ int last_block() const { return block_of(at - first + x.units - 1); }
+  __device__ int block_of(int64_t step) const { return (int)quotient((step + 1) * blocks - 1, total); }
+  __device__ int first_block() const { return block_of(at - first / grain); }
+  __device__ int last_block() const { return block_of(at - first / grain + steps_of(x.units) - 1); }
 
   __device__ void next() {
-    at += last() - first;
+    at += steps_of(last() - first);
     first = 0;
     if (at >= end) return;
     ++x.t;

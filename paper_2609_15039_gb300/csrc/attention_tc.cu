@@ -85,7 +85,7 @@ struct Layout {
   static constexpr uint32_t BAD = VMAX + (I8 ? kSteps * 32 : 0), BARS = BAD + (I8 ? 0 : kSteps * 16);
   static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
   static_assert(BARS % 8 == 0 && PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
-  static_assert(kMaxSeqs * kPrefixBytes <= AUX, "the prefix sums fit where the tiles go");
+  static_assert(kMaxSeqs * kPrefixBytes + 8192 <= AUX, "the prefix sums fit where the tiles go");
   static constexpr uint32_t S = 0, O = 256;                // tensor memory columns (+ 128 and + D for the other place)
   static constexpr uint32_t IDESC_S = make_idesc(0, 128, kKeys);
   static constexpr uint32_t IDESC_O = make_idesc(0, 128, D) | (1u << 16);  // B: the values, dims contiguous
