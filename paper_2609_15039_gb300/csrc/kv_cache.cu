@@ -9,8 +9,8 @@
 // Both kernels move each byte once and are bound by HBM, or by their latency for few rows.  One warp takes the heads
 // of one row of K or of V, kHeadsInFlight at a time, a lane four neighbours of the vector: the loads of a row are
 // whole 512-byte vectors and those of several heads are in flight together.  Measured with 8 heads of 128 dims: 64000
-// tokens written and read 116, 117 us as binary16 (6.8 TB/s, the rate of a copy), 108, 99 us as int8 (6.1, 6.6 TB/s);
-// one token 2.1 us and 3.3 us (int8), a launch and three dependent loads.
+// tokens written and read 116, 117 us as binary16 (6.8 TB/s, the rate of a copy), 103, 100 us as int8 (6.4, 6.6 TB/s);
+// one token 2.0 us and 2.7 us (int8), a launch and three dependent loads.
 
 #include <algorithm>
 
@@ -81,9 +81,10 @@ kv_append_kernel(const PagedCache cache, const PagedBatch batch, const float* __
         const float scale = finite ? __fdiv_rn(__uint_as_float(top), 127.0f) : __uint_as_float(0x7fc00000u);
         // rint(x / s) by a product with 1 / s, within 2^-14 of the quotient; where that is closer than 2^-13 to the middle
         // of two codes, or 1 / s is out of range, by the division itself (some 3% of the warps; dividing always was bound
-        // by arithmetic, 149 us for 64000 tokens of 8 heads of 128 instead of 108).
+        // by arithmetic, 149 us for 64000 tokens of 8 heads of 128 instead of 103).
         const float magic = 12582912.0f;  // 1.5 2^23: x + magic holds rint(x) in its low bits
-        const float inverse = __frcp_rn(scale);
+        float inverse;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(scale));
         const float q[4] = {x[u].x * inverse, x[u].y * inverse, x[u].z * inverse, x[u].w * inverse};
         float t[4], off = 0.f;
 #pragma unroll
