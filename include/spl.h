@@ -10,20 +10,22 @@
  * the same scale is also offered.  Delta f comes from Thms. 1-3 (Sec. 4.3).
  *
  * Conventions for every call
- *  - Tensors are fp32, row-major and contiguous.  Rows are tokens.
+ *  - Tensors are fp32, row-major and contiguous, unless an entry says otherwise
+ *    (the paged cache; rows ld elements apart).  Rows are tokens.
  *    X, X~ and the noise N are [M, K]; weights W are [N, K] (K contiguous,
  *    the nn.Linear layout); outputs are [M, N].  The paper writes the same
  *    product with column vectors (W x); here it is X W^T.
  *  - Device pointers are owned by the caller.  Every base pointer must be
- *    16-byte aligned and K must be a multiple of 4 (SPL_EALIGN otherwise).
+ *    16-byte aligned (4 where an entry says so) and K must be a multiple of 4
+ *    (SPL_EALIGN otherwise).
  *  - Work is enqueued asynchronously on `stream` (0 = legacy default stream);
  *    no call synchronises the host except spl_get_device_status and
  *    spl_spectral_norm.  A zero-sized problem returns SPL_OK and does nothing.
  *  - Arguments are validated before anything is launched; an invalid call
  *    launches nothing.  Launch failures return SPL_ECUDA.
  *  - The library keeps no allocation of its own beyond one device status
- *    word (set by kernels whose bounded waits expire, read by
- *    spl_get_device_status).  Scratch memory is passed in as `workspace`.
+ *    word (set by kernels whose bounded waits expire or that meet an index
+ *    outside its range, read by spl_get_device_status).  Scratch memory is passed in as `workspace`.
  */
 #ifndef SPL_H
 #define SPL_H
@@ -45,7 +47,7 @@ typedef enum spl_status {
   SPL_ECUDA = 4,        /* a CUDA runtime or driver call failed */
   SPL_ETIMEOUT = 5,     /* a bounded device-side wait expired (see spl_get_device_status) */
   SPL_EUNSUPPORTED = 6, /* the requested path cannot run on this device or with these operands */
-  SPL_EWORKSPACE = 7    /* workspace missing or smaller than spl_linear_workspace_bytes() */
+  SPL_EWORKSPACE = 7    /* workspace missing or smaller than the call's *_workspace_bytes() */
 } spl_status;
 
 /* Noise law.  GAUSSIAN is the paper's mechanism (Sec. 4.4); LAPLACE uses the
@@ -648,8 +650,8 @@ spl_status spl_kv_read(float* K, float* V, const spl_kv_cache* cache, const spl_
  * one that sees a NaN or infinity the outputs concerned, or all, are NaN.
  * fp32 accuracy from the stored values: query rows and probabilities enter the
  * tensor cores as two binary16 terms (hi + lo, scaled by powers of two; a
- * probability far below its row's largest keeps an absolute 2^-38 of it), the
- * softmax is held in fp32.
+ * probability far below its row's largest keeps an absolute 2^-33 of it, over I8
+ * of its product with the largest value scale), the softmax is held in fp32.
  * Workspace: spl_paged_attention_workspace_bytes, zero-filled before its first
  * use; its first 64 KiB (arrival counters) are zero again after every call that
  * completes, so the product workspace can be shared.  Errors: as spl_kv_append,
