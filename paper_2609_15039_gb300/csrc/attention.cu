@@ -12,8 +12,9 @@
 // are byte permutes).
 // Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 337 us (the rate of
 // a copy), int8 216 us (0.8 of it: bound by widening int8 to binary16); one sequence of 300 keys 10.7 us, bound by the
-// latency of a launch, four dependent loads and the join.  More rows a tile (up to 32) share the reads but not the
-// products, at whose rate such tiles are bound: 32 rows took 36 us for each 8, the tensor-core kernel 80 in all.
+// latency of a launch, four dependent loads and the join.  More rows a tile (16 to 32) share the reads, but their
+// chains of dependent steps grow with them: 16 sequences of 8 rows of 4 heads took 147 us so, 137 as four tiles, 80 on
+// the tensor-core kernel.
 
 #include <algorithm>
 #include <cmath>
@@ -650,8 +651,9 @@ extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* 
   a.scale_log2 = (float)(scale * 1.4426950408889634);
   a.counters = static_cast<unsigned int*>(workspace);
   a.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
-  a.least = s.few ? 1 : 2;
+  a.least = s.few ? 1 : 3;
   a.slack = s.few ? 1 : 3;
+  a.join = s.few ? 2 : 3;
   const int d = (int)cache->head_dim;
   const bool i8 = cache->format == SPL_KV_I8;
   return s.few ? run_attention_rows(a, d, i8, s.blocks, stream) : run_attention_tc(a, d, i8, s.blocks, stream);

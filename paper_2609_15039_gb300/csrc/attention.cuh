@@ -9,7 +9,8 @@
 // (slot 0) and one that only ends inside one (slot 1).
 // A further piece costs a block as much as several units.  So where there are few tiles, each is cut into pieces of
 // `grain` units, the least of kGrains with which every piece has a block of its own, if that is little above the mean
-// (512 rows over themselves, 96 tiles of 1 to 4 units: 29 -> 23 us; 15 short sequences of one row 17.8 -> 16.5).
+// (512 rows over themselves, 96 tiles of 1 to 4 units: 29 us in equal runs, 23 in pieces of 2, 20.6 as whole tiles; 15
+// short int8 sequences of one row 17.8, 16.5, 14.2).
 #pragma once
 
 #include "paged.cuh"
@@ -27,7 +28,8 @@ struct AttnArgs {
   float scale_log2;  // scale log2(e): softmax in powers of two
   unsigned int* counters;
   float* slots;      // [blocks][2][slot floats]
-  int least, slack;  // units that a piece has at least, and that it may have above the mean for being a block's only one
+  // Units that a piece has at least, that it may have above the mean for being a block's only one, that a join costs.
+  int least, slack, join;
 };
 
 constexpr int kFewTiles = 4;  // tiles of a sequence that one thread counts
@@ -137,21 +139,7 @@ struct AttnRun {
     __syncthreads();
     if (warp == 0) {
       int64_t carry = scan(prefix, seqs);
-      if (few && carry > (a.least > 1 ? 0 : (int)gridDim.x) && carry <= (int64_t)kGrains * gridDim.x) {
-        const int mean = (int)(((uint32_t)carry + gridDim.x - 1) / gridDim.x);
-        for (int k = max(mean, a.least) - 1; k < min(mean + a.slack, kGrains); ++k) {
-          int sum = 0;
-          for (int b = lane; b < seqs; b += 32) sum += steps(prefix, b)[k];
-          sum = __reduce_add_sync(0xffffffffu, sum) * heads;
-          if (sum <= (int)gridDim.x) {
-            for (int b = lane; b < seqs; b += 32) prefix[b] = (int64_t)steps(prefix, b)[k] * heads;
-            __syncwarp();
-            scan(prefix, seqs);
-            grain = k + 1;
-            break;
-          }
-        }
-      }
+      if (few && carry <= (int64_t)kGrains * gridDim.x) grain = choose_grain(prefix, (int)carry);
       if (lane == 0) *steps(prefix, few ? seqs : 0) = grain;
     }
     __syncthreads();
@@ -201,6 +189,32 @@ struct AttnRun {
     }
     first = (int)rest * grain;
     tile_span<RT, U>(x, a.group, a.window);
+  }
+  // The grain by which all pieces have blocks, and then the prefix sums are of its steps; by warp 0, of `sum` units in all.
+  // Whole tiles, which need no join, where they are little longer.
+  __device__ int choose_grain(int64_t* prefix, int sum) const {
+    const int lane = threadIdx.x & 31, seqs = a.batch.seqs, heads = a.cache.heads, grid = (int)gridDim.x;
+    const int mean = max(1, (int)((uint32_t)(sum + grid - 1) / (uint32_t)grid));
+    int tiles = 0, split = 0, whole = 0;
+    for (int b = lane; b < seqs; b += 32) tiles += (kept(prefix, b).n * a.group + RT - 1) / RT;
+    tiles = min(__reduce_add_sync(0xffffffffu, tiles), 1 << 20) * heads;
+    for (int k = mean; k <= kGrains && k <= (split ? split : mean + a.slack) + a.join; ++k) {
+      int n = 0;
+      for (int b = lane; b < seqs; b += 32) n += steps(prefix, b)[k - 1];
+      n = __reduce_add_sync(0xffffffffu, n) * heads;
+      if (split == 0 && n <= grid && k >= a.least && k <= max(mean + a.slack, a.least)) split = k;
+      if (n == tiles) {
+        whole = n <= grid ? k : 0;
+        break;
+      }
+    }
+    const int g = whole ? whole : max(split, 1);
+    if (g > 1) {
+      for (int b = lane; b < seqs; b += 32) prefix[b] = (int64_t)steps(prefix, b)[g - 1] * heads;
+      __syncwarp();
+      scan(prefix, seqs);
+    }
+    return g;
   }
   // Sums up to each in place, by a warp; returns the last.
   static __device__ int64_t scan(int64_t* prefix, int seqs) {

@@ -21,6 +21,10 @@
 // its other place while the sums' warps add the first to an fp32 sum in the workspace, rounding to nearest.
 // Divided tiles are joined by a second, small launch over all SMs.
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its copies and MMAs done.
+// Measured with 32 query heads on 8 of 128 dims, 2048 rows over 12049 keys: binary16 475 us, 0.9 of the instructions'
+// 2560 clocks a tile (S takes 96 an instruction, both its operands being in shared memory, O 64); int8 688 us, bound by
+// the widening and shared memory; 64 dims 389 and 638 us, bound by the softmax.  24 heads on 8, 512 rows over themselves
+// 23 us: some 14 us of one tile's latency, launches and the join.
 
 #include <algorithm>
 #include <cmath>
@@ -43,9 +47,10 @@ constexpr float kLazy = 5.0f;    // and may reach 2^(kShift + kLazy), times a sc
 constexpr int kMinExp = -100, kMaxExp = 126;
 constexpr int kSteps = 4;        // key tiles whose scales or marks have a place (see the barriers of the producer)
 
-// Barriers by index: kFull, kEmpty a stage; kRawFull, kRawEmpty a stage of int8 tiles as stored; kScale a place of K's scales; kQ a piece's q; kSFull, kPFull a place of S and
-// the p in it (whose waiter may be a tile behind); kPv a tile's product with V; kOFull, kOFree, kMFull a place of O: its chain is complete, has been added up, its rows'
-// maxima are there; kEdge the copies of V's edge tiles; kPieceFull, kPieceFree a piece's place.
+// Barriers by index: kFull, kEmpty a stage; kRawFull, kRawEmpty a stage of int8 tiles as stored; kScale a place of K's
+// scales; kQ a piece's q; kSFull, kPFull a place of S and the p in it (whose waiter may be a tile behind); kPv a tile's
+// product with V; kOFull, kOFree, kMFull a place of O: its chain is complete, has been added up, its rows' maxima are
+// there; kEdge the copies of V's edge tiles; kPieceFull, kPieceFree a piece's place.
 enum {
   kFull = 0, kEmpty = 5, kScale = 10, kQ = 14, kSFull = 15, kPFull = 17, kPv = 19, kOFull = 20, kOFree = 22, kMFull = 24,
   kDrain = 26, kEdge = 27, kPieceFull = 28, kPieceFree = 30, kRawFull = 32, kRawEmpty = 35, kBars = 38
@@ -1024,7 +1029,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 }
 
 // The pieces of the divided tiles, joined in the order of their blocks: blockIdx.x the block in whose run the tile
-// begins, blockIdx.y a part of its (row, dims).  A warp takes 32 rows and 4 dims of each.
+// begins, blockIdx.y a part of its (row, dims).  A warp takes 4 rows of 32 dims at a time.
 constexpr int kJoinParts = 8, kJoinThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const AttnArgs a, const Divided* divided) {
