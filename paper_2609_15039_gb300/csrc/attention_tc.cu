@@ -648,8 +648,12 @@ struct Kernel {
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       float top = fmaxf(fmaxf(fabsf(v[i].x), fabsf(v[i].y)), fmaxf(fabsf(v[i].z), fabsf(v[i].w)));
+      if constexpr (LANES == 32) {  // (of positive numbers the larger has the larger bits)
+        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top, 0.f))));
+      } else {
 #pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      }
       const int e = fp16_row_exponent(top);
       const float up = sign * pow2f(e);
 #pragma unroll
