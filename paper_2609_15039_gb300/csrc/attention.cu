@@ -10,9 +10,9 @@
 // make the sums, each of its 16 or 32 keys of a unit.  The order of the dimensions in a product is free, so a lane reads
 // 16 neighbouring bytes for its fragments (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys
 // are byte permutes).
-// Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 337 us (the rate of
-// a copy), int8 216 us (0.8 of it: bound by widening int8 to binary16); one sequence of 300 keys 10.7 us, bound by the
-// latency of a launch, four dependent loads and the join.  More rows a tile (16 to 32) share the reads, but their
+// Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 328 us (the rate of
+// a copy), int8 194 us (0.9 of it: bound by widening int8 to binary16); one sequence of 300 keys 10 us, bound by the
+// latency of a launch, four dependent loads and three units.  More rows a tile (16 to 32) share the reads, but their
 // chains of dependent steps grow with them: 16 sequences of 8 rows of 4 heads took 147 us so, 137 as four tiles, 80 on
 // the tensor-core kernel.
 
@@ -588,20 +588,22 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
   return paged_batch_view(b, *c, batch, rows);
 }
 
-// The few-row kernel where every sequence's rows of a key head fit its tile (int8: two of them, which costs it less than
-// the tensor cores' widening to binary16), or where the units (64 keys of a tile) that the batch can have, by its longest
-// chunk and its page table, are few: the tensor-core kernel costs some 8 us more at the start and a tenth as much per
-// unit.  Measured, few rows and tensor cores, us: 16 sequences of 4 rows of 32 query heads on 8 over 800 to 8000 keys,
-// int8 75, 97, binary16 92, 78; of 5 rows, int8 105, 97; 64 of 4 rows over 1024, int8 77, 118.  24 query heads on 8,
-// binary16: 16 rows over 2048 keys 19, 22, over 8192 36, 28; 64 rows over 512 22, 21, over 2048 38, 28; 16 sequences of 8
-// rows over 128 17, 17, over 512 33, 20; 128 rows over 128 17, 17.
+// The few-row kernel where every sequence's rows of a key head fit one of its tiles, or a few of them: three over int8,
+// which the tensor-core kernel first widens to binary16, two of 64 dims, whose softmax bounds that kernel; or where the
+// units (64 keys of a tile) that the batch can have, by its longest chunk and its page table, are few: the tensor-core
+// kernel costs some 8 us more at the start and a tenth as much per unit.  Measured, few rows and tensor cores, us, 32 query
+// heads on 8, 16 sequences over 800 to 8000 keys: of 4 rows (two tiles) int8 63, 87, binary16 78, 68, 64 dims 44, 54; of
+// 5 rows (three) int8 86, 87, binary16 117, 68, 64 dims int8 70, 81, binary16 60, 54; 64 sequences of 5 rows over 1000,
+// int8 100, 113.  24 query heads on 8, binary16: 16 rows over 2048 keys 18, 21, over 8192 33, 28; 64 rows over 512 21, 21,
+// over 2048 35, 25; 16 sequences of 8 rows over 128 16, 17, over 512 27, 20; 128 rows over 128 16, 17.
 constexpr int64_t kFewUnits = 1600;
 Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_heads) {
   const int d = (int)cache->head_dim, sms = device_sm_count();
   Shape s;
   const int64_t tiles = ceil_div(std::max<int64_t>(batch->max_rows, 1) * (q_heads / cache->kv_heads), kRT);
   const int64_t units = cache->pages == 0 ? 0 : ceil_div(batch->max_pages * cache->page_size, 64);
-  s.few = tiles <= (cache->format == SPL_KV_I8 ? 2 : 1) || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;
+  const int most = cache->format == SPL_KV_I8 ? 3 : d == 64 ? 2 : 1;
+  s.few = tiles <= most || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;
   if (s.few) {
     s.blocks = sms;
     s.bytes = kCounterBytes + (size_t)s.blocks * 2 * kRT * (d + kSlotStats) * sizeof(float);
@@ -654,6 +656,7 @@ extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* 
   a.least = s.few ? 1 : 3;
   a.slack = s.few ? 1 : 3;
   a.join = s.few ? 2 : 3;
+  a.start = s.few ? 2 : 3;
   const int d = (int)cache->head_dim;
   const bool i8 = cache->format == SPL_KV_I8;
   return s.few ? run_attention_rows(a, d, i8, s.blocks, stream) : run_attention_tc(a, d, i8, s.blocks, stream);
