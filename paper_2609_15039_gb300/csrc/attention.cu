@@ -5,13 +5,13 @@
 // a key head); its products run on mma.m16n8k16.  q . k: the 8 rows' high and low halves are the 16 rows of A, so that one
 // instruction makes both terms of q = (hi + lo) 2^-e.  p . v is made transposed, v^T as A and the high, then the low
 // halves of p as B, into the same sums.  The stored binary16 (or int8) values are exact in those products: fp32 accuracy.
-// A block has an SM.  One warp copies units of 128 or 256 keys (some 64 KB of keys and values) into a ring by bulk copies
+// A block has an SM.  Two or four warps copy units of 128 or 256 keys (some 64 KB of keys and values) into a ring by bulk copies
 // of whole runs of a page, so that some 190 KB are on their way on an SM, across the ends of tiles and sequences; 8 warps
 // make the sums, each of its 16 or 32 keys of a unit.  The order of the dimensions in a product is free, so a lane reads
 // 16 neighbouring bytes for its fragments (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys
 // are byte permutes).
 // Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 328 us (the rate of
-// a copy), int8 194 us (0.9 of it: bound by widening int8 to binary16); one sequence of 300 keys 10 us, bound by the
+// a copy), int8 188 us (0.94 of it: bound by widening int8 to binary16); one sequence of 300 keys 10 us, bound by the
 // latency of a launch, four dependent loads and three units.  More rows a tile (16 to 32) share the reads, but their
 // chains of dependent steps grow with them: 16 sequences of 8 rows of 4 heads took 147 us so, 137 as four tiles, 80 on
 // the tensor-core kernel.
@@ -27,7 +27,7 @@
 namespace spl {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * (kWarps + 4);  // and a warpgroup of which one warp copies
+constexpr int kWarps = 8, kThreads = 32 * (kWarps + 4);  // and a warpgroup that copies
 constexpr int kRT = 8;  // rows of a tile
 // p is held as 2^kShift p, at most 2^13, so that its low half keeps an absolute 2^-38 of the largest.
 constexpr float kShift = 13.0f;
@@ -79,9 +79,11 @@ struct Frag {
   static __device__ __forceinline__ int v_dim(int nb, int n) { return (nb / VE) * 8 * VE + n * VE + nb % VE; }
 };
 
-// The copying warp: unit after unit of the block's run into the ring's stages in turn.
+// A copying warp: unit after unit of the block's run into the ring's stages in turn.  Each has a part of what a unit
+// consists of (keys, values, their scales): with pages of 16 tokens, 64 copies a unit, one warp alone was the
+// bound (64 sequences of one row over 1600 to 15775 keys, int8, 352 us instead of 193).
 template <int D, bool I8>
-__device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8_t* smem) {
+__device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8_t* smem, int part) {
   using F = Frag<D, I8>;
   constexpr int BLOCKS = F::UNIT / 16;
   const PagedCache& cache = run.a.cache;
@@ -118,21 +120,20 @@ __device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8
       const uint32_t page_mask = ((1u << per_page) - 1u) << (lane / per_page * per_page) & mask;
       const bool leads = slot >= 0 && (page_mask & ((1u << lane) - 1u)) == 0;
       const uint32_t keys = 16u * __popc(page_mask);
-      if (lane == 0) {
+      if (part == 0 && lane == 0) {
         *reinterpret_cast<volatile uint32_t*>(smem + F::MASK + 4 * stage) = mask;
         mbar_expect_tx(full, 16u * __popc(mask) * (2u * D * F::ESZ + (I8 ? 8u : 0u)));
       }
       __syncwarp();
       if (leads) {
         const uint32_t key0 = 16u * lane;
-        bulk_load(at + F::K + key0 * D * F::ESZ, static_cast<const char*>(cache.k) + slot * (D * F::ESZ),
-                  keys * D * F::ESZ, full, policy);
-        bulk_load(at + F::V + key0 * D * F::ESZ, static_cast<const char*>(cache.v) + slot * (D * F::ESZ),
-                  keys * D * F::ESZ, full, policy);
-        if constexpr (I8) {
-          bulk_load(at + F::KS + key0 * 4u, cache.k_scale + slot, keys * 4u, full, policy);
-          bulk_load(at + F::VS + key0 * 4u, cache.v_scale + slot, keys * 4u, full, policy);
-        }
+        const bool v = part & 1;
+        if (part < 2)
+          bulk_load(at + (v ? F::V : F::K) + key0 * D * F::ESZ,
+                    static_cast<const char*>(v ? cache.v : cache.k) + slot * (D * F::ESZ), keys * D * F::ESZ, full, policy);
+        else
+          bulk_load(at + (v ? F::VS : F::KS) + key0 * 4u, (v ? cache.v_scale : cache.k_scale) + slot, keys * 4u, full,
+                    policy);
       }
       look_up(u + 1);
     }
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   // 168 registers a thread at the start; 3 x 168 = 2 x 232 + 40
   if (warp >= kWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (warp == kWarps) copy_units<D, I8>(run, smem);
+    if (warp < kWarps + (I8 ? 4 : 2)) copy_units<D, I8>(run, smem, warp - kWarps);
     return;
   }
   asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
@@ -593,7 +594,7 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
 // units (64 keys of a tile) that the batch can have, by its longest chunk and its page table, are few: the tensor-core
 // kernel costs some 8 us more at the start and a tenth as much per unit.  Measured, few rows and tensor cores, us, 32 query
 // heads on 8, 16 sequences over 800 to 8000 keys: of 4 rows (two tiles) int8 63, 87, binary16 78, 68, 64 dims 44, 54; of
-// 5 rows (three) int8 86, 87, binary16 117, 68, 64 dims int8 70, 81, binary16 60, 54; 64 sequences of 5 rows over 1000,
+// 5 rows (three) int8 86, 87, binary16 117, 68, 64 dims int8 58, 80, binary16 60, 54; 64 sequences of 5 rows over 1000,
 // int8 100, 113.  24 query heads on 8, binary16: 16 rows over 2048 keys 18, 21, over 8192 33, 28; 64 rows over 512 21, 21,
 // over 2048 35, 25; 16 sequences of 8 rows over 128 16, 17, over 512 27, 20; 128 rows over 128 16, 17.
 constexpr int64_t kFewUnits = 1600;

@@ -453,21 +453,22 @@ struct Kernel {
     const uint32_t q = sdesc_lo(smem + L::Q);
     const uint32_t k = sdesc_lo(smem + L::KV + (uint32_t)(tile % STAGES) * L::TILE);
     const uint32_t d = tmem + L::S + 128u * place;
+    // The low halves first: each product truncates its sum, which is still small for them.
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
+    for (int i = 0; i < D / 8; ++i) {
+      const int s = i % (D / 16);
       const uint32_t off = ((uint32_t)(s / 4) * L::PANEL + (uint32_t)(s % 4) * 32u) >> 4;
-      mma_ss(d, q + off, k + off, kSdescHi128, L::IDESC_S, s > 0 ? 1u : 0u, leader);
-      mma_ss(d, q + off + (L::TILE >> 4), k + off, kSdescHi128, L::IDESC_S, 1u, leader);
+      mma_ss(d, q + off + (i < D / 16 ? L::TILE >> 4 : 0u), k + off, kSdescHi128, L::IDESC_S, i > 0 ? 1u : 0u, leader);
     }
   }
   __device__ void issue_pv(int place, int o, int tile, bool fresh, uint32_t leader) const {
     const uint32_t v = sdesc_lo_mn(smem + L::KV + (uint32_t)(tile % STAGES) * L::TILE);
     const uint32_t p = tmem + L::S + 128u * place, d = tmem + L::O + (uint32_t)D * o;
 #pragma unroll
-    for (int s = 0; s < kKeys / 16; ++s) {
-      const uint32_t at = p + 32u * (s / 2) + 8u * (s % 2), off = (uint32_t)(s * 16 * 128) >> 4;
-      mma_ts(d, at, v + off, kSdescHi128, L::IDESC_O, fresh && s == 0 ? 0u : 1u, leader);
-      mma_ts(d, at + 16u, v + off, kSdescHi128, L::IDESC_O, 1u, leader);
+    for (int i = 0; i < kKeys / 8; ++i) {
+      const int s = i % (kKeys / 16);
+      const uint32_t at = p + 32u * (s / 2) + 8u * (s % 2) + (i < kKeys / 16 ? 16u : 0u);
+      mma_ts(d, at, v + ((uint32_t)(s * 16 * 128) >> 4), kSdescHi128, L::IDESC_O, fresh && i == 0 ? 0u : 1u, leader);
     }
   }
   __device__ void issuer() const {
