@@ -11,7 +11,7 @@
 // 16 neighbouring bytes for its fragments (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys
 // are byte permutes).
 // Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 328 us (the rate of
-// a copy), int8 188 us (0.94 of it: bound by widening int8 to binary16); one sequence of 300 keys 10 us, bound by the
+// a copy), int8 188 us (0.92 of it: bound by widening int8 to binary16); one sequence of 300 keys 10 us, bound by the
 // latency of a launch, four dependent loads and three units.  More rows a tile (16 to 32) share the reads, but their
 // chains of dependent steps grow with them: 16 sequences of 8 rows of 4 heads took 147 us so, 137 as four tiles, 80 on
 // the tensor-core kernel.
