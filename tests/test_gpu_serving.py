@@ -675,3 +675,21 @@ def test_int8_codes_are_the_rounded_quotients(spl, heads):
         at = torch.as_tensor(t % 16).to(DEV)
         assert np.array_equal(getattr(c.cache, which)[page, :, at].cpu().numpy(), code)
         assert np.array_equal(getattr(c.cache, which + "_scale")[page, :, at].cpu().numpy(), scale)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("count", [13, 64, 300])
+@pytest.mark.parametrize("rows", [1, 3, 40])
+def test_batches_of_many_lengths(spl, rows, count, fmt):
+    """Shares of blocks that begin and end anywhere: many short tiles beside long ones, sequences without rows or tokens."""
+    g = np.random.default_rng(100 * rows + count)
+    seqs = []
+    for i in range(count):
+        n = int(g.integers(0, (40, 200, 3000)[i % 3]))
+        r = 0 if i % 7 == 3 else int(g.integers(1, rows + 1))
+        seqs.append((min(r, n) if i % 5 else r, n))
+    c = Case(spl, seqs, (8, 2, 64) if rows == 3 else (4, 2, 128), fmt, 32, seed=count)
+    c.fill()
+    check_sample(c, 3)
+    many(c)
+    check_sample(c, 2, window=int(g.integers(1, 300)))
