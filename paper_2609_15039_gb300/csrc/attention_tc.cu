@@ -21,10 +21,10 @@
 // its other place while the sums' warps add the first to an fp32 sum in the workspace, rounding to nearest.
 // Divided tiles are joined by a second, small launch over all SMs.
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its copies and MMAs done.
-// Measured with 32 query heads on 8 of 128 dims, 2048 rows over 12049 keys: binary16 475 us, 0.9 of the instructions'
-// 2560 clocks a tile (S takes 96 an instruction, both its operands being in shared memory, O 64); int8 688 us, bound by
-// the widening and shared memory; 64 dims 389 and 638 us, bound by the softmax.  24 heads on 8, 512 rows over themselves
-// 23 us: some 14 us of one tile's latency, launches and the join.
+// Measured with 32 query heads on 8 of 128 dims, 2048 rows over 12049 keys: binary16 466 us, 0.9 of the instructions'
+// 2560 clocks a tile (S takes 96 an instruction, both its operands being in shared memory, O 64); int8 684 us, bound by
+// the widening and shared memory; 64 dims 386 and 637 us, bound by the softmax.  24 heads on 8, 512 rows over themselves
+// 21 us: some 14 us of one tile's latency, launches and the join.
 
 #include <algorithm>
 #include <cmath>
@@ -235,9 +235,10 @@ struct Kernel {
       if (run.busy()) run.next();
       const Piece* place = piece(k, ok);
       if (!ok) break;
-      const int n = place->tiles;
+      const Piece x = *place;  // (in registers)
+      const int n = x.tiles;
       if (n == 0) break;
-      ok = I8 ? load_i8(*place, y) : load_f16(*place, y);
+      ok = I8 ? load_i8(x, y) : load_f16(x, y);
       y.step += n;
       piece_done(k);
     }
