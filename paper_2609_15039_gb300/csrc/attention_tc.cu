@@ -1009,6 +1009,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
   }
   if (warp == 0) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
   Run run(a, reinterpret_cast<int64_t*>(base));  // the prefix sums lie where the tiles will
+  fence_proxy_async_smem();                      // and are read and written before the copies overwrite them
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

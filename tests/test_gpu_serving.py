@@ -693,3 +693,17 @@ def test_batches_of_many_lengths(spl, rows, count, fmt):
     check_sample(c, 3)
     many(c)
     check_sample(c, 2, window=int(g.integers(1, 300)))
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (4, 2, 128)], ids=str)
+def test_many_rows_of_as_many_sequences_as_there_may_be(spl, heads, fmt):
+    """The prefix sums of 4096 sequences lie where the first copies of keys and values go."""
+    g = np.random.default_rng(heads[2])
+    seqs = [(int(r), int(r + n)) for r, n in zip(g.integers(1, 3, 4096), g.integers(0, 40, 4096))]
+    seqs[0] = seqs[-1] = (40, 500)
+    c = many(Case(spl, seqs, heads, fmt, 16, seed=heads[2]))
+    c.fill()
+    got = check_sample(c, 1)
+    for _ in range(3):
+        assert np.array_equal(c.attend(), got)
