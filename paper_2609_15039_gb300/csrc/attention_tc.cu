@@ -896,6 +896,7 @@ struct Kernel {
             for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * (i & 2 ? f1 : f0));
             tmem_st_16x64(to + 64u * c, v);
           }
+          tmem_st_wait();  // (a second rescaling in the same tile reads what this one wrote)
           return true;
         };
         float down[2] = {1.f, 1.f};

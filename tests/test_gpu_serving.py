@@ -707,3 +707,18 @@ def test_many_rows_of_as_many_sequences_as_there_may_be(spl, heads, fmt):
     got = check_sample(c, 1)
     for _ in range(3):
         assert np.array_equal(c.attend(), got)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 2, 128)], ids=str)
+@pytest.mark.parametrize("rows,keys", [(150, 1200), (33, 2500)])
+def test_many_rows_scores_and_values_that_grow_together(spl, rows, keys, heads, fmt):
+    """In every tile of 128 keys the scores pass the maximum before it and the values (their scales) those before them, so
+    that a tile's sums are rescaled for both."""
+    c = many(Case(spl, [(rows, keys)], heads, fmt, 64, seed=rows))
+    tile = (np.arange(keys) // 128)[:, None, None]
+    c.q = (c.q * 0.25 + 1.0).astype(np.float32)
+    c.k[0] = (c.k[0] * 0.25 + 0.6 * (64 / c.d) ** 0.5 * tile).astype(np.float32)  # steps of some 7 powers of two
+    c.v[0] *= np.exp2(3.0 * (tile % 8)).astype(np.float32)
+    c.fill()
+    check_sample(c, 24)
