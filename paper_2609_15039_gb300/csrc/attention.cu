@@ -67,6 +67,7 @@ struct Frag {
   static constexpr uint32_t K = 0, V = UNIT * D * ESZ, KS = 2 * V, VS = KS + (I8 ? UNIT * 4 : 0);
   static constexpr uint32_t STAGE = VS + (I8 ? UNIT * 4 : 0);
   static constexpr int STAGES = V > 24576 ? 3 : 4;
+  static constexpr int COPIERS = I8 ? 4 : 2;  // copying warps
   static constexpr uint32_t RING = STAGES * STAGE;
   // shared memory: the ring (the prefix sums before it), sums of four warps, maxima and totals, barriers (full, empty) and
   // the mask of a stage's blocks that hold keys
@@ -81,7 +82,8 @@ struct Frag {
 
 // A copying warp: unit after unit of the block's run into the ring's stages in turn.  Each has a part of what a unit
 // consists of (keys, values, their scales): with pages of 16 tokens, 64 copies a unit, one warp alone was the
-// bound (64 sequences of one row over 1600 to 15775 keys, int8, 352 us instead of 193).
+// bound (64 sequences of one row over 1600 to 15775 keys, int8, 352 us instead of 193).  Each arrives at every unit, also
+// where it copies nothing: none can fall a turn of the ring behind the others and wait for a phase that has passed.
 template <int D, bool I8>
 __device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8_t* smem, int part) {
   using F = Frag<D, I8>;
@@ -123,6 +125,8 @@ __device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8
       if (part == 0 && lane == 0) {
         *reinterpret_cast<volatile uint32_t*>(smem + F::MASK + 4 * stage) = mask;
         mbar_expect_tx(full, 16u * __popc(mask) * (2u * D * F::ESZ + (I8 ? 8u : 0u)));
+      } else if (lane == 0) {
+        mbar_arrive(full);
       }
       __syncwarp();
       if (leads) {
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   if (threadIdx.x == 0) *abort = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t bars = smem_u32(smem + F::BARS);
-  if (threadIdx.x < 2 * F::STAGES) mbar_init(bars + 8u * threadIdx.x, threadIdx.x < F::STAGES ? 1 : kWarps);
+  if (threadIdx.x < 2 * F::STAGES) mbar_init(bars + 8u * threadIdx.x, threadIdx.x < F::STAGES ? F::COPIERS : kWarps);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   AttnRun<kRT, F::UNIT, kThreads> run(a, reinterpret_cast<int64_t*>(smem));
   fence_proxy_async_smem();
@@ -168,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   // 168 registers a thread at the start; 3 x 168 = 2 x 232 + 40
   if (warp >= kWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (warp < kWarps + (I8 ? 4 : 2)) copy_units<D, I8>(run, smem, warp - kWarps);
+    if (warp < kWarps + F::COPIERS) copy_units<D, I8>(run, smem, warp - kWarps);
     return;
   }
   asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");

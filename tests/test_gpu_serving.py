@@ -722,3 +722,15 @@ def test_many_rows_scores_and_values_that_grow_together(spl, rows, keys, heads, 
     c.v[0] *= np.exp2(3.0 * (tile % 8)).astype(np.float32)
     c.fill()
     check_sample(c, 24)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_long_runs_of_sequences_without_keys(spl, dim, fmt):
+    """Units of which no key is copied, by the hundred, before, between and behind those that have some."""
+    seqs = [(1, 300 if b in (700, 701, 1900) else 0) for b in range(3000)]
+    c = Case(spl, seqs, (4, 2, dim), fmt, 16, seed=dim)
+    c.fill()
+    for _ in range(3):
+        got = check_sample(c, 1)
+        assert np.all(got[[b for b, (_, n) in enumerate(seqs) if n == 0]] == 0)
