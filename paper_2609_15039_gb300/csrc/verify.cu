@@ -20,6 +20,7 @@ namespace spl {
 namespace {
 
 constexpr int kThreads = 256, kBlocksPerSm = 3;
+constexpr int64_t kMostEntries = int64_t(1) << 30;  // of a row that are counted at once: indexes are 32-bit
 
 struct VerifyState {  // one a sequence, in the zeroed workspace; left zero
   unsigned long long key;
@@ -222,8 +223,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) verify_kernel(const Ve
   __syncthreads();
   if (s_role == kDone) return;
   if (s_role == kAgain) {  // p is nowhere above q: the draw is from p
-    first.load_random(e, (VEC ? 4 : 1) * threadIdx.x, (int)a.vocab);
-    key = block_max(race_row<VEC>(p, nullptr, e, 0, (int)a.vocab, first, positive), keys);
+    key = 0;
+    for (int64_t from = 0; from < a.vocab; from += kMostEntries) {
+      const int some = (int)min(kMostEntries, a.vocab - from);
+      first.load_random(e + from, (VEC ? 4 : 1) * threadIdx.x, some);
+      key = max(key, race_row<VEC>(p, nullptr, e, from, some, first, positive));
+    }
+    key = block_max(key, keys);
   } else if (threadIdx.x == 0) {
     key = __ldcg(&st->key);
   }
@@ -264,9 +270,10 @@ extern "C" spl_status spl_verify_drafts(int32_t* accepted, int32_t* token, const
   if (!aligned16(workspace)) return SPL_EALIGN;
   unsigned int* status = device_status_word();
   if (!status) return SPL_ECUDA;
-  // Blocks for one wave, each with at least a trip of its threads' loads; slices are whole 16-byte units.
+  // Blocks for one wave, each with at least a trip of its threads' loads and at most kMostEntries; slices are whole 16-byte
+  // units.
   const int64_t most = ceil_div(vocab, (int64_t)4 * kThreads);
-  const int64_t want = std::max<int64_t>(1, (int64_t)kBlocksPerSm * device_sm_count() / seqs);
+  const int64_t want = std::max((int64_t)kBlocksPerSm * device_sm_count() / seqs, ceil_div(vocab, kMostEntries));
   const int64_t per_split = round_up(ceil_div(vocab, std::min(most, want)), 4);
   const bool vec = ldp % 4 == 0 && ldq % 4 == 0 && lde % 4 == 0 && aligned16(P) && aligned16(Q) && aligned16(e);
   const VerifyArgs a = {accepted, token, P,   Q,   draft, u,    e,      row_start,  draft_start,

@@ -734,3 +734,18 @@ def test_long_runs_of_sequences_without_keys(spl, dim, fmt):
     for _ in range(3):
         got = check_sample(c, 1)
         assert np.all(got[[b for b, (_, n) in enumerate(seqs) if n == 0]] == 0)
+
+
+@pytest.mark.parametrize("vocab", [2 ** 31 - 1, 2 ** 31 - 4])
+def test_verify_draws_again_from_the_longest_row(spl, vocab):
+    """A draft that is rejected where p is nowhere above q, over as many entries as there may be: the second draw's indexes
+    reach 2^31."""
+    P, e = torch.zeros((2, vocab), device=DEV), torch.ones((1, vocab), device=DEV)
+    P[0, 7] = 0.25
+    P[0, vocab - 2:] = 0.5
+    accepted, token = i32([-9]), i32([-9])
+    spl.spl_verify_drafts(accepted, token, P, P[:1], i32([7]), torch.ones(1, device=DEV), e, i32([0, 2]), i32([0, 1]))
+    assert accepted.tolist() == [0] and token.tolist() == [vocab - 2]
+    assert spl.spl_get_device_status() == spl.SPL_OK
+    del P, e
+    torch.cuda.empty_cache()
