@@ -47,11 +47,16 @@ class Pages:
         lens = torch.tensor(self.lens, dtype=torch.int32)
         return spl.KVBatch(start.cuda(), lens.cuda(), self.table.cuda(), int(start[-1]), max(new))
 
-    def cut(self, lens):
-        """Drops the tokens past the given lengths, and the pages that then hold none."""
+    def rewind(self, lens):
+        """Drops the tokens past the given lengths; their pages stay with the sequences, for the same tokens again."""
         for b, n in enumerate(lens):
             assert n <= self.lens[b]
             self.lens[b] = n
+
+    def cut(self, lens):
+        """Drops the tokens past the given lengths, and the pages that then hold none."""
+        self.rewind(lens)
+        for b, n in enumerate(lens):
             while len(self.own[b]) > -(-n // self.page_size):
                 self.free.append(self.own[b].pop())
 
@@ -140,7 +145,7 @@ def generate(target, draft, pages, prompts, drafts, rounds, seed=0):
             if i < drafts:
                 proposals.append(probs(logits))
                 chosen.append(sample(proposals[-1], gen))
-        pages.cut(base)  # the target sees the same tokens, all at once
+        pages.rewind(base)  # the target sees the same tokens, all at once, where the draft has them
         rows = torch.stack(chosen, dim=1)  # [n, drafts + 1]
         P = probs(target.forward(rows.reshape(-1), pages.grow([drafts + 1] * n)))
         Q = torch.stack(proposals, dim=1).reshape(n * drafts, -1)

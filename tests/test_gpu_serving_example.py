@@ -77,6 +77,16 @@ def test_a_decoder_accepts_its_own_drafts(serving):
     assert pages.lens == lens and len(pages.free) == total - sum(-(-n // 64) for n in lens)
 
 
+def test_sequences_that_pass_the_end_of_a_page_together(serving):
+    """Equal prompts of 62 tokens on pages of 64, and the decoder itself as draft: all drafts are accepted, so each sequence
+    finds its own keys and values in both caches."""
+    target, draft, pages = serving.synthetic(1, seqs=4, max_len=200, formats=("f16", "f16"))
+    prompts = [list(range(100 * b, 100 * b + 62)) for b in range(4)]
+    out, history = serving.generate(target, draft, pages, prompts, drafts=3, rounds=20)
+    assert sum(map(sum, history)) >= 4 * 3 * 20 - 2  # (a draw within rounding of the edge is a chance of 1e-4)
+    assert pages.lens == [62 + len(o) - 1 for o in out]
+
+
 def test_a_smaller_draft_and_int8(serving, capsys):
     assert serving.main(["--sequences", "3", "--layers", "2", "--rounds", "5", "--prompt", "33", "--eps", "4"]) == 0
     line = capsys.readouterr().out

@@ -1,5 +1,6 @@
 """The serving operators' refusals and empty calls, which need no GPU, and the oracle against closed forms."""
 
+import collections
 import ctypes
 import os
 
@@ -194,3 +195,58 @@ def test_pages_are_taken_and_given_back(monkeypatch):
     p.grow([32, 0])
     with pytest.raises(ValueError):
         p.grow([0, 17])  # no page left
+
+
+Batch = collections.namedtuple("Batch", "row_start kv_len table rows max_rows")
+
+
+class Slots:
+    """A decoder that only keeps which token lies in which slot, and looks that its sequences find their own."""
+
+    def __init__(self, pages, vocab):
+        import torch
+        self.pages, self.vocab, self.held = pages, vocab, {}
+        self.embedding = torch.zeros((vocab, 1))
+        self.seen = [[] for _ in pages.lens]
+
+    def at(self, b, pos):
+        size = self.pages.page_size
+        return int(self.pages.table[b, pos // size]), pos % size
+
+    def forward(self, tokens, batch):
+        import torch
+        start, lens = batch.row_start.tolist(), batch.kv_len.tolist()
+        for b, n in enumerate(lens):
+            new = tokens[start[b]:start[b + 1]].tolist()
+            self.seen[b] = self.seen[b][:n - len(new)] + new
+            for i, t in enumerate(new):
+                self.held[self.at(b, n - len(new) + i)] = (b, t)
+        for b, n in enumerate(lens):
+            assert [self.held.get(self.at(b, i)) for i in range(n)] == [(b, t) for t in self.seen[b][:n]]
+        return torch.zeros((len(tokens), self.vocab))
+
+
+@pytest.mark.parametrize("prompts,page", [([14] * 4, 16), ([62] * 8, 64), ([16, 15, 14, 13, 12], 16)], ids=str)
+def test_drafts_and_target_find_their_own_tokens(monkeypatch, prompts, page):
+    """Sequences that pass the end of a page in one round: whatever is accepted, each finds its own tokens in its slots,
+    in the draft's cache as in the target's."""
+    import torch
+    from paper_2609_15039_gb300 import serving
+    g = torch.Generator()
+    g.manual_seed(5)
+    monkeypatch.setattr(serving.spl, "KVBatch", Batch)
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self: self)
+
+    def verify(accepted, token, P, Q, x, u, e, row_start, draft_start):
+        accepted.copy_(torch.randint(0, 5, accepted.shape, generator=g))
+        token.copy_(torch.randint(0, P.shape[1], token.shape, generator=g))
+
+    monkeypatch.setattr(serving.spl, "spl_verify_drafts", verify)
+    n, count = len(prompts), len(prompts) * -(-200 // page)
+    pages = serving.Pages(count, page, n, 200)
+    target, draft = Slots(pages, 1000), Slots(pages, 1000)
+    out, history = serving.generate(target, draft, pages, [[100 * b + i for i in range(m)] for b, m in enumerate(prompts)],
+                                    drafts=4, rounds=12)
+    lens = [m + len(o) - 1 for m, o in zip(prompts, out)]
+    assert pages.lens == lens and len(history) == 12
+    assert len(pages.free) == count - sum(-(-m // page) for m in lens)
