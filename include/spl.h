@@ -584,7 +584,9 @@ size_t spl_test_tc_swap_workspace_bytes(int64_t M, int64_t K, int64_t N, int til
  * trusted party, Sec. 5.1).  Array contents on the device are not read by the
  * host: a length, page id or token id outside its range is skipped by the
  * kernels, never followed, and reported by the next spl_get_device_status as
- * SPL_EINVAL. */
+ * SPL_EINVAL.  A negative length counts as 0; of one past the page table the
+ * tokens past its end are left out (neither written, read nor seen), while rows
+ * keep the positions that the length gives them. */
 
 /* Format of a cache's vectors.
  *  F16 -- fp16(x), rounded to nearest, values beyond +-65504 saturated.

@@ -50,7 +50,7 @@ struct AttnTile {
 
 // Keys [lo, hi) that token i of sequence s sees.
 __device__ __forceinline__ void row_keys(const PagedSeq& s, int window, int i, int& lo, int& hi) {
-  const int pos = s.len - s.n + i;
+  const int pos = s.pos0 + i;
   hi = max(0, min(pos + 1, s.len));
   lo = pos >= window ? min(pos - window + 1, hi) : 0;
 }

@@ -63,7 +63,7 @@ struct Piece {
   int key_lo, key_hi;  // keys that some row sees
   int all_lo, all_hi;  // keys that every row sees
   int b, h;            // sequence, key head
-  int row0, n, len;    // the sequence's first row, rows and length
+  int row0, len, pos0; // the sequence's first row, length and first row's position
   int r0, rows;        // rows of the tile among the sequence's rows of the key head
   int first;           // the first tile's index among the whole tile's
   int whole;           // the piece is the whole tile
@@ -106,7 +106,7 @@ constexpr int64_t slot_floats() {
 // A divided tile that begins in a block's run, for the join.
 struct Divided {
   int last_block;  // 0: none (a divided tile never ends in block 0)
-  int head, row0, n, r0, rows;
+  int head, row0, r0, rows;
 };
 
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc,
@@ -193,7 +193,7 @@ struct Kernel {
       if (run.busy()) {
         const AttnTile& x = run.x;
         y = {run.last() - run.first, (x.unit0 + run.first) * kKeys, x.key_lo, x.key_hi, x.all_lo, x.all_hi, x.b, x.h,
-             (int)x.s.row0, x.s.n, x.s.len, x.r0, x.rows, run.first, run.whole() ? 1 : 0, run.last_block()};
+             x.s.row0, x.s.len, x.s.pos0, x.r0, x.rows, run.first, run.whole() ? 1 : 0, run.last_block()};
       }
       mbar_arrive(bar(kPieceFull + k % kPieces));
     }
@@ -619,7 +619,7 @@ struct Kernel {
         ev_slot = ev;
       }
       if (ok && x.whole == 0 && x.first == 0 && own == 0)
-        *divided = {x.last_block, x.h, x.row0, x.n, x.r0, x.rows};
+        *divided = {x.last_block, x.h, x.row0, x.r0, x.rows};
       piece_done(k);
     }
     if (!ok && (threadIdx.x & 31) == 0) give_up();
@@ -877,7 +877,7 @@ struct Kernel {
 #pragma unroll
           for (int r = 0; r < 2; ++r) {  // (rows past the last see all: nothing reads them)
             int lo = j0, hi = j0 + kKeys;
-            if (own0 + 8 * r < x.rows) row_keys({0, x.n, x.len}, a.window, (x.r0 + own0 + 8 * r) / a.group, lo, hi);
+            if (own0 + 8 * r < x.rows) row_keys({0, 0, x.len, x.pos0}, a.window, (x.r0 + own0 + 8 * r) / a.group, lo, hi);
             sc.lo[r] = lo - j0;
             sc.hi[r] = hi - j0;
           }

@@ -54,8 +54,8 @@ kv_append_kernel(const PagedCache cache, const PagedBatch batch, const float* __
   const int b = paged_find(batch.row_start, batch.seqs, row);
   const PagedSeq s = paged_seq(batch, cache.page_shift, b);
   const int64_t i = row - s.row0;
-  const int64_t pos = (int64_t)s.len - s.n + i;
-  if (i < 0 || i >= s.n || pos < 0) return;  // no sequence's row, or before its first position
+  const int64_t pos = s.pos0 + i;
+  if (i < 0 || i >= s.n || pos < 0 || pos >= s.len) return;  // no sequence's row, or without a place in its table
   const int page = paged_page(cache, batch, b, (int)pos);
   if (page < 0) return;
   void* dst = is_v ? cache.v : cache.k;

@@ -28,21 +28,23 @@ struct PagedBatch {
   unsigned int* status;
 };
 
-// Sequence b's first row, rows and length, brought inside the arrays whatever the device arrays hold.
+// Sequence b's first row, rows, stored tokens and first row's position, brought inside the arrays whatever the device
+// arrays hold.  A length past the table ends there, but its rows stand where it says: those past the end have no place.
 struct PagedSeq {
-  int64_t row0;
-  int n, len;
+  int row0, n, len, pos0;
 };
 __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& batch, int page_shift, int b) {
   PagedSeq s;
   const int64_t a = __ldg(batch.row_start + b), e = __ldg(batch.row_start + b + 1);
-  s.row0 = a < 0 ? 0 : (a > batch.rows ? batch.rows : a);
-  const int64_t end = e < s.row0 ? s.row0 : (e > batch.rows ? batch.rows : e);
-  s.n = (int)(end - s.row0);
+  const int64_t row0 = a < 0 ? 0 : (a > batch.rows ? batch.rows : a);
+  const int64_t end = e < row0 ? row0 : (e > batch.rows ? batch.rows : e);
+  s.row0 = (int)row0;
+  s.n = (int)(end - row0);
   const int64_t room = batch.max_pages << page_shift;
-  const int len = __ldg(batch.kv_len + b);
-  s.len = len < 0 ? 0 : (len > room ? (int)room : len);
-  if (len > room) atomicOr(batch.status, kStatusIndex);
+  const int said = __ldg(batch.kv_len + b), len = said < 0 ? 0 : said;
+  s.len = len > room ? (int)room : len;
+  s.pos0 = len - s.n;
+  if (said > room) atomicOr(batch.status, kStatusIndex);
   return s;
 }
 

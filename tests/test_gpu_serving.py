@@ -749,3 +749,38 @@ def test_verify_draws_again_from_the_longest_row(spl, vocab):
     assert spl.spl_get_device_status() == spl.SPL_OK
     del P, e
     torch.cuda.empty_cache()
+
+
+def bits(t):
+    """For comparisons in which a NaN equals itself."""
+    return t.view(torch.int16) if t.dtype is torch.float16 else t
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("window", [0, 2, 30])
+def test_a_length_past_the_table(spl, window, fmt):
+    """Rows stand where the length says, not where the table ends: those past it are not written (nor any earlier token
+    overwritten), and see the keys that there are."""
+    for kernel in (lambda c: c, many):
+        c = kernel(Case(spl, [(6, 80), (2, 20)], (4, 2, 64), fmt, 16, seed=6))
+        c.table = np.ascontiguousarray(c.table[:, :5])  # room for 80 tokens
+        c.fill()
+        batch = c.batch()
+        batch.kv_len.copy_(i32([83, 20]))
+        c.batch = lambda all_rows=False, batch=batch: batch
+        got = c.attend(window)
+        assert spl.spl_get_device_status() == spl.SPL_EINVAL
+        k, v = c.stored("k", 0), c.stored("v", 0)
+        for i in range(6):
+            lo, hi = serving.visible(77 + i, 80, window)
+            q = c.q[i:i + 1]
+            ref, mass = serving.attention(q, k[lo:hi], v[lo:hi], hi - lo, 2, 0.125)
+            assert np.all(np.abs(got[i] - ref[0]) <= tolerance(q, k[lo:hi], 0.125, hi - lo, 2, mass)[0]), i
+        assert window != 2 or np.all(got[5] == 0)  # position 82 sees 81 and 82
+        before = bits(c.cache.k).clone()
+        x = torch.randn((8, 128), device=DEV)
+        spl.spl_kv_append(c.cache, batch, x, x)
+        assert spl.spl_get_device_status() == spl.SPL_EINVAL
+        changed = (bits(c.cache.k) != before).any(-1).any(1).nonzero().tolist()
+        want = [[int(c.table[b, p // 16]), p % 16] for b, p in ((0, 77), (0, 78), (0, 79), (1, 18), (1, 19))]
+        assert sorted(changed) == sorted(want)
