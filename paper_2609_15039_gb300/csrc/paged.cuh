@@ -44,7 +44,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& batch, int page_
   const int said = __ldg(batch.kv_len + b), len = said < 0 ? 0 : said;
   s.len = len > room ? (int)room : len;
   s.pos0 = len - s.n;
-  if (said > room) atomicOr(batch.status, kStatusIndex);
+  if (s.len != said) atomicOr(batch.status, kStatusIndex);
   return s;
 }
 

@@ -784,3 +784,28 @@ def test_a_length_past_the_table(spl, window, fmt):
         changed = (bits(c.cache.k) != before).any(-1).any(1).nonzero().tolist()
         want = [[int(c.table[b, p // 16]), p % 16] for b, p in ((0, 77), (0, 78), (0, 79), (1, 18), (1, 19))]
         assert sorted(changed) == sorted(want)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("length", [-1, -3, -2 ** 31])
+def test_a_negative_length_is_reported(spl, length, fmt):
+    c = Case(spl, [(3, 40), (2, 20)], (4, 2, 64), fmt, 16, seed=6)
+    c.fill()
+    want = c.check()
+    before = bits(c.cache.k).clone()
+    batch = c.batch()
+    batch.kv_len.copy_(i32([length, 20]))
+    c.batch = lambda all_rows=False: batch
+    x = torch.zeros((5, 128), device=DEV)
+    K, V = torch.full((60, 128), 3.0, device=DEV), torch.full((60, 128), 3.0, device=DEV)
+    spl.spl_kv_read(K, V, c.cache, batch, i32([0, 40, 60]))
+    assert spl.spl_get_device_status() == spl.SPL_EINVAL
+    assert bool((K[:40] == 3.0).all()) and not bool((K[40:] == 3.0).any())
+    for kernel in (lambda c: c, many):
+        got = kernel(c).attend()
+        assert spl.spl_get_device_status() == spl.SPL_EINVAL
+        assert np.all(got[:3] == 0) and np.allclose(got[3:], want[3:], rtol=0, atol=1e-5)
+    spl.spl_kv_append(c.cache, batch, x, x)
+    assert spl.spl_get_device_status() == spl.SPL_EINVAL
+    slots = {tuple(t) for t in (bits(c.cache.k) != before).any(-1).any(1).nonzero().tolist()}
+    assert slots == {(int(c.table[1, 1]), 2), (int(c.table[1, 1]), 3)}
