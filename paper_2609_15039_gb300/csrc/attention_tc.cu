@@ -48,7 +48,7 @@ constexpr int kMinExp = -100, kMaxExp = 126;
 constexpr int kSteps = 4;        // key tiles whose scales or marks have a place (see the barriers of the producer)
 
 // Barriers by index: kFull, kEmpty a stage; kRawFull, kRawEmpty a stage of int8 tiles as stored; kScale a place of K's
-// scales; kQ a piece's q; kSFull, kPFull a place of S and the p in it (whose waiter may be a tile behind); kPv a tile's
+// scales and of the mark of its missing pages; kQ a piece's q; kSFull, kPFull a place of S and the p in it (whose waiter may be a tile behind); kPv a tile's
 // product with V; kOFull, kOFree, kMFull a place of O: its chain is complete, has been added up, its rows' maxima are
 // there; kEdge the copies of V's edge tiles; kPieceFull, kPieceFree a piece's place.
 enum {
@@ -88,7 +88,8 @@ struct Layout {
   static constexpr uint32_t M = AUX, LT = M + 2 * kRows * 4, EV = LT + 2 * kRows * 4, KS = EV + (I8 ? 2 * kRows * 4 : 0);
   static constexpr uint32_t VS = KS + (I8 ? kSteps * kKeys * 4 : 0), VMAX = VS + (I8 ? kSteps * kKeys * 4 : 0);
   static constexpr uint32_t BAD = VMAX + (I8 ? kSteps * 32 : 0), BARS = BAD + (I8 ? 0 : kSteps * 16);
-  static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
+  static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece);
+  static constexpr uint32_t GONE = MISC + 16, SMEM = GONE + 4 * kSteps;  // boxes of a tile whose page is outside the pool
   static_assert(BARS % 8 == 0 && PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
   static_assert(kMaxSeqs * kPrefixBytes + 8192 <= AUX, "the prefix sums fit where the tiles go");
   static constexpr uint32_t S = 0, O = 256;                // tensor memory columns (+ 128 and + D for the other place)
@@ -134,6 +135,9 @@ __device__ __forceinline__ uint32_t sdesc_lo_mn(uint32_t saddr) {
 }
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_shared4(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
   uint4 v;
@@ -212,10 +216,14 @@ struct Kernel {
     u = i == 0 ? 0 : (v ? (i == 2 * n - 1 ? n - 1 : i / 2 - 1) : (i + 1) / 2);
     return v;
   }
-  // The page of the first 16 keys from j on that some row sees of the `size` from there (in one page), -1 if there is none.
+  // The page of the first 16 keys from j on that some row sees of the `size` from there (in one page), kUnseen if there is
+  // none, kGone if its id is outside the pool.
+  static constexpr int kUnseen = -1, kGone = -2;
   __device__ int page_of(const Piece& x, int j, int size) const {
     const int from = max(j, x.key_lo & ~15);
-    return from < min(j + size, x.key_hi) ? paged_page(a.cache, a.batch, x.b, from) : -1;
+    if (from >= min(j + size, x.key_hi)) return kUnseen;
+    const int page = paged_page(a.cache, a.batch, x.b, from);
+    return page >= 0 ? page : kGone;
   }
   static __device__ __forceinline__ void mbar_arrive_more(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -250,8 +258,8 @@ struct Kernel {
         mbar_wait(bar(first + t % stages), (uint32_t)(t / stages) & 1u, kDrainNs, nullptr);
     }
   }
-  // The first slots of a piece's boxes (a page's tokens, at most 128), those of kAhead tiles in a lane each, -1 where no
-  // row sees any key of them; those of the next kAhead tiles are looked up meanwhile.
+  // The first slots of a piece's boxes (a page's tokens, at most 128), those of kAhead tiles in a lane each, kUnseen where no
+  // row sees any key of them, or kGone; those of the next kAhead tiles are looked up meanwhile.
   static constexpr int kAhead = 4;
   struct Boxes {
     const Kernel& k;
@@ -268,14 +276,14 @@ struct Kernel {
     }
     __device__ int64_t look_up(int u0) const {
       const int lane = threadIdx.x & 31, u = u0 + lane / per_tile, j = x.j0 + u * kKeys + lane % per_tile * box;
-      const int page = lane < kAhead * per_tile && u < x.tiles ? k.page_of(x, j, box) : -1;
-      return page >= 0 ? ((((int64_t)page * k.a.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : -1;
+      const int page = lane < kAhead * per_tile && u < x.tiles ? k.page_of(x, j, box) : kUnseen;
+      return page >= 0 ? ((((int64_t)page * k.a.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : page;
     }
     // The slot of the lane's box of tile u, which is in the window.
     __device__ int64_t of(int u) const {
       const int lane = threadIdx.x & 31, at = u % kAhead * per_tile + lane;
       const int64_t a = __shfl_sync(0xffffffffu, now, at & 31), b = __shfl_sync(0xffffffffu, next, at & 31);
-      return lane >= per_tile ? -1 : (u >= base + kAhead ? b : a);
+      return lane >= per_tile ? kUnseen : (u >= base + kAhead ? b : a);
     }
     int base = 0;
     __device__ void advance() {  // past the last tile of the window's first half
@@ -299,11 +307,16 @@ struct Kernel {
       if (edge) y.edge_tile = y.tile;
       if (ok && y.tile >= STAGES) ok = wait(kEmpty + stage, (uint32_t)(y.tile / STAGES - 1) & 1u);
       if (!ok) break;
+      const int64_t slot = boxes.of(u);
+      const uint32_t gone = __ballot_sync(0xffffffffu, slot == kGone);
       if (lane == 0) {
         mbar_expect_tx(bar(to), L::TILE);
         if (!edge) mbar_arrive_more(bar(to), kHelpers - 1);
+        if (!v) {
+          st_shared4(smem + L::GONE + 4u * ((y.step + u) % kSteps), gone);
+          mbar_arrive(bar(kScale + (y.step + u) % kSteps));
+        }
       }
-      const int64_t slot = boxes.of(u);
       if (lane < boxes.per_tile) {
         const uint32_t dst = smem + L::KV + (uint32_t)stage * L::TILE + (uint32_t)(lane * boxes.box) * 128u;
 #pragma unroll
@@ -328,8 +341,10 @@ struct Kernel {
       const int64_t slot = boxes.of(u);
       const uint32_t raw = smem + L::RAW + (uint32_t)stage * L::RAW_STAGE, full = bar(kRawFull + stage);
       const uint32_t mask = __ballot_sync(0xffffffffu, slot >= 0);  // of boxes
+      const uint32_t gone = __ballot_sync(0xffffffffu, slot == kGone);
       if (lane == 0) {
-        asm volatile("st.shared.b32 [%0], %1;" ::"r"(raw + L::RAW_MASK), "r"(mask) : "memory");
+        st_shared4(raw + L::RAW_MASK, mask);
+        st_shared4(raw + L::RAW_MASK + 4u, gone);
         mbar_expect_tx(full, (uint32_t)(__popc(mask) * boxes.box * (D + 4)));
       }
       __syncwarp();
@@ -410,8 +425,9 @@ struct Kernel {
     for (int k = 0; k < PER; ++k)
       if (key0 + KEY_STEP * k < kKeys) q[k] = ld_shared16(raw + (uint32_t)(key0 + KEY_STEP * k) * D + 16u * part);
     float scale = 0.f;
-    uint32_t mask = 0u;
+    uint32_t mask = 0u, gone = 0u;
     if (i < kKeys) {
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(gone) : "r"(raw + L::RAW_MASK + 4u));
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(mask) : "r"(raw + L::RAW_MASK));
       asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(raw + L::RAW_SCALE + 4u * i));
       if (!(mask >> (i >> a.cache.page_shift) & 1u)) scale = 0.f;
@@ -443,6 +459,7 @@ struct Kernel {
                        : "memory");
       }
     }
+    if (!v && i == 0) st_shared4(smem + L::GONE + 4u * (step % kSteps), gone);
     fence_proxy_async_smem();
     arrive(kFull + stage);
     if (!v && lane == 0) mbar_arrive(bar(kScale + step % kSteps));
@@ -676,9 +693,10 @@ struct Kernel {
   }
 
   // A key tile's scores in tensor memory, and what they meet: the scales of the keys and values (int8), the marks of bad
-  // values, the keys [lo, hi) that the thread's rows see, the rows' own scales.
+  // values (if there are any), the boxes of 2^shift keys whose pages are outside the pool, the keys [lo, hi) that the thread's
+  // rows see, the rows' own scales.
   struct Scores {
-    uint32_t ts, ks, vs, bad;
+    uint32_t ts, ks, vs, bad, gone, shift;
     int lo[2], hi[2];
     float row_scale[2];
   };
@@ -716,8 +734,8 @@ struct Kernel {
     }
     if constexpr (EDGE) {
       if constexpr (!I8) {
-        uint32_t bad;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(bad) : "r"(x.bad + 4u * c));
+        uint32_t bad = 0u;
+        if (x.bad) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(bad) : "r"(x.bad + 4u * c));
         if (bad) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -731,6 +749,11 @@ struct Kernel {
       for (int i = 0; i < 16; ++i) {
         const int j = 8 * (i >> 2) + (i & 1), r = i >> 1 & 1;
         if (j < lo[r] || j >= hi[r]) s[i] = 0xff800000u;
+      }
+      if (x.gone) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (x.gone >> ((32 * c + 8 * (i >> 2)) >> x.shift) & 1u) s[i] = 0xff800000u;
       }
     }
   }
@@ -852,6 +875,7 @@ struct Kernel {
       const int n = x.tiles;
       if (n == 0) break;
       Scores sc;
+      sc.shift = (uint32_t)min(a.cache.page_shift, 7);
       split_q(x, row0, sc.row_scale);
       fence_proxy_async_smem();
       arrive(kQ);
@@ -862,7 +886,7 @@ struct Kernel {
         const int j0 = x.j0 + j * kKeys, s4 = step % kSteps;
         const bool edge = edge_of(x, j0), fresh = j % kChain == 0;
         ok = wait(kSFull + (step & 1), (uint32_t)(step >> 1) & 1u);
-        if (ok && I8) ok = wait(kScale + s4, (uint32_t)(step / kSteps) & 1u);
+        if (ok) ok = wait(kScale + s4, (uint32_t)(step / kSteps) & 1u);
         if (ok && (I8 || edge)) {  // V's scales, or marks
           const int tv = tile0 + (j < n - 1 ? 2 * j + 2 : 2 * j + 1);
           ok = wait(kFull + tv % STAGES, (uint32_t)(tv / STAGES) & 1u);
@@ -872,8 +896,10 @@ struct Kernel {
         sc.ts = tmem + lanes + L::S + 128u * (step & 1);
         sc.ks = smem + L::KS + (uint32_t)s4 * (kKeys * 4);
         sc.vs = smem + L::VS + (uint32_t)s4 * (kKeys * 4);
-        sc.bad = smem + L::BAD + 16u * s4;
-        if (edge) {
+        sc.bad = edge ? smem + L::BAD + 16u * s4 : 0u;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc.gone) : "r"(smem + L::GONE + 4u * s4));
+        const bool masked = edge || sc.gone != 0;
+        if (masked) {
 #pragma unroll
           for (int r = 0; r < 2; ++r) {  // (rows past the last see all: nothing reads them)
             int lo = j0, hi = j0 + kKeys;
@@ -902,7 +928,7 @@ struct Kernel {
         float down[2] = {1.f, 1.f};
         if constexpr (I8) {  // the largest value scale that a row sees sets its sums' units
           float big[2] = {0.f, 0.f};
-          if (edge) {
+          if (masked) {
             for (int i = 2 * t; i < kKeys; i += 8) {
               const uint2 w = ld_shared8(sc.vs + 4u * i);
 #pragma unroll
@@ -929,7 +955,7 @@ struct Kernel {
           ok = rescale_o(f[0], f[1]);
           if (!ok) break;
         }
-        ok = edge ? make_p<true>(sc, m, l, down, rescale_o) : make_p<false>(sc, m, l, down, rescale_o);
+        ok = masked ? make_p<true>(sc, m, l, down, rescale_o) : make_p<false>(sc, m, l, down, rescale_o);
         if (!ok) break;
         tc_fence_before();
         arrive(kPFull + (step & 1));
@@ -986,7 +1012,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
       init(kFull + s, kHelpers);
       init(kEmpty + s, 1);
     }
-    for (int s = 0; s < kSteps; ++s) init(kScale + s, kHelpers);
+    for (int s = 0; s < kSteps; ++s) init(kScale + s, I8 ? kHelpers : 1);
     init(kQ, kSoftmax);
     init(kPv, 1);
     for (int i = 0; i < 2; ++i) {

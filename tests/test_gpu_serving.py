@@ -809,3 +809,32 @@ def test_a_negative_length_is_reported(spl, length, fmt):
     assert spl.spl_get_device_status() == spl.SPL_EINVAL
     slots = {tuple(t) for t in (bits(c.cache.k) != before).any(-1).any(1).nonzero().tolist()}
     assert slots == {(int(c.table[1, 1]), 2), (int(c.table[1, 1]), 3)}
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("page", [16, 64, 128, 256])
+@pytest.mark.parametrize("window", [0, 200])
+def test_keys_on_pages_outside_the_pool_are_hidden(spl, window, page, fmt):
+    """Both kernels leave out the keys of a page whose id is outside the pool, as if they were not visible."""
+    for kernel in (lambda c: c, many):
+        c = kernel(Case(spl, [(40, 1000), (3, 150), (130, 130)], (4, 2, 64), fmt, page, seed=page))
+        c.fill()
+        gone = [np.zeros(n, dtype=bool) for _, n in c.seqs]
+        for b, at, bad in ((0, 3, -5), (0, 1000 // page, 1 << 30), (0, 900 // page, -1), (1, 0, c.cache.pages), (2, 0, -2 ** 31)):
+            c.table[b, at] = bad
+            gone[b][at * page:(at + 1) * page] = True
+        got = c.attend(window)
+        assert spl.spl_get_device_status() == spl.SPL_EINVAL
+        for b, (r, n) in enumerate(c.seqs):
+            k, v = c.stored("k", b), c.stored("v", b)
+            for i in range(0, r, 1 if r < 40 else 7):
+                lo, hi = serving.visible(n - r + i, n, window)
+                q, mine = c.q[c.start[b] + i:c.start[b] + i + 1], got[c.start[b] + i]
+                at = np.flatnonzero(~gone[b][lo:hi]) + lo
+                if len(at) == 0:
+                    assert np.all(mine == 0)
+                    continue
+                ref, mass = serving.attention(q, k[at], v[at], len(at), 2, 0.125)
+                tol = tolerance(q, k[at], 0.125, n, 2, mass)[0] + 2.0 ** -32 * n * np.max(np.abs(v))
+                assert np.all(np.abs(mine - ref[0]) <= tol), (b, i)
+        assert spl.spl_get_device_status() == spl.SPL_OK
