@@ -3,8 +3,10 @@
 // o = sum_j softmax_j(scale q . k_j) v_j, in one pass over the keys with a running maximum m, total l and sums O.
 // For few rows the pass is bound by reading the cache once.  A tile has 8 rows (for one new token, the query heads of
 // a key head); its products run on mma.m16n8k16.  q . k: the 8 rows' high and low halves are the 16 rows of A, so that one
-// instruction makes both terms of q = (hi + lo) 2^-e.  p . v is made transposed, v^T as A and the high, then the low
-// halves of p as B, into the same sums.  The stored binary16 (or int8) values are exact in those products: fp32 accuracy.
+// instruction makes both terms of q = (hi + lo) 2^-e.  p . v is made transposed, v^T as A and the low, then the high
+// halves of p as B.  The stored binary16 (or int8) values are exact in those products: fp32 accuracy.  The tensor core
+// truncates as it accumulates, so the products of 16 keys are added to the sums by themselves, rounding to nearest (131072
+// keys in one piece were off by up to 5e-5 in one chain; the additions cost int8 1%, binary16 nothing).
 // A block has an SM.  Two or four warps copy units of 128 or 256 keys (some 64 KB of keys and values) into a ring by bulk copies
 // of whole runs of a page, so that some 190 KB are on their way on an SM, across the ends of tiles and sequences; 8 warps
 // make the sums, each of its 16 or 32 keys of a unit.  The order of the dimensions in a product is free, so a lane reads
@@ -375,8 +377,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
           split_f16(p[4 * blk + 2], p[4 * blk + 3], hi[1], lo[1]);
           auto add = [&](int i, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
             const uint4 v = make_uint4(a0, a1, a2, a3);
-            mma16816(o[i], v, hi[0], hi[1]);
-            mma16816(o[i], v, lo[0], lo[1]);
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
+            mma16816(c, v, lo[0], lo[1]);
+            mma16816(c, v, hi[0], hi[1]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] += c[j];
           };
 #pragma unroll
           for (int i = 0; i < F::VC; ++i) {

@@ -838,3 +838,30 @@ def test_keys_on_pages_outside_the_pool_are_hidden(spl, window, page, fmt):
                 tol = tolerance(q, k[at], 0.125, n, 2, mass)[0] + 2.0 ** -32 * n * np.max(np.abs(v))
                 assert np.all(np.abs(mine - ref[0]) <= tol), (b, i)
         assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("scale", [0.0, None])
+def test_errors_do_not_grow_with_the_length(spl, scale, dim, fmt):
+    """131072 keys in one block's piece (as many sequences as SMs, all of them on the same pages), with values whose sums
+    grow.  Relative to the output a chain of 16 keys truncates at most 2^-22 of its size (1.2 times the output's share);
+    of the 1024 sums of each of 8 warps, rounded to nearest, the errors add up as sqrt(1024 / 3 / 8) 2^-24 / sqrt(3), three of
+    them 7e-7; exp is within 2^-21 and a probability's halves within 2^-22, of either sign: 1.5e-6 in all."""
+    keys, page = 131072, 256
+    seqs = torch.cuda.get_device_properties(0).multi_processor_count
+    c = Case(spl, [(1, keys)], (4, 1, dim), fmt, page, seed=dim)
+    c.fill()
+    g = np.random.default_rng(1)
+    q = g.standard_normal((seqs, 4 * dim)).astype(np.float32)
+    batch = spl.KVBatch(i32(list(range(seqs + 1))), i32([keys] * seqs),
+                        torch.as_tensor(np.repeat(c.table[:, :keys // page], seqs, axis=0)).to(DEV), seqs, 1)
+    out = torch.empty((seqs, 4 * dim), device=DEV)
+    spl.spl_paged_attention(out, torch.as_tensor(q).to(DEV), c.cache, batch, 4, scale=scale)
+    got = out.cpu().numpy().reshape(seqs, 4, dim)
+    k, v = c.stored("k", 0), c.stored("v", 0)
+    for b in (0, seqs // 2, seqs - 1):
+        ref, _ = serving.attention(q[b].reshape(1, 4, dim), k, v, keys, 4, 1 / np.sqrt(dim) if scale is None else scale)
+        err = np.linalg.norm(got[b] - ref[0]) / np.linalg.norm(ref)
+        assert err < 1.5e-6, f"sequence {b}: {err:.3g}"
+    assert spl.spl_get_device_status() == spl.SPL_OK
