@@ -98,10 +98,12 @@ struct Layout {
 };
 constexpr uint32_t kTmemCols = 512;
 
-// A workspace slot: sums as [dim / 4][128 rows][4], then the rows' maxima and totals.
+// A workspace slot: sums as [dim / 4][128 rows][4], then the rows' maxima and totals, and (int8) the exponents of the sums'
+// units, which the totals do not share.
+constexpr int kTcStats = kSlotStats + 1;
 template <int D>
 constexpr int64_t slot_floats() {
-  return (int64_t)kRows * (D + kSlotStats);
+  return (int64_t)kRows * (D + kTcStats);
 }
 
 // A divided tile that begins in a block's run, for the join.
@@ -628,9 +630,10 @@ struct Kernel {
         }
         tc_fence_before();
         arrive(kOFree + o);
-        if (last && !out) {  // the sums' exponent goes to the maximum
-          slot[(int64_t)kRows * D + own] = I8 ? m + (float)ev : m;
-          slot[(int64_t)kRows * D + kRows + own] = I8 ? l * exp2_int(-ev) : l;
+        if (last && !out) {
+          slot[kRows * D + own] = m;
+          slot[kRows * D + kRows + own] = l;
+          if constexpr (I8) slot[kRows * D + 2 * kRows + own] = (float)ev;
         }
         m_slot = m;
         ev_slot = ev;
@@ -1065,7 +1068,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 // The pieces of the divided tiles, joined in the order of their blocks: blockIdx.x the block in whose run the tile
 // begins, blockIdx.y a part of its (row, dims).  A warp takes 4 rows of 32 dims at a time.
 constexpr int kJoinParts = 8, kJoinThreads = 256;
-template <int D>
+template <int D, bool I8>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const AttnArgs a, const Divided* divided) {
   pdl_wait();  // launched while the pieces are made
   const Divided x = divided[blockIdx.x];
@@ -1077,20 +1080,24 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Attn
     const int row = task / (D / 32) * 4 + (lane & 3), d4 = task % (D / 32) * 8 + (lane >> 2);
     if (row >= x.rows) continue;
     auto slot = [&](int c) { return a.slots + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * slot_floats<D>(); };
-    float m = -INFINITY;
-    for (int c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(slot(c) + (int64_t)kRows * D + row));
+    float m = -INFINITY, ev = kMinExp;
+    for (int c = c0; c <= c1; ++c) {
+      m = fmaxf(m, __ldcg(slot(c) + kRows * D + row));
+      if constexpr (I8) ev = fmaxf(ev, __ldcg(slot(c) + kRows * D + 2 * kRows + row));
+    }
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll 4
     for (int c = c0; c <= c1; ++c) {
       const float* s = slot(c);
-      const float mc = __ldcg(s + (int64_t)kRows * D + row), lc = __ldcg(s + (int64_t)kRows * D + kRows + row);
+      const float mc = __ldcg(s + kRows * D + row), lc = __ldcg(s + kRows * D + kRows + row);
       const float4 p = __ldcg(reinterpret_cast<const float4*>(s) + d4 * kRows + row);
-      const float w = mc == -INFINITY ? 1.f : exp2_approx(mc - m);  // without keys: zeros, or NaN
-      v = make_float4(fmaf(p.x, w, v.x), fmaf(p.y, w, v.y), fmaf(p.z, w, v.z), fmaf(p.w, w, v.w));
+      float w = mc == -INFINITY ? 1.f : exp2_approx(mc - m);  // without keys: zeros, or NaN
       l = fmaf(lc, w, l);
+      if constexpr (I8) w *= exp2_int((int)(__ldcg(s + kRows * D + 2 * kRows + row) - ev));
+      v = make_float4(fmaf(p.x, w, v.x), fmaf(p.y, w, v.y), fmaf(p.z, w, v.z), fmaf(p.w, w, v.w));
     }
-    const float f = l == 0.f ? 0.f : 1.0f / l;
+    const float f = (l == 0.f ? 0.f : 1.0f / l) * (I8 ? exp2_int((int)ev) : 1.f);
     const int fr = x.r0 + row;
     *reinterpret_cast<float4*>(a.out + (int64_t)(x.row0 + fr / a.group) * a.ldo +
                                (int64_t)(x.head * a.group + fr % a.group) * D + 4 * d4) =
@@ -1114,7 +1121,7 @@ spl_status launch(const AttnArgs& a, int blocks, cudaStream_t stream) {
   attention_tc_kernel<D, I8><<<blocks, kThreads, smem, stream>>>(a, map_k, map_v, divided);
   const spl_status st = launch_status();
   if (st != SPL_OK) return st;
-  return launch_pdl(attention_join_kernel<D>, dim3(blocks, kJoinParts), dim3(kJoinThreads), 0, stream, a,
+  return launch_pdl(attention_join_kernel<D, I8>, dim3(blocks, kJoinParts), dim3(kJoinThreads), 0, stream, a,
                     static_cast<const Divided*>(divided));
 }
 

@@ -865,3 +865,17 @@ def test_errors_do_not_grow_with_the_length(spl, scale, dim, fmt):
         err = np.linalg.norm(got[b] - ref[0]) / np.linalg.norm(ref)
         assert err < 1.5e-6, f"sequence {b}: {err:.3g}"
     assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("small,large", [(0.0, 1e12), (1e-20, 1e12), (1e-30, 1e9), (0.0, 1e25), (1e25, 0.0)])
+def test_int8_values_of_very_different_sizes(spl, small, large, dim):
+    """The first half of the keys have values far smaller than the second (or none): their weight counts all the same, also
+    where other blocks have them."""
+    for kernel in (lambda c: c, many):
+        c = kernel(Case(spl, [(200, 6000)], (4, 1, dim), "i8", 64, seed=dim))
+        c.v[0][:3000] *= np.float32(small)
+        c.v[0][3000:] *= np.float32(large)
+        c.fill()
+        for scale in (0.0, None):
+            check_sample(c, 12, scale=scale)
