@@ -32,7 +32,7 @@ namespace {
 constexpr int kWarps = 8, kThreads = 32 * (kWarps + 4);  // and a warpgroup that copies
 constexpr int kRT = 8;  // rows of a tile
 // p is held as 2^kShift p, at most 2^13, so that its low half keeps an absolute 2^-38 of the largest.
-constexpr float kShift = 13.0f;
+constexpr float kShift = 13.0f, kUnshift = 0x1p-13f;
 constexpr int kMinExp = -100, kMaxExp = 126;  // of the values' scales
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1) {
@@ -423,13 +423,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
     sync();  // the shared arrays' last readers are done
     if (t == 0) {
       s_m[warp][g] = m;
-      s_l[warp][g] = l;
+      s_l[warp][g] = l * kUnshift;  // from here on in units of 1: values next to fp32's largest are not multiplied
     }
     sync();
     float m_all = s_m[0][g];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) m_all = fmaxf(m_all, s_m[w][g]);
-    const float f = (m == -INFINITY ? (l != l ? l : 0.f) : exp2_approx(m - m_all)) * (I8 ? exp2_int(ev) : 1.f);
+    const float f = (m == -INFINITY ? (l != l ? l : 0.f) : exp2_approx(m - m_all)) * (I8 ? exp2_int(ev) : 1.f) * kUnshift;
     const float f0 = __shfl_sync(0xffffffffu, f, 8 * t), f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
 #pragma unroll 1
     for (int turn = kWarps / F::PARTS - 1; turn >= 0; --turn) {

@@ -879,3 +879,16 @@ def test_int8_values_of_very_different_sizes(spl, small, large, dim):
         c.fill()
         for scale in (0.0, None):
             check_sample(c, 12, scale=scale)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 200])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_int8_values_next_to_the_largest(spl, rows, dim):
+    """Values of some 1e34, whose sums in units of 2^-13 would pass fp32's range: outputs are as large as the values."""
+    for kernel in (lambda c: c, many):
+        c = kernel(Case(spl, [(rows, 3000), (rows, 700)], (4, 2, dim), "i8", 64, seed=rows))
+        for v in c.v:
+            v *= np.float32(1e34)
+        c.fill()
+        got = check_sample(c, 12)
+        assert np.isfinite(got).all()
