@@ -180,8 +180,9 @@ def synthetic(layers, vocab=1024, heads=(8, 2, 64), d_ff=1024, seqs=8, max_len=5
     embedding, head = (torch.randn((vocab, shape.d_model), generator=g, device="cuda") for _ in range(2))
     head *= 4.0 / shape.d_model ** 0.5  # (not the embedding's: such a decoder would repeat its input)
     count = seqs * -(-max_len // page_size)
-    make = lambda n, f: CachedDecoder(built[:n], embedding, head, hk, dim, count, page_size, f, eps, seed=seed + n)  # noqa: E731
-    return make(layers, formats[0]), make(1, formats[1]), Pages(count, page_size, seqs, max_len)
+    make = lambda n, f, s: CachedDecoder(built[:n], embedding, head, hk, dim, count, page_size, f, eps, seed=s)  # noqa: E731
+    draws = 2 * seed, 2 * seed + 1  # each decoder's own: noise hides one input only
+    return make(layers, formats[0], draws[0]), make(1, formats[1], draws[1]), Pages(count, page_size, seqs, max_len)
 
 
 def main(argv=None):

@@ -87,6 +87,23 @@ def test_sequences_that_pass_the_end_of_a_page_together(serving):
     assert pages.lens == [62 + len(o) - 1 for o in out]
 
 
+@pytest.mark.parametrize("layers", [1, 2])
+def test_no_noise_is_drawn_twice(serving, monkeypatch, layers):
+    """Blocks of the generator that hide an input, of target and draft together: none hides two."""
+    target, draft, pages = serving.synthetic(layers, seqs=2, max_len=64, page_size=16, eps=8.0)
+    drawn = []
+    for name, at in (("spl_noise_mask", 2), ("spl_noise_mask_f64", 1)):
+        def call(*args, call=getattr(serving.spl, name), at=at, offset=0):
+            drawn.append((args[-1], offset, offset + -(-args[at].numel() // 4)))
+            return call(*args, offset=offset)
+        monkeypatch.setattr(serving.spl, name, call)
+    serving.generate(target, draft, pages, [[1, 2, 3], [4]], drafts=2, rounds=2)
+    assert len(drawn) == 4 * (layers * 3 + 1 * 7)
+    drawn.sort()
+    for (seed, _, end), (other, begin, _) in zip(drawn, drawn[1:]):
+        assert seed != other or end <= begin
+
+
 def test_a_smaller_draft_and_int8(serving, capsys):
     assert serving.main(["--sequences", "3", "--layers", "2", "--rounds", "5", "--prompt", "33", "--eps", "4"]) == 0
     line = capsys.readouterr().out
