@@ -34,10 +34,13 @@ class Pages:
 
     def grow(self, new):
         """Adds new[b] tokens to each sequence; returns the batch of those rows."""
-        for b, n in enumerate(new):
-            need = -(-(self.lens[b] + n) // self.page_size)
-            if need > self.table.shape[1] or need - len(self.own[b]) > len(self.free):
+        needs, left = [], len(self.free)
+        for b, n in enumerate(new):  # all of them or none
+            needs.append(-(-(self.lens[b] + n) // self.page_size))
+            left -= max(0, needs[b] - len(self.own[b]))
+            if needs[b] > self.table.shape[1] or left < 0:
                 raise ValueError(f"Pages: no room for {n} more tokens of sequence {b}")
+        for b, (n, need) in enumerate(zip(new, needs)):
             while len(self.own[b]) < need:
                 page = self.free.pop()
                 self.table[b, len(self.own[b])] = page

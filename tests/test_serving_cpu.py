@@ -250,3 +250,18 @@ def test_drafts_and_target_find_their_own_tokens(monkeypatch, prompts, page):
     lens = [m + len(o) - 1 for m, o in zip(prompts, out)]
     assert pages.lens == lens and len(history) == 12
     assert len(pages.free) == count - sum(-(-m // page) for m in lens)
+
+
+def test_a_batch_without_room_takes_nothing(monkeypatch):
+    """A batch that does not fit is refused as a whole: no sequence has grown, no page is gone."""
+    import torch
+    from paper_2609_15039_gb300 import serving
+    monkeypatch.setattr(serving.spl, "KVBatch", Batch)
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self: self)
+    p = serving.Pages(pages=3, page_size=16, seqs=2, max_len=48)
+    p.grow([5, 5])
+    for new in ([17, 33], [28, 28], [1, 44]):  # pages of both, of the second alone, past the table
+        with pytest.raises(ValueError):
+            p.grow(new)
+        assert p.lens == [5, 5] and len(p.free) == 1 and [len(o) for o in p.own] == [1, 1]
+    assert p.grow([27, 11]).kv_len.tolist() == [32, 16]
