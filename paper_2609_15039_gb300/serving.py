@@ -151,7 +151,7 @@ def generate(target, draft, pages, prompts, drafts, rounds, seed=0):
         pages.rewind(base)  # the target sees the same tokens, all at once, where the draft has them
         rows = torch.stack(chosen, dim=1)  # [n, drafts + 1]
         P = probs(target.forward(rows.reshape(-1), pages.grow([drafts + 1] * n)))
-        Q = torch.stack(proposals, dim=1).reshape(n * drafts, -1)
+        Q = torch.stack(proposals, dim=1).flatten(0, 1) if drafts else P[:0]
         x = rows[:, 1:].reshape(-1).to(torch.int32)
         u = torch.rand(n * drafts, generator=gen, device=dev)
         e = torch.empty((n, P.shape[1]), device=dev).exponential_(generator=gen)

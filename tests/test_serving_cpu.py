@@ -265,3 +265,21 @@ def test_a_batch_without_room_takes_nothing(monkeypatch):
             p.grow(new)
         assert p.lens == [5, 5] and len(p.free) == 1 and [len(o) for o in p.own] == [1, 1]
     assert p.grow([27, 11]).kv_len.tolist() == [32, 16]
+
+
+def test_generation_without_drafts(monkeypatch):
+    """No drafts: a token a round, by the target alone."""
+    import torch
+    from paper_2609_15039_gb300 import serving
+    monkeypatch.setattr(serving.spl, "KVBatch", Batch)
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self: self)
+
+    def verify(accepted, token, P, Q, x, u, e, row_start, draft_start):
+        assert Q.shape == (0, 50) and x.numel() == u.numel() == 0 and draft_start.tolist() == [0, 0, 0]
+        accepted.zero_()
+        token.copy_(P.argmax(-1))
+
+    monkeypatch.setattr(serving.spl, "spl_verify_drafts", verify)
+    pages = serving.Pages(8, 16, 2, 64)
+    out, history = serving.generate(Slots(pages, 50), Slots(pages, 50), pages, [[1, 2, 3], [4]], drafts=0, rounds=5)
+    assert [len(o) for o in out] == [6, 6] and history == [[0, 0]] * 5 and pages.lens == [8, 6]
