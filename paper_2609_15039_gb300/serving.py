@@ -128,6 +128,8 @@ def sample(p, generator):
 def generate(target, draft, pages, prompts, drafts, rounds, seed=0):
     """Prompts (lists of token ids) continued for ``rounds`` rounds of up to drafts + 1 tokens each, by the target's
     distribution; both decoders' caches lie on ``pages``.  Returns (tokens per sequence, accepted drafts per round)."""
+    if not all(map(len, prompts)):
+        raise ValueError("generate: a prompt has at least one token")
     dev, n = target.embedding.device, len(prompts)
     gen = torch.Generator(device=dev)
     gen.manual_seed(seed)

@@ -283,3 +283,16 @@ def test_generation_without_drafts(monkeypatch):
     pages = serving.Pages(8, 16, 2, 64)
     out, history = serving.generate(Slots(pages, 50), Slots(pages, 50), pages, [[1, 2, 3], [4]], drafts=0, rounds=5)
     assert [len(o) for o in out] == [6, 6] and history == [[0, 0]] * 5 and pages.lens == [8, 6]
+
+
+def test_an_empty_prompt_is_refused(monkeypatch):
+    """It has no row whose logits its first token could follow."""
+    import torch
+    from paper_2609_15039_gb300 import serving
+    monkeypatch.setattr(serving.spl, "KVBatch", Batch)
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self: self)
+    for prompts in ([[1, 2, 3], []], [[], [4]]):
+        pages = serving.Pages(8, 16, 2, 64)
+        with pytest.raises(ValueError):
+            serving.generate(Slots(pages, 50), Slots(pages, 50), pages, prompts, drafts=0, rounds=0)
+        assert pages.lens == [0, 0] and len(pages.free) == 8
