@@ -170,9 +170,11 @@ struct Kernel {
   Piece* pieces;
 
   __device__ uint32_t bar(int i) const { return smem + L::BARS + 8u * i; }
-  __device__ bool wait(int i, uint32_t parity) const {
-    return __all_sync(0xffffffffu, mbar_wait_soon(bar(i), parity, kWaitNs, abort));
+  __device__ bool wait(int i, uint32_t parity, unsigned long long ns = kWaitNs) const {
+    return __all_sync(0xffffffffu, mbar_wait_soon(bar(i), parity, ns, abort));
   }
+  // For a warp that may wait while others work on all of `tiles` key tiles (1.4 to 2.4 us each).
+  static __device__ unsigned long long wait_ns(int tiles) { return kWaitNs + 20000ull * (unsigned)tiles; }
   // One arrival for the warp, after all its lanes' work.
   __device__ void arrive(int i) const {
     __syncwarp();
@@ -185,8 +187,8 @@ struct Kernel {
   // Whether some row of the tile sees only a part of the 128 keys from j0 on.
   static __device__ bool edge_of(const Piece& x, int j0) { return j0 < x.all_lo || j0 + kKeys > x.all_hi; }
   // The k-th piece, when it is there; a warp that has done with it says so (it may not read it afterwards).
-  __device__ const Piece* piece(int k, bool& ok) const {
-    ok = ok && wait(kPieceFull + k % kPieces, (uint32_t)(k / kPieces) & 1u);
+  __device__ const Piece* piece(int k, bool& ok, unsigned long long ns = kWaitNs) const {
+    ok = ok && wait(kPieceFull + k % kPieces, (uint32_t)(k / kPieces) & 1u, ns);
     return pieces + k % kPieces;
   }
   __device__ void piece_done(int k) const { arrive(kPieceFree + k % kPieces); }
@@ -366,8 +368,9 @@ struct Kernel {
   __device__ void helper() const {
     bool ok = true;
     Loads y;
+    int last = 0;  // tiles of the piece before: binary16 has nothing to do with most of them
     for (int k = 0; ok; ++k) {
-      const Piece* place = piece(k, ok);
+      const Piece* place = piece(k, ok, wait_ns(last));
       if (!ok) break;
       const Piece& x = *place;
       const int n = x.tiles;
@@ -378,7 +381,7 @@ struct Kernel {
         if constexpr (I8) {
           ok = widen(y.tile, y.step + u, v);
         } else if (v && edge_of(x, x.j0 + u * kKeys)) {
-          ok = wait(kEdge, (uint32_t)y.edge_phase);
+          ok = wait(kEdge, (uint32_t)y.edge_phase, wait_ns(n));
           if (!ok) break;
           y.edge_phase ^= 1;
           look_over(x, x.j0 + u * kKeys, smem + L::KV + (uint32_t)(y.tile % STAGES) * L::TILE, y.step + u);
@@ -386,6 +389,7 @@ struct Kernel {
         }
       }
       y.step += n;
+      last = n;
       piece_done(k);
     }
     if (!ok && (threadIdx.x & 31) == 0) give_up();

@@ -892,3 +892,19 @@ def test_int8_values_next_to_the_largest(spl, rows, dim):
         c.fill()
         got = check_sample(c, 12)
         assert np.isfinite(got).all()
+
+
+def test_a_piece_that_takes_longer_than_a_wait_may(spl):
+    """2^27 keys (on the same few pages) for every block: some warps have nothing to do for more than a second, and wait.
+    All scores are 0 and the values small integers, the same for every key: every sum but a row's last ones is exact."""
+    keys, page, dim = 1 << 27, 256, 64
+    rows = 128 * torch.cuda.get_device_properties(0).multi_processor_count
+    cache = spl.KVCache.empty(4, 1, dim, page, "f16")
+    v = torch.arange(dim, device=DEV) - 20.0
+    cache.k.fill_(1.0)
+    cache.v.copy_(v.expand_as(cache.v))
+    table = i32([[3, 1, 0, 2] * (keys // (4 * page))])
+    q, out = torch.ones((rows, dim), device=DEV), torch.empty((rows, dim), device=DEV)
+    spl.spl_paged_attention(out, q, cache, spl.KVBatch(i32([0, rows]), i32([keys]), table, rows), 1, scale=0.0)
+    assert spl.spl_get_device_status() == spl.SPL_OK
+    assert bool(((out - v).abs() <= 2.0 ** -21 * v.abs()).all())  # the last sum, the total's, the quotient, the product
