@@ -48,7 +48,7 @@ constexpr int kMinExp = -100, kMaxExp = 126;
 constexpr int kSteps = 4;        // key tiles whose scales or marks have a place (see the barriers of the producer)
 
 // Barriers by index: kFull, kEmpty a stage; kRawFull, kRawEmpty a stage of int8 tiles as stored; kScale a place of K's
-// scales and of the mark of its missing pages; kQ a piece's q; kSFull, kPFull a place of S and the p in it (whose waiter may be a tile behind); kPv a tile's
+// scales; kQ a piece's q; kSFull, kPFull a place of S and the p in it (whose waiter may be a tile behind); kPv a tile's
 // product with V; kOFull, kOFree, kMFull a place of O: its chain is complete, has been added up, its rows' maxima are
 // there; kEdge the copies of V's edge tiles; kPieceFull, kPieceFree a piece's place.
 enum {
@@ -57,7 +57,7 @@ enum {
 };
 
 // A block's piece of a tile, as warp 1 hands it to the others (two in shared memory, in turn).
-struct Piece {
+struct alignas(16) Piece {
   int tiles;           // key tiles, 0 after the last piece
   int j0;              // first key of the first
   int key_lo, key_hi;  // keys that some row sees
@@ -68,6 +68,7 @@ struct Piece {
   int first;           // the first tile's index among the whole tile's
   int whole;           // the piece is the whole tile
   int last_block;      // the block that has the whole tile's end
+  int plain_hi;        // all_hi, or where the first key tile with a page outside the pool begins, as soon as it is met
 };
 constexpr int kPieces = 2;
 
@@ -89,7 +90,8 @@ struct Layout {
   static constexpr uint32_t VS = KS + (I8 ? kSteps * kKeys * 4 : 0), VMAX = VS + (I8 ? kSteps * kKeys * 4 : 0);
   static constexpr uint32_t BAD = VMAX + (I8 ? kSteps * 32 : 0), BARS = BAD + (I8 ? 0 : kSteps * 16);
   static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece);
-  static constexpr uint32_t GONE = MISC + 16, SMEM = GONE + 4 * kSteps;  // boxes of a tile whose page is outside the pool
+  // boxes of a tile whose page is outside the pool; 16 bytes of no marks
+  static constexpr uint32_t GONE = MISC + 16, ZERO = GONE + 4 * kSteps, SMEM = ZERO + 16;
   static_assert(BARS % 8 == 0 && PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
   static_assert(kMaxSeqs * kPrefixBytes + 8192 <= AUX, "the prefix sums fit where the tiles go");
   static constexpr uint32_t S = 0, O = 256;                // tensor memory columns (+ 128 and + D for the other place)
@@ -201,7 +203,7 @@ struct Kernel {
       if (run.busy()) {
         const AttnTile& x = run.x;
         y = {run.last() - run.first, (x.unit0 + run.first) * kKeys, x.key_lo, x.key_hi, x.all_lo, x.all_hi, x.b, x.h,
-             x.s.row0, x.s.len, x.s.pos0, x.r0, x.rows, run.first, run.whole() ? 1 : 0, run.last_block()};
+             x.s.row0, x.s.len, x.s.pos0, x.r0, x.rows, run.first, run.whole() ? 1 : 0, run.last_block(), x.all_hi};
       }
       mbar_arrive(bar(kPieceFull + k % kPieces));
     }
@@ -250,7 +252,7 @@ struct Kernel {
       const Piece x = *place;  // (in registers)
       const int n = x.tiles;
       if (n == 0) break;
-      ok = I8 ? load_i8(x, y) : load_f16(x, y);
+      ok = I8 ? load_i8(x, pieces + k % kPieces, y) : load_f16(x, pieces + k % kPieces, y);
       y.step += n;
       piece_done(k);
     }
@@ -296,7 +298,7 @@ struct Kernel {
       next = look_up(base + kAhead);
     }
   };
-  __device__ bool load_f16(const Piece& x, Loads& y) const {
+  __device__ bool load_f16(const Piece& x, Piece* place, Loads& y) const {
     const int lane = threadIdx.x & 31, n = x.tiles;
     Boxes boxes(*this, x);
     const int none = (int)((int64_t)a.cache.pages * a.cache.heads << boxes.shift);  // past the pool: filled with zeros
@@ -311,28 +313,22 @@ struct Kernel {
       if (edge) y.edge_tile = y.tile;
       if (ok && y.tile >= STAGES) ok = wait(kEmpty + stage, (uint32_t)(y.tile / STAGES - 1) & 1u);
       if (!ok) break;
+      if (lane == 0) mbar_expect_tx(bar(to), L::TILE);
       const int64_t slot = boxes.of(u);
-      const uint32_t gone = __ballot_sync(0xffffffffu, slot == kGone);
-      if (lane == 0) {
-        mbar_expect_tx(bar(to), L::TILE);
-        if (!edge) mbar_arrive_more(bar(to), kHelpers - 1);
-        if (!v) {
-          st_shared4(smem + L::GONE + 4u * ((y.step + u) % kSteps), gone);
-          mbar_arrive(bar(kScale + (y.step + u) % kSteps));
-        }
-      }
       if (lane < boxes.per_tile) {
         const uint32_t dst = smem + L::KV + (uint32_t)stage * L::TILE + (uint32_t)(lane * boxes.box) * 128u;
 #pragma unroll
         for (int p = 0; p < L::PANELS; ++p)
           tma_load_2d(dst + p * L::PANEL, v ? &map_v : &map_k, bar(to), 64 * p, slot >= 0 ? (int)slot : none, boxes.policy);
       }
+      if (!v) mark_gone(place, smem + L::GONE + 4u * ((y.step + u) % kSteps), slot, x.j0 + u * kKeys);
+      if (lane == 0 && !edge) mbar_arrive_more(bar(to), kHelpers - 1);
       __syncwarp();
       if (v && u % kAhead == kAhead - 1) boxes.advance();
     }
     return ok;
   }
-  __device__ bool load_i8(const Piece& x, Loads& y) const {
+  __device__ bool load_i8(const Piece& x, Piece* place, Loads& y) const {
     const int lane = threadIdx.x & 31, n = x.tiles;
     Boxes boxes(*this, x);
     bool ok = true;
@@ -345,10 +341,9 @@ struct Kernel {
       const int64_t slot = boxes.of(u);
       const uint32_t raw = smem + L::RAW + (uint32_t)stage * L::RAW_STAGE, full = bar(kRawFull + stage);
       const uint32_t mask = __ballot_sync(0xffffffffu, slot >= 0);  // of boxes
-      const uint32_t gone = __ballot_sync(0xffffffffu, slot == kGone);
+      if (!v) mark_gone(place, raw + L::RAW_MASK + 4u, slot, x.j0 + u * kKeys);
       if (lane == 0) {
         st_shared4(raw + L::RAW_MASK, mask);
-        st_shared4(raw + L::RAW_MASK + 4u, gone);
         mbar_expect_tx(full, (uint32_t)(__popc(mask) * boxes.box * (D + 4)));
       }
       __syncwarp();
@@ -417,8 +412,8 @@ struct Kernel {
       fence_proxy_async_smem();
     }
   }
-  // A tile of int8 to binary16 in the MMAs' layout, and its scales (0 for keys that were not copied).  A thread has the
-  // same 16 dims of every KEY_STEP-th key; all its loads run side by side.
+  // A tile of int8 to binary16 in the MMAs' layout, and its scales (of keys that were not copied K's 1, V's 0).  A thread has
+  // the same 16 dims of every KEY_STEP-th key; all its loads run side by side.
   __device__ bool widen(int tile, int step, bool v) const {
     constexpr int PARTS = D / 16, KEY_STEP = 32 * kHelpers / PARTS, PER = (kKeys + KEY_STEP - 1) / KEY_STEP;
     const int i = threadIdx.x - 64, lane = i & 31, stage = tile % STAGES, raw_stage = tile % L::RAW_STAGES;
@@ -436,7 +431,7 @@ struct Kernel {
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(gone) : "r"(raw + L::RAW_MASK + 4u));
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(mask) : "r"(raw + L::RAW_MASK));
       asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(raw + L::RAW_SCALE + 4u * i));
-      if (!(mask >> (i >> a.cache.page_shift) & 1u)) scale = 0.f;
+      if (!(mask >> (i >> a.cache.page_shift) & 1u)) scale = v ? 0.f : 1.f;  // (a hidden score stays -inf)
     }
     arrive(kRawEmpty + raw_stage);
     if (tile >= STAGES && !wait(kEmpty + stage, (uint32_t)(tile / STAGES - 1) & 1u)) return false;
@@ -519,6 +514,7 @@ struct Kernel {
       full(tile);
       if (!ok) break;
       issue_s(step & 1, tile, leader);
+      if (leader) mbar_arrive(bar(kSFull + (step & 1)));
       commit(kSFull + (step & 1));
       commit(kEmpty + tile % STAGES);
       ++tile;
@@ -527,6 +523,7 @@ struct Kernel {
           full(tile);
           if (!ok) break;
           issue_s((step + 1) & 1, tile, leader);
+          if (leader) mbar_arrive(bar(kSFull + ((step + 1) & 1)));
           commit(kSFull + ((step + 1) & 1));
           commit(kEmpty + tile % STAGES);
           ++tile;
@@ -700,10 +697,9 @@ struct Kernel {
   }
 
   // A key tile's scores in tensor memory, and what they meet: the scales of the keys and values (int8), the marks of bad
-  // values (if there are any), the boxes of 2^shift keys whose pages are outside the pool, the keys [lo, hi) that the thread's
-  // rows see, the rows' own scales.
+  // values, the keys [lo, hi) that the thread's rows see, the rows' own scales.
   struct Scores {
-    uint32_t ts, ks, vs, bad, gone, shift;
+    uint32_t ts, ks, vs, bad;
     int lo[2], hi[2];
     float row_scale[2];
   };
@@ -741,8 +737,8 @@ struct Kernel {
     }
     if constexpr (EDGE) {
       if constexpr (!I8) {
-        uint32_t bad = 0u;
-        if (x.bad) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(bad) : "r"(x.bad + 4u * c));
+        uint32_t bad;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(bad) : "r"(x.bad + 4u * c));
         if (bad) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -757,12 +753,24 @@ struct Kernel {
         const int j = 8 * (i >> 2) + (i & 1), r = i >> 1 & 1;
         if (j < lo[r] || j >= hi[r]) s[i] = 0xff800000u;
       }
-      if (x.gone) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (x.gone >> ((32 * c + 8 * (i >> 2)) >> x.shift) & 1u) s[i] = 0xff800000u;
-      }
     }
+  }
+  // Warp 1, before its last arrival for a K tile: the tile's boxes whose pages are outside the pool, for the softmax.  That
+  // reads them only where plain_hi sends it (at every tile they took 1 to 2.5% of its time).
+  __device__ void mark_gone(Piece* place, uint32_t at, int64_t slot, int j0) const {
+    const uint32_t gone = __ballot_sync(0xffffffffu, slot == kGone);
+    if ((threadIdx.x & 31) == 0) {
+      st_shared4(at, gone);
+      if (gone) place->plain_hi = min(place->plain_hi, j0);
+    }
+  }
+  // The scores of those boxes become -inf where they lie.
+  __device__ void hide(uint32_t ts, uint32_t gone) const {
+    const int shift = min(a.cache.page_shift, 7);
+#pragma unroll 1
+    for (int j = 0; j < kKeys; j += 16)
+      if (gone >> (j >> shift) & 1u) tmem_fill_16x16(ts + (uint32_t)j, 0xff800000u);
+    tmem_st_wait();
   }
   // Over the chunks of 32 scores, the load of one beside the work on the one before it.  The loops are kept short: the
   // roles' code together does not fit the instruction caches when this is unrolled over the whole tile.
@@ -882,7 +890,6 @@ struct Kernel {
       const int n = x.tiles;
       if (n == 0) break;
       Scores sc;
-      sc.shift = (uint32_t)min(a.cache.page_shift, 7);
       split_q(x, row0, sc.row_scale);
       fence_proxy_async_smem();
       arrive(kQ);
@@ -891,9 +898,10 @@ struct Kernel {
       int ev[2] = {kMinExp, kMinExp};
       for (int j = 0; j < n; ++j, ++step) {
         const int j0 = x.j0 + j * kKeys, s4 = step % kSteps;
-        const bool edge = edge_of(x, j0), fresh = j % kChain == 0;
+        const bool fresh = j % kChain == 0;
         ok = wait(kSFull + (step & 1), (uint32_t)(step >> 1) & 1u);
-        if (ok) ok = wait(kScale + s4, (uint32_t)(step / kSteps) & 1u);
+        if (ok && I8) ok = wait(kScale + s4, (uint32_t)(step / kSteps) & 1u);
+        const bool edge = j0 < x.all_lo || j0 + kKeys > x.plain_hi;
         if (ok && (I8 || edge)) {  // V's scales, or marks
           const int tv = tile0 + (j < n - 1 ? 2 * j + 2 : 2 * j + 1);
           ok = wait(kFull + tv % STAGES, (uint32_t)(tv / STAGES) & 1u);
@@ -903,10 +911,11 @@ struct Kernel {
         sc.ts = tmem + lanes + L::S + 128u * (step & 1);
         sc.ks = smem + L::KS + (uint32_t)s4 * (kKeys * 4);
         sc.vs = smem + L::VS + (uint32_t)s4 * (kKeys * 4);
-        sc.bad = edge ? smem + L::BAD + 16u * s4 : 0u;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc.gone) : "r"(smem + L::GONE + 4u * s4));
-        const bool masked = edge || sc.gone != 0;
-        if (masked) {
+        if (edge) {
+          sc.bad = smem + (edge_of(x, j0) ? L::BAD + 16u * s4 : L::ZERO);
+          uint32_t gone;
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(gone) : "r"(smem + L::GONE + 4u * s4));
+          if (gone) hide(sc.ts, gone);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {  // (rows past the last see all: nothing reads them)
             int lo = j0, hi = j0 + kKeys;
@@ -935,7 +944,7 @@ struct Kernel {
         float down[2] = {1.f, 1.f};
         if constexpr (I8) {  // the largest value scale that a row sees sets its sums' units
           float big[2] = {0.f, 0.f};
-          if (masked) {
+          if (edge) {
             for (int i = 2 * t; i < kKeys; i += 8) {
               const uint2 w = ld_shared8(sc.vs + 4u * i);
 #pragma unroll
@@ -962,7 +971,7 @@ struct Kernel {
           ok = rescale_o(f[0], f[1]);
           if (!ok) break;
         }
-        ok = masked ? make_p<true>(sc, m, l, down, rescale_o) : make_p<false>(sc, m, l, down, rescale_o);
+        ok = edge ? make_p<true>(sc, m, l, down, rescale_o) : make_p<false>(sc, m, l, down, rescale_o);
         if (!ok) break;
         tc_fence_before();
         arrive(kPFull + (step & 1));
@@ -1019,11 +1028,11 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
       init(kFull + s, kHelpers);
       init(kEmpty + s, 1);
     }
-    for (int s = 0; s < kSteps; ++s) init(kScale + s, I8 ? kHelpers : 1);
+    for (int s = 0; s < kSteps; ++s) init(kScale + s, kHelpers);
     init(kQ, kSoftmax);
     init(kPv, 1);
     for (int i = 0; i < 2; ++i) {
-      init(kSFull + i, 1);
+      init(kSFull + i, 2);  // the products, and the issuer for what it has seen of K's tile
       init(kPFull + i, kSoftmax);
       init(kOFull + i, 1);
       init(kOFree + i, 4);
@@ -1038,6 +1047,7 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
       init(kRawEmpty + s, kHelpers);
     }
     *abort = 0;
+    *reinterpret_cast<uint4*>(base + L::ZERO) = make_uint4(0u, 0u, 0u, 0u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async_smem();
   }

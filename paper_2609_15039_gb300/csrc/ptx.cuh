@@ -244,6 +244,10 @@ __device__ __forceinline__ void tmem_st_16x16(uint32_t taddr, const uint32_t (&r
                "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
+// 16 lanes x 16 columns of one value.
+__device__ __forceinline__ void tmem_fill_16x16(uint32_t taddr, uint32_t v) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"r"(taddr), "r"(v) : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Map of a row-major [rows, cols] binary16 matrix in boxes of 64 columns x box_rows rows, 128-byte swizzle (gemm_tc.cu).
