@@ -712,6 +712,8 @@ class KVCache:
     @classmethod
     def empty(cls, pages, kv_heads, head_dim, page_size=64, format="f16", device="cuda"):
         """A cache of unwritten pages."""
+        if format not in KV_FORMATS:
+            raise ValueError(f"KVCache: format is one of {', '.join(KV_FORMATS)}")
         shape = (pages, kv_heads, page_size, head_dim)
         dtype = torch.int8 if format == "i8" else torch.float16
         scales = [torch.empty(shape[:3], device=device) for _ in range(2)] if format == "i8" else [None, None]

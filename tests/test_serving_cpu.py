@@ -296,3 +296,9 @@ def test_an_empty_prompt_is_refused(monkeypatch):
         with pytest.raises(ValueError):
             serving.generate(Slots(pages, 50), Slots(pages, 50), pages, prompts, drafts=0, rounds=0)
         assert pages.lens == [0, 0] and len(pages.free) == 8
+
+
+def test_an_unknown_format_is_refused(spl):
+    for name in ("int8", "fp16", None):
+        with pytest.raises(ValueError):
+            spl.KVCache.empty(1, 1, 64, 16, name)
