@@ -44,11 +44,6 @@ template <class T>
 __device__ __forceinline__ T lds(const uint8_t* p) {
   return *reinterpret_cast<const T*>(p);
 }
-// Whether a pair of binary16 holds an infinity or NaN.
-__device__ __forceinline__ bool f16_special(uint32_t h) {
-  return (h & 0x7c00u) == 0x7c00u || (h & 0x7c000000u) == 0x7c000000u;
-}
-
 // How a lane (g = lane / 4, t = lane % 4) holds 16 keys, and which dimensions those are.
 template <int D, bool I8>
 struct Frag {

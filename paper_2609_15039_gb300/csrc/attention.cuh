@@ -292,6 +292,10 @@ __device__ __forceinline__ float2 unpack_f16(uint32_t h) {
       : "r"(h));
   return r;
 }
+// Whether a pair of binary16 holds an infinity or NaN.
+__device__ __forceinline__ bool f16_special(uint32_t h) {
+  return (h & 0x7c00u) == 0x7c00u || (h & 0x7c000000u) == 0x7c000000u;
+}
 // (a, b) = hi + lo, each a pair of binary16: 22 significant bits above 2^-14, an absolute 2^-25 below.
 __device__ __forceinline__ void split_f16(float a, float b, uint32_t& hi, uint32_t& lo) {
   hi = pack_f16(a, b);

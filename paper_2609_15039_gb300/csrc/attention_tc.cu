@@ -148,10 +148,6 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
   asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
   return v;
 }
-__device__ __forceinline__ bool f16_special2(uint32_t h) {
-  return (h & 0x7c00u) == 0x7c00u || (h & 0x7c000000u) == 0x7c000000u;
-}
-
 __device__ __forceinline__ void st_global32(float* p, float4 a, float4 b) {
   asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w),
                "f"(b.x), "f"(b.y), "f"(b.z), "f"(b.w)
@@ -401,7 +397,7 @@ struct Kernel {
       for (int c = 0; c < D / 8; ++c) {
         const uint32_t at = base + (c >> 3) * L::PANEL + key * 128 + (((c & 7) ^ (key & 7)) << 4);
         const uint4 v = ld_shared16(at);
-        const bool special = f16_special2(v.x) || f16_special2(v.y) || f16_special2(v.z) || f16_special2(v.w);
+        const bool special = f16_special(v.x) || f16_special(v.y) || f16_special(v.z) || f16_special(v.w);
         bad |= special;
         if (special || !seen) st_shared16(at, make_uint4(0u, 0u, 0u, 0u));
       }
