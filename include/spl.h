@@ -653,7 +653,8 @@ spl_status spl_kv_read(float* K, float* V, const spl_kv_cache* cache, const spl_
  * fp32 accuracy from the stored values: query rows and probabilities enter the
  * tensor cores as two binary16 terms (hi + lo, scaled by powers of two; a
  * probability far below its row's largest keeps an absolute 2^-33 of it, over I8
- * of its product with the largest value scale), the softmax is held in fp32.
+ * of its product with the largest value scale).  The softmax is held in fp32,
+ * and so are the sums: a tensor core accumulates 16 or 512 keys at a time.
  * Workspace: spl_paged_attention_workspace_bytes, zero-filled before its first
  * use; its first 64 KiB (arrival counters) are zero again after every call that
  * completes, so the product workspace can be shared.  Errors: as spl_kv_append,

@@ -12,11 +12,11 @@
 // make the sums, each of its 16 or 32 keys of a unit.  The order of the dimensions in a product is free, so a lane reads
 // 16 neighbouring bytes for its fragments (dims of a key for q . k, dims of four keys for p . v, whose pairs of keys
 // are byte permutes).
-// Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 328 us (the rate of
-// a copy), int8 188 us (0.92 of it: bound by widening int8 to binary16); one sequence of 300 keys 10 us, bound by the
-// latency of a launch, four dependent loads and three units.  More rows a tile (16 to 32) share the reads, but their
-// chains of dependent steps grow with them: 16 sequences of 8 rows of 4 heads took 147 us so, 137 as four tiles, 80 on
-// the tensor-core kernel.
+// Measured with 64 sequences of 1600 to 15775 keys, one row, 24 query heads on 8, 128 dims: binary16 329 us (the rate of
+// a copy), int8 191 us (0.91 of it: bound by widening int8 to binary16); one sequence of 300 keys 10 us, bound by the
+// latency of a launch, four dependent loads and three units.  Tiles of 16 to 32 rows, which would share the reads, were not
+// faster as they were built: 16 sequences of 8 rows of 4 heads 147 us as one tile of 32 and 137 as four of 8, some 36 us
+// an eight of rows, 4.5 times what its products take at the instruction's rate.  That is latency, not a bound.
 
 #include <algorithm>
 #include <cmath>
@@ -597,10 +597,11 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
 // which the tensor-core kernel first widens to binary16, two of 64 dims, whose softmax bounds that kernel; or where the
 // units (64 keys of a tile) that the batch can have, by its longest chunk and its page table, are few: the tensor-core
 // kernel costs some 8 us more at the start and a tenth as much per unit.  Measured, few rows and tensor cores, us, 32 query
-// heads on 8, 16 sequences over 800 to 8000 keys: of 4 rows (two tiles) int8 63, 87, binary16 78, 68, 64 dims 44, 54; of
-// 5 rows (three) int8 86, 87, binary16 117, 68, 64 dims int8 58, 80, binary16 60, 54; 64 sequences of 5 rows over 1000,
-// int8 100, 113.  24 query heads on 8, binary16: 16 rows over 2048 keys 18, 21, over 8192 33, 28; 64 rows over 512 21, 21,
-// over 2048 35, 25; 16 sequences of 8 rows over 128 16, 17, over 512 27, 20; 128 rows over 128 16, 17.
+// heads on 8, 16 sequences over 800 to 8000 keys: of 4 rows (two tiles) int8 64, 88, binary16 81, 68, 64 dims 45, 55; of
+// 5 rows (three) int8 86, 88, binary16 125, 69, 64 dims int8 58, 82, binary16 63, 55; 64 sequences of 5 rows over 1000,
+// int8 102, 115.  24 query heads on 8, binary16: 16 rows over 2048 keys 19, 21, over 8192 34, 29; 64 rows over 512 22, 21,
+// over 2048 35, 26; 16 sequences of 8 rows over 128 16, 17, over 512 27, 21; 128 rows over 128 16, 17.  The limits go by
+// what the host knows, max_rows and the page table's width: one long chunk takes all sequences of its batch along.
 constexpr int64_t kFewUnits = 1600;
 Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_heads) {
   const int d = (int)cache->head_dim, sms = device_sm_count();

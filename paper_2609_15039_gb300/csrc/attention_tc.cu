@@ -19,11 +19,12 @@
 // largest.  The running maximum is raised only where it would let p pass 2^5, so that O is seldom rescaled.  The tensor
 // core truncates as it accumulates, and an unbroken chain's bias grows with its length: after kChain tiles O goes on in
 // its other place while the sums' warps add the first to an fp32 sum in the workspace, rounding to nearest.
-// Divided tiles are joined by a second, small launch over all SMs.
+// Divided tiles are joined by a second, small launch over all SMs.  Keys on pages outside the pool are hidden: in place of
+// a copy there are zeros (int8: what was there), and their scores are overwritten with -inf.
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its copies and MMAs done.
-// Measured with 32 query heads on 8 of 128 dims, 2048 rows over 12049 keys: binary16 466 us, 0.9 of the instructions'
-// 2560 clocks a tile (S takes 96 an instruction, both its operands being in shared memory, O 64); int8 684 us, bound by
-// the widening and shared memory; 64 dims 386 and 637 us, bound by the softmax.  24 heads on 8, 512 rows over themselves
+// Measured with 32 query heads on 8 of 128 dims, 2048 rows over 12049 keys: binary16 469 us, 0.9 of the instructions'
+// 2560 clocks a tile (S takes 96 an instruction, both its operands being in shared memory, O 64); int8 696 us, bound by
+// the widening and shared memory; 64 dims 397 and 653 us, bound by the softmax.  24 heads on 8, 512 rows over themselves
 // 21 us: some 14 us of one tile's latency, launches and the join.
 
 #include <algorithm>
