@@ -666,6 +666,93 @@ spl_status spl_paged_attention(float* out, int64_t ldo, const float* Q, int64_t 
                                const spl_kv_batch* batch, int64_t rows, int64_t q_heads, float scale,
                                int64_t window, void* workspace, size_t workspace_bytes, cudaStream_t stream);
 
+/* Attention of rows that form a tree over the cache, such as drafted tokens of
+ * which several may follow one another (append them first, in any order in which
+ * a token stands behind the one that it follows).  With c = kv_len[b] less the
+ * sequence's rows, its row i sees the keys before them, j < c, and of its rows
+ * those whose bits are set, key c + j for bit j % 32 of word j / 32 of seen[row,
+ * words] (a bit for its ancestors and itself; any other set will do; rows past
+ * the last word are not seen, bits past the last row not looked at).  window > 0:
+ * of the keys that it sees, in their order, the last `window`.  All else --
+ * formula, strides, empty rows, NaN, accuracy, workspace
+ * (spl_paged_attention_workspace_bytes), errors -- is as in spl_paged_attention;
+ * EINVAL also for words < 0 and for words > 0 without `seen`, EALIGN for `seen`
+ * not 4-byte aligned. */
+spl_status spl_tree_attention(float* out, int64_t ldo, const float* Q, int64_t ldq, const spl_kv_cache* cache,
+                              const spl_kv_batch* batch, const uint32_t* seen, int64_t words, int64_t rows,
+                              int64_t q_heads, float scale, int64_t window, void* workspace, size_t workspace_bytes,
+                              cudaStream_t stream);
+
+/* Adds up the attention weight of stored tokens.  score [pages, kv_heads,
+ * page_size] fp32 lies like the cache's scales; for token j < kv_len[b] of each
+ * sequence and key head
+ *   score_j <- decay score_j + sum of softmax_j(scale q . k)
+ * over the batch's rows and the key head's query heads, softmax and window as in
+ * spl_paged_attention.  The rows' own tokens (append them first) start from 0:
+ * what their slots held does not count.  A row that sees a NaN or infinity makes
+ * the scores of the keys that it sees NaN; one that sees nothing adds nothing;
+ * slots of no token, and of pages outside the pool, are left as they are.  A page
+ * holds tokens of one sequence of the batch only.  Sums are fp32, in the rows'
+ * order.  Q [rows, q_heads head_dim] as there; 0 <= decay <= 1.  Workspace:
+ * spl_kv_weigh_workspace_bytes, any contents.  Errors: as spl_paged_attention,
+ * EINVAL for a decay outside [0, 1]. */
+size_t spl_kv_weigh_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows,
+                                    int64_t q_heads);
+spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, const spl_kv_cache* cache,
+                        const spl_kv_batch* batch, int64_t rows, int64_t q_heads, float scale, int64_t window,
+                        float decay, void* workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* Cuts sequences to `keep` tokens.  Of a sequence of more, every key head keeps the
+ * last `recent` and of the others the keep - recent with the largest scores
+ * (score as above), the earliest of equal ones, a NaN counting as less than any
+ * number; they move, keys, values, scales and scores, to the positions 0 .. keep
+ * - 1 in the order they had (their positions then count from there, for rows that
+ * follow and for windows).  out_len[b] = min(kv_len[b], keep), which may be
+ * written over kv_len.  out_table NULL: they move where they lie; what the slots
+ * from keep on hold is then not to be read.  Else to the pages of out_table
+ * [seqs, max_pages], and of shorter sequences all tokens do; those pages hold no
+ * other token of the batch.  Pages that are moved into belong to one sequence
+ * only.  A score, source or target on a page outside the pool: the token counts
+ * as the lightest, or is not moved.  batch->row_start is not used (but not NULL).
+ * Workspace: spl_kv_evict_workspace_bytes, any contents.  Errors: as
+ * spl_kv_append, EINVAL for recent > keep or negative ones, EWORKSPACE. */
+size_t spl_kv_evict_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t keep);
+spl_status spl_kv_evict(const spl_kv_cache* cache, float* score, const spl_kv_batch* batch, int64_t keep,
+                        int64_t recent, const int32_t* out_table, int32_t* out_len, void* workspace,
+                        size_t workspace_bytes, cudaStream_t stream);
+
+/* Brings an accepted path's tokens together: the batch's rows are trees whose row
+ * 0 stays, and of sequence b the row path[b, i] moves to the place of row 1 + i,
+ * for i < accepted[b] (spl_verify_tree's outputs), keys, values, scales and, if
+ * not NULL, scores.  The caller then counts 1 + accepted[b] of its rows.  path
+ * [seqs, levels], rows ldpath elements apart, ascends; where it does not, or
+ * leaves the sequence's rows, the rest stays where it is, and accepted outside
+ * [0, levels] counts as 0 (reported like an index out of range).  Errors as
+ * spl_kv_append. */
+spl_status spl_kv_keep_path(const spl_kv_cache* cache, float* score, const spl_kv_batch* batch, int64_t rows,
+                            const int32_t* path, int64_t ldpath, const int32_t* accepted, int64_t levels,
+                            cudaStream_t stream);
+
+/* Decides on a tree of drafts, from given random numbers.  Rows row_start[b] ..
+ * are sequence b's nodes: node 0 the token that is chosen already, node i > 0 the
+ * draft x[row] that follows node parent[row] (an index in the sequence, below i).
+ * P [rows, vocab] has the target's distribution after each node (any
+ * non-negative weights), e [seqs levels, vocab] exponential numbers (> 0), row b
+ * levels + d for level d.  From node 0 at level 0 the target's token is
+ *   t = argmax_v P[node, v] / e[b levels + d, v], the lowest v of equal ones
+ * (one fp32 rounding); the walk goes on, a level down, at the first child that
+ * holds t, and ends where there is none or at the last level:
+ *   accepted[b] the drafts on the way, path[b, 0 .. accepted - 1] their nodes (-1
+ *   behind), token[b] the t at which it ended.
+ * The tokens are distributed as if the target had sampled them, whatever the
+ * drafts; e = 1 everywhere takes the largest.  A sequence without rows gets 0 and
+ * -1; where no entry takes part (all NaN) the token is -1.  Errors: as
+ * spl_verify_drafts, EINVAL for levels < 1 or path rows closer than levels. */
+spl_status spl_verify_tree(int32_t* accepted, int32_t* path, int64_t ldpath, int32_t* token, const float* P,
+                           int64_t ldp, const int32_t* x, const int32_t* parent, const float* e, int64_t lde,
+                           const int32_t* row_start, int64_t rows, int64_t seqs, int64_t levels, int64_t vocab,
+                           cudaStream_t stream);
+
 /* Decides on drafted tokens, from given random numbers.  Sequence b has the
  * drafts draft[draft_start[b]] .. draft[draft_start[b + 1] - 1], the rows of Q
  * [drafts, vocab] are the distributions they were sampled from, and P [rows,

@@ -81,8 +81,8 @@ struct Frag {
 // consists of (keys, values, their scales): with pages of 16 tokens, 64 copies a unit, one warp alone was the
 // bound (64 sequences of one row over 1600 to 15775 keys, int8, 352 us instead of 193).  Each arrives at every unit, also
 // where it copies nothing: none can fall a turn of the ring behind the others and wait for a phase that has passed.
-template <int D, bool I8>
-__device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8_t* smem, int part) {
+template <int D, bool I8, bool TREE>
+__device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads, TREE>& run, uint8_t* smem, int part) {
   using F = Frag<D, I8>;
   constexpr int BLOCKS = F::UNIT / 16;
   const PagedCache& cache = run.a.cache;
@@ -147,7 +147,7 @@ __device__ void copy_units(AttnRun<kRT, Frag<D, I8>::UNIT, kThreads>& run, uint8
   }
 }
 
-template <int D, bool I8>
+template <int D, bool I8, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __grid_constant__ AttnArgs a) {
   using F = Frag<D, I8>;
   constexpr int ESZ = F::ESZ, BLOCKS = F::BLOCKS;
@@ -163,13 +163,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   const uint32_t bars = smem_u32(smem + F::BARS);
   if (threadIdx.x < 2 * F::STAGES) mbar_init(bars + 8u * threadIdx.x, threadIdx.x < F::STAGES ? F::COPIERS : kWarps);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  AttnRun<kRT, F::UNIT, kThreads> run(a, reinterpret_cast<int64_t*>(smem));
+  AttnRun<kRT, F::UNIT, kThreads, TREE> run(a, reinterpret_cast<int64_t*>(smem));
   fence_proxy_async_smem();
   __syncthreads();  // the prefix sums have been read: their place is the ring's
   // 168 registers a thread at the start; 3 x 168 = 2 x 232 + 40
   if (warp >= kWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (warp < kWarps + F::COPIERS) copy_units<D, I8>(run, smem, warp - kWarps);
+    if (warp < kWarps + F::COPIERS) copy_units<D, I8, TREE>(run, smem, warp - kWarps);
     return;
   }
   asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
@@ -203,7 +203,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
       }
     }
     int row_lo, row_hi;
-    row_keys(x.s, a.window, token, row_lo, row_hi);
+    const uint32_t* seen = nullptr;  // (of a tree)
+    if constexpr (TREE) {
+      seen = a.seen + (x.s.row0 + token) * a.words;
+      row_lo = tree_lo(seen, a.words, a.window, x.s.pos0, x.s.len);
+      row_hi = x.s.len;
+    } else {
+      row_keys(x.s, a.window, token, row_lo, row_hi);
+    }
 
     // The sums, transposed: dims (16 of an m-block) x rows; a lane has dims g, g + 8 and rows 2t, 2t + 1 of each.  (As rows
     // x dims, with the high and low halves of p as A, they would take twice the registers: 64 sequences, int8, 230 us
@@ -295,6 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
         uint32_t hidden = 0, zap = 0;  // bits: scores that the row does not see; keys whose values become zeros
         if (edge) {
           uint32_t bad = 0;  // keys whose values hold an infinity or NaN
+          const uint32_t sees = TREE ? tree_keys(seen, a.words, x.s.pos0, row_lo, row_hi, j0) : 0u;
           if constexpr (!I8) {  // a value that only some rows see must not reach the others as 0 times NaN
 #pragma unroll
             for (int blk = 0; blk < BLOCKS; ++blk) {
@@ -321,7 +329,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
 #pragma unroll
           for (int c = 0; c < 4 * BLOCKS; ++c) {
             const int j = j0 + 16 * (c >> 2) + 8 * (c >> 1 & 1) + 2 * t + (c & 1);
-            if (!(mask >> (c >> 2) & 1u) || j < row_lo || j >= row_hi) {
+            const bool out_of_sight = TREE ? !(sees >> (j - j0) & 1u) : j < row_lo || j >= row_hi;
+            if (!(mask >> (c >> 2) & 1u) || out_of_sight) {
               s[c] = -INFINITY;
               hidden |= 1u << c;
             } else if (bad >> c & 1u) {
@@ -559,20 +568,25 @@ __global__ void __launch_bounds__(kThreads, 1) attention_rows_kernel(const __gri
   }
 }
 
-template <int D, bool I8>
+template <int D, bool I8, bool TREE>
 spl_status launch_rows(const AttnArgs& a, int blocks, cudaStream_t stream) {
   constexpr uint32_t smem = Frag<D, I8>::SMEM;
   static bool done[kMaxDevices] = {false};
-  if (!allow_shared(reinterpret_cast<const void*>(attention_rows_kernel<D, I8>), smem, done)) return SPL_ECUDA;
-  attention_rows_kernel<D, I8><<<blocks, kThreads, smem, stream>>>(a);
+  if (!allow_shared(reinterpret_cast<const void*>(attention_rows_kernel<D, I8, TREE>), smem, done)) return SPL_ECUDA;
+  attention_rows_kernel<D, I8, TREE><<<blocks, kThreads, smem, stream>>>(a);
   return launch_status();
 }
 
 }  // namespace
 
-spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream) {
-  if (head_dim == 128) return i8 ? launch_rows<128, true>(a, blocks, stream) : launch_rows<128, false>(a, blocks, stream);
-  return i8 ? launch_rows<64, true>(a, blocks, stream) : launch_rows<64, false>(a, blocks, stream);
+template <bool TREE>
+spl_status pick_rows(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream) {
+  if (head_dim == 128)
+    return i8 ? launch_rows<128, true, TREE>(a, blocks, stream) : launch_rows<128, false, TREE>(a, blocks, stream);
+  return i8 ? launch_rows<64, true, TREE>(a, blocks, stream) : launch_rows<64, false, TREE>(a, blocks, stream);
+}
+spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, bool tree, int blocks, cudaStream_t stream) {
+  return tree ? pick_rows<true>(a, head_dim, i8, blocks, stream) : pick_rows<false>(a, head_dim, i8, blocks, stream);
 }
 
 namespace {
@@ -633,19 +647,19 @@ extern "C" size_t spl_paged_attention_workspace_bytes(const spl_kv_cache* cache,
   return shape_of(cache, batch, q_heads).bytes;
 }
 
-extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* Q, int64_t ldq,
-                                          const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows,
-                                          int64_t q_heads, float scale, int64_t window, void* workspace,
-                                          size_t workspace_bytes, cudaStream_t stream) {
+static spl_status attend(float* out, int64_t ldo, const float* Q, int64_t ldq, const spl_kv_cache* cache,
+                         const spl_kv_batch* batch, bool tree, const uint32_t* seen, int64_t words, int64_t rows,
+                         int64_t q_heads, float scale, int64_t window, void* workspace, size_t workspace_bytes,
+                         cudaStream_t stream) {
   AttnArgs a = {};
   spl_status st = check(cache, batch, rows, q_heads, &a.cache, &a.batch);
   if (st != SPL_OK) return st;
   const int64_t width = q_heads * cache->head_dim;
-  if (ldo < 0 || ldq < 0 || window < 0 || !std::isfinite(scale)) return SPL_EINVAL;
+  if (ldo < 0 || ldq < 0 || window < 0 || words < 0 || !std::isfinite(scale)) return SPL_EINVAL;
   if (rows == 0 || a.batch.seqs == 0) return SPL_OK;
-  if (!out || !Q) return SPL_EINVAL;
+  if (!out || !Q || (words > 0 && !seen)) return SPL_EINVAL;
   if (rows > 1 && (ldo < width || ldq < width)) return SPL_EINVAL;
-  if (!aligned16(out) || !aligned16(Q) || (rows > 1 && (ldo % 4 != 0 || ldq % 4 != 0))) return SPL_EALIGN;
+  if (!aligned16(out) || !aligned16(Q) || !aligned4(seen) || (rows > 1 && (ldo % 4 != 0 || ldq % 4 != 0))) return SPL_EALIGN;
   const Shape s = shape_of(cache, batch, q_heads);
   if (!workspace || workspace_bytes < s.bytes) return SPL_EWORKSPACE;
   if (!aligned16(workspace)) return SPL_EALIGN;
@@ -663,7 +677,26 @@ extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* 
   a.slack = s.few ? 1 : 3;
   a.join = s.few ? 2 : 3;
   a.start = s.few ? 2 : 3;
+  a.seen = seen;
+  a.words = words;
   const int d = (int)cache->head_dim;
   const bool i8 = cache->format == SPL_KV_I8;
-  return s.few ? run_attention_rows(a, d, i8, s.blocks, stream) : run_attention_tc(a, d, i8, s.blocks, stream);
+  return s.few ? run_attention_rows(a, d, i8, tree, s.blocks, stream)
+               : run_attention_tc(a, d, i8, tree, s.blocks, stream);
+}
+
+extern "C" spl_status spl_paged_attention(float* out, int64_t ldo, const float* Q, int64_t ldq,
+                                          const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows,
+                                          int64_t q_heads, float scale, int64_t window, void* workspace,
+                                          size_t workspace_bytes, cudaStream_t stream) {
+  return attend(out, ldo, Q, ldq, cache, batch, false, nullptr, 0, rows, q_heads, scale, window, workspace,
+                workspace_bytes, stream);
+}
+
+extern "C" spl_status spl_tree_attention(float* out, int64_t ldo, const float* Q, int64_t ldq, const spl_kv_cache* cache,
+                                         const spl_kv_batch* batch, const uint32_t* seen, int64_t words, int64_t rows,
+                                         int64_t q_heads, float scale, int64_t window, void* workspace,
+                                         size_t workspace_bytes, cudaStream_t stream) {
+  return attend(out, ldo, Q, ldq, cache, batch, true, seen, words, rows, q_heads, scale, window, workspace,
+                workspace_bytes, stream);
 }

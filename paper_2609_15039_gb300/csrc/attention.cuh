@@ -34,6 +34,9 @@ struct AttnArgs {
   // Units that a piece has at least, that it may have above the mean for being a block's only one, that a join costs, that
   // the start of a tile costs.
   int least, slack, join, start;
+  // Trees: what the rows see of their sequence's rows, a bit each, `words` words a row (TREE kernels only).
+  const uint32_t* seen;
+  int64_t words;
 };
 
 constexpr int kFewTiles = 4;  // tiles of a sequence that one thread counts
@@ -55,12 +58,54 @@ __device__ __forceinline__ void row_keys(const PagedSeq& s, int window, int i, i
   lo = pos >= window ? min(pos - window + 1, hi) : 0;
 }
 
-template <int RT, int U>
+// Rows that form a tree see the keys before the sequence's rows and, of these, those whose bits in the row's mask are set;
+// with a window the last so many of all that.  With `lo` of tree_lo a row sees the keys j >= lo that are before the rows or
+// set.  Which of the 32 keys from j on it sees of [lo, hi):
+__device__ __forceinline__ uint32_t tree_keys(const uint32_t* mask, int64_t words, int pos0, int lo, int hi, int j) {
+  const int64_t bit = (int64_t)j - pos0, w = bit >> 5;
+  auto word = [&](int64_t i) { return i < 0 ? ~0u : (i < words ? __ldg(mask + i) : 0u); };
+  uint32_t v = __funnelshift_r(word(w), word(w + 1), (uint32_t)bit & 31u);
+  if (lo > j) v &= lo - j >= 32 ? 0u : ~0u << (lo - j);
+  if (hi < j + 32) v &= hi <= j ? 0u : ~0u >> (j + 32 - hi);
+  return v;
+}
+__device__ __forceinline__ int tree_lo(const uint32_t* mask, int64_t words, int window, int pos0, int len) {
+  if (window == INT32_MAX) return 0;
+  const int first = max(0, pos0);  // the first key among the rows
+  const int64_t some = min(words, ((int64_t)len - pos0 + 31) >> 5);
+  int64_t count = 0;
+  for (int64_t w = (first - (int64_t)pos0) >> 5; w < some; ++w)
+    count += __popc(tree_keys(mask, words, pos0, first, len, (int)(pos0 + 32 * w)));
+  if (count <= window) return (int)max((int64_t)0, pos0 - (window - count));
+  int64_t skip = count - window;  // of the lowest
+  for (int64_t w = (first - (int64_t)pos0) >> 5; w < some; ++w) {
+    uint32_t v = tree_keys(mask, words, pos0, first, len, (int)(pos0 + 32 * w));
+    const int n = __popc(v);
+    if (skip >= n) {
+      skip -= n;
+      continue;
+    }
+    for (; skip > 0; --skip) v &= v - 1u;
+    return (int)(pos0 + 32 * w) + __ffs(v) - 1;
+  }
+  return len;
+}
+
+// (A tree's rows are taken together: some may see less than the keys from key_lo on, or more than those of [all_lo, all_hi).)
+template <int RT, int U, bool TREE>
 __device__ __forceinline__ void tile_span(AttnTile& x, int group, int window) {
   x.r0 = x.t * RT;
   x.rows = min(RT, x.s.n * group - x.r0);
-  row_keys(x.s, window, x.r0 / group, x.key_lo, x.all_hi);
-  row_keys(x.s, window, (x.r0 + x.rows - 1) / group, x.all_lo, x.key_hi);
+  if constexpr (TREE) {
+    const int context = max(0, min(x.s.pos0, x.s.len));
+    x.key_lo = context > window ? context - window : 0;
+    x.key_hi = x.s.len;
+    x.all_lo = window == INT32_MAX ? 0 : (int)max((int64_t)0, min((int64_t)context, (int64_t)x.s.pos0 - window + x.s.n));
+    x.all_hi = context;
+  } else {
+    row_keys(x.s, window, x.r0 / group, x.key_lo, x.all_hi);
+    row_keys(x.s, window, (x.r0 + x.rows - 1) / group, x.all_lo, x.key_hi);
+  }
   x.unit0 = x.key_lo / U;
   x.units = max(1, (x.key_hi + U - 1) / U - x.unit0);
 }
@@ -74,7 +119,7 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 // blocks) is filled by the constructor, which every thread of the block calls; afterwards every thread walks the same
 // tiles by itself.
 constexpr int kPrefixBytes = 8 + sizeof(PagedSeq);
-template <int RT, int U, int THREADS>
+template <int RT, int U, int THREADS, bool TREE = false>
 struct AttnRun {
   AttnTile x;
   int grain, start;        // units of a step; steps before a tile's units
@@ -104,7 +149,7 @@ struct AttnRun {
       int64_t sum = 0;
       int of[kGrains] = {};
       for (y.t = 0; tiles <= kFewTiles && y.t < tiles; ++y.t) {
-        tile_span<RT, U>(y, a.group, a.window);
+        tile_span<RT, U, TREE>(y, a.group, a.window);
         sum += y.units;
 #pragma unroll
         for (int k = 0; k < kGrains; ++k) of[k] += (int)((uint32_t)(y.units + k) / (uint32_t)(k + 1));
@@ -123,7 +168,7 @@ struct AttnRun {
       int64_t sum = 0;
       int of[kGrains] = {};
       for (y.t = lane; y.t < tiles; y.t += 32) {
-        tile_span<RT, U>(y, a.group, a.window);
+        tile_span<RT, U, TREE>(y, a.group, a.window);
         sum += y.units;
         if (!few || tiles > (int)gridDim.x) continue;
 #pragma unroll
@@ -177,7 +222,7 @@ struct AttnRun {
       y.t = t0 + lane;
       int64_t v = 0;
       if (y.t < tiles) {
-        tile_span<RT, U>(y, a.group, a.window);
+        tile_span<RT, U, TREE>(y, a.group, a.window);
         v = start + steps_of(y.units);
       }
       const int64_t own = v;
@@ -197,7 +242,7 @@ struct AttnRun {
     }
     off = rest;
     first = (int)max((int64_t)0, rest - start) * grain;
-    tile_span<RT, U>(x, a.group, a.window);
+    tile_span<RT, U, TREE>(x, a.group, a.window);
     if (off + (end - at) <= start) at = end;
   }
   // The grain by which all pieces have blocks, and then the prefix sums are of its steps, or 0; by warp 0, of `sum` steps
@@ -268,7 +313,7 @@ struct AttnRun {
         while (x.s.n == 0 && x.b + 1 < a.batch.seqs);
       }
     }
-    tile_span<RT, U>(x, a.group, a.window);
+    tile_span<RT, U, TREE>(x, a.group, a.window);
   }
 };
 
@@ -314,8 +359,8 @@ __device__ __forceinline__ uint32_t i8_pair(uint32_t bytes, uint32_t select) {
 constexpr int kSlotStats = 2;  // per row: maximum (in units of log2) and total
 
 // The two kernels' launches and the workspace behind the counters.
-spl_status run_attention_tc(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
+spl_status run_attention_tc(const AttnArgs& a, int head_dim, bool i8, bool tree, int blocks, cudaStream_t stream);
 size_t attention_tc_bytes(int head_dim, int blocks);
-spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream);
+spl_status run_attention_rows(const AttnArgs& a, int head_dim, bool i8, bool tree, int blocks, cudaStream_t stream);
 
 }  // namespace spl

@@ -155,10 +155,9 @@ __device__ __forceinline__ void st_global32(float* p, float4 a, float4 b) {
                : "memory");
 }
 
-using Run = AttnRun<kRows, kKeys, kThreads>;
-
-template <int D, bool I8>
+template <int D, bool I8, bool TREE>
 struct Kernel {
+  using Run = AttnRun<kRows, kKeys, kThreads, TREE>;
   using L = Layout<D, I8>;
   static constexpr int STAGES = L::STAGES;
   const AttnArgs& a;
@@ -699,6 +698,14 @@ struct Kernel {
     uint32_t ts, ks, vs, bad;
     int lo[2], hi[2];
     float row_scale[2];
+    // Trees: the rows' masks, the first of their bits' keys as the tile counts them, words; lo and hi limit them.
+    const uint32_t* seen[2];
+    int pos0;
+    int64_t words;
+    // Which of the tile's 32 keys from j on row r sees.
+    __device__ uint32_t sees(int r, int j) const {
+      return seen[r] ? tree_keys(seen[r], words, pos0, lo[r], hi[r], j) : ~0u;
+    }
   };
   static __device__ __forceinline__ void mul2(uint32_t& a, uint32_t& b, uint32_t x, uint32_t y) {
     asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tmul.rn.f32x2 p, p, q;\n\t"
@@ -741,6 +748,13 @@ struct Kernel {
           for (int i = 0; i < 16; ++i)
             if (bad >> (8 * (i >> 2) + 2 * t + (i & 1)) & 1u) s[i] = 0x7fc00000u;
         }
+      }
+      if constexpr (TREE) {
+        const uint32_t sees[2] = {x.sees(0, 32 * c) >> (2 * t), x.sees(1, 32 * c) >> (2 * t)};
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!(sees[i >> 1 & 1] >> (8 * (i >> 2) + (i & 1)) & 1u)) s[i] = 0xff800000u;
+        return;
       }
       // of the thread's keys, 8 b + {0, 1} from 32 c + 2 t on, a row sees [lo, hi)
       const int lo[2] = {x.lo[0] - 32 * c - 2 * t, x.lo[1] - 32 * c - 2 * t};
@@ -916,9 +930,23 @@ struct Kernel {
 #pragma unroll
           for (int r = 0; r < 2; ++r) {  // (rows past the last see all: nothing reads them)
             int lo = j0, hi = j0 + kKeys;
-            if (own0 + 8 * r < x.rows) row_keys({0, 0, x.len, x.pos0}, a.window, (x.r0 + own0 + 8 * r) / a.group, lo, hi);
+            const int token = (x.r0 + own0 + 8 * r) / a.group;
+            if constexpr (TREE) {
+              sc.seen[r] = nullptr;
+              if (own0 + 8 * r < x.rows) {
+                sc.seen[r] = a.seen + (x.row0 + token) * a.words;
+                lo = tree_lo(sc.seen[r], a.words, a.window, x.pos0, x.len);
+                hi = x.len;
+              }
+            } else if (own0 + 8 * r < x.rows) {
+              row_keys({0, 0, x.len, x.pos0}, a.window, token, lo, hi);
+            }
             sc.lo[r] = lo - j0;
             sc.hi[r] = hi - j0;
+          }
+          if constexpr (TREE) {
+            sc.pos0 = x.pos0 - j0;
+            sc.words = a.words;
           }
         }
         auto rescale_o = [&](float f0, float f1) {
@@ -946,8 +974,14 @@ struct Kernel {
               const uint2 w = ld_shared8(sc.vs + 4u * i);
 #pragma unroll
               for (int r = 0; r < 2; ++r) {
-                if (i >= sc.lo[r] && i < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.x));
-                if (i + 1 >= sc.lo[r] && i + 1 < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.y));
+                if constexpr (TREE) {
+                  const uint32_t sees = sc.sees(r, i & ~31) >> (i & 31);
+                  if (sees & 1u) big[r] = fmaxf(big[r], __uint_as_float(w.x));
+                  if (sees & 2u) big[r] = fmaxf(big[r], __uint_as_float(w.y));
+                } else {
+                  if (i >= sc.lo[r] && i < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.x));
+                  if (i + 1 >= sc.lo[r] && i + 1 < sc.hi[r]) big[r] = fmaxf(big[r], __uint_as_float(w.y));
+                }
               }
             }
             big[0] = quad_max(big[0]);
@@ -1004,7 +1038,7 @@ struct Kernel {
   }
 };
 
-template <int D, bool I8>
+template <int D, bool I8, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v, Divided* divided) {
@@ -1049,13 +1083,13 @@ attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     fence_proxy_async_smem();
   }
   if (warp == 0) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
-  Run run(a, reinterpret_cast<int64_t*>(base));  // the prefix sums lie where the tiles will
+  typename Kernel<D, I8, TREE>::Run run(a, reinterpret_cast<int64_t*>(base));  // the prefix sums lie where the tiles will
   fence_proxy_async_smem();                      // and are read and written before the copies overwrite them
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   pdl_trigger();  // the join may be launched: it waits for this kernel's end
-  const Kernel<D, I8> k{a, map_k, map_v, smem, __shfl_sync(0xffffffffu, *tmem_slot, 0), abort,
+  const Kernel<D, I8, TREE> k{a, map_k, map_v, smem, __shfl_sync(0xffffffffu, *tmem_slot, 0), abort,
                         reinterpret_cast<Piece*>(base + L::PIECES)};
   // 96 registers a thread at the start; 3 x 72 + 2 x 128 <= 5 x 96
   if (warp < 12) {
@@ -1116,11 +1150,11 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Attn
   }
 }
 
-template <int D, bool I8>
+template <int D, bool I8, bool TREE>
 spl_status launch(const AttnArgs& a, int blocks, cudaStream_t stream) {
   constexpr uint32_t smem = Layout<D, I8>::SMEM;
   static bool done[kMaxDevices] = {false};
-  if (!allow_shared(reinterpret_cast<const void*>(attention_tc_kernel<D, I8>), smem, done)) return SPL_ECUDA;
+  if (!allow_shared(reinterpret_cast<const void*>(attention_tc_kernel<D, I8, TREE>), smem, done)) return SPL_ECUDA;
   Divided* divided = reinterpret_cast<Divided*>(a.slots + (int64_t)blocks * 2 * slot_floats<D>());
   CUtensorMap map_k = {}, map_v = {};
   if (!I8) {
@@ -1129,7 +1163,7 @@ spl_status launch(const AttnArgs& a, int blocks, cudaStream_t stream) {
     if (!tma_panel_map(&map_k, a.cache.k, slots, D, box) || !tma_panel_map(&map_v, a.cache.v, slots, D, box))
       return SPL_ECUDA;
   }
-  attention_tc_kernel<D, I8><<<blocks, kThreads, smem, stream>>>(a, map_k, map_v, divided);
+  attention_tc_kernel<D, I8, TREE><<<blocks, kThreads, smem, stream>>>(a, map_k, map_v, divided);
   const spl_status st = launch_status();
   if (st != SPL_OK) return st;
   return launch_pdl(attention_join_kernel<D, I8>, dim3(blocks, kJoinParts), dim3(kJoinThreads), 0, stream, a,
@@ -1143,9 +1177,13 @@ size_t attention_tc_bytes(int head_dim, int blocks) {
   return (size_t)blocks * (2 * floats * sizeof(float) + sizeof(Divided));
 }
 
-spl_status run_attention_tc(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream) {
-  if (head_dim == 128) return i8 ? launch<128, true>(a, blocks, stream) : launch<128, false>(a, blocks, stream);
-  return i8 ? launch<64, true>(a, blocks, stream) : launch<64, false>(a, blocks, stream);
+template <bool TREE>
+static spl_status pick(const AttnArgs& a, int head_dim, bool i8, int blocks, cudaStream_t stream) {
+  if (head_dim == 128) return i8 ? launch<128, true, TREE>(a, blocks, stream) : launch<128, false, TREE>(a, blocks, stream);
+  return i8 ? launch<64, true, TREE>(a, blocks, stream) : launch<64, false, TREE>(a, blocks, stream);
+}
+spl_status run_attention_tc(const AttnArgs& a, int head_dim, bool i8, bool tree, int blocks, cudaStream_t stream) {
+  return tree ? pick<true>(a, head_dim, i8, blocks, stream) : pick<false>(a, head_dim, i8, blocks, stream);
 }
 
 }  // namespace spl

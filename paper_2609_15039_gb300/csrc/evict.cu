@@ -1,0 +1,416 @@
+// Moves within a paged cache: the eviction of all but the heaviest and the latest tokens, and an accepted path's rows.
+//
+// Eviction, for each sequence and key head by itself: of `len` tokens the last `recent` stay and of the others the
+// keep - recent with the largest scores, the earliest of equal ones; they keep their order and go to the positions 0 ..
+// keep - 1.  Two launches.  The first chooses: the scores become whole numbers that order as they do, the smallest that
+// stays is found digit by digit (8 bits a round, a histogram in shared memory), and the positions that stay are written
+// down in order, strip after strip, by a prefix sum.  The second moves, bound by HBM: a block has some columns of K or of V
+// (32 or 128 bytes of every vector) of one head.  In place a target lies at or before its source, and a block's trips are
+// in the targets' order, so that it suffices that a trip's loads are done before its stores: what a trip overwrites are
+// sources of itself or of trips before it.  Into other pages there is no such order, and a head's tokens are shared out.
+//
+// An accepted path (a handful of tokens): a thread has 16 bytes of a vector, or a scale, and moves them one after another.
+
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace spl {
+namespace {
+
+constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32;
+constexpr int kHeld = 24576;  // scores held in shared memory (96 KB: two blocks an SM); past them they are read again
+constexpr int kPer = 4, kStrip = kPer * kSelectThreads;
+
+constexpr int kPlan = 3;
+struct EvictArgs {
+  PagedCache cache;
+  PagedBatch batch;
+  float* score;          // [pages, heads, page]
+  const int* out_table;  // where the tokens go: [seqs, max_pages], or null for where they are
+  int* out_len;
+  int keep, recent;
+  int64_t chosen;  // places of a (sequence, head) in `list`
+  int* list;       // the positions that stay of those before the last `recent`, in order
+  int* plan;       // [seqs][kPlan]: tokens that move, length after and before
+};
+
+// A whole number that orders like the score: -inf .. +inf from 1 on (both zeros are one), NaN below them as 0.
+__device__ __forceinline__ uint32_t score_order(float x) {
+  if (x != x) return 0u;
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+// One block a (key head, sequence).
+__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictArgs a) {
+  extern __shared__ uint32_t held[];
+  __shared__ int histogram[256], warp_sums[kSelectWarps], s_digit, s_left;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
+  const bool over = s.len > a.keep;
+  if (h == 0 && tid == 0) {
+    a.plan[kPlan * b] = over ? a.keep : (a.out_table ? s.len : 0);
+    a.plan[kPlan * b + 1] = over ? a.keep : s.len;
+    a.plan[kPlan * b + 2] = s.len;
+  }
+  const int early = s.len - a.recent, want = a.keep - a.recent;
+  if (!over || want == 0) return;
+  int* list = a.list + ((int64_t)b * a.cache.heads + h) * a.chosen;
+  auto read = [&](int pos) -> uint32_t {
+    const int page = paged_page(a.cache, a.batch, b, pos);
+    return page < 0 ? 0u : score_order(__ldg(a.score + paged_slot(a.cache, page, h, pos)));
+  };
+  const bool all_held = early <= kHeld;
+  const int kept = min(early, kHeld);
+  for (int p0 = tid; p0 < kept; p0 += 8 * kSelectThreads) {
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p0 + i * kSelectThreads < kept ? read(p0 + i * kSelectThreads) : 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p0 + i * kSelectThreads < kept) held[p0 + i * kSelectThreads] = v[i];
+  }
+  // The smallest that stays, and how many equal to it do.
+  uint32_t least = 0, mask = 0;
+  int left = want;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) histogram[tid] = 0;
+    __syncthreads();
+    for (int p = tid; p < kept; p += kSelectThreads)
+      if ((held[p] & mask) == least) atomicAdd(histogram + (held[p] >> shift & 255u), 1);
+    if (!all_held) {
+#pragma unroll 4
+      for (int p = kHeld + tid; p < early; p += kSelectThreads) {
+        const uint32_t v = read(p);
+        if ((v & mask) == least) atomicAdd(histogram + (v >> shift & 255u), 1);
+      }
+    }
+    __syncthreads();
+    if (warp == 0) {  // lane i: the digits from 255 - 8 i down
+      int own = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) own += histogram[255 - 8 * lane - i];
+      int sum = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int other = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += other;
+      }
+      // the lane in whose digits the count reaches `left` (there are more than `left` in all)
+      const unsigned reach = __ballot_sync(0xffffffffu, sum >= left);
+      if (reach && lane == __ffs(reach) - 1) {
+        int above = sum - own, i = 0;
+        while (i < 7 && above + histogram[255 - 8 * lane - i] < left) above += histogram[255 - 8 * lane - i++];
+        s_digit = 255 - 8 * lane - i;
+        s_left = left - above;
+      }
+    }
+    __syncthreads();
+    least |= (uint32_t)s_digit << shift;
+    mask |= 255u << shift;
+    left = s_left;
+  }
+  // Those above `least`, and the first `left` equal to it, in order of their positions.
+  int above0 = 0, equal0 = 0;  // in the strips before
+  for (int p0 = 0; p0 < early; p0 += kStrip) {
+    const int p = p0 + kPer * tid;
+    uint32_t v[kPer];
+    int packed = 0;  // those above in the low half, those equal in the high one (a strip has 4096)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      v[i] = p + i < kept ? held[p + i] : (p + i < early ? read(p + i) : 0u);
+      if (p + i < early) packed += v[i] > least ? 1 : (v[i] == least ? 1 << 16 : 0);
+    }
+    int sum = packed;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int other = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += other;
+    }
+    if (lane == 31) warp_sums[warp] = sum;
+    __syncthreads();
+    const int other = warp_sums[lane];
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? other : 0) + sum - packed;
+    const int total = __reduce_add_sync(0xffffffffu, other);
+    __syncthreads();
+    int above = above0 + (before & 0xffff), equal = equal0 + (before >> 16);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (p + i >= early) break;
+      if (v[i] > least) {
+        list[above + min(equal, left)] = p + i;
+        ++above;
+      } else if (v[i] == least) {
+        if (equal < left) list[above + equal] = p + i;
+        ++equal;
+      }
+    }
+    above0 += total & 0xffff;
+    equal0 += total >> 16;
+  }
+}
+
+// W bytes of each vector a block, 16 a thread.  blockIdx.x: the part of the vector (K's, then V's, then the scores and scales),
+// and of the tokens (into other pages only); blockIdx.y: key head; blockIdx.z: sequence.
+constexpr int kMoveThreads = 256;
+template <int ROW, int W>  // bytes of a vector
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArgs a, int shares) {
+  constexpr int SLICES = ROW / W;
+  const int part = blockIdx.x / shares, share = blockIdx.x % shares, h = blockIdx.y, b = blockIdx.z;
+  const int moves = a.plan[kPlan * b], len = a.plan[kPlan * b + 1], before = a.plan[kPlan * b + 2];
+  if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) a.out_len[b] = len;
+  const int want = a.keep - a.recent;
+  const bool over = before > a.keep;  // (else all of them move, to the same positions elsewhere)
+  const int* list = a.list + ((int64_t)b * a.cache.heads + h) * a.chosen;
+  auto source = [&](int i) { return !over ? i : (i < want ? __ldg(list + i) : before - a.keep + i); };
+  auto slot_of = [&](const int* table, int pos) -> int64_t {
+    const int page = __ldg(table + b * a.batch.max_pages + (pos >> a.cache.page_shift));
+    if ((unsigned)page >= (unsigned)a.cache.pages) {
+      atomicOr(a.batch.status, kStatusIndex);
+      return -1;
+    }
+    return paged_slot(a.cache, page, h, pos);
+  };
+  const int* to_table = a.out_table ? a.out_table : a.batch.table;
+  const int first = (int)((int64_t)moves * share / shares), last = (int)((int64_t)moves * (share + 1) / shares);
+  if (part < 2 * SLICES) {
+    constexpr int LANES = W / 16, ROWS = kMoveThreads / LANES, U = 8;
+    char* base = static_cast<char*>(part < SLICES ? a.cache.k : a.cache.v) + part % SLICES * W + threadIdx.x % LANES * 16;
+    const int row = threadIdx.x / LANES;
+    for (int i0 = first; i0 < last; i0 += ROWS * U) {
+      int64_t from[U], to[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * ROWS + row;
+        from[u] = to[u] = -1;
+        if (i >= last) continue;
+        const int pos = source(i);
+        if (pos == i && !a.out_table) continue;
+        from[u] = slot_of(a.batch.table, pos);
+        to[u] = slot_of(to_table, i);
+      }
+      uint4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (from[u] >= 0 && to[u] >= 0) v[u] = *reinterpret_cast<const uint4*>(base + from[u] * ROW);
+      if (!a.out_table) __syncthreads();
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (from[u] >= 0 && to[u] >= 0) *reinterpret_cast<uint4*>(base + to[u] * ROW) = v[u];
+    }
+  } else {
+    constexpr int U = 4;
+    for (int i0 = first; i0 < last; i0 += kMoveThreads * U) {
+      int64_t from[U], to[U];
+      float v[U], k[U], w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * kMoveThreads + threadIdx.x;
+        from[u] = to[u] = -1;
+        if (i >= last) continue;
+        const int pos = source(i);
+        if (pos == i && !a.out_table) continue;
+        from[u] = slot_of(a.batch.table, pos);
+        to[u] = slot_of(to_table, i);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (from[u] < 0 || to[u] < 0) continue;
+        v[u] = a.score[from[u]];
+        if (a.cache.k_scale) {
+          k[u] = a.cache.k_scale[from[u]];
+          w[u] = a.cache.v_scale[from[u]];
+        }
+      }
+      if (!a.out_table) __syncthreads();
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (from[u] < 0 || to[u] < 0) continue;
+        a.score[to[u]] = v[u];
+        if (a.cache.k_scale) {
+          a.cache.k_scale[to[u]] = k[u];
+          a.cache.v_scale[to[u]] = w[u];
+        }
+      }
+    }
+  }
+}
+
+template <int ROW>
+spl_status launch_move(const EvictArgs& a, int blocks, cudaStream_t stream) {
+  // Whole vectors' lines where there are blocks enough, 32 bytes each where a block an SM would be missing (32 sequences cut
+  // from 16000 tokens to 6000: %%; one of 1250 to 1000: %%).
+  const int heads = a.cache.heads, seqs = a.batch.seqs;
+  constexpr int WIDE = ROW < 128 ? ROW : 128;
+  const bool wide = (int64_t)heads * seqs * (2 * ROW / WIDE) >= blocks;
+  const int parts = 2 * ROW / (wide ? WIDE : 32) + 1;
+  int shares = 1;  // of a head's tokens, where their order does not matter
+  if (a.out_table) shares = (int)std::max<int64_t>(1, std::min<int64_t>(4 * blocks / ((int64_t)parts * heads * seqs), 64));
+  const dim3 grid(parts * shares, heads, seqs);
+  if (wide)
+    evict_move_kernel<ROW, WIDE><<<grid, kMoveThreads, 0, stream>>>(a, shares);
+  else
+    evict_move_kernel<ROW, 32><<<grid, kMoveThreads, 0, stream>>>(a, shares);
+  return launch_status();
+}
+
+// ---- an accepted path ----
+struct PathArgs {
+  PagedCache cache;
+  PagedBatch batch;
+  float* score;  // or null
+  const int *path, *accepted;
+  int64_t ldpath;
+  int levels;
+};
+constexpr int kPathThreads = 256, kPathBatch = 4;
+
+// A sequence's places, T a thread's part of each: the nodes path[0] < path[1] < ... of its rows to those from 1 on.  A node
+// lies at or behind its place, so moving them in order overwrites no later one's source.
+template <class T, class At>
+__device__ void move_path(const PathArgs& a, const PagedSeq& s, int b, int count, At at) {
+  const int* path = a.path + b * a.ldpath;
+  int last = 0;  // the node before
+  for (int i0 = 0; i0 < count; i0 += kPathBatch) {
+    T v[kPathBatch] = {};
+    T* to[kPathBatch];
+#pragma unroll
+    for (int i = 0; i < kPathBatch; ++i) {
+      to[i] = nullptr;
+      if (i0 + i >= count) continue;
+      const int node = __ldg(path + i0 + i);
+      if (node <= last || node >= s.n) {  // not a path: what follows stays where it is
+        atomicOr(a.batch.status, kStatusIndex);
+        count = i0 + i;
+        continue;
+      }
+      last = node;
+      const int from = s.pos0 + node, place = s.pos0 + 1 + i0 + i;
+      if (from == place || place < 0 || from >= s.len) continue;  // (rows without a place in the table)
+      const int p0 = paged_page(a.cache, a.batch, b, from), p1 = paged_page(a.cache, a.batch, b, place);
+      if (p0 < 0 || p1 < 0) continue;
+      v[i] = *at(p0, from);
+      to[i] = at(p1, place);
+    }
+#pragma unroll
+    for (int i = 0; i < kPathBatch; ++i)
+      if (to[i]) *to[i] = v[i];
+  }
+}
+
+template <int ROW>
+__global__ void __launch_bounds__(kPathThreads) keep_path_kernel(const PathArgs a) {
+  constexpr int LANES = ROW / 16;
+  const int b = blockIdx.y, heads = a.cache.heads;
+  const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
+  int count = __ldg(a.accepted + b);
+  if (count < 0 || count > a.levels) {
+    atomicOr(a.batch.status, kStatusIndex);
+    count = 0;
+  }
+  const int64_t vectors = (int64_t)2 * heads * LANES;
+  int64_t task = (int64_t)blockIdx.x * kPathThreads + threadIdx.x;
+  if (task < vectors) {
+    const int part = (int)(task % LANES), h = (int)(task / LANES % heads);
+    char* base = static_cast<char*>(task < vectors / 2 ? a.cache.k : a.cache.v) + 16 * part;
+    move_path<uint4>(a, s, b, count, [&](int page, int pos) {
+      return reinterpret_cast<uint4*>(base + paged_slot(a.cache, page, h, pos) * ROW);
+    });
+    return;
+  }
+  task -= vectors;
+  float* of[3] = {a.score, a.cache.k_scale, a.cache.v_scale};
+  if (task >= 3 * heads || !of[task / heads]) return;
+  move_path<float>(a, s, b, count, [&](int page, int pos) {
+    return of[task / heads] + paged_slot(a.cache, page, (int)(task % heads), pos);
+  });
+}
+
+// The tokens that a page table has room for.
+int64_t room_of(const PagedCache& c, const PagedBatch& b) { return b.max_pages << c.page_shift; }
+size_t chosen_of(const PagedCache& c, const PagedBatch& b, int64_t keep) {
+  return (size_t)std::min(keep, room_of(c, b)) * c.heads * b.seqs;
+}
+size_t evict_bytes(const PagedCache& c, const PagedBatch& b, int64_t keep) {
+  return round_up((int64_t)b.seqs * kPlan * sizeof(int), 16) + chosen_of(c, b, keep) * sizeof(int);
+}
+
+}  // namespace
+}  // namespace spl
+
+using namespace spl;
+
+extern "C" size_t spl_kv_evict_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t keep) {
+  PagedCache c;
+  PagedBatch b;
+  if (paged_cache_view(&c, cache) != SPL_OK || paged_batch_view(&b, c, batch, 0) != SPL_OK || keep < 0 || b.seqs == 0)
+    return 0;
+  return evict_bytes(c, b, keep);
+}
+
+extern "C" spl_status spl_kv_evict(const spl_kv_cache* cache, float* score, const spl_kv_batch* batch, int64_t keep,
+                                   int64_t recent, const int32_t* out_table, int32_t* out_len, void* workspace,
+                                   size_t workspace_bytes, cudaStream_t stream) {
+  EvictArgs a = {};
+  spl_status st = paged_cache_view(&a.cache, cache);
+  if (st != SPL_OK) return st;
+  if ((st = paged_batch_view(&a.batch, a.cache, batch, 0)) != SPL_OK) return st;
+  if (keep < 0 || recent < 0 || recent > keep) return SPL_EINVAL;
+  if (a.batch.seqs == 0) return SPL_OK;
+  if (!out_len || (a.cache.pages > 0 && !score)) return SPL_EINVAL;
+  if (!aligned4(score) || !aligned4(out_table) || !aligned4(out_len)) return SPL_EALIGN;
+  if (!workspace || workspace_bytes < evict_bytes(a.cache, a.batch, keep)) return SPL_EWORKSPACE;
+  if (!aligned16(workspace)) return SPL_EALIGN;
+  if (!(a.batch.status = device_status_word())) return SPL_ECUDA;
+  const bool i8 = cache->format == SPL_KV_I8;
+  if (!i8) a.cache.k_scale = a.cache.v_scale = nullptr;
+  a.score = score;
+  a.out_table = out_table == batch->page_table ? nullptr : out_table;
+  a.out_len = out_len;
+  a.keep = (int)std::min(keep, kMaxLength);
+  a.recent = (int)std::min(recent, kMaxLength);
+  a.chosen = std::min(keep, room_of(a.cache, a.batch));
+  a.plan = static_cast<int*>(workspace);
+  a.list = a.plan + round_up((int64_t)a.batch.seqs * kPlan, 4);
+  const size_t held = (size_t)std::min<int64_t>(kHeld, room_of(a.cache, a.batch)) * sizeof(uint32_t);
+  static bool done[kMaxDevices] = {false};
+  if (!allow_shared(reinterpret_cast<const void*>(evict_select_kernel), kHeld * sizeof(uint32_t), done)) return SPL_ECUDA;
+  evict_select_kernel<<<dim3(a.cache.heads, a.batch.seqs), kSelectThreads, held, stream>>>(a);
+  if ((st = launch_status()) != SPL_OK) return st;
+  const int sms = device_sm_count(), row = (int)cache->head_dim * (i8 ? 1 : 2);
+  return row == 256 ? launch_move<256>(a, sms, stream)
+                    : (row == 128 ? launch_move<128>(a, sms, stream) : launch_move<64>(a, sms, stream));
+}
+
+extern "C" spl_status spl_kv_keep_path(const spl_kv_cache* cache, float* score, const spl_kv_batch* batch, int64_t rows,
+                                       const int32_t* path, int64_t ldpath, const int32_t* accepted, int64_t levels,
+                                       cudaStream_t stream) {
+  PathArgs a = {};
+  spl_status st = paged_cache_view(&a.cache, cache);
+  if (st != SPL_OK) return st;
+  if (levels < 0 || ldpath < 0) return SPL_EINVAL;
+  if ((st = paged_batch_view(&a.batch, a.cache, batch, rows)) != SPL_OK) return st;
+  if (a.batch.seqs == 0 || levels == 0 || rows == 0) return SPL_OK;
+  if (!path || !accepted || (a.batch.seqs > 1 && ldpath < levels)) return SPL_EINVAL;
+  if (levels > INT32_MAX) return SPL_ESHAPE;
+  if (!aligned4(score) || !aligned4(path) || !aligned4(accepted)) return SPL_EALIGN;
+  if (a.batch.max_pages == 0 || a.cache.pages == 0) return SPL_OK;
+  if (!(a.batch.status = device_status_word())) return SPL_ECUDA;
+  const bool i8 = cache->format == SPL_KV_I8;
+  if (!i8) a.cache.k_scale = a.cache.v_scale = nullptr;
+  a.score = score;
+  a.path = path;
+  a.accepted = accepted;
+  a.ldpath = ldpath;
+  a.levels = (int)levels;
+  const int row = (int)cache->head_dim * (i8 ? 1 : 2);
+  const int64_t tasks = (int64_t)a.cache.heads * (2 * row / 16 + 3);
+  const dim3 grid((unsigned)ceil_div(tasks, kPathThreads), a.batch.seqs);
+  auto launch = [&](auto kernel) {
+    kernel<<<grid, kPathThreads, 0, stream>>>(a);
+    return launch_status();
+  };
+  return row == 256 ? launch(keep_path_kernel<256>)
+                    : (row == 128 ? launch(keep_path_kernel<128>) : launch(keep_path_kernel<64>));
+}

@@ -13,6 +13,7 @@
 // their probabilities, rows and arrival.
 
 #include <algorithm>
+#include <climits>
 
 #include "paged.cuh"
 
@@ -242,10 +243,142 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) verify_kernel(const Ve
   }
 }
 
+// ---- a tree of drafts ----
+// The target's token at a node is drawn by the same race, argmax_v p(v) / e(v), and the walk goes on at the child that holds
+// it: whatever the drafts are, the tokens are distributed as the target's.  Level after level follows from the one before,
+// so a sequence has a cluster of blocks, each with a slice of the vocabulary, which exchange their best through shared
+// memory; the exponentials of a level are its own.
+struct TreeArgs {
+  int *accepted, *path, *token;
+  const float *p, *e;
+  const int *x, *parent, *row_start;
+  int64_t ldp, lde, ldpath, vocab, rows;
+  int levels;
+  unsigned int* status;
+};
+constexpr int kMostBlocks = 16;  // of a cluster
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Stores a value in another block's shared memory, at the place that `at` is in this one's.
+__device__ __forceinline__ void store_in_block(unsigned long long* at, uint32_t block, unsigned long long v) {
+  uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at));
+  asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(to) : "r"(block));
+  asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(v) : "memory");
+}
+
+template <bool VEC>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) verify_tree_kernel(const TreeArgs a, int64_t per_split, int blocks) {
+  __shared__ unsigned long long keys[kThreads / 32], bests[2][kMostBlocks];  // (of two levels in turn)
+  __shared__ int s_child[2];
+  const int b = blockIdx.x / blocks;
+  const uint32_t rank = cluster_rank();
+  const int64_t row0 = min(max((int64_t)__ldg(a.row_start + b), (int64_t)0), a.rows);
+  const int64_t row1 = min(max((int64_t)__ldg(a.row_start + b + 1), row0), a.rows);
+  const int nodes = (int)(row1 - row0);
+  const int64_t v0 = min(a.vocab, rank * per_split), v1 = min(a.vocab, v0 + per_split);
+  if (threadIdx.x < 2) s_child[threadIdx.x] = INT_MAX;
+  cluster_sync();  // every block has begun: its shared memory may be written
+  int at = 0, depth = 0, token = -1;
+  for (; nodes > 0; ++depth) {  // every block of the cluster makes every turn
+    const float* p = a.p + (row0 + at) * a.ldp;
+    const float* e = a.e + ((int64_t)b * a.levels + depth) * a.lde;
+    unsigned long long key = 0;
+    bool positive = false;
+    for (int64_t from = v0; from < v1; from += kMostEntries) {
+      const int some = (int)min(kMostEntries, v1 - from);
+      Trip<VEC> first;
+      first.load_random(e + from, (VEC ? 4 : 1) * threadIdx.x, some);
+      key = max(key, race_row<VEC>(p, nullptr, e, from, some, first, positive));
+    }
+    key = block_max(key, keys);
+    key = __shfl_sync(0xffffffffu, key, 0);
+    if (threadIdx.x < blocks) store_in_block(&bests[depth & 1][rank], threadIdx.x, key);
+    cluster_sync();
+    for (int r = 0; r < blocks; ++r) key = r == 0 ? bests[depth & 1][0] : max(key, bests[depth & 1][r]);
+    token = key == 0 ? -1 : (int)(0xffffffffu - (uint32_t)key);  // 0: no entry took part
+    if (token < 0 || depth + 1 == a.levels) break;
+    // The first child that holds it.
+    int child = INT_MAX;
+    for (int i = 1 + threadIdx.x; i < nodes; i += kThreads)
+      if (__ldg(a.parent + row0 + i) == at && __ldg(a.x + row0 + i) == token) child = min(child, i);
+    child = __reduce_min_sync(0xffffffffu, child);
+    if ((threadIdx.x & 31) == 0 && child != INT_MAX) atomicMin(&s_child[depth & 1], child);
+    __syncthreads();
+    child = s_child[depth & 1];
+    if (threadIdx.x == 0) s_child[(depth + 1) & 1] = INT_MAX;
+    __syncthreads();
+    if (child == INT_MAX) break;
+    if (rank == 0 && threadIdx.x == 0) a.path[b * a.ldpath + depth] = child;
+    at = child;
+  }
+  if (rank == 0) {
+    for (int d = depth + threadIdx.x; d < a.levels; d += kThreads) a.path[b * a.ldpath + d] = -1;
+    if (threadIdx.x == 0) {
+      a.accepted[b] = depth;
+      a.token[b] = token;
+    }
+  }
+}
+
 }  // namespace
 }  // namespace spl
 
 using namespace spl;
+
+extern "C" spl_status spl_verify_tree(int32_t* accepted, int32_t* path, int64_t ldpath, int32_t* token, const float* P,
+                                      int64_t ldp, const int32_t* x, const int32_t* parent, const float* e, int64_t lde,
+                                      const int32_t* row_start, int64_t rows, int64_t seqs, int64_t levels, int64_t vocab,
+                                      cudaStream_t stream) {
+  if (rows < 0 || seqs < 0 || levels < 0 || vocab < 0 || ldp < 0 || lde < 0 || ldpath < 0) return SPL_EINVAL;
+  if (seqs == 0) return SPL_OK;
+  if (!accepted || !path || !token || !row_start || levels == 0 || vocab == 0) return SPL_EINVAL;
+  if (rows > 0 && (!P || !e || !x || !parent)) return SPL_EINVAL;
+  if ((rows > 1 && ldp < vocab) || ((seqs > 1 || levels > 1) && lde < vocab) || (seqs > 1 && ldpath < levels))
+    return SPL_EINVAL;
+  if (seqs > kMaxSeqs || vocab > INT32_MAX || rows > INT32_MAX || levels > INT32_MAX) return SPL_ESHAPE;
+  for (const void* ptr : {(const void*)accepted, (const void*)path, (const void*)token, (const void*)P, (const void*)x,
+                          (const void*)parent, (const void*)e, (const void*)row_start})
+    if (!aligned4(ptr)) return SPL_EALIGN;
+  unsigned int* status = device_status_word();
+  if (!status) return SPL_ECUDA;
+  // A cluster of the blocks of one wave that a sequence's share has, each with at least a trip of its threads' loads.
+  const int64_t most = std::min(ceil_div(vocab, (int64_t)4 * kThreads), (int64_t)kBlocksPerSm * device_sm_count() / seqs);
+  int blocks = 1;
+  while (blocks < kMostBlocks && 2 * blocks <= most) blocks *= 2;
+  const int64_t per_split = round_up(ceil_div(vocab, blocks), 4);
+  const bool vec = ldp % 4 == 0 && lde % 4 == 0 && aligned16(P) && aligned16(e);
+  const TreeArgs a = {accepted, path, token, P, e, x, parent, row_start, ldp, lde, ldpath, vocab, rows, (int)levels, status};
+  auto launch = [&](auto kernel, bool(&done)[kMaxDevices]) {
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return SPL_ECUDA;
+    if (device >= kMaxDevices || !done[device]) {
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SPL_ECUDA;
+      if (device < kMaxDevices) done[device] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(blocks * seqs));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, a, per_split, blocks);
+    note_launches(1);
+    return err == cudaSuccess ? SPL_OK : SPL_ECUDA;
+  };
+  static bool done[2][kMaxDevices] = {};
+  return vec ? launch(verify_tree_kernel<true>, done[0]) : launch(verify_tree_kernel<false>, done[1]);
+}
 
 extern "C" size_t spl_verify_drafts_workspace_bytes(int64_t seqs) {
   return seqs > 0 && seqs <= kMaxSeqs ? (size_t)seqs * sizeof(VerifyState) : 0;

@@ -116,6 +116,13 @@ _SIGS = {
     "spl_kv_read": (_I, [_P, _P, _PC, _PB, _P, _I64, _P]),
     "spl_paged_attention_workspace_bytes": (_SZ, [_PC, _PB, _I64, _I64]),
     "spl_paged_attention": (_I, [_P, _I64, _P, _I64, _PC, _PB, _I64, _I64, ctypes.c_float, _I64, _P, _SZ, _P]),
+    "spl_tree_attention": (_I, [_P, _I64, _P, _I64, _PC, _PB, _P, _I64, _I64, _I64, ctypes.c_float, _I64, _P, _SZ, _P]),
+    "spl_kv_weigh_workspace_bytes": (_SZ, [_PC, _PB, _I64, _I64]),
+    "spl_kv_weigh": (_I, [_P, _P, _I64, _PC, _PB, _I64, _I64, ctypes.c_float, _I64, ctypes.c_float, _P, _SZ, _P]),
+    "spl_kv_evict_workspace_bytes": (_SZ, [_PC, _PB, _I64]),
+    "spl_kv_evict": (_I, [_PC, _P, _PB, _I64, _I64, _P, _P, _P, _SZ, _P]),
+    "spl_kv_keep_path": (_I, [_PC, _P, _PB, _I64, _P, _I64, _P, _I64, _P]),
+    "spl_verify_tree": (_I, [_P, _P, _I64, _P, _P, _I64, _P, _P, _P, _I64, _P, _I64, _I64, _I64, _I64, _P]),
     "spl_verify_drafts_workspace_bytes": (_SZ, [_I64]),
     "spl_verify_drafts": (_I, [_P, _P, _P, _I64, _P, _I64, _P, _P, _P, _I64, _P, _P, _I64, _I64, _I64, _I64, _P, _SZ,
                                _P]),
@@ -784,6 +791,103 @@ def spl_paged_attention(out, Q, cache, batch, q_heads, scale=None, window=0, wor
     _check(lib().spl_paged_attention(op, ldo, qp, ldq, cache.c_struct(),
                                      batch.c_struct(), batch.rows, int(q_heads), float(scale),
                                      int(window), wsp, wsb, _stream(stream)), "spl_paged_attention")
+
+
+def spl_tree_attention(out, Q, cache, batch, seen, q_heads, scale=None, window=0, workspace=None, stream=None):
+    """Attention of rows that form trees: row i of a sequence sees the keys before its rows and, of these, those whose bits
+    are set in seen [rows, words] int32 (bit j % 32 of word j / 32: its row j); window: the last so many of them.  The
+    rest, and the workspace, as in spl_paged_attention."""
+    width = int(q_heads) * cache.head_dim
+    (op, ldo), (qp, ldq) = _rows_view(out, "out", width), _rows_view(Q, "Q", width)
+    if out.shape[0] != batch.rows or Q.shape[0] != batch.rows or seen.dim() != 2 or seen.shape[0] != batch.rows:
+        raise ValueError("spl_tree_attention: shape mismatch")
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.head_dim)
+    if workspace is None:
+        workspace = _scratch(spl_paged_attention_workspace_bytes(cache, batch, q_heads), Q.device, stream)
+    wsp, wsb = _ws(workspace)
+    _check(lib().spl_tree_attention(op, ldo, qp, ldq, cache.c_struct(), batch.c_struct(),
+                                    _vector(seen, "seen", torch.int32)[0], seen.shape[1], batch.rows, int(q_heads),
+                                    float(scale), int(window), wsp, wsb, _stream(stream)), "spl_tree_attention")
+
+
+def spl_kv_weigh_workspace_bytes(cache, batch, q_heads):
+    return int(lib().spl_kv_weigh_workspace_bytes(cache.c_struct(), batch.c_struct(), batch.rows, int(q_heads)))
+
+
+def _score(score, cache):
+    if tuple(score.shape) != (cache.pages, cache.kv_heads, cache.page_size):
+        raise ValueError("score must be [pages, kv_heads, page_size]")
+    return _vector(score, "score", torch.float32)[0]
+
+
+def spl_kv_weigh(score, Q, cache, batch, q_heads, scale=None, window=0, decay=1.0, workspace=None, stream=None):
+    """score [pages, kv_heads, page_size] fp32 of the sequences' tokens <- decay score + the attention weight that the
+    batch's rows Q [rows, q_heads head_dim] give them; the rows' own tokens start from 0."""
+    qp, ldq = _rows_view(Q, "Q", int(q_heads) * cache.head_dim)
+    if Q.shape[0] != batch.rows:
+        raise ValueError("spl_kv_weigh: shape mismatch")
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.head_dim)
+    if workspace is None:
+        workspace = _scratch(spl_kv_weigh_workspace_bytes(cache, batch, q_heads), Q.device, stream)
+    wsp, wsb = _ws(workspace)
+    _check(lib().spl_kv_weigh(_score(score, cache), qp, ldq, cache.c_struct(), batch.c_struct(), batch.rows,
+                              int(q_heads), float(scale), int(window), float(decay), wsp, wsb, _stream(stream)),
+           "spl_kv_weigh")
+
+
+def spl_kv_evict_workspace_bytes(cache, batch, keep):
+    return int(lib().spl_kv_evict_workspace_bytes(cache.c_struct(), batch.c_struct(), int(keep)))
+
+
+def spl_kv_evict(cache, score, batch, keep, recent, out_len, out_table=None, workspace=None, stream=None):
+    """Cuts the batch's sequences to ``keep`` tokens: of each key head the last ``recent`` and the heaviest others by score
+    [pages, kv_heads, page_size] stay and move together, where they lie or to the pages of out_table (int32 [seqs,
+    max_pages]); out_len (int32 [seqs]; kv_len itself will do) receives the lengths."""
+    lp, seqs = _vector(out_len, "out_len", torch.int32)
+    if seqs != batch.seqs or (out_table is not None and out_table.shape != batch.page_table.shape):
+        raise ValueError("spl_kv_evict: shape mismatch")
+    if workspace is None:
+        workspace = _scratch(spl_kv_evict_workspace_bytes(cache, batch, keep), score.device, stream)
+    wsp, wsb = _ws(workspace)
+    table = None if out_table is None else _vector(out_table, "out_table", torch.int32)[0]
+    _check(lib().spl_kv_evict(cache.c_struct(), _score(score, cache), batch.c_struct(), int(keep), int(recent), table, lp,
+                              wsp, wsb, _stream(stream)), "spl_kv_evict")
+
+
+def spl_kv_keep_path(cache, batch, path, accepted, score=None, stream=None):
+    """Moves the rows path [seqs, levels] (int32, the first accepted [seqs] of each) of the batch's trees, and their scores
+    if given, to the places behind their row 0."""
+    ap, seqs = _vector(accepted, "accepted", torch.int32)
+    pp, _ = _vector(path, "path", torch.int32)
+    if seqs != batch.seqs or path.dim() != 2 or path.shape[0] != seqs:
+        raise ValueError("spl_kv_keep_path: shape mismatch")
+    levels = path.shape[1]
+    _check(lib().spl_kv_keep_path(cache.c_struct(), None if score is None else _score(score, cache), batch.c_struct(),
+                                  batch.rows, pp, levels, ap, levels, _stream(stream)), "spl_kv_keep_path")
+
+
+def spl_verify_tree(accepted, path, token, P, x, parent, e, row_start, stream=None):
+    """The walk down each sequence's tree of drafts (accepted, token int32 [seqs]; path int32 [seqs, levels], -1 behind the
+    accepted ones): P [rows, vocab] the target's probabilities after each node, x and parent [rows] int32 the nodes' tokens
+    and the nodes that they follow (by their place in the sequence), e [seqs levels, vocab] exponential; sequence b's nodes
+    start at row_start[b] (int32 [seqs + 1])."""
+    (pp, ldp), (ep, lde) = _rows_view(P, "P", None), _rows_view(e, "e", P.shape[1])
+    i32 = torch.int32
+    ap, seqs = _vector(accepted, "accepted", i32)
+    tp, tokens = _vector(token, "token", i32)
+    wp, _ = _vector(path, "path", i32)
+    xp, nodes = _vector(x, "x", i32)
+    op, others = _vector(parent, "parent", i32)
+    rp, starts = _vector(row_start, "row_start", i32)
+    rows, vocab = P.shape
+    if path.dim() != 2 or path.shape[0] != seqs or not (
+            tokens == seqs and nodes == others == rows and starts == seqs + 1 and e.shape[0] == path.numel()):
+        raise ValueError("spl_verify_tree: shape mismatch")
+    levels = path.shape[1]
+    _check(lib().spl_verify_tree(ap, wp, levels, tp, pp, ldp, xp, op, ep, lde, rp, rows, seqs, levels, vocab,
+                                 _stream(stream)), "spl_verify_tree")
 
 
 def spl_verify_drafts_workspace_bytes(seqs):
