@@ -698,13 +698,15 @@ struct Kernel {
     uint32_t ts, ks, vs, bad;
     int lo[2], hi[2];
     float row_scale[2];
-    // Trees: the rows' masks, the first of their bits' keys as the tile counts them, words; lo and hi limit them.
+    // Trees: the rows' masks (of rows past the last none: they see all), the first of their bits' keys as the tile counts
+    // them, words; lo and hi limit them.
     const uint32_t* seen[2];
+    bool there[2];
     int pos0;
     int64_t words;
     // Which of the tile's 32 keys from j on row r sees.
     __device__ uint32_t sees(int r, int j) const {
-      return seen[r] ? tree_keys(seen[r], words, pos0, lo[r], hi[r], j) : ~0u;
+      return there[r] ? tree_keys(seen[r], words, pos0, lo[r], hi[r], j) : ~0u;
     }
   };
   static __device__ __forceinline__ void mul2(uint32_t& a, uint32_t& b, uint32_t x, uint32_t y) {
@@ -932,8 +934,8 @@ struct Kernel {
             int lo = j0, hi = j0 + kKeys;
             const int token = (x.r0 + own0 + 8 * r) / a.group;
             if constexpr (TREE) {
-              sc.seen[r] = nullptr;
-              if (own0 + 8 * r < x.rows) {
+              sc.there[r] = own0 + 8 * r < x.rows;
+              if (sc.there[r]) {
                 sc.seen[r] = a.seen + (x.row0 + token) * a.words;
                 lo = tree_lo(sc.seen[r], a.words, a.window, x.pos0, x.len);
                 hi = x.len;
