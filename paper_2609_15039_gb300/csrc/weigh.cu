@@ -11,8 +11,8 @@
 
 #include <cuda_fp16.h>
 
-#include "attention.cuh"
 #include "ptx.cuh"
+#include "weigh.cuh"
 
 namespace spl {
 namespace {
@@ -316,12 +316,21 @@ spl_status launch_scores(const WeighArgs& w, int blocks, cudaStream_t stream) {
   return launch_status();
 }
 
+// Few rows: of a key head at most kFewRows, by max_rows, and scores that take no more than kMostScores bytes.
+constexpr int64_t kFewRows = 16, kMostScores = int64_t(1) << 31;
 struct Shape {
+  bool few;
   int64_t cap;
   size_t s, parts, stats, bytes;
 };
-Shape shape_of(const PagedCache& c, const PagedBatch& b, int64_t q_heads) {
+Shape shape_of(const PagedCache& c, const PagedBatch& b, const spl_kv_batch* batch, int64_t q_heads, int head_dim) {
   Shape x;
+  x.few = batch->max_rows * (q_heads / c.heads) <= kFewRows &&
+          (double)b.rows * (double)q_heads * (double)(b.max_pages << c.page_shift) * 4 <= (double)kMostScores;
+  if (!x.few) {
+    x.bytes = b.rows == 0 ? 0 : weigh_tc_bytes(c, b, q_heads, head_dim);
+    return x;
+  }
   x.cap = round_up(std::max<int64_t>(1, b.max_pages << c.page_shift), kUnit);
   x.s = (size_t)b.rows * q_heads * x.cap * sizeof(float);
   x.parts = x.s / kPart * 2;
@@ -338,7 +347,7 @@ spl_status check(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t r
   if (q_heads / cache->kv_heads > 1024 || rows > INT32_MAX / 2 / (q_heads / cache->kv_heads))
     return SPL_ESHAPE;
   if ((st = paged_batch_view(b, *c, batch, rows)) != SPL_OK) return st;
-  if ((double)rows * (double)q_heads * (double)(b->max_pages << c->page_shift) > 0x1p44) return SPL_ESHAPE;
+  if (rows > (INT32_MAX - 1024) / q_heads) return SPL_ESHAPE;  // rows of a copy's coordinates
   return SPL_OK;
 }
 
@@ -352,7 +361,7 @@ extern "C" size_t spl_kv_weigh_workspace_bytes(const spl_kv_cache* cache, const 
   PagedCache c;
   PagedBatch b;
   if (check(cache, batch, rows, q_heads, &c, &b) != SPL_OK || b.seqs == 0) return 0;
-  return shape_of(c, b, q_heads).bytes;
+  return shape_of(c, b, batch, q_heads, (int)cache->head_dim).bytes;
 }
 
 extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, const spl_kv_cache* cache,
@@ -367,7 +376,8 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   if (rows > 0 && !Q) return SPL_EINVAL;
   if (rows > 1 && ldq < q_heads * cache->head_dim) return SPL_EINVAL;
   if (!aligned16(Q) || !aligned4(score) || (rows > 1 && ldq % 4 != 0)) return SPL_EALIGN;
-  const Shape s = shape_of(a.cache, a.batch, q_heads);
+  const int dim = (int)cache->head_dim;
+  const Shape s = shape_of(a.cache, a.batch, batch, q_heads, dim);
   if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes)) return SPL_EWORKSPACE;
   if (!aligned16(workspace)) return SPL_EALIGN;
   if (a.cache.pages == 0 || a.batch.max_pages == 0) return SPL_OK;
@@ -382,6 +392,10 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   a.slack = 1;
   a.join = 0;
   a.start = 1;
+  const bool i8 = cache->format == SPL_KV_I8;
+  if (rows > 0 && !s.few)
+    return run_weigh_tc({score, Q, ldq, a.cache, a.batch, a.group, (int)q_heads, a.window, a.scale_log2, decay, workspace}, dim,
+                        i8, stream);
   w.score = score;
   w.decay = decay;
   w.q_heads = (int)q_heads;
@@ -391,7 +405,6 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   w.parts = reinterpret_cast<float2*>(at + s.s);
   w.stats = reinterpret_cast<float2*>(at + s.s + s.parts);
   const int sms = device_sm_count();
-  const bool i8 = cache->format == SPL_KV_I8;
   if (rows > 0) {
     st = cache->head_dim == 128 ? (i8 ? launch_scores<128, true>(w, sms, stream) : launch_scores<128, false>(w, sms, stream))
                                 : (i8 ? launch_scores<64, true>(w, sms, stream) : launch_scores<64, false>(w, sms, stream));

@@ -1,0 +1,842 @@
+// The attention weight that stored tokens gather from many rows (chunks, prompts), on the 5th-generation tensor cores.
+//
+//   score_j <- decay score_j + sum_i 2^(s_ij - lse_i),   s_ij = scale log2(e) q_i . k_j,   lse_i = log2 sum_j 2^s_ij
+// The sum over rows needs every row's lse first, so the scores are made twice, over tiles of 128 rows (a token's `group`
+// query heads side by side) and 128 keys:
+//   S = q_hi K^T + q_lo K^T    q = (hi + lo) 2^-e in binary16, split ahead; the stored values are exact in binary16
+// A first pass keeps the rows' maxima and totals of each range of key tiles, a small kernel joins those, and a second pass
+// adds up p for each key.  Both walk the same way, a tile of rows after another and its key tiles in turn, and differ in
+// which operand is the MMA's A: S has the rows in tensor memory's lanes in the first pass, so that a thread has a row, and
+// K q^T the keys in the second, so that a thread has a key and its sum: neither reduces across threads, and nothing is
+// added by atomics, whose order would change the bits.  Roles:
+//   warp 0       MMA issuer.
+//   warp 1       hands out the block's pieces of work and loads tiles of q and (binary16) of K, by TMA, a box a page.
+//   warp 2       second pass: the rows' scales and lse.
+//   warps 4-11   two groups that take the key tiles in turn: maxima and totals, or sums.
+//   warps 12-19  int8: two groups widen the key tiles to binary16 in turn.
+// Tensor memory: four places of S.  Every wait is bounded; on expiry the status word is raised and the block leaves with its
+// copies and MMAs done.
+
+#include <algorithm>
+#include <cmath>
+
+#include <cuda_fp16.h>
+
+#include "ptx.cuh"
+#include "weigh.cuh"
+
+namespace spl {
+namespace {
+
+constexpr int kTile = 128;          // rows and keys
+constexpr int kEpilogue = 8;        // warps
+constexpr int kThreads = 32 * (4 + kEpilogue), kThreadsI8 = kThreads + 32 * 8;
+constexpr int kQStages = 2, kS = 4;
+constexpr int kMostTiles = 8;       // key tiles of a piece of the second pass (a thread has every other one's sum)
+constexpr int kMostRange = 16;      // key tiles of a piece of the first pass
+constexpr int kNotes = 8;           // key tiles whose marks or scales have a place: the loader is at most 3 ahead of the
+                                    // issuer, which is at most kS ahead of the epilogue
+constexpr int kPieces = 4;
+
+// What the blocks go by, made on the device: key tiles of a piece of each pass, pieces of each, and behind it the first
+// pieces of the sequences, [seqs] for each pass.
+struct WeighPlan {
+  int range, tiles;
+  int64_t pieces[2];
+};
+
+struct TcArgs {
+  WeighCall w;
+  uint16_t *q_hi, *q_lo;  // [heads][total][dim], total = rows group
+  float2* rows;           // [heads][total]: scale, lse
+  float2* parts;          // [heads][total][splits][2]: maximum, total
+  int splits;             // places of a row
+  int64_t total;
+  WeighPlan* plan;
+  int64_t* first[2];
+};
+
+struct alignas(16) Piece {
+  int b, h;
+  int row0, n, len, pos0;
+  int rt0, rt1;  // row tiles [rt0, rt1), of the first pass one
+  int t0, t1;    // key tiles
+  int split;     // the range's index among the sequence's
+  int last;      // no piece: the end
+};
+
+// ---------------------------------------------------------------- before the passes
+// Block 0: the plan.  The others: q's rows as hi + lo, a warp a row or two.
+constexpr int kPrepThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __grid_constant__ TcArgs a, int grid) {
+  const WeighCall& w = a.w;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seqs = w.batch.seqs;
+  if (blockIdx.x == 0) {
+    constexpr int kRanges = 5, kSplits = 4;  // 16, 8, 4, 2, 1 and 8, 4, 2, 1
+    __shared__ unsigned long long sums[kRanges + kSplits], scan[2][kPrepThreads];
+    __shared__ int longest, chosen[2];
+    if (threadIdx.x < kRanges + kSplits) sums[threadIdx.x] = 0;
+    if (threadIdx.x == 0) longest = 0;
+    __syncthreads();
+    for (int b = threadIdx.x; b < seqs; b += kPrepThreads) {
+      const PagedSeq s = paged_seq(w.batch, w.cache.page_shift, b);
+      const int64_t kt = (s.len + kTile - 1) / kTile, rt = ((int64_t)s.n * w.group + kTile - 1) / kTile;
+      for (int i = 0; i < kRanges; ++i) atomicAdd(sums + i, (unsigned long long)(rt * ((kt + (16 >> i) - 1) / (16 >> i))));
+      for (int i = 0; i < kSplits; ++i)
+        atomicAdd(sums + kRanges + i, (unsigned long long)((kt + (8 >> i) - 1) / (8 >> i)));
+      atomicMax(&longest, (int)kt);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {  // the longest pieces of which every block has some
+      int i = 0, k = 0;
+      while (i + 1 < kRanges && sums[i] * w.cache.heads < 4ull * grid && (longest + (16 >> (i + 1)) - 1) / (16 >> (i + 1)) <= a.splits) ++i;
+      while (k + 1 < kSplits && sums[kRanges + k] * w.cache.heads < 3ull * grid) ++k;
+      chosen[0] = 16 >> i;
+      chosen[1] = 8 >> k;
+      *a.plan = {chosen[0], chosen[1], {(int64_t)sums[i] * w.cache.heads, (int64_t)sums[kRanges + k] * w.cache.heads}};
+    }
+    __syncthreads();
+    // Each sequence's first piece: sums before it, a run of sequences a thread.
+    const int per = (seqs + kPrepThreads - 1) / kPrepThreads, b0 = min(seqs, per * (int)threadIdx.x), b1 = min(seqs, b0 + per);
+    auto count = [&](int b, int pass) {
+      const PagedSeq s = paged_seq(w.batch, w.cache.page_shift, b);
+      const int64_t kt = (s.len + kTile - 1) / kTile, rt = ((int64_t)s.n * w.group + kTile - 1) / kTile;
+      return (unsigned long long)((pass == 0 ? rt : 1) * ((kt + chosen[pass] - 1) / chosen[pass]) * w.cache.heads);
+    };
+    for (int pass = 0; pass < 2; ++pass) {
+      unsigned long long own = 0;
+      for (int b = b0; b < b1; ++b) own += count(b, pass);
+      scan[pass][threadIdx.x] = own;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+      unsigned long long sum = 0;
+      for (int i = 0; i < kPrepThreads; ++i) {
+        const unsigned long long own = scan[threadIdx.x][i];
+        scan[threadIdx.x][i] = sum;
+        sum += own;
+      }
+    }
+    __syncthreads();
+    for (int pass = 0; pass < 2; ++pass) {
+      unsigned long long sum = scan[pass][threadIdx.x];
+      for (int b = b0; b < b1; ++b) {
+        a.first[pass][b] = (int64_t)sum;
+        sum += count(b, pass);
+      }
+    }
+    return;
+  }
+  constexpr int LANES = D / 4, PER = 32 / LANES;
+  const int sub = lane / LANES, at = lane % LANES;
+  const int64_t all = w.batch.rows * w.q_heads;
+  for (int64_t i0 = ((int64_t)(blockIdx.x - 1) * (kPrepThreads / 32) + warp) * PER; i0 < all;
+       i0 += (int64_t)(gridDim.x - 1) * (kPrepThreads / 32) * PER) {
+    const int64_t i = i0 + sub;
+    const bool there = i < all;
+    const int64_t token = there ? i / w.q_heads : 0;
+    const int head = there ? (int)(i % w.q_heads) : 0;
+    const float4 v = there ? __ldcs(reinterpret_cast<const float4*>(w.q + token * w.ldq + (int64_t)head * D) + at)
+                           : make_float4(0.f, 0.f, 0.f, 0.f);
+    float top = fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const int e = fp16_row_exponent(top);
+    const float up = pow2f(e);
+    uint32_t h0, l0, h1, l1;
+    split_f16(v.x * up, v.y * up, h0, l0);
+    split_f16(v.z * up, v.w * up, h1, l1);
+    if (!there) continue;
+    const int64_t row = (int64_t)(head / w.group) * a.total + token * w.group + head % w.group;
+    reinterpret_cast<uint2*>(a.q_hi + row * D)[at] = make_uint2(h0, h1);
+    reinterpret_cast<uint2*>(a.q_lo + row * D)[at] = make_uint2(l0, l1);
+    if (at == 0) a.rows[row].x = w.scale_log2 * pow2f(-e);
+  }
+}
+
+// ---------------------------------------------------------------- the passes
+template <int D, bool I8>
+struct Layout {
+  static constexpr int PANELS = D / 64, STAGES = I8 ? 2 : 3;
+  static constexpr uint32_t PANEL = 128 * 128, TILE = PANELS * PANEL;
+  static constexpr uint32_t Q = 0, K = kQStages * 2 * TILE;  // stages of [q_hi, q_lo]; of K
+  // second pass: the rows' scales and lse of each stage of q; first pass, int8: the keys' scales
+  static constexpr uint32_t COL = K + STAGES * TILE, SCALE = COL;
+  static constexpr uint32_t GONE = COL + (I8 ? kNotes * kTile * 4 : kQStages * kTile * 8);  // marks of keys without a page
+  static constexpr uint32_t BARS = GONE + kNotes * 16;
+  enum { kKFull = 0, kKEmpty = 3, kQFull = 6, kQEmpty = 8, kSFull = 10, kSFree = 14, kPieceFull = 18, kPieceFree = 22, kDrain = 26,
+         kBars = 27 };
+  static constexpr uint32_t PIECES = BARS + 8 * 28, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
+  static_assert(PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
+  static constexpr uint32_t IDESC = make_idesc(0, 128, 128);
+};
+constexpr uint32_t kTmemCols = 512;
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc,
+                                       uint32_t accumulate, uint32_t leader) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(hi), "r"(leader)
+      : "memory");
+}
+// 32 lanes x 32 columns (thread t gets lane base + t); read after tmem_ld_wait.
+__device__ __forceinline__ void tmem_ld_32x32_begin(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_shared4(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+template <int D, bool I8, bool SUM>
+struct Kernel {
+  using L = Layout<D, I8>;
+  const TcArgs& a;
+  const CUtensorMap &map_hi, &map_lo, &map_k;
+  uint32_t smem, tmem;
+  volatile int* abort;
+  Piece* pieces;
+
+  __device__ uint32_t bar(int i) const { return smem + L::BARS + 8u * i; }
+  __device__ bool wait(int i, uint32_t parity) const {
+    return __all_sync(0xffffffffu, mbar_wait_soon(bar(i), parity, kWaitNs, abort));
+  }
+  __device__ void arrive(int i) const {  // one for the warp, after all its lanes' work
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar(i));
+  }
+  __device__ void give_up() const {
+    *abort = 1;
+    atomicOr(a.w.batch.status, kStatusTimeout);
+  }
+
+  // ---------------------------------------------------------------- the walk
+  // Of a row tile: its rows, the key tiles of the piece that it meets, and the keys that all its rows see.
+  struct Span {
+    int r0, rows, k0, k1, all_lo, all_hi;
+  };
+  __device__ Span span(const Piece& x, int rt) const {
+    const int group = a.w.group;
+    Span y;
+    y.r0 = rt * kTile;
+    y.rows = min(kTile, x.n * group - y.r0);
+    const PagedSeq s = {x.row0, x.n, x.len, x.pos0};
+    int lo, hi;
+    row_keys(s, a.w.window, y.r0 / group, lo, y.all_hi);
+    row_keys(s, a.w.window, (y.r0 + y.rows - 1) / group, y.all_lo, hi);
+    y.k0 = max(x.t0, lo / kTile);
+    y.k1 = hi > lo ? min(x.t1, (hi + kTile - 1) / kTile) : y.k0;
+    return y;
+  }
+  // For every piece begin(piece), for each of its row tiles that meets key tiles tile(piece, span, its number), for each of
+  // these step(piece, span, key tile, its number), end(piece); all return whether to go on.
+  template <class Begin, class Rows, class Step, class RowsEnd, class End>
+  __device__ bool walk(Begin begin, Rows rows, Step step, RowsEnd rows_end, End end) const {
+    int tile = 0, key = 0;
+    for (int k = 0;; ++k) {
+      if (!wait(L::kPieceFull + k % kPieces, (uint32_t)(k / kPieces) & 1u)) return false;
+      const Piece x = pieces[k % kPieces];
+      arrive(L::kPieceFree + k % kPieces);
+      if (x.last) return true;
+      if (!begin(x)) return false;
+      for (int rt = x.rt0; rt < x.rt1; ++rt) {
+        const Span y = span(x, rt);
+        if (y.k0 >= y.k1) continue;
+        if (!rows(x, y, tile)) return false;
+        for (int kt = y.k0; kt < y.k1; ++kt, ++key)
+          if (!step(x, y, kt, key, tile)) return false;
+        if (!rows_end(x, y, tile)) return false;
+        ++tile;
+      }
+      if (!end(x)) return false;
+    }
+  }
+  static constexpr auto nothing = [](auto&&...) { return true; };
+
+  // The k-th piece of the block, by warp 1.
+  __device__ bool hand_out(int k) const {
+    const int lane = threadIdx.x & 31, seqs = a.w.batch.seqs, group = a.w.group;
+    if (k >= kPieces && !wait(L::kPieceFree + k % kPieces, (uint32_t)(k / kPieces - 1) & 1u)) return false;
+    const int64_t item = blockIdx.x + (int64_t)k * gridDim.x;
+    Piece x = {};
+    x.last = 1;
+    if (item < a.plan->pieces[SUM]) {
+      const int64_t* first = a.first[SUM];
+      int lo = 0, n = seqs;  // the last sequence that begins at or before it
+      while (n > 1) {
+        const int step = (n + 31) >> 5, i = lane * step;
+        const unsigned below = __ballot_sync(0xffffffffu, i < n && first[lo + (i < n ? i : 0)] <= item);
+        const int pick = below ? 31 - __clz(below) : 0;
+        lo += pick * step;
+        n = n - pick * step < step ? n - pick * step : step;
+      }
+      const PagedSeq s = paged_seq(a.w.batch, a.w.cache.page_shift, lo);
+      const int per = SUM ? a.plan->tiles : a.plan->range;
+      const int tiles = (s.len + kTile - 1) / kTile, rows = s.n * group, row_tiles = (rows + kTile - 1) / kTile;
+      const int splits = (tiles + per - 1) / per;
+      int64_t rest = item - first[lo];
+      const int64_t of_head = (int64_t)splits * (SUM ? 1 : row_tiles);
+      x.b = lo;
+      x.h = (int)quotient(rest, of_head);
+      rest -= x.h * of_head;
+      x.row0 = s.row0, x.n = s.n, x.len = s.len, x.pos0 = s.pos0;
+      x.split = (int)(rest % splits);
+      x.t0 = x.split * per;
+      x.t1 = min(tiles, x.t0 + per);
+      if constexpr (SUM) {  // the tokens that may see a key of the range
+        const int64_t i0 = max((int64_t)0, (int64_t)x.t0 * kTile - s.pos0);
+        const int64_t i1 = a.w.window == INT32_MAX ? s.n : min((int64_t)s.n, (int64_t)x.t1 * kTile - s.pos0 + a.w.window);
+        x.rt0 = i0 < i1 ? (int)(i0 * group / kTile) : 0;
+        x.rt1 = i0 < i1 ? (int)((i1 * group + kTile - 1) / kTile) : 0;
+      } else {
+        x.rt0 = (int)quotient(rest, splits);
+        x.rt1 = x.rt0 + 1;
+      }
+      x.last = 0;
+    }
+    if (lane == 0) {
+      pieces[k % kPieces] = x;
+      mbar_arrive(bar(L::kPieceFull + k % kPieces));
+    }
+    __syncwarp();
+    return true;
+  }
+
+  // ---------------------------------------------------------------- loads
+  static constexpr int kUnseen = -1, kGone = -2;
+  // The page of the keys from j on (all in one), kUnseen past the sequence's end, kGone if it is outside the pool.
+  __device__ int page_of(const Piece& x, int j) const {
+    if (j >= x.len) return kUnseen;
+    const int page = paged_page(a.w.cache, a.w.batch, x.b, j);
+    return page >= 0 ? page : kGone;
+  }
+  // Warp 1.  The pieces are handed out kPieces ahead of its own walk over them.
+  __device__ void loader() const {
+    const int lane = threadIdx.x & 31, shift = a.w.cache.page_shift;
+    const int box = min(kTile, 1 << shift), boxes = kTile / box;
+    const int none = (int)((int64_t)a.w.cache.pages * a.w.cache.heads << shift);  // past the pool: filled with zeros
+    const uint64_t policy = l2_evict_last();  // other blocks read the same tiles
+    int tiles = 0, keys = 0;  // loaded so far
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      ok = hand_out(k);
+      if (!ok) break;
+      const Piece x = pieces[k % kPieces];
+      __syncwarp();
+      arrive(L::kPieceFree + k % kPieces);
+      if (x.last) break;
+      for (int rt = x.rt0; ok && rt < x.rt1; ++rt) {
+        const Span y = span(x, rt);
+        if (y.k0 >= y.k1) continue;
+        const int q = tiles % kQStages;
+        if (tiles >= kQStages) ok = wait(L::kQEmpty + q, (uint32_t)(tiles / kQStages - 1) & 1u);
+        if (!ok) break;
+        if (lane == 0) {
+          const uint32_t to = smem + L::Q + (uint32_t)q * 2u * L::TILE;
+          const int row = (int)((int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0);
+          mbar_expect_tx(bar(L::kQFull + q), 2u * L::TILE);
+#pragma unroll
+          for (int p = 0; p < L::PANELS; ++p) {
+            tma_load_2d(to + p * L::PANEL, &map_hi, bar(L::kQFull + q), 64 * p, row, policy);
+            tma_load_2d(to + L::TILE + p * L::PANEL, &map_lo, bar(L::kQFull + q), 64 * p, row, policy);
+          }
+        }
+        __syncwarp();
+        ++tiles;
+        if constexpr (I8) continue;
+        auto look_up = [&](int kt) {  // the lane's box of a key tile
+          const int j = kt * kTile + lane * box;
+          const int page = lane < boxes && kt < y.k1 ? page_of(x, j) : kUnseen;
+          return page >= 0 ? ((((int64_t)page * a.w.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : (int64_t)page;
+        };
+        int64_t slot = look_up(y.k0);
+        for (int kt = y.k0; ok && kt < y.k1; ++kt) {
+          const int64_t next = look_up(kt + 1);
+          const int stage = keys % L::STAGES;
+          if (keys >= L::STAGES) ok = wait(L::kKEmpty + stage, (uint32_t)(keys / L::STAGES - 1) & 1u);
+          if (!ok) break;
+          const unsigned gone = __ballot_sync(0xffffffffu, slot == kGone);
+          if (lane < 4) {  // a bit a key
+            uint32_t word = 0;
+            for (int i = 0; i < 32; i += 16)
+              if (gone >> ((32 * lane + i) / box) & 1u) word |= 0xffffu << i;
+            st_shared4(smem + L::GONE + 16u * (keys % kNotes) + 4u * lane, word);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_expect_tx(bar(L::kKFull + stage), L::TILE);
+          __syncwarp();
+          if (lane < boxes) {
+            const uint32_t to = smem + L::K + (uint32_t)stage * L::TILE + (uint32_t)(lane * box) * 128u;
+#pragma unroll
+            for (int p = 0; p < L::PANELS; ++p)
+              tma_load_2d(to + p * L::PANEL, &map_k, bar(L::kKFull + stage), 64 * p, slot >= 0 ? (int)slot : none, policy);
+          }
+          __syncwarp();
+          slot = next;
+          ++keys;
+        }
+      }
+    }
+    if (!ok) {
+      if (lane == 0) give_up();
+      // no copy in flight when the block leaves
+      for (int t = max(0, tiles - kQStages); t < tiles; ++t)
+        mbar_wait(bar(L::kQFull + t % kQStages), (uint32_t)(t / kQStages) & 1u, kDrainNs, nullptr);
+      for (int t = max(0, keys - L::STAGES); t < keys; ++t)
+        mbar_wait(bar(L::kKFull + t % L::STAGES), (uint32_t)(t / L::STAGES) & 1u, kDrainNs, nullptr);
+    }
+  }
+  // Warp 2, second pass: scale and lse of a tile's rows; of rows that are not there an lse that leaves nothing.
+  __device__ void columns() const {
+    const int lane = threadIdx.x & 31;
+    const bool ok = walk(
+        nothing,
+        [&](const Piece& x, const Span& y, int tile) {
+          const int q = tile % kQStages;
+          if (tile >= kQStages && !wait(L::kQEmpty + q, (uint32_t)(tile / kQStages - 1) & 1u)) return false;
+          const float2* rows = a.rows + (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0;
+#pragma unroll
+          for (int i = lane; i < kTile; i += 32) {
+            const float2 v = i < y.rows ? rows[i] : make_float2(0.f, INFINITY);
+            asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(smem + L::COL + 8u * (q * kTile + i)), "f"(v.x), "f"(v.y)
+                         : "memory");
+          }
+          arrive(L::kQFull + q);
+          return true;
+        },
+        nothing, nothing, nothing);
+    if (!ok && lane == 0) give_up();
+  }
+  // Warps 12-19 (int8): every other key tile widened to binary16 in the MMAs' layout, a thread the same 16 dims of every
+  // KEY_STEP-th key; marks of keys without a page and, in the first pass, the keys' scales.
+  __device__ void widen() const {
+    constexpr int PARTS = D / 16, KEY_STEP = 128 / PARTS, PER = kTile / KEY_STEP;
+    const int i = threadIdx.x & 127, set = (threadIdx.x >> 7) - kThreads / 128, lane = i & 31;
+    const int part = i % PARTS, key0 = i / PARTS, c0 = (2 * part) & 7, shift = a.w.cache.page_shift;
+    const int8_t* codes = static_cast<const int8_t*>(a.w.cache.k);
+    const bool ok = walk(
+        nothing, nothing,
+        [&](const Piece& x, const Span&, int kt, int key, int) {
+          if ((key & 1) != set) return true;
+          const int stage = key % L::STAGES;
+          auto slot_of = [&](int j) -> int64_t {
+            const int page = page_of(x, j);
+            return page >= 0 ? ((((int64_t)page * a.w.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : (int64_t)page;
+          };
+          uint4 q[PER];
+#pragma unroll
+          for (int k = 0; k < PER; ++k) {
+            const int64_t slot = slot_of(kt * kTile + key0 + KEY_STEP * k);
+            q[k] = slot >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + slot * D) + part) : make_uint4(0u, 0u, 0u, 0u);
+          }
+          const int64_t own = slot_of(kt * kTile + i);
+          const float scale = !SUM && own >= 0 ? __ldg(a.w.cache.k_scale + own) : 0.f;
+          const unsigned gone = __ballot_sync(0xffffffffu, own == kGone);
+          if (key >= L::STAGES && !wait(L::kKEmpty + stage, (uint32_t)(key / L::STAGES - 1) & 1u)) return false;
+          const uint32_t panel = smem + L::K + (uint32_t)stage * L::TILE + (uint32_t)(part >> 2) * L::PANEL;
+#pragma unroll
+          for (int k = 0; k < PER; ++k) {
+            const int at = key0 + KEY_STEP * k;
+            const uint32_t v[4] = {q[k].x ^ 0x80808080u, q[k].y ^ 0x80808080u, q[k].z ^ 0x80808080u, q[k].w ^ 0x80808080u};
+            const uint32_t row = panel + at * 128;
+            st_shared16(row + ((c0 ^ (at & 7)) << 4), make_uint4(i8_pair(v[0], 0x4140u), i8_pair(v[0], 0x4342u),
+                                                                 i8_pair(v[1], 0x4140u), i8_pair(v[1], 0x4342u)));
+            st_shared16(row + (((c0 + 1) ^ (at & 7)) << 4), make_uint4(i8_pair(v[2], 0x4140u), i8_pair(v[2], 0x4342u),
+                                                                       i8_pair(v[3], 0x4140u), i8_pair(v[3], 0x4342u)));
+          }
+          if constexpr (!SUM) st_shared4(smem + L::SCALE + 4u * (key % kNotes * kTile + i), __float_as_uint(scale));
+          if (lane == 0) st_shared4(smem + L::GONE + 16u * (key % kNotes) + 4u * (i >> 5), gone);
+          fence_proxy_async_smem();
+          arrive(L::kKFull + stage);
+          return true;
+        },
+        nothing, nothing);
+    if (!ok && lane == 0) give_up();
+  }
+
+  // ---------------------------------------------------------------- MMA issuer
+  __device__ void issuer() const {
+    const uint32_t leader = elect_one();
+    auto commit = [&](int i) {
+      if (leader) mma_commit(bar(i));
+      __syncwarp();
+    };
+    const bool ok = walk(
+        nothing,
+        [&](const Piece&, const Span&, int tile) { return wait(L::kQFull + tile % kQStages, (uint32_t)(tile / kQStages) & 1u); },
+        [&](const Piece&, const Span&, int, int key, int tile) {
+          const int stage = key % L::STAGES, place = key % kS;
+          if (!wait(L::kKFull + stage, (uint32_t)(key / L::STAGES) & 1u)) return false;
+          if (key >= kS && !wait(L::kSFree + place, (uint32_t)(key / kS - 1) & 1u)) return false;
+          tc_fence_after();
+          const uint32_t q = sdesc_lo(smem + L::Q + (uint32_t)__shfl_sync(0xffffffffu, tile % kQStages, 0) * 2u * L::TILE);
+          const uint32_t kd = sdesc_lo(smem + L::K + (uint32_t)__shfl_sync(0xffffffffu, stage, 0) * L::TILE);
+          const uint32_t d = tmem + 128u * (uint32_t)__shfl_sync(0xffffffffu, place, 0);
+          // The low halves first: each product truncates its sum, which is still small for them.
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) {
+            const int s = i % (D / 16);
+            const uint32_t off = ((uint32_t)(s / 4) * L::PANEL + (uint32_t)(s % 4) * 32u) >> 4;
+            const uint32_t qi = q + off + (i < D / 16 ? L::TILE >> 4 : 0u), ki = kd + off;
+            mma_ss(d, SUM ? ki : qi, SUM ? qi : ki, kSdescHi128, L::IDESC, i > 0 ? 1u : 0u, leader);
+          }
+          commit(L::kKEmpty + stage);
+          if (leader) mbar_arrive(bar(L::kSFull + place));
+          commit(L::kSFull + place);
+          return true;
+        },
+        [&](const Piece&, const Span&, int tile) {
+          commit(L::kQEmpty + tile % kQStages);
+          return true;
+        },
+        nothing);
+    if (!ok && leader) give_up();
+    commit(L::kDrain);  // every MMA done before tensor and shared memory are given back
+    mbar_wait(bar(L::kDrain), 0u, kDrainNs, nullptr);
+  }
+
+  // ---------------------------------------------------------------- epilogue
+  // The 128 scores of a thread's lane, 32 at a time, the load of some beside the work on those before.
+  template <class Take>
+  __device__ void over_chunks(uint32_t ts, Take take) const {
+    uint32_t v[2][32];
+    tmem_ld_32x32_begin(ts, v[0]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      tmem_ld_wait(v[c & 1]);
+      if (c < 3) tmem_ld_32x32_begin(ts + 32u * (c + 1), v[(c + 1) & 1]);
+      take(c, v[c & 1]);
+    }
+  }
+  __device__ void epilogue() const {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, set = (warp - 4) >> 2;
+    const int own = 32 * (warp & 3) + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+    bool ok;
+    if constexpr (!SUM) {
+      float m = -INFINITY, l = 0.f, scale = 0.f;
+      int lo = 0, hi = 0;
+      ok = walk(
+          nothing,
+          [&](const Piece& x, const Span& y, int) {
+            m = -INFINITY, l = 0.f, scale = 0.f, lo = hi = 0;
+            if (own < y.rows) {
+              scale = a.rows[(int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0 + own].x;
+              row_keys({x.row0, x.n, x.len, x.pos0}, a.w.window, (y.r0 + own) / a.w.group, lo, hi);
+            }
+            return true;
+          },
+          [&](const Piece& x, const Span& y, int kt, int key, int) {
+            if (((kt - x.t0) & 1) != set) return true;
+            const int place = key % kS, j0 = kt * kTile;
+            if (!wait(L::kSFull + place, (uint32_t)(key / kS) & 1u)) return false;
+            tc_fence_after();
+            const uint32_t note = smem + L::GONE + 16u * (key % kNotes);
+            const uint4 gone = ld_shared16(note);
+            const bool edge = j0 < y.all_lo || j0 + kTile > y.all_hi || (gone.x | gone.y | gone.z | gone.w) != 0;
+            over_chunks(lanes + 128u * place, [&](int c, uint32_t (&r)[32]) {
+              float s[32];
+#pragma unroll
+              for (int k = 0; k < 32; ++k) s[k] = __uint_as_float(r[k]) * scale;
+              if constexpr (I8) {
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                  const uint4 w = ld_shared16(smem + L::SCALE + 4u * (key % kNotes * kTile + 32 * c + k));
+                  s[k] *= __uint_as_float(w.x), s[k + 1] *= __uint_as_float(w.y);
+                  s[k + 2] *= __uint_as_float(w.z), s[k + 3] *= __uint_as_float(w.w);
+                }
+              }
+              if (edge) {
+                const uint32_t g = c == 0 ? gone.x : (c == 1 ? gone.y : (c == 2 ? gone.z : gone.w));
+                const int from = lo - j0 - 32 * c, to = hi - j0 - 32 * c;
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                  if (k < from || k >= to || (g >> k & 1u)) s[k] = -INFINITY;
+              }
+              float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+              for (int k = 4; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], s[k]);
+              const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+              if (t > m) {
+                l *= exp2_approx(m - t);
+                m = t;
+              }
+              const float base = m == -INFINITY ? 0.f : m;
+              float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int k = 0; k < 32; ++k) sum[k & 3] += exp2_approx(s[k] - base);
+              l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            });
+            tc_fence_before();
+            arrive(L::kSFree + place);
+            return true;
+          },
+          [&](const Piece& x, const Span& y, int tile) {
+            arrive(L::kQEmpty + tile % kQStages);
+            if (own < y.rows) {
+              const int64_t row = (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0 + own;
+              a.parts[(row * a.splits + x.split) * 2 + set] = make_float2(m, l);
+            }
+            return true;
+          },
+          nothing);
+    } else {
+      constexpr int OWN = kMostTiles / 2;  // key tiles of a group
+      float sum[OWN], scale[OWN];
+      int slot[OWN];  // of the thread's key of each, -1 where there is none
+      ok = walk(
+          [&](const Piece& x) {
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) {
+              const int kt = x.t0 + set + 2 * i, j = kt * kTile + own;
+              sum[i] = 0.f, scale[i] = 1.f, slot[i] = -1;
+              if (kt >= x.t1 || j >= x.len) continue;
+              const int page = paged_page(a.w.cache, a.w.batch, x.b, j);
+              if (page < 0) continue;
+              slot[i] = (int)paged_slot(a.w.cache, page, x.h, j);
+              if constexpr (I8) scale[i] = __ldg(a.w.cache.k_scale + slot[i]);
+            }
+            return true;
+          },
+          [&](const Piece&, const Span&, int tile) {
+            return wait(L::kQFull + tile % kQStages, (uint32_t)(tile / kQStages) & 1u);
+          },
+          [&](const Piece& x, const Span& y, int kt, int key, int tile) {
+            if (((kt - x.t0) & 1) != set) return true;
+            const int place = key % kS, j0 = kt * kTile, which = (kt - x.t0) >> 1;
+            if (!wait(L::kSFull + place, (uint32_t)(key / kS) & 1u)) return false;
+            tc_fence_after();
+            const bool edge = j0 < y.all_lo || j0 + kTile > y.all_hi || y.rows < kTile;
+            int from = 0, to = kTile;  // columns that see the thread's key
+            if (edge) {
+              const int64_t i0 = max((int64_t)0, (int64_t)j0 + own - x.pos0);
+              const int64_t i1 =
+                  a.w.window == INT32_MAX ? x.n : min((int64_t)x.n, (int64_t)j0 + own - x.pos0 + a.w.window);
+              from = (int)min((int64_t)kTile, max((int64_t)0, i0 * a.w.group - y.r0));
+              to = (int)min((int64_t)kTile, max((int64_t)0, i1 * a.w.group - y.r0));
+            }
+            float ks = 1.f;
+            if constexpr (I8) {
+#pragma unroll
+              for (int i = 0; i < OWN; ++i) ks = i == which ? scale[i] : ks;
+            }
+            const uint32_t col = smem + L::COL + 8u * (tile % kQStages * kTile);
+            float p[4] = {0.f, 0.f, 0.f, 0.f};
+            over_chunks(lanes + 128u * place, [&](int c, uint32_t (&r)[32]) {
+#pragma unroll
+              for (int k = 0; k < 32; k += 2) {
+                const uint4 w = ld_shared16(col + 8u * (32 * c + k));  // scale and lse of two rows
+                float s0 = __uint_as_float(r[k]), s1 = __uint_as_float(r[k + 1]);
+                if constexpr (I8) s0 *= ks, s1 *= ks;
+                float p0 = exp2_approx(fmaf(s0, __uint_as_float(w.x), -__uint_as_float(w.y)));
+                float p1 = exp2_approx(fmaf(s1, __uint_as_float(w.z), -__uint_as_float(w.w)));
+                if (edge) {
+                  p0 = 32 * c + k >= from && 32 * c + k < to ? p0 : 0.f;
+                  p1 = 32 * c + k + 1 >= from && 32 * c + k + 1 < to ? p1 : 0.f;
+                }
+                p[k & 3] += p0;
+                p[(k + 1) & 3] += p1;
+              }
+            });
+            tc_fence_before();
+            arrive(L::kSFree + place);
+            const float all = (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) sum[i] += i == which ? all : 0.f;
+            return true;
+          },
+          [&](const Piece&, const Span&, int tile) {
+            arrive(L::kQEmpty + tile % kQStages);
+            return true;
+          },
+          [&](const Piece& x) {
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) {
+              if (slot[i] < 0) continue;
+              float* score = a.w.score + slot[i];
+              const int j = (x.t0 + set + 2 * i) * kTile + own;
+              *score = (j < x.pos0 ? *score * a.w.decay : 0.f) + sum[i];
+            }
+            return true;
+          });
+    }
+    if (!ok && lane == 0) give_up();
+  }
+};
+
+template <int D, bool I8, bool SUM>
+__global__ void __launch_bounds__(I8 ? kThreadsI8 : kThreads, 1)
+weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtensorMap map_hi,
+                const __grid_constant__ CUtensorMap map_lo, const __grid_constant__ CUtensorMap map_k) {
+  using L = Layout<D, I8>;
+  extern __shared__ __align__(1024) uint8_t base[];
+  const uint32_t smem = smem_u32(base);
+  volatile int* abort = reinterpret_cast<volatile int*>(base + L::MISC);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base + L::MISC + 8);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
+  if (smem & 1023u) {  // the swizzled tiles need it; never taken where the declared alignment holds
+    if (threadIdx.x == 0) atomicOr(a.w.batch.status, kStatusTimeout);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    auto init = [&](int i, int count) { mbar_init(smem + L::BARS + 8u * i, count); };
+    for (int s = 0; s < L::STAGES; ++s) {
+      init(L::kKFull + s, I8 ? 4 : 1);
+      init(L::kKEmpty + s, 1);
+    }
+    for (int s = 0; s < kQStages; ++s) {
+      init(L::kQFull + s, SUM ? 2 : 1);
+      init(L::kQEmpty + s, 1 + kEpilogue);
+    }
+    for (int s = 0; s < kS; ++s) {
+      init(L::kSFull + s, 2);  // the products, and the issuer for what it has seen of the key tile's notes
+      init(L::kSFree + s, 4);
+    }
+    // issuer, loader, epilogue and, where they work, warp 2 and the widening warps
+    const int readers = 2 + kEpilogue + (SUM ? 1 : 0) + (I8 ? 8 : 0);
+    for (int s = 0; s < kPieces; ++s) {
+      init(L::kPieceFull + s, 1);
+      init(L::kPieceFree + s, readers);
+    }
+    init(L::kDrain, 1);
+    *abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async_smem();
+  }
+  if (warp == 0) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();
+  pdl_trigger();
+  const Kernel<D, I8, SUM> k{a, map_hi, map_lo, map_k, smem, __shfl_sync(0xffffffffu, *tmem_slot, 0), abort,
+                             reinterpret_cast<Piece*>(base + L::PIECES)};
+  if (warp == 0) k.issuer();
+  else if (warp == 1) k.loader();
+  else if (SUM && warp == 2) k.columns();
+  else if (warp >= 4 && warp < 4 + kEpilogue) k.epilogue();
+  else if (I8 && warp >= 4 + kEpilogue) k.widen();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(k.tmem, kTmemCols);
+  }
+}
+
+// Between the passes, a thread a row: its lse, of rows that see nothing one that leaves nothing.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads) weigh_join_rows_kernel(const __grid_constant__ TcArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t row = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
+  if (row >= a.total * a.w.cache.heads) return;
+  const int64_t token = row % a.total / a.w.group;
+  int b = 0, end = a.w.batch.seqs;  // the last sequence that begins at or before the token
+  while (end - b > 1) {
+    const int mid = (b + end) >> 1;
+    if (__ldg(a.w.batch.row_start + mid) <= token) b = mid;
+    else end = mid;
+  }
+  const PagedSeq s = paged_seq(a.w.batch, a.w.cache.page_shift, b);
+  const int64_t i = token - s.row0;
+  int lo = 0, hi = 0;
+  if (i >= 0 && i < s.n) row_keys(s, a.w.window, (int)i, lo, hi);
+  float m = -INFINITY, l = 0.f;
+  if (lo < hi) {
+    const int keys = a.plan->range * kTile;
+    for (int split = lo / keys; split <= (hi - 1) / keys; ++split) {
+      const float4 v = *reinterpret_cast<const float4*>(a.parts + (row * a.splits + split) * 2);
+      const float top = fmaxf(fmaxf(m, v.x), v.z), base = top == -INFINITY ? 0.f : top;
+      l = l * exp2_approx(m - base) + (v.y * exp2_approx(v.x - base) + v.w * exp2_approx(v.z - base));
+      m = top;
+    }
+  }
+  a.rows[row].y = l == 0.f ? INFINITY : m + log2f(l);
+}
+
+int splits_of(const PagedCache& c, const PagedBatch& b) {
+  const int64_t tiles = ceil_div(b.max_pages << c.page_shift, kTile);
+  return (int)std::max<int64_t>(8, ceil_div(tiles, kMostRange));
+}
+struct Sizes {
+  size_t q, rows, parts, plan;
+};
+Sizes sizes_of(const PagedCache& c, const PagedBatch& b, int64_t q_heads, int head_dim) {
+  const int64_t rows = b.rows * q_heads;
+  return {(size_t)rows * head_dim * 2, (size_t)round_up(rows * sizeof(float2), 16),
+          (size_t)rows * splits_of(c, b) * 2 * sizeof(float2),
+          (size_t)round_up(sizeof(WeighPlan) + (int64_t)b.seqs * 2 * sizeof(int64_t), 16)};
+}
+
+template <int D, bool I8, bool SUM>
+spl_status launch_pass(const TcArgs& a, const CUtensorMap (&maps)[3], int blocks, cudaStream_t stream) {
+  constexpr uint32_t smem = Layout<D, I8>::SMEM;
+  static bool done[kMaxDevices] = {false};
+  if (!allow_shared(reinterpret_cast<const void*>(weigh_tc_kernel<D, I8, SUM>), smem, done)) return SPL_ECUDA;
+  return launch_pdl(weigh_tc_kernel<D, I8, SUM>, dim3(blocks), dim3(I8 ? kThreadsI8 : kThreads), smem, stream, a, maps[0],
+                    maps[1], maps[2]);
+}
+
+template <int D, bool I8>
+spl_status launch(const TcArgs& a, int blocks, cudaStream_t stream) {
+  const WeighCall& w = a.w;
+  CUtensorMap maps[3] = {};
+  const int64_t rows = a.total * w.cache.heads, slots = (int64_t)w.cache.pages * w.cache.heads << w.cache.page_shift;
+  if (!tma_panel_map(&maps[0], a.q_hi, rows, D, kTile) || !tma_panel_map(&maps[1], a.q_lo, rows, D, kTile)) return SPL_ECUDA;
+  if (!I8 && !tma_panel_map(&maps[2], w.cache.k, slots, D, std::min(kTile, 1 << w.cache.page_shift))) return SPL_ECUDA;
+  const int64_t warps = ceil_div(rows * (D / 4), 32);
+  const unsigned prep = 1 + (unsigned)std::min<int64_t>(ceil_div(warps, kPrepThreads / 32), 8 * blocks);
+  weigh_prepare_kernel<D><<<prep, kPrepThreads, 0, stream>>>(a, blocks);
+  spl_status st = launch_status();
+  if (st != SPL_OK) return st;
+  if ((st = launch_pass<D, I8, false>(a, maps, blocks, stream)) != SPL_OK) return st;
+  st = launch_pdl(weigh_join_rows_kernel, dim3((unsigned)ceil_div(rows, kJoinThreads)), dim3(kJoinThreads), 0, stream, a);
+  if (st != SPL_OK) return st;
+  return launch_pass<D, I8, true>(a, maps, blocks, stream);
+}
+
+}  // namespace
+
+size_t weigh_tc_bytes(const PagedCache& c, const PagedBatch& b, int64_t q_heads, int head_dim) {
+  const Sizes s = sizes_of(c, b, q_heads, head_dim);
+  return 2 * s.q + s.rows + s.parts + s.plan;
+}
+
+spl_status run_weigh_tc(const WeighCall& w, int head_dim, bool i8, cudaStream_t stream) {
+  const Sizes s = sizes_of(w.cache, w.batch, w.q_heads, head_dim);
+  TcArgs a = {};
+  a.w = w;
+  char* at = static_cast<char*>(w.workspace);
+  a.q_hi = reinterpret_cast<uint16_t*>(at);
+  a.q_lo = reinterpret_cast<uint16_t*>(at + s.q);
+  a.parts = reinterpret_cast<float2*>(at + 2 * s.q);
+  a.rows = reinterpret_cast<float2*>(at + 2 * s.q + s.parts);
+  a.plan = reinterpret_cast<WeighPlan*>(at + 2 * s.q + s.parts + s.rows);
+  a.first[0] = reinterpret_cast<int64_t*>(a.plan + 1);
+  a.first[1] = a.first[0] + w.batch.seqs;
+  a.splits = splits_of(w.cache, w.batch);
+  a.total = w.batch.rows * w.group;
+  const int blocks = device_sm_count();
+  if (head_dim == 128) return i8 ? launch<128, true>(a, blocks, stream) : launch<128, false>(a, blocks, stream);
+  return i8 ? launch<64, true>(a, blocks, stream) : launch<64, false>(a, blocks, stream);
+}
+
+}  // namespace spl
