@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
 // and of the tokens (into other pages only); blockIdx.y: key head; blockIdx.z: sequence.
 constexpr int kMoveThreads = 256;
 template <int ROW, int W>  // bytes of a vector
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArgs a, int shares) {
+__global__ void __launch_bounds__(kMoveThreads, 5) evict_move_kernel(const EvictArgs a, int shares) {
   constexpr int SLICES = ROW / W;
   const int part = blockIdx.x / shares, share = blockIdx.x % shares, h = blockIdx.y, b = blockIdx.z;
   const int moves = a.plan[kPlan * b], len = a.plan[kPlan * b + 1], before = a.plan[kPlan * b + 2];
@@ -164,22 +164,22 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArg
   const bool over = before > a.keep;  // (else all of them move, to the same positions elsewhere)
   const int* list = a.list + ((int64_t)b * a.cache.heads + h) * a.chosen;
   auto source = [&](int i) { return !over ? i : (i < want ? __ldg(list + i) : before - a.keep + i); };
-  auto slot_of = [&](const int* table, int pos) -> int64_t {
+  auto slot_of = [&](const int* table, int pos) -> int {  // (a pool has fewer than 2^31)
     const int page = __ldg(table + b * a.batch.max_pages + (pos >> a.cache.page_shift));
     if ((unsigned)page >= (unsigned)a.cache.pages) {
       atomicOr(a.batch.status, kStatusIndex);
       return -1;
     }
-    return paged_slot(a.cache, page, h, pos);
+    return (int)paged_slot(a.cache, page, h, pos);
   };
   const int* to_table = a.out_table ? a.out_table : a.batch.table;
   const int first = (int)((int64_t)moves * share / shares), last = (int)((int64_t)moves * (share + 1) / shares);
   if (part < 2 * SLICES) {
-    constexpr int LANES = W / 16, ROWS = kMoveThreads / LANES, U = 8;
+    constexpr int LANES = W / 16, ROWS = kMoveThreads / LANES, U = 4;
     char* base = static_cast<char*>(part < SLICES ? a.cache.k : a.cache.v) + part % SLICES * W + threadIdx.x % LANES * 16;
     const int row = threadIdx.x / LANES;
     for (int i0 = first; i0 < last; i0 += ROWS * U) {
-      int64_t from[U], to[U];
+      int from[U], to[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int i = i0 + u * ROWS + row;
@@ -193,16 +193,16 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictArg
       uint4 v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (from[u] >= 0 && to[u] >= 0) v[u] = *reinterpret_cast<const uint4*>(base + from[u] * ROW);
+        if (from[u] >= 0 && to[u] >= 0) v[u] = *reinterpret_cast<const uint4*>(base + (int64_t)from[u] * ROW);
       if (!a.out_table) __syncthreads();
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (from[u] >= 0 && to[u] >= 0) *reinterpret_cast<uint4*>(base + to[u] * ROW) = v[u];
+        if (from[u] >= 0 && to[u] >= 0) *reinterpret_cast<uint4*>(base + (int64_t)to[u] * ROW) = v[u];
     }
   } else {
     constexpr int U = 4;
     for (int i0 = first; i0 < last; i0 += kMoveThreads * U) {
-      int64_t from[U], to[U];
+      int from[U], to[U];
       float v[U], k[U], w[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {

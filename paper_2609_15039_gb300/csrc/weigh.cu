@@ -3,7 +3,7 @@
 // Few rows a sequence and key head (decode, drafts), bound by reading the keys once.  One kernel makes the scores
 // s = scale log2(e) q . k of tiles of 8 rows on mma.m16n8k16 (the 8 rows' high and low halves are the 16 rows of A; the
 // stored values are exact in binary16, so the result has fp32 accuracy) and writes them to the workspace, with the largest
-// and the total of 2^(s - largest) of every 32 keys and row.  One joins those by rows, and one sums 2^(s - m) / l over the
+// and the total of 2^(s - largest) of every 32 keys and row.  Another joins those by rows and sums 2^(s - m) / l over the
 // rows for each key: a score is 4 bytes beside the 2 D of its key.
 
 #include <algorithm>
@@ -30,7 +30,6 @@ struct WeighArgs {
   int64_t cap;         // keys that a row has places for, a multiple of kUnit
   float* s;            // [rows][q_heads][cap]
   float2* parts;       // [rows][q_heads][cap / kPart]: largest, total
-  float2* stats;       // [rows][q_heads]: maximum, 1 / total
 };
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1) {
@@ -248,62 +247,101 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_scores_kernel(const __grid_
   }
 }
 
-// A warp a row and query head: its maximum and 1 / total over the keys that it sees.
-constexpr int kJoinThreads = 256;
-__global__ void __launch_bounds__(kJoinThreads) weigh_join_kernel(const __grid_constant__ WeighArgs w) {
-  pdl_wait();
-  const int64_t row = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  const int64_t token = row / w.q_heads;
-  if (token >= w.attn.batch.rows) return;
-  const int b = paged_find(w.attn.batch.row_start, w.attn.batch.seqs, token);
-  const PagedSeq s = paged_seq(w.attn.batch, w.attn.cache.page_shift, b);
-  const int64_t i = token - s.row0;
-  int lo = 0, hi = 0;
-  if (i >= 0 && i < s.n) row_keys(s, w.attn.window, (int)i, lo, hi);
-  const float2* parts = w.parts + row * (w.cap / kPart);
-  float m = -INFINITY, l = 0.f;
-  for (int p = lo / kPart + lane; p * kPart < hi; p += 32) {
-    const float2 v = parts[p];
-    const float top = fmaxf(m, v.x);
-    const float base = top == -INFINITY ? 0.f : top;
-    l = l * exp2_approx(m - base) + v.y * exp2_approx(v.x - base);
-    m = top;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float om = __shfl_xor_sync(0xffffffffu, m, o), ol = __shfl_xor_sync(0xffffffffu, l, o);
-    const float top = fmaxf(m, om), base = top == -INFINITY ? 0.f : top;
-    l = l * exp2_approx(m - base) + ol * exp2_approx(om - base);
-    m = top;
-  }
-  if (lane == 0) w.stats[row] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
-}
-
-// A thread a key of a (sequence, key head): the rows' weights in their order.  blockIdx: keys, key head, sequence.
-constexpr int kSumThreads = 256;
+// A block has kSumKeys keys of a (sequence, key head): first the rows' maxima and totals, a warp a row, from what the scores'
+// kernel left of every 32 keys, then the rows' weights in their order, a thread four neighbouring keys at a time.
+// blockIdx: keys, key head, sequence.
+constexpr int kSumThreads = 256, kSumKeys = 2048, kSumRows = 64;
 __global__ void __launch_bounds__(kSumThreads) weigh_sum_kernel(const __grid_constant__ WeighArgs w) {
-  pdl_wait();
+  __shared__ float2 stats[kSumRows];  // maximum, 1 / total
   const AttnArgs& a = w.attn;
-  const int h = blockIdx.y, b = blockIdx.z;
+  const int h = blockIdx.y, b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (what the scores' kernel does not write may be read before it ends)
   const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
-  for (int64_t j = (int64_t)blockIdx.x * kSumThreads + threadIdx.x; j < s.len; j += (int64_t)gridDim.x * kSumThreads) {
-    const int page = paged_page(a.cache, a.batch, b, (int)j);
-    if (page < 0) continue;
-    float* score = w.score + paged_slot(a.cache, page, h, (int)j);
-    float sum = 0.f;
-    // the rows that see key j: from its own position on, as far as the window
-    const int first = (int)max((int64_t)0, j - s.pos0);
-    const int last = a.window == INT32_MAX ? s.n : (int)min((int64_t)s.n, j - s.pos0 + a.window);
-    for (int i = first; i < last; ++i) {
-      const int64_t row = (s.row0 + i) * (int64_t)w.q_heads + h * a.group;
-      for (int g = 0; g < a.group; ++g) {
-        const float2 stat = __ldg(w.stats + row + g);
-        sum += exp2_approx(w.s[(row + g) * w.cap + j] - stat.x) * stat.y;
+  const int64_t rows = (int64_t)s.n * a.group;
+  constexpr int PER = kSumKeys / (4 * kSumThreads);
+  for (int64_t k0 = (int64_t)blockIdx.x * kSumKeys; k0 < s.len; k0 += (int64_t)gridDim.x * kSumKeys) {
+    float* score[PER];
+    float4 sum[PER], before[PER];
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
+      score[u] = nullptr;
+      sum[u] = before[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (j >= s.len) continue;
+      const int page = paged_page(a.cache, a.batch, b, (int)j);
+      if (page >= 0) score[u] = w.score + paged_slot(a.cache, page, h, (int)j);  // (four keys lie in one page)
+    }
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
+      if (!score[u]) continue;
+      if (j < s.pos0) before[u].x = score[u][0];
+      if (j + 1 < s.pos0) before[u].y = score[u][1];
+      if (j + 2 < s.pos0) before[u].z = score[u][2];
+      if (j + 3 < s.pos0) before[u].w = score[u][3];
+    }
+    pdl_wait();
+    for (int64_t r0 = 0; r0 < rows; r0 += kSumRows) {
+      const int some = (int)min((int64_t)kSumRows, rows - r0);
+      // row r of the key head: query head r % group of token r / group
+      auto row_of = [&](int64_t r) { return (s.row0 + r / a.group) * w.q_heads + h * a.group + r % a.group; };
+      __syncthreads();
+      for (int r = warp; r < some; r += kSumThreads / 32) {
+        int lo, hi;
+        row_keys(s, a.window, (int)((r0 + r) / a.group), lo, hi);
+        const float2* parts = w.parts + row_of(r0 + r) * (w.cap / kPart);
+        float m = -INFINITY, l = 0.f;
+        for (int p0 = lo / kPart; p0 * kPart < hi; p0 += 4 * 32) {
+          float2 v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int p = p0 + 32 * k + lane;
+            v[k] = p * kPart < hi ? parts[p] : make_float2(-INFINITY, 0.f);
+          }
+          const float top = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), m), base = top == -INFINITY ? 0.f : top;
+          l *= exp2_approx(m - base);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) l += v[k].y * exp2_approx(v[k].x - base);
+          m = top;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const float om = __shfl_xor_sync(0xffffffffu, m, o), ol = __shfl_xor_sync(0xffffffffu, l, o);
+          const float top = fmaxf(m, om), base = top == -INFINITY ? 0.f : top;
+          l = l * exp2_approx(m - base) + ol * exp2_approx(om - base);
+          m = top;
+        }
+        if (lane == 0) stats[r] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
+        if (!score[u]) continue;
+        const float* at = w.s + j;
+#pragma unroll 4
+        for (int r = 0; r < some; ++r) {
+          int lo, hi;
+          row_keys(s, a.window, (int)((r0 + r) / a.group), lo, hi);
+          if (j + 3 < lo || j >= hi) continue;
+          const float4 v = *reinterpret_cast<const float4*>(at + row_of(r0 + r) * w.cap);
+          const float2 st = stats[r];
+          sum[u].x += j >= lo ? exp2_approx(v.x - st.x) * st.y : 0.f;
+          sum[u].y += j + 1 >= lo && j + 1 < hi ? exp2_approx(v.y - st.x) * st.y : 0.f;
+          sum[u].z += j + 2 >= lo && j + 2 < hi ? exp2_approx(v.z - st.x) * st.y : 0.f;
+          sum[u].w += j + 3 < hi ? exp2_approx(v.w - st.x) * st.y : 0.f;
+        }
       }
     }
-    const float before = j < s.pos0 ? *score * w.decay : 0.f;
-    *score = before + sum;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
+      if (!score[u]) continue;
+      score[u][0] = before[u].x * w.decay + sum[u].x;
+      if (j + 1 < s.len) score[u][1] = before[u].y * w.decay + sum[u].y;
+      if (j + 2 < s.len) score[u][2] = before[u].z * w.decay + sum[u].z;
+      if (j + 3 < s.len) score[u][3] = before[u].w * w.decay + sum[u].w;
+    }
   }
 }
 
@@ -321,7 +359,7 @@ constexpr int64_t kFewRows = 16, kMostScores = int64_t(1) << 31;
 struct Shape {
   bool few;
   int64_t cap;
-  size_t s, parts, stats, bytes;
+  size_t s, parts, bytes;
 };
 Shape shape_of(const PagedCache& c, const PagedBatch& b, const spl_kv_batch* batch, int64_t q_heads, int head_dim) {
   Shape x;
@@ -334,8 +372,7 @@ Shape shape_of(const PagedCache& c, const PagedBatch& b, const spl_kv_batch* bat
   x.cap = round_up(std::max<int64_t>(1, b.max_pages << c.page_shift), kUnit);
   x.s = (size_t)b.rows * q_heads * x.cap * sizeof(float);
   x.parts = x.s / kPart * 2;
-  x.stats = round_up((int64_t)(b.rows * q_heads * sizeof(float2)), 16);
-  x.bytes = x.s + x.parts + x.stats;
+  x.bytes = x.s + x.parts;
   return x;
 }
 
@@ -403,17 +440,15 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   char* at = static_cast<char*>(workspace);
   w.s = reinterpret_cast<float*>(at);
   w.parts = reinterpret_cast<float2*>(at + s.s);
-  w.stats = reinterpret_cast<float2*>(at + s.s + s.parts);
   const int sms = device_sm_count();
   if (rows > 0) {
     st = cache->head_dim == 128 ? (i8 ? launch_scores<128, true>(w, sms, stream) : launch_scores<128, false>(w, sms, stream))
                                 : (i8 ? launch_scores<64, true>(w, sms, stream) : launch_scores<64, false>(w, sms, stream));
     if (st != SPL_OK) return st;
-    const int64_t blocks = ceil_div(rows * q_heads, kJoinThreads / 32);
-    st = launch_pdl(weigh_join_kernel, dim3((unsigned)blocks), dim3(kJoinThreads), 0, stream, w);
-    if (st != SPL_OK) return st;
   }
   const int64_t room = a.batch.max_pages << a.cache.page_shift;
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(room, kSumThreads), 1 << 16), a.cache.heads, a.batch.seqs);
-  return launch_pdl(weigh_sum_kernel, grid, dim3(kSumThreads), 0, stream, w);
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(room, kSumKeys), 1 << 16), a.cache.heads, a.batch.seqs);
+  if (rows > 0) return launch_pdl(weigh_sum_kernel, grid, dim3(kSumThreads), 0, stream, w);
+  weigh_sum_kernel<<<grid, kSumThreads, 0, stream>>>(w);  // (what is before it may have written the scores)
+  return launch_status();
 }

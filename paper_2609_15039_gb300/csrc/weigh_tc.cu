@@ -73,30 +73,35 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
   const WeighCall& w = a.w;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seqs = w.batch.seqs;
   if (blockIdx.x == 0) {
-    constexpr int kRanges = 5, kSplits = 4;  // 16, 8, 4, 2, 1 and 8, 4, 2, 1
-    __shared__ unsigned long long sums[kRanges + kSplits], scan[2][kPrepThreads];
+    __shared__ unsigned long long sums[kMostRange + kMostTiles], scan[2][kPrepThreads];  // pieces of a head, by their length
     __shared__ int longest, chosen[2];
-    if (threadIdx.x < kRanges + kSplits) sums[threadIdx.x] = 0;
+    if (threadIdx.x < kMostRange + kMostTiles) sums[threadIdx.x] = 0;
     if (threadIdx.x == 0) longest = 0;
     __syncthreads();
     for (int b = threadIdx.x; b < seqs; b += kPrepThreads) {
       const PagedSeq s = paged_seq(w.batch, w.cache.page_shift, b);
-      const int64_t kt = (s.len + kTile - 1) / kTile, rt = ((int64_t)s.n * w.group + kTile - 1) / kTile;
-      for (int i = 0; i < kRanges; ++i) atomicAdd(sums + i, (unsigned long long)(rt * ((kt + (16 >> i) - 1) / (16 >> i))));
-      for (int i = 0; i < kSplits; ++i)
-        atomicAdd(sums + kRanges + i, (unsigned long long)((kt + (8 >> i) - 1) / (8 >> i)));
-      atomicMax(&longest, (int)kt);
+      const int kt = (s.len + kTile - 1) / kTile;
+      const int64_t rt = ((int64_t)s.n * w.group + kTile - 1) / kTile;
+      for (int i = 0; i < kMostRange; ++i) atomicAdd(sums + i, (unsigned long long)(rt * ((kt + i) / (i + 1))));
+      for (int i = 0; i < kMostTiles; ++i) atomicAdd(sums + kMostRange + i, (unsigned long long)((kt + i) / (i + 1)));
+      atomicMax(&longest, kt);
     }
     __syncthreads();
-    if (threadIdx.x == 0) {  // the longest pieces of which every block has some
-      int i = 0, k = 0;
-      while (i + 1 < kRanges && sums[i] * w.cache.heads < 4ull * grid && (longest + (16 >> (i + 1)) - 1) / (16 >> (i + 1)) <= a.splits) ++i;
-      while (k + 1 < kSplits && sums[kRanges + k] * w.cache.heads < 3ull * grid) ++k;
-      chosen[0] = 16 >> i;
-      chosen[1] = 8 >> k;
-      *a.plan = {chosen[0], chosen[1], {(int64_t)sums[i] * w.cache.heads, (int64_t)sums[kRanges + k] * w.cache.heads}};
+    if (threadIdx.x < 64) {  // the length that gives the fewest key tiles to any block; beginning a piece costs some too
+      const int pass = threadIdx.x >> 5, n = lane + 1, most = pass == 0 ? kMostRange : kMostTiles;
+      unsigned long long cost = ~0ull;
+      if (n <= most && (pass == 1 || (longest + n - 1) / n <= a.splits)) {
+        const unsigned long long pieces = sums[pass * kMostRange + lane] * w.cache.heads;
+        cost = (pieces + grid - 1) / grid * (n + (pass == 0 ? 2 : 1)) * 32 + (31 - lane);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) cost = min(cost, __shfl_xor_sync(0xffffffffu, cost, o));
+      if (lane == 0) chosen[pass] = 32 - (int)(cost & 31);  // (of equal ones the longest)
     }
     __syncthreads();
+    if (threadIdx.x == 0)
+      *a.plan = {chosen[0], chosen[1], {(int64_t)sums[chosen[0] - 1] * w.cache.heads,
+                                        (int64_t)sums[kMostRange + chosen[1] - 1] * w.cache.heads}};
     // Each sequence's first piece: sums before it, a run of sequences a thread.
     const int per = (seqs + kPrepThreads - 1) / kPrepThreads, b0 = min(seqs, per * (int)threadIdx.x), b1 = min(seqs, b0 + per);
     auto count = [&](int b, int pass) {
@@ -166,8 +171,8 @@ struct Layout {
   static constexpr uint32_t GONE = COL + (I8 ? kNotes * kTile * 4 : kQStages * kTile * 8);  // marks of keys without a page
   static constexpr uint32_t BARS = GONE + kNotes * 16;
   enum { kKFull = 0, kKEmpty = 3, kQFull = 6, kQEmpty = 8, kSFull = 10, kSFree = 14, kPieceFull = 18, kPieceFree = 22, kDrain = 26,
-         kBars = 27 };
-  static constexpr uint32_t PIECES = BARS + 8 * 28, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
+         kColFull = 27, kColEmpty = 29, kBars = 31 };
+  static constexpr uint32_t PIECES = BARS + 8 * 32, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
   static_assert(PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
   static constexpr uint32_t IDESC = make_idesc(0, 128, 128);
 };
@@ -410,7 +415,7 @@ struct Kernel {
         nothing,
         [&](const Piece& x, const Span& y, int tile) {
           const int q = tile % kQStages;
-          if (tile >= kQStages && !wait(L::kQEmpty + q, (uint32_t)(tile / kQStages - 1) & 1u)) return false;
+          if (tile >= kQStages && !wait(L::kColEmpty + q, (uint32_t)(tile / kQStages - 1) & 1u)) return false;
           const float2* rows = a.rows + (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0;
 #pragma unroll
           for (int i = lane; i < kTile; i += 32) {
@@ -418,35 +423,39 @@ struct Kernel {
             asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(smem + L::COL + 8u * (q * kTile + i)), "f"(v.x), "f"(v.y)
                          : "memory");
           }
-          arrive(L::kQFull + q);
+          arrive(L::kColFull + q);
           return true;
         },
         nothing, nothing, nothing);
     if (!ok && lane == 0) give_up();
   }
+  // The slot of key j, or the reason that it has none.
+  __device__ int slot_of(const Piece& x, int j) const {
+    const int page = page_of(x, j);
+    return page >= 0 ? (int)paged_slot(a.w.cache, page, x.h, j) : page;
+  }
   // Warps 12-19 (int8): every other key tile widened to binary16 in the MMAs' layout, a thread the same 16 dims of every
   // KEY_STEP-th key; marks of keys without a page and, in the first pass, the keys' scales.
   __device__ void widen() const {
-    constexpr int PARTS = D / 16, KEY_STEP = 128 / PARTS, PER = kTile / KEY_STEP;
+    constexpr int PARTS = D / 16, KEY_STEP = 128 / PARTS, PER = kTile / KEY_STEP, KEYS = 32 / PARTS;
+    static_assert(PER * KEYS == 32, "a warp's keys");
     const int i = threadIdx.x & 127, set = (threadIdx.x >> 7) - kThreads / 128, lane = i & 31;
-    const int part = i % PARTS, key0 = i / PARTS, c0 = (2 * part) & 7, shift = a.w.cache.page_shift;
+    const int part = i % PARTS, key0 = i / PARTS, c0 = (2 * part) & 7;
     const int8_t* codes = static_cast<const int8_t*>(a.w.cache.k);
     const bool ok = walk(
         nothing, nothing,
         [&](const Piece& x, const Span&, int kt, int key, int) {
           if ((key & 1) != set) return true;
           const int stage = key % L::STAGES;
-          auto slot_of = [&](int j) -> int64_t {
-            const int page = page_of(x, j);
-            return page >= 0 ? ((((int64_t)page * a.w.cache.heads + x.h) << shift) + (j & ((1 << shift) - 1))) : (int64_t)page;
-          };
+          // The warp's 32 keys, a lane each, and (for its scale and mark) the thread's own.
+          const int key_of_lane = lane % KEYS + KEYS * (i >> 5) + KEY_STEP * (lane / KEYS);
+          const int mine = slot_of(x, kt * kTile + key_of_lane), own = slot_of(x, kt * kTile + i);
           uint4 q[PER];
 #pragma unroll
           for (int k = 0; k < PER; ++k) {
-            const int64_t slot = slot_of(kt * kTile + key0 + KEY_STEP * k);
-            q[k] = slot >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + slot * D) + part) : make_uint4(0u, 0u, 0u, 0u);
+            const int slot = __shfl_sync(0xffffffffu, mine, k * KEYS + key0 % KEYS);
+            q[k] = slot >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + (int64_t)slot * D) + part) : make_uint4(0u, 0u, 0u, 0u);
           }
-          const int64_t own = slot_of(kt * kTile + i);
           const float scale = !SUM && own >= 0 ? __ldg(a.w.cache.k_scale + own) : 0.f;
           const unsigned gone = __ballot_sync(0xffffffffu, own == kGone);
           if (key >= L::STAGES && !wait(L::kKEmpty + stage, (uint32_t)(key / L::STAGES - 1) & 1u)) return false;
@@ -588,8 +597,7 @@ struct Kernel {
             arrive(L::kSFree + place);
             return true;
           },
-          [&](const Piece& x, const Span& y, int tile) {
-            arrive(L::kQEmpty + tile % kQStages);
+          [&](const Piece& x, const Span& y, int) {
             if (own < y.rows) {
               const int64_t row = (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0 + own;
               a.parts[(row * a.splits + x.split) * 2 + set] = make_float2(m, l);
@@ -599,24 +607,31 @@ struct Kernel {
           nothing);
     } else {
       constexpr int OWN = kMostTiles / 2;  // key tiles of a group
-      float sum[OWN], scale[OWN];
+      float sum[OWN], scale[OWN], before[OWN];
       int slot[OWN];  // of the thread's key of each, -1 where there is none
       ok = walk(
           [&](const Piece& x) {
+            const int* table = a.w.batch.table + x.b * a.w.batch.max_pages;
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) {  // (the pages first, so that the loads run side by side)
+              const int kt = x.t0 + set + 2 * i, j = kt * kTile + own;
+              sum[i] = 0.f;
+              slot[i] = kt < x.t1 && j < x.len ? __ldg(table + (j >> a.w.cache.page_shift)) : -1;
+              bad |= kt < x.t1 && j < x.len && (unsigned)slot[i] >= (unsigned)a.w.cache.pages;
+            }
+            if (bad) atomicOr(a.w.batch.status, kStatusIndex);
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-              const int kt = x.t0 + set + 2 * i, j = kt * kTile + own;
-              sum[i] = 0.f, scale[i] = 1.f, slot[i] = -1;
-              if (kt >= x.t1 || j >= x.len) continue;
-              const int page = paged_page(a.w.cache, a.w.batch, x.b, j);
-              if (page < 0) continue;
-              slot[i] = (int)paged_slot(a.w.cache, page, x.h, j);
-              if constexpr (I8) scale[i] = __ldg(a.w.cache.k_scale + slot[i]);
+              const int j = (x.t0 + set + 2 * i) * kTile + own;
+              slot[i] = (unsigned)slot[i] < (unsigned)a.w.cache.pages ? (int)paged_slot(a.w.cache, slot[i], x.h, j) : -1;
+              if constexpr (I8) scale[i] = slot[i] >= 0 ? __ldg(a.w.cache.k_scale + slot[i]) : 0.f;
+              before[i] = slot[i] >= 0 && j < x.pos0 ? a.w.score[slot[i]] : 0.f;
             }
             return true;
           },
           [&](const Piece&, const Span&, int tile) {
-            return wait(L::kQFull + tile % kQStages, (uint32_t)(tile / kQStages) & 1u);
+            return wait(L::kColFull + tile % kQStages, (uint32_t)(tile / kQStages) & 1u);
           },
           [&](const Piece& x, const Span& y, int kt, int key, int tile) {
             if (((kt - x.t0) & 1) != set) return true;
@@ -663,16 +678,14 @@ struct Kernel {
             return true;
           },
           [&](const Piece&, const Span&, int tile) {
-            arrive(L::kQEmpty + tile % kQStages);
+            arrive(L::kColEmpty + tile % kQStages);
             return true;
           },
           [&](const Piece& x) {
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-              if (slot[i] < 0) continue;
-              float* score = a.w.score + slot[i];
               const int j = (x.t0 + set + 2 * i) * kTile + own;
-              *score = (j < x.pos0 ? *score * a.w.decay : 0.f) + sum[i];
+              if (slot[i] >= 0) a.w.score[slot[i]] = (j < x.pos0 ? before[i] * a.w.decay : 0.f) + sum[i];
             }
             return true;
           });
@@ -702,8 +715,10 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
       init(L::kKEmpty + s, 1);
     }
     for (int s = 0; s < kQStages; ++s) {
-      init(L::kQFull + s, SUM ? 2 : 1);
-      init(L::kQEmpty + s, 1 + kEpilogue);
+      init(L::kQFull + s, 1);
+      init(L::kQEmpty + s, 1);
+      init(L::kColFull + s, 1);
+      init(L::kColEmpty + s, kEpilogue);
     }
     for (int s = 0; s < kS; ++s) {
       init(L::kSFull + s, 2);  // the products, and the issuer for what it has seen of the key tile's notes
