@@ -46,6 +46,7 @@ __device__ __forceinline__ uint32_t score_order(float x) {
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictArgs a) {
   extern __shared__ uint32_t held[];
   __shared__ int histogram[256], warp_sums[kSelectWarps], s_digit, s_left;
+  __shared__ uint32_t s_low, s_high;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
   const bool over = s.len > a.keep;
@@ -63,28 +64,55 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   };
   const bool all_held = early <= kHeld;
   const int kept = min(early, kHeld);
+  uint32_t low = ~0u, high = 0u;
   for (int p0 = tid; p0 < kept; p0 += 8 * kSelectThreads) {
     uint32_t v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = p0 + i * kSelectThreads < kept ? read(p0 + i * kSelectThreads) : 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (p0 + i * kSelectThreads < kept) held[p0 + i * kSelectThreads] = v[i];
+      if (p0 + i * kSelectThreads < kept) {
+        held[p0 + i * kSelectThreads] = v[i];
+        low = min(low, v[i]);
+        high = max(high, v[i]);
+      }
   }
-  // The smallest that stays, and how many equal to it do.
-  uint32_t least = 0, mask = 0;
+  if (!all_held) {
+#pragma unroll 4
+    for (int p = kHeld + tid; p < early; p += kSelectThreads) {
+      const uint32_t v = read(p);
+      low = min(low, v);
+      high = max(high, v);
+    }
+  }
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
+  if (tid == 0) s_low = ~0u, s_high = 0u;
+  __syncthreads();
+  if (lane == 0) {
+    atomicMin(&s_low, low);
+    atomicMax(&s_high, high);
+  }
+  __syncthreads();
+  low = s_low;
+  // The smallest that stays, less the smallest of all, and how many equal to it do.  Digits of the difference: those of the
+  // numbers themselves would be few in the first round (the exponents' upper bits), and the counts would wait for one another.
+  const int width = s_high > low ? 32 - __clz(s_high - low) : 0;
+  uint32_t least = 0;
   int left = want;
-  for (int shift = 24; shift >= 0; shift -= 8) {
+  for (int above = width; above > 0;) {
+    const int shift = max(0, above - 8);
+    const uint32_t digits = (1u << (above - shift)) - 1u, prefix = above < 32 ? least >> above : 0u;
     if (tid < 256) histogram[tid] = 0;
     __syncthreads();
-    for (int p = tid; p < kept; p += kSelectThreads)
-      if ((held[p] & mask) == least) atomicAdd(histogram + (held[p] >> shift & 255u), 1);
+    auto count = [&](uint32_t v) {
+      v -= low;
+      if ((above < 32 ? v >> above : 0u) == prefix) atomicAdd(histogram + (v >> shift & digits), 1);
+    };
+    for (int p = tid; p < kept; p += kSelectThreads) count(held[p]);
     if (!all_held) {
 #pragma unroll 4
-      for (int p = kHeld + tid; p < early; p += kSelectThreads) {
-        const uint32_t v = read(p);
-        if ((v & mask) == least) atomicAdd(histogram + (v >> shift & 255u), 1);
-      }
+      for (int p = kHeld + tid; p < early; p += kSelectThreads) count(read(p));
     }
     __syncthreads();
     if (warp == 0) {  // lane i: the digits from 255 - 8 i down
@@ -108,9 +136,10 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     }
     __syncthreads();
     least |= (uint32_t)s_digit << shift;
-    mask |= 255u << shift;
     left = s_left;
+    above = shift;
   }
+  least += low;
   // Those above `least`, and the first `left` equal to it, in order of their positions.
   int above0 = 0, equal0 = 0;  // in the strips before
   for (int p0 = 0; p0 < early; p0 += kStrip) {
@@ -178,26 +207,37 @@ __global__ void __launch_bounds__(kMoveThreads, 5) evict_move_kernel(const Evict
     constexpr int LANES = W / 16, ROWS = kMoveThreads / LANES, U = 4;
     char* base = static_cast<char*>(part < SLICES ? a.cache.k : a.cache.v) + part % SLICES * W + threadIdx.x % LANES * 16;
     const int row = threadIdx.x / LANES;
-    for (int i0 = first; i0 < last; i0 += ROWS * U) {
-      int from[U], to[U];
+    int from[U], to[U], next_from[U], next_to[U];
+    auto places = [&](int i0, int (&f)[U], int (&g)[U]) {  // of a trip's tokens
+      int pos[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int i = i0 + u * ROWS + row;
-        from[u] = to[u] = -1;
-        if (i >= last) continue;
-        const int pos = source(i);
-        if (pos == i && !a.out_table) continue;
-        from[u] = slot_of(a.batch.table, pos);
-        to[u] = slot_of(to_table, i);
+        f[u] = g[u] = -1;
+        pos[u] = i < last ? source(i) : i;
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * ROWS + row;
+        if (i >= last || (pos[u] == i && !a.out_table)) continue;
+        f[u] = slot_of(a.batch.table, pos[u]);
+        g[u] = slot_of(to_table, i);
+      }
+    };
+    places(first, from, to);
+    for (int i0 = first; i0 < last; i0 += ROWS * U) {
       uint4 v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (from[u] >= 0 && to[u] >= 0) v[u] = *reinterpret_cast<const uint4*>(base + (int64_t)from[u] * ROW);
+      places(i0 + ROWS * U, next_from, next_to);  // while the vectors are on their way
       if (!a.out_table) __syncthreads();
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
         if (from[u] >= 0 && to[u] >= 0) *reinterpret_cast<uint4*>(base + (int64_t)to[u] * ROW) = v[u];
+        from[u] = next_from[u];
+        to[u] = next_to[u];
+      }
     }
   } else {
     constexpr int U = 4;
@@ -242,7 +282,7 @@ spl_status launch_move(const EvictArgs& a, int blocks, cudaStream_t stream) {
   // Whole vectors' lines where there are blocks enough, 32 bytes each where a block an SM would be missing (32 sequences cut
   // from 16000 tokens to 6000: %%; one of 1250 to 1000: %%).
   const int heads = a.cache.heads, seqs = a.batch.seqs;
-  constexpr int WIDE = ROW < 128 ? ROW : 128;
+  constexpr int WIDE = ROW;
   const bool wide = (int64_t)heads * seqs * (2 * ROW / WIDE) >= blocks;
   const int parts = 2 * ROW / (wide ? WIDE : 32) + 1;
   int shares = 1;  // of a head's tokens, where their order does not matter

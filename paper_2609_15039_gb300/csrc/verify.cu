@@ -257,6 +257,7 @@ struct TreeArgs {
   unsigned int* status;
 };
 constexpr int kMostBlocks = 16;  // of a cluster
+constexpr int kHeldNodes = 2;
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -284,19 +285,32 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) verify_tree_kernel(con
   const int nodes = (int)(row1 - row0);
   const int64_t v0 = min(a.vocab, rank * per_split), v1 = min(a.vocab, v0 + per_split);
   if (threadIdx.x < 2) s_child[threadIdx.x] = INT_MAX;
+  const float* e = a.e + (int64_t)b * a.levels * a.lde;  // of the level
+  auto load_first = [&](Trip<VEC>& t, int64_t from) {
+    t.load_random(e + from, (VEC ? 4 : 1) * threadIdx.x, (int)max((int64_t)0, min(kMostEntries, v1 - from)));
+  };
+  Trip<VEC> first;
+  if (nodes > 0) load_first(first, v0);
+  // A thread's nodes, in its registers where they are few.
+  int parent[kHeldNodes], held[kHeldNodes];
+#pragma unroll
+  for (int u = 0; u < kHeldNodes; ++u) {
+    const int i = 1 + (int)threadIdx.x + u * kThreads;
+    parent[u] = i < nodes ? __ldg(a.parent + row0 + i) : -1;
+    held[u] = i < nodes ? __ldg(a.x + row0 + i) : -1;
+  }
   cluster_sync();  // every block has begun: its shared memory may be written
   int at = 0, depth = 0, token = -1;
   for (; nodes > 0; ++depth) {  // every block of the cluster makes every turn
     const float* p = a.p + (row0 + at) * a.ldp;
-    const float* e = a.e + ((int64_t)b * a.levels + depth) * a.lde;
     unsigned long long key = 0;
     bool positive = false;
     for (int64_t from = v0; from < v1; from += kMostEntries) {
-      const int some = (int)min(kMostEntries, v1 - from);
-      Trip<VEC> first;
-      first.load_random(e + from, (VEC ? 4 : 1) * threadIdx.x, some);
-      key = max(key, race_row<VEC>(p, nullptr, e, from, some, first, positive));
+      if (from > v0) load_first(first, from);
+      key = max(key, race_row<VEC>(p, nullptr, e, from, (int)min(kMostEntries, v1 - from), first, positive));
     }
+    e += a.lde;
+    if (depth + 1 < a.levels) load_first(first, v0);  // the next level's first entries do not wait for the outcome
     key = block_max(key, keys);
     key = __shfl_sync(0xffffffffu, key, 0);
     if (threadIdx.x < blocks) store_in_block(&bests[depth & 1][rank], threadIdx.x, key);
@@ -306,7 +320,12 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) verify_tree_kernel(con
     if (token < 0 || depth + 1 == a.levels) break;
     // The first child that holds it.
     int child = INT_MAX;
-    for (int i = 1 + threadIdx.x; i < nodes; i += kThreads)
+#pragma unroll
+    for (int u = 0; u < kHeldNodes; ++u) {
+      const int i = 1 + (int)threadIdx.x + u * kThreads;
+      if (i < nodes && parent[u] == at && held[u] == token) child = min(child, i);
+    }
+    for (int i = 1 + threadIdx.x + kHeldNodes * kThreads; i < nodes; i += kThreads)
       if (__ldg(a.parent + row0 + i) == at && __ldg(a.x + row0 + i) == token) child = min(child, i);
     child = __reduce_min_sync(0xffffffffu, child);
     if ((threadIdx.x & 31) == 0 && child != INT_MAX) atomicMin(&s_child[depth & 1], child);

@@ -247,12 +247,13 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_scores_kernel(const __grid_
   }
 }
 
-// A block has kSumKeys keys of a (sequence, key head): first the rows' maxima and totals, a warp a row, from what the scores'
+// A block has kSumKeys keys of a (sequence, key head): first the rows' maxima and totals, from what the scores'
 // kernel left of every 32 keys, then the rows' weights in their order, a thread four neighbouring keys at a time.
 // blockIdx: keys, key head, sequence.
 constexpr int kSumThreads = 256, kSumKeys = 2048, kSumRows = 64;
 __global__ void __launch_bounds__(kSumThreads) weigh_sum_kernel(const __grid_constant__ WeighArgs w) {
   __shared__ float2 stats[kSumRows];  // maximum, 1 / total
+  __shared__ float2 teams[kSumThreads / 32];
   const AttnArgs& a = w.attn;
   const int h = blockIdx.y, b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // (what the scores' kernel does not write may be read before it ends)
@@ -285,17 +286,19 @@ __global__ void __launch_bounds__(kSumThreads) weigh_sum_kernel(const __grid_con
       const int some = (int)min((int64_t)kSumRows, rows - r0);
       // row r of the key head: query head r % group of token r / group
       auto row_of = [&](int64_t r) { return (s.row0 + r / a.group) * w.q_heads + h * a.group + r % a.group; };
+      const int team = some > 4 ? 1 : (some > 2 ? 2 : (some > 1 ? 4 : 8));
       __syncthreads();
-      for (int r = warp; r < some; r += kSumThreads / 32) {
+      for (int q0 = 0; q0 < some * team; q0 += kSumThreads / 32) {  // `team` warps a row
+        const int r = min((q0 + warp) / team, some - 1), mate = warp % team;
         int lo, hi;
         row_keys(s, a.window, (int)((r0 + r) / a.group), lo, hi);
         const float2* parts = w.parts + row_of(r0 + r) * (w.cap / kPart);
         float m = -INFINITY, l = 0.f;
-        for (int p0 = lo / kPart; p0 * kPart < hi; p0 += 4 * 32) {
+        for (int p0 = lo / kPart + 32 * mate; p0 * kPart < hi; p0 += 4 * 32 * team) {
           float2 v[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const int p = p0 + 32 * k + lane;
+            const int p = p0 + 32 * team * k + lane;
             v[k] = p * kPart < hi ? parts[p] : make_float2(-INFINITY, 0.f);
           }
           const float top = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), m), base = top == -INFINITY ? 0.f : top;
@@ -311,9 +314,19 @@ __global__ void __launch_bounds__(kSumThreads) weigh_sum_kernel(const __grid_con
           l = l * exp2_approx(m - base) + ol * exp2_approx(om - base);
           m = top;
         }
-        if (lane == 0) stats[r] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
+        if (lane == 0) teams[warp] = make_float2(m, l);
+        __syncthreads();
+        if (lane == 0 && mate == 0 && q0 + warp < some * team) {
+          for (int k = 1; k < team; ++k) {
+            const float2 o = teams[warp + k];
+            const float top = fmaxf(m, o.x), base = top == -INFINITY ? 0.f : top;
+            l = l * exp2_approx(m - base) + o.y * exp2_approx(o.x - base);
+            m = top;
+          }
+          stats[r] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
+        }
+        __syncthreads();
       }
-      __syncthreads();
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
         const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);

@@ -12,7 +12,7 @@
 //   warp 0       MMA issuer.
 //   warp 1       hands out the block's pieces of work and loads tiles of q and (binary16) of K, by TMA, a box a page.
 //   warp 2       second pass: the rows' scales and lse.
-//   warps 4-11   two groups that take the key tiles in turn: maxima and totals, or sums.
+//   warps 4-11   two groups: maxima and totals (the key tiles in turn), or sums (half of a tile's rows each).
 //   warps 12-19  int8: two groups widen the key tiles to binary16 in turn.
 // Tensor memory: four places of S.  Every wait is bounded; on expiry the status word is raised and the block leaves with its
 // copies and MMAs done.
@@ -22,6 +22,7 @@
 
 #include <cuda_fp16.h>
 
+#include "noise.cuh"  // packed fp32 pairs
 #include "ptx.cuh"
 #include "weigh.cuh"
 
@@ -115,12 +116,19 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
       scan[pass][threadIdx.x] = own;
     }
     __syncthreads();
-    if (threadIdx.x < 2) {
-      unsigned long long sum = 0;
-      for (int i = 0; i < kPrepThreads; ++i) {
-        const unsigned long long own = scan[threadIdx.x][i];
-        scan[threadIdx.x][i] = sum;
-        sum += own;
+    if (warp < 2) {
+      unsigned long long carry = 0;
+#pragma unroll 1
+      for (int i0 = 0; i0 < kPrepThreads && i0 < seqs; i0 += 32) {  // (a thread has a sequence or more)
+        const unsigned long long own = scan[warp][i0 + lane];
+        unsigned long long v = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned long long other = __shfl_up_sync(0xffffffffu, v, o);
+          if (lane >= o) v += other;
+        }
+        scan[warp][i0 + lane] = carry + v - own;
+        carry += __shfl_sync(0xffffffffu, v, 31);
       }
     }
     __syncthreads();
@@ -166,13 +174,13 @@ struct Layout {
   static constexpr int PANELS = D / 64, STAGES = I8 ? 2 : 3;
   static constexpr uint32_t PANEL = 128 * 128, TILE = PANELS * PANEL;
   static constexpr uint32_t Q = 0, K = kQStages * 2 * TILE;  // stages of [q_hi, q_lo]; of K
-  // second pass: the rows' scales and lse of each stage of q; first pass, int8: the keys' scales
-  static constexpr uint32_t COL = K + STAGES * TILE, SCALE = COL;
-  static constexpr uint32_t GONE = COL + (I8 ? kNotes * kTile * 4 : kQStages * kTile * 8);  // marks of keys without a page
+  // second pass: the rows' scales and lse of each stage of q; int8: the keys' scales; first pass: marks of keys without a page
+  static constexpr uint32_t COL = K + STAGES * TILE, SCALE = COL + kQStages * kTile * 8;
+  static constexpr uint32_t GONE = SCALE + (I8 ? kNotes * kTile * 4 : 0);
   static constexpr uint32_t BARS = GONE + kNotes * 16;
   enum { kKFull = 0, kKEmpty = 3, kQFull = 6, kQEmpty = 8, kSFull = 10, kSFree = 14, kPieceFull = 18, kPieceFree = 22, kDrain = 26,
-         kColFull = 27, kColEmpty = 29, kBars = 31 };
-  static constexpr uint32_t PIECES = BARS + 8 * 32, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
+         kColFull = 27, kColEmpty = 29, kFirst = 31, kSecond = 32, kBars = 34 };
+  static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
   static_assert(PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
   static constexpr uint32_t IDESC = make_idesc(0, 128, 128);
 };
@@ -408,7 +416,7 @@ struct Kernel {
         mbar_wait(bar(L::kKFull + t % L::STAGES), (uint32_t)(t / L::STAGES) & 1u, kDrainNs, nullptr);
     }
   }
-  // Warp 2, second pass: scale and lse of a tile's rows; of rows that are not there an lse that leaves nothing.
+  // Warp 2, second pass: scales and -lse of a tile's rows, in pairs; of rows that are not there an lse that leaves nothing.
   __device__ void columns() const {
     const int lane = threadIdx.x & 31;
     const bool ok = walk(
@@ -418,10 +426,11 @@ struct Kernel {
           if (tile >= kQStages && !wait(L::kColEmpty + q, (uint32_t)(tile / kQStages - 1) & 1u)) return false;
           const float2* rows = a.rows + (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0;
 #pragma unroll
-          for (int i = lane; i < kTile; i += 32) {
-            const float2 v = i < y.rows ? rows[i] : make_float2(0.f, INFINITY);
-            asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(smem + L::COL + 8u * (q * kTile + i)), "f"(v.x), "f"(v.y)
-                         : "memory");
+          for (int i = lane; i < kTile / 2; i += 32) {
+            const float2 none = make_float2(0.f, INFINITY);
+            const float2 v = 2 * i < y.rows ? rows[2 * i] : none, u = 2 * i + 1 < y.rows ? rows[2 * i + 1] : none;
+            st_shared16(smem + L::COL + 16u * (q * (kTile / 2) + i),
+                        make_uint4(__float_as_uint(v.x), __float_as_uint(u.x), __float_as_uint(-v.y), __float_as_uint(-u.y)));
           }
           arrive(L::kColFull + q);
           return true;
@@ -442,41 +451,53 @@ struct Kernel {
     const int i = threadIdx.x & 127, set = (threadIdx.x >> 7) - kThreads / 128, lane = i & 31;
     const int part = i % PARTS, key0 = i / PARTS, c0 = (2 * part) & 7;
     const int8_t* codes = static_cast<const int8_t*>(a.w.cache.k);
+    // A tile's codes, on their way while the one before is widened (but not across pieces: the next one may be handed out
+    // only after what is held here has been worked on).
+    uint4 q[PER];
+    float scale = 0.f;
+    unsigned gone = 0;
+    int held = -1;  // which tile
+    auto finish = [&]() {
+      if (held < 0) return true;
+      const int stage = held % L::STAGES;
+      if (held >= L::STAGES && !wait(L::kKEmpty + stage, (uint32_t)(held / L::STAGES - 1) & 1u)) return false;
+      const uint32_t panel = smem + L::K + (uint32_t)stage * L::TILE + (uint32_t)(part >> 2) * L::PANEL;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        const int at = key0 + KEY_STEP * k;
+        const uint32_t v[4] = {q[k].x ^ 0x80808080u, q[k].y ^ 0x80808080u, q[k].z ^ 0x80808080u, q[k].w ^ 0x80808080u};
+        const uint32_t row = panel + at * 128;
+        st_shared16(row + ((c0 ^ (at & 7)) << 4), make_uint4(i8_pair(v[0], 0x4140u), i8_pair(v[0], 0x4342u),
+                                                             i8_pair(v[1], 0x4140u), i8_pair(v[1], 0x4342u)));
+        st_shared16(row + (((c0 + 1) ^ (at & 7)) << 4), make_uint4(i8_pair(v[2], 0x4140u), i8_pair(v[2], 0x4342u),
+                                                                   i8_pair(v[3], 0x4140u), i8_pair(v[3], 0x4342u)));
+      }
+      st_shared4(smem + L::SCALE + 4u * (held % kNotes * kTile + i), __float_as_uint(scale));
+      if (lane == 0) st_shared4(smem + L::GONE + 16u * (held % kNotes) + 4u * (i >> 5), gone);
+      fence_proxy_async_smem();
+      arrive(L::kKFull + stage);
+      held = -1;
+      return true;
+    };
     const bool ok = walk(
         nothing, nothing,
         [&](const Piece& x, const Span&, int kt, int key, int) {
           if ((key & 1) != set) return true;
-          const int stage = key % L::STAGES;
           // The warp's 32 keys, a lane each, and (for its scale and mark) the thread's own.
           const int key_of_lane = lane % KEYS + KEYS * (i >> 5) + KEY_STEP * (lane / KEYS);
           const int mine = slot_of(x, kt * kTile + key_of_lane), own = slot_of(x, kt * kTile + i);
-          uint4 q[PER];
+          if (!finish()) return false;
 #pragma unroll
           for (int k = 0; k < PER; ++k) {
             const int slot = __shfl_sync(0xffffffffu, mine, k * KEYS + key0 % KEYS);
             q[k] = slot >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + (int64_t)slot * D) + part) : make_uint4(0u, 0u, 0u, 0u);
           }
-          const float scale = !SUM && own >= 0 ? __ldg(a.w.cache.k_scale + own) : 0.f;
-          const unsigned gone = __ballot_sync(0xffffffffu, own == kGone);
-          if (key >= L::STAGES && !wait(L::kKEmpty + stage, (uint32_t)(key / L::STAGES - 1) & 1u)) return false;
-          const uint32_t panel = smem + L::K + (uint32_t)stage * L::TILE + (uint32_t)(part >> 2) * L::PANEL;
-#pragma unroll
-          for (int k = 0; k < PER; ++k) {
-            const int at = key0 + KEY_STEP * k;
-            const uint32_t v[4] = {q[k].x ^ 0x80808080u, q[k].y ^ 0x80808080u, q[k].z ^ 0x80808080u, q[k].w ^ 0x80808080u};
-            const uint32_t row = panel + at * 128;
-            st_shared16(row + ((c0 ^ (at & 7)) << 4), make_uint4(i8_pair(v[0], 0x4140u), i8_pair(v[0], 0x4342u),
-                                                                 i8_pair(v[1], 0x4140u), i8_pair(v[1], 0x4342u)));
-            st_shared16(row + (((c0 + 1) ^ (at & 7)) << 4), make_uint4(i8_pair(v[2], 0x4140u), i8_pair(v[2], 0x4342u),
-                                                                       i8_pair(v[3], 0x4140u), i8_pair(v[3], 0x4342u)));
-          }
-          if constexpr (!SUM) st_shared4(smem + L::SCALE + 4u * (key % kNotes * kTile + i), __float_as_uint(scale));
-          if (lane == 0) st_shared4(smem + L::GONE + 16u * (key % kNotes) + 4u * (i >> 5), gone);
-          fence_proxy_async_smem();
-          arrive(L::kKFull + stage);
+          scale = own >= 0 ? __ldg(a.w.cache.k_scale + own) : 0.f;
+          gone = __ballot_sync(0xffffffffu, own == kGone);
+          held = key;
           return true;
         },
-        nothing, nothing);
+        nothing, [&](const Piece&) { return finish(); });
     if (!ok && lane == 0) give_up();
   }
 
@@ -606,27 +627,27 @@ struct Kernel {
           },
           nothing);
     } else {
-      constexpr int OWN = kMostTiles / 2;  // key tiles of a group
-      float sum[OWN], scale[OWN], before[OWN];
-      int slot[OWN];  // of the thread's key of each, -1 where there is none
+      // Each group has half of the columns of every key tile; the second group adds its sums to the first one's.
+      float sum[kMostTiles], before[kMostTiles];
+      int slot[kMostTiles];  // of the thread's key of each, -1 where there is none
+      int number = 0;        // of pieces
       ok = walk(
           [&](const Piece& x) {
             const int* table = a.w.batch.table + x.b * a.w.batch.max_pages;
             bool bad = false;
 #pragma unroll
-            for (int i = 0; i < OWN; ++i) {  // (the pages first, so that the loads run side by side)
-              const int kt = x.t0 + set + 2 * i, j = kt * kTile + own;
+            for (int i = 0; i < kMostTiles; ++i) {  // (the pages first, so that the loads run side by side)
+              const int kt = x.t0 + i, j = kt * kTile + own;
               sum[i] = 0.f;
               slot[i] = kt < x.t1 && j < x.len ? __ldg(table + (j >> a.w.cache.page_shift)) : -1;
               bad |= kt < x.t1 && j < x.len && (unsigned)slot[i] >= (unsigned)a.w.cache.pages;
             }
             if (bad) atomicOr(a.w.batch.status, kStatusIndex);
 #pragma unroll
-            for (int i = 0; i < OWN; ++i) {
-              const int j = (x.t0 + set + 2 * i) * kTile + own;
+            for (int i = 0; i < kMostTiles; ++i) {
+              const int j = (x.t0 + i) * kTile + own;
               slot[i] = (unsigned)slot[i] < (unsigned)a.w.cache.pages ? (int)paged_slot(a.w.cache, slot[i], x.h, j) : -1;
-              if constexpr (I8) scale[i] = slot[i] >= 0 ? __ldg(a.w.cache.k_scale + slot[i]) : 0.f;
-              before[i] = slot[i] >= 0 && j < x.pos0 ? a.w.score[slot[i]] : 0.f;
+              before[i] = set == 0 && slot[i] >= 0 && j < x.pos0 ? a.w.score[slot[i]] : 0.f;
             }
             return true;
           },
@@ -634,8 +655,7 @@ struct Kernel {
             return wait(L::kColFull + tile % kQStages, (uint32_t)(tile / kQStages) & 1u);
           },
           [&](const Piece& x, const Span& y, int kt, int key, int tile) {
-            if (((kt - x.t0) & 1) != set) return true;
-            const int place = key % kS, j0 = kt * kTile, which = (kt - x.t0) >> 1;
+            const int place = key % kS, j0 = kt * kTile, which = kt - x.t0;
             if (!wait(L::kSFull + place, (uint32_t)(key / kS) & 1u)) return false;
             tc_fence_after();
             const bool edge = j0 < y.all_lo || j0 + kTile > y.all_hi || y.rows < kTile;
@@ -648,33 +668,48 @@ struct Kernel {
               to = (int)min((int64_t)kTile, max((int64_t)0, i1 * a.w.group - y.r0));
             }
             float ks = 1.f;
-            if constexpr (I8) {
+            if constexpr (I8)
+              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(smem + L::SCALE + 4u * (key % kNotes * kTile + own)));
+            const unsigned long long ks2 = p2(ks, ks), zero2 = p2(-0.f, -0.f);
+            const uint32_t col = smem + L::COL + 16u * (tile % kQStages * (kTile / 2)) + 512u * set;
+            unsigned long long p[2] = {p2(0.f, 0.f), p2(0.f, 0.f)};
+            uint32_t v[2][32];
+            tmem_ld_32x32_begin(lanes + 128u * place + 64u * set, v[0]);
+            tmem_ld_32x32_begin(lanes + 128u * place + 64u * set + 32u, v[1]);
+            tmem_ld_wait(v[0]);
+            tmem_ld_wait(v[1]);
 #pragma unroll
-              for (int i = 0; i < OWN; ++i) ks = i == which ? scale[i] : ks;
-            }
-            const uint32_t col = smem + L::COL + 8u * (tile % kQStages * kTile);
-            float p[4] = {0.f, 0.f, 0.f, 0.f};
-            over_chunks(lanes + 128u * place, [&](int c, uint32_t (&r)[32]) {
+            for (int c = 0; c < 2; ++c) {
+              uint4 w[8];
 #pragma unroll
               for (int k = 0; k < 32; k += 2) {
-                const uint4 w = ld_shared16(col + 8u * (32 * c + k));  // scale and lse of two rows
-                float s0 = __uint_as_float(r[k]), s1 = __uint_as_float(r[k + 1]);
-                if constexpr (I8) s0 *= ks, s1 *= ks;
-                float p0 = exp2_approx(fmaf(s0, __uint_as_float(w.x), -__uint_as_float(w.y)));
-                float p1 = exp2_approx(fmaf(s1, __uint_as_float(w.z), -__uint_as_float(w.w)));
-                if (edge) {
-                  p0 = 32 * c + k >= from && 32 * c + k < to ? p0 : 0.f;
-                  p1 = 32 * c + k + 1 >= from && 32 * c + k + 1 < to ? p1 : 0.f;
+                if (k % 16 == 0) {
+#pragma unroll
+                  for (int u = 0; u < 8; ++u) w[u] = ld_shared16(col + 16u * (16 * c + k / 2 + u));
                 }
-                p[k & 3] += p0;
-                p[(k + 1) & 3] += p1;
+                const uint4 x4 = w[k / 2 % 8];  // scales and -lse of two rows
+                unsigned long long s = p2(__uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
+                if constexpr (I8) s = fma2(s, ks2, zero2);
+                float t0, t1;
+                up2(fma2(s, p2(__uint_as_float(x4.x), __uint_as_float(x4.y)), p2(__uint_as_float(x4.z), __uint_as_float(x4.w))),
+                    t0, t1);
+                float p0 = exp2_approx(t0), p1 = exp2_approx(t1);
+                if (edge) {
+                  const int at = 64 * set + 32 * c + k;
+                  p0 = at >= from && at < to ? p0 : 0.f;
+                  p1 = at + 1 >= from && at + 1 < to ? p1 : 0.f;
+                }
+                p[k / 2 & 1] = add2(p[k / 2 & 1], p2(p0, p1));
               }
-            });
+            }
             tc_fence_before();
             arrive(L::kSFree + place);
-            const float all = (p[0] + p[1]) + (p[2] + p[3]);
+            float s0, s1, s2, s3;
+            up2(p[0], s0, s1);
+            up2(p[1], s2, s3);
+            const float all = (s0 + s1) + (s2 + s3);
 #pragma unroll
-            for (int i = 0; i < OWN; ++i) sum[i] += i == which ? all : 0.f;
+            for (int i = 0; i < kMostTiles; ++i) sum[i] += i == which ? all : 0.f;
             return true;
           },
           [&](const Piece&, const Span&, int tile) {
@@ -682,11 +717,20 @@ struct Kernel {
             return true;
           },
           [&](const Piece& x) {
+            // A piece at a time: neither group's barrier gets a phase ahead of its waiter.
+            if (set == 1 && !wait(L::kFirst, (uint32_t)number & 1u)) return false;
+            if (set == 0 && number > 0 && !wait(L::kSecond, (uint32_t)(number - 1) & 1u)) return false;
 #pragma unroll
-            for (int i = 0; i < OWN; ++i) {
-              const int j = (x.t0 + set + 2 * i) * kTile + own;
-              if (slot[i] >= 0) a.w.score[slot[i]] = (j < x.pos0 ? before[i] * a.w.decay : 0.f) + sum[i];
+            for (int i = 0; i < kMostTiles; ++i) {
+              const int j = (x.t0 + i) * kTile + own;
+              if (set == 1) before[i] = slot[i] >= 0 ? a.w.score[slot[i]] : 0.f;
+              else before[i] = j < x.pos0 ? before[i] * a.w.decay : 0.f;
             }
+#pragma unroll
+            for (int i = 0; i < kMostTiles; ++i)
+              if (slot[i] >= 0) a.w.score[slot[i]] = before[i] + sum[i];
+            arrive(set == 0 ? L::kFirst : L::kSecond);
+            ++number;
             return true;
           });
     }
@@ -722,7 +766,7 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
     }
     for (int s = 0; s < kS; ++s) {
       init(L::kSFull + s, 2);  // the products, and the issuer for what it has seen of the key tile's notes
-      init(L::kSFree + s, 4);
+      init(L::kSFree + s, SUM ? kEpilogue : kEpilogue / 2);
     }
     // issuer, loader, epilogue and, where they work, warp 2 and the widening warps
     const int readers = 2 + kEpilogue + (SUM ? 1 : 0) + (I8 ? 8 : 0);
@@ -730,6 +774,8 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
       init(L::kPieceFull + s, 1);
       init(L::kPieceFree + s, readers);
     }
+    init(L::kFirst, kEpilogue / 2);
+    init(L::kSecond, kEpilogue / 2);
     init(L::kDrain, 1);
     *abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -743,11 +789,19 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
   pdl_trigger();
   const Kernel<D, I8, SUM> k{a, map_hi, map_lo, map_k, smem, __shfl_sync(0xffffffffu, *tmem_slot, 0), abort,
                              reinterpret_cast<Piece*>(base + L::PIECES)};
-  if (warp == 0) k.issuer();
-  else if (warp == 1) k.loader();
-  else if (SUM && warp == 2) k.columns();
-  else if (warp >= 4 && warp < 4 + kEpilogue) k.epilogue();
-  else if (I8 && warp >= 4 + kEpilogue) k.widen();
+  // int8: 96 registers a thread at the start; 64 + 2 x 120 + 2 x 88 <= 5 x 96
+  if (warp < 4) {
+    if constexpr (I8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 0) k.issuer();
+    else if (warp == 1) k.loader();
+    else if (SUM && warp == 2) k.columns();
+  } else if (warp < 4 + kEpilogue) {
+    if constexpr (I8) asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
+    k.epilogue();
+  } else if constexpr (I8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    k.widen();
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 0) {
