@@ -44,10 +44,11 @@ __device__ __forceinline__ uint32_t score_order(float x) {
 
 // One block a (key head, sequence).
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictArgs a) {
-  extern __shared__ uint32_t held[];
+  extern __shared__ __align__(16) uint32_t held[];
   __shared__ int histogram[256], warp_sums[kSelectWarps], s_digit, s_left;
   __shared__ uint32_t s_low, s_high;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_trigger();
   const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
   const bool over = s.len > a.keep;
   if (h == 0 && tid == 0) {
@@ -58,33 +59,46 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   const int early = s.len - a.recent, want = a.keep - a.recent;
   if (!over || want == 0) return;
   int* list = a.list + ((int64_t)b * a.cache.heads + h) * a.chosen;
-  auto read = [&](int pos) -> uint32_t {
+  const bool wide = (reinterpret_cast<uintptr_t>(a.score) & 15u) == 0;
+  // Four scores at a time: they lie in one page.
+  auto read = [&](int pos) {
     const int page = paged_page(a.cache, a.batch, b, pos);
-    return page < 0 ? 0u : score_order(__ldg(a.score + paged_slot(a.cache, page, h, pos)));
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (page >= 0) {
+      const float* at = a.score + paged_slot(a.cache, page, h, pos);
+      if (wide) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(at));
+        v = make_uint4(score_order(x.x), score_order(x.y), score_order(x.z), score_order(x.w));
+      } else {
+        v = make_uint4(score_order(__ldg(at)), score_order(__ldg(at + 1)), score_order(__ldg(at + 2)), score_order(__ldg(at + 3)));
+      }
+    }
+    return v;
   };
-  const bool all_held = early <= kHeld;
   const int kept = min(early, kHeld);
   uint32_t low = ~0u, high = 0u;
-  for (int p0 = tid; p0 < kept; p0 += 8 * kSelectThreads) {
-    uint32_t v[8];
+  auto look = [&](const uint4& v, int pos) {
+    const uint32_t x[kPer] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p0 + i * kSelectThreads < kept ? read(p0 + i * kSelectThreads) : 0u;
+    for (int i = 0; i < kPer; ++i)
+      if (pos + i < early) {
+        low = min(low, x[i]);
+        high = max(high, x[i]);
+      }
+  };
+  uint4* held4 = reinterpret_cast<uint4*>(held);
+  for (int p0 = kPer * tid; p0 < kept; p0 += 4 * kStrip) {
+    uint4 v[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (p0 + i * kSelectThreads < kept) {
-        held[p0 + i * kSelectThreads] = v[i];
-        low = min(low, v[i]);
-        high = max(high, v[i]);
+    for (int i = 0; i < 4; ++i) v[i] = p0 + i * kStrip < kept ? read(p0 + i * kStrip) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p0 + i * kStrip < kept) {
+        held4[(p0 + i * kStrip) / kPer] = v[i];
+        look(v[i], p0 + i * kStrip);
       }
   }
-  if (!all_held) {
-#pragma unroll 4
-    for (int p = kHeld + tid; p < early; p += kSelectThreads) {
-      const uint32_t v = read(p);
-      low = min(low, v);
-      high = max(high, v);
-    }
-  }
+  for (int p = kHeld + kPer * tid; p < early; p += kStrip) look(read(p), p);
   low = __reduce_min_sync(0xffffffffu, low);
   high = __reduce_max_sync(0xffffffffu, high);
   if (tid == 0) s_low = ~0u, s_high = 0u;
@@ -105,15 +119,16 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     const uint32_t digits = (1u << (above - shift)) - 1u, prefix = above < 32 ? least >> above : 0u;
     if (tid < 256) histogram[tid] = 0;
     __syncthreads();
-    auto count = [&](uint32_t v) {
-      v -= low;
-      if ((above < 32 ? v >> above : 0u) == prefix) atomicAdd(histogram + (v >> shift & digits), 1);
+    auto count = [&](const uint4& v, int pos) {
+      const uint32_t x[kPer] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const uint32_t d = x[i] - low;
+        if (pos + i < early && (above < 32 ? d >> above : 0u) == prefix) atomicAdd(histogram + (d >> shift & digits), 1);
+      }
     };
-    for (int p = tid; p < kept; p += kSelectThreads) count(held[p]);
-    if (!all_held) {
-#pragma unroll 4
-      for (int p = kHeld + tid; p < early; p += kSelectThreads) count(read(p));
-    }
+    for (int p = kPer * tid; p < kept; p += kStrip) count(held4[p / kPer], p);
+    for (int p = kHeld + kPer * tid; p < early; p += kStrip) count(read(p), p);
     __syncthreads();
     if (warp == 0) {  // lane i: the digits from 255 - 8 i down
       int own = 0;
@@ -144,13 +159,12 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
   int above0 = 0, equal0 = 0;  // in the strips before
   for (int p0 = 0; p0 < early; p0 += kStrip) {
     const int p = p0 + kPer * tid;
-    uint32_t v[kPer];
+    const uint4 v4 = p < kept ? held4[p / kPer] : (p < early ? read(p) : make_uint4(0u, 0u, 0u, 0u));
+    const uint32_t v[kPer] = {v4.x, v4.y, v4.z, v4.w};
     int packed = 0;  // those above in the low half, those equal in the high one (a strip has 4096)
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      v[i] = p + i < kept ? held[p + i] : (p + i < early ? read(p + i) : 0u);
+    for (int i = 0; i < kPer; ++i)
       if (p + i < early) packed += v[i] > least ? 1 : (v[i] == least ? 1 << 16 : 0);
-    }
     int sum = packed;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -187,6 +201,7 @@ template <int ROW, int W>  // bytes of a vector
 __global__ void __launch_bounds__(kMoveThreads, 5) evict_move_kernel(const EvictArgs a, int shares) {
   constexpr int SLICES = ROW / W;
   const int part = blockIdx.x / shares, share = blockIdx.x % shares, h = blockIdx.y, b = blockIdx.z;
+  pdl_wait();
   const int moves = a.plan[kPlan * b], len = a.plan[kPlan * b + 1], before = a.plan[kPlan * b + 2];
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) a.out_len[b] = len;
   const int want = a.keep - a.recent;
@@ -288,11 +303,8 @@ spl_status launch_move(const EvictArgs& a, int blocks, cudaStream_t stream) {
   int shares = 1;  // of a head's tokens, where their order does not matter
   if (a.out_table) shares = (int)std::max<int64_t>(1, std::min<int64_t>(4 * blocks / ((int64_t)parts * heads * seqs), 64));
   const dim3 grid(parts * shares, heads, seqs);
-  if (wide)
-    evict_move_kernel<ROW, WIDE><<<grid, kMoveThreads, 0, stream>>>(a, shares);
-  else
-    evict_move_kernel<ROW, 32><<<grid, kMoveThreads, 0, stream>>>(a, shares);
-  return launch_status();
+  return launch_pdl(wide ? evict_move_kernel<ROW, WIDE> : evict_move_kernel<ROW, 32>, grid, dim3(kMoveThreads), 0, stream, a,
+                    shares);
 }
 
 // ---- an accepted path ----
@@ -413,7 +425,7 @@ extern "C" spl_status spl_kv_evict(const spl_kv_cache* cache, float* score, cons
   a.chosen = std::min(keep, room_of(a.cache, a.batch));
   a.plan = static_cast<int*>(workspace);
   a.list = a.plan + round_up((int64_t)a.batch.seqs * kPlan, 4);
-  const size_t held = (size_t)std::min<int64_t>(kHeld, room_of(a.cache, a.batch)) * sizeof(uint32_t);
+  const size_t held = (size_t)std::min<int64_t>(kHeld, room_of(a.cache, a.batch)) * sizeof(uint32_t);  // (room: whole pages)
   static bool done[kMaxDevices] = {false};
   if (!allow_shared(reinterpret_cast<const void*>(evict_select_kernel), kHeld * sizeof(uint32_t), done)) return SPL_ECUDA;
   evict_select_kernel<<<dim3(a.cache.heads, a.batch.seqs), kSelectThreads, held, stream>>>(a);

@@ -251,8 +251,13 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_scores_kernel(const __grid_
 // kernel left of every 32 keys, then the rows' weights in their order, a thread four neighbouring keys at a time.
 // blockIdx: keys, key head, sequence.
 constexpr int kSumThreads = 256, kSumKeys = 2048, kSumRows = 64;
-__global__ void __launch_bounds__(kSumThreads) weigh_sum_kernel(const __grid_constant__ WeighArgs w) {
-  __shared__ float2 stats[kSumRows];  // maximum, 1 / total
+__global__ void __launch_bounds__(kSumThreads, 4) weigh_sum_kernel(const __grid_constant__ WeighArgs w) {
+  struct Row {
+    float m, inverse;  // maximum, 1 / total
+    int lo, hi;        // keys that it sees
+  };
+  __shared__ __align__(16) Row rows_of[kSumRows];
+  __shared__ const float* scores_of[kSumRows];
   __shared__ float2 teams[kSumThreads / 32];
   const AttnArgs& a = w.attn;
   const int h = blockIdx.y, b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -323,7 +328,8 @@ __global__ void __launch_bounds__(kSumThreads) weigh_sum_kernel(const __grid_con
             l = l * exp2_approx(m - base) + o.y * exp2_approx(o.x - base);
             m = top;
           }
-          stats[r] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
+          rows_of[r] = {m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l, lo, hi};
+          scores_of[r] = w.s + row_of(r0 + r) * w.cap;
         }
         __syncthreads();
       }
@@ -331,18 +337,16 @@ __global__ void __launch_bounds__(kSumThreads) weigh_sum_kernel(const __grid_con
       for (int u = 0; u < PER; ++u) {
         const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
         if (!score[u]) continue;
-        const float* at = w.s + j;
+        const int key = (int)j;
 #pragma unroll 4
         for (int r = 0; r < some; ++r) {
-          int lo, hi;
-          row_keys(s, a.window, (int)((r0 + r) / a.group), lo, hi);
-          if (j + 3 < lo || j >= hi) continue;
-          const float4 v = *reinterpret_cast<const float4*>(at + row_of(r0 + r) * w.cap);
-          const float2 st = stats[r];
-          sum[u].x += j >= lo ? exp2_approx(v.x - st.x) * st.y : 0.f;
-          sum[u].y += j + 1 >= lo && j + 1 < hi ? exp2_approx(v.y - st.x) * st.y : 0.f;
-          sum[u].z += j + 2 >= lo && j + 2 < hi ? exp2_approx(v.z - st.x) * st.y : 0.f;
-          sum[u].w += j + 3 < hi ? exp2_approx(v.w - st.x) * st.y : 0.f;
+          const Row x = rows_of[r];
+          if (key + 3 < x.lo || key >= x.hi) continue;
+          const float4 v = *reinterpret_cast<const float4*>(scores_of[r] + key);
+          sum[u].x += key >= x.lo ? exp2_approx(v.x - x.m) * x.inverse : 0.f;
+          sum[u].y += key + 1 >= x.lo && key + 1 < x.hi ? exp2_approx(v.y - x.m) * x.inverse : 0.f;
+          sum[u].z += key + 2 >= x.lo && key + 2 < x.hi ? exp2_approx(v.z - x.m) * x.inverse : 0.f;
+          sum[u].w += key + 3 < x.hi ? exp2_approx(v.w - x.m) * x.inverse : 0.f;
         }
       }
     }

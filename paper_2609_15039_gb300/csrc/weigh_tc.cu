@@ -19,6 +19,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include <cuda_fp16.h>
 
@@ -75,17 +76,25 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seqs = w.batch.seqs;
   if (blockIdx.x == 0) {
     __shared__ unsigned long long sums[kMostRange + kMostTiles], scan[2][kPrepThreads];  // pieces of a head, by their length
-    __shared__ int longest, chosen[2];
-    if (threadIdx.x < kMostRange + kMostTiles) sums[threadIdx.x] = 0;
+    __shared__ int key_tiles[kMaxSeqs], row_tiles[kMaxSeqs], longest, chosen[2];
     if (threadIdx.x == 0) longest = 0;
     __syncthreads();
     for (int b = threadIdx.x; b < seqs; b += kPrepThreads) {
       const PagedSeq s = paged_seq(w.batch, w.cache.page_shift, b);
-      const int kt = (s.len + kTile - 1) / kTile;
-      const int64_t rt = ((int64_t)s.n * w.group + kTile - 1) / kTile;
-      for (int i = 0; i < kMostRange; ++i) atomicAdd(sums + i, (unsigned long long)(rt * ((kt + i) / (i + 1))));
-      for (int i = 0; i < kMostTiles; ++i) atomicAdd(sums + kMostRange + i, (unsigned long long)((kt + i) / (i + 1)));
-      atomicMax(&longest, kt);
+      key_tiles[b] = (s.len + kTile - 1) / kTile;
+      row_tiles[b] = (s.n * w.group + kTile - 1) / kTile;
+      atomicMax(&longest, key_tiles[b]);
+    }
+    __syncthreads();
+    for (int i = warp; i < kMostRange + kMostTiles; i += kPrepThreads / 32) {
+      const bool first = i < kMostRange;
+      const uint32_t n = (uint32_t)(first ? i : i - kMostRange) + 1u;
+      unsigned long long sum = 0;
+      for (int b = lane; b < seqs; b += 32)
+        sum += (unsigned long long)(((uint32_t)key_tiles[b] + n - 1u) / n) * (first ? (uint32_t)row_tiles[b] : 1u);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (lane == 0) sums[i] = sum;
     }
     __syncthreads();
     if (threadIdx.x < 64) {  // the length that gives the fewest key tiles to any block; beginning a piece costs some too
@@ -106,9 +115,9 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
     // Each sequence's first piece: sums before it, a run of sequences a thread.
     const int per = (seqs + kPrepThreads - 1) / kPrepThreads, b0 = min(seqs, per * (int)threadIdx.x), b1 = min(seqs, b0 + per);
     auto count = [&](int b, int pass) {
-      const PagedSeq s = paged_seq(w.batch, w.cache.page_shift, b);
-      const int64_t kt = (s.len + kTile - 1) / kTile, rt = ((int64_t)s.n * w.group + kTile - 1) / kTile;
-      return (unsigned long long)((pass == 0 ? rt : 1) * ((kt + chosen[pass] - 1) / chosen[pass]) * w.cache.heads);
+      const uint32_t n = (uint32_t)chosen[pass];
+      return (unsigned long long)(((uint32_t)key_tiles[b] + n - 1u) / n) * (pass == 0 ? (uint32_t)row_tiles[b] : 1u) *
+             (unsigned)w.cache.heads;
     };
     for (int pass = 0; pass < 2; ++pass) {
       unsigned long long own = 0;
@@ -678,32 +687,37 @@ struct Kernel {
             tmem_ld_32x32_begin(lanes + 128u * place + 64u * set + 32u, v[1]);
             tmem_ld_wait(v[0]);
             tmem_ld_wait(v[1]);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              uint4 w[8];
-#pragma unroll
-              for (int k = 0; k < 32; k += 2) {
-                if (k % 16 == 0) {
-#pragma unroll
-                  for (int u = 0; u < 8; ++u) w[u] = ld_shared16(col + 16u * (16 * c + k / 2 + u));
-                }
-                const uint4 x4 = w[k / 2 % 8];  // scales and -lse of two rows
-                unsigned long long s = p2(__uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
-                if constexpr (I8) s = fma2(s, ks2, zero2);
-                float t0, t1;
-                up2(fma2(s, p2(__uint_as_float(x4.x), __uint_as_float(x4.y)), p2(__uint_as_float(x4.z), __uint_as_float(x4.w))),
-                    t0, t1);
-                float p0 = exp2_approx(t0), p1 = exp2_approx(t1);
-                if (edge) {
-                  const int at = 64 * set + 32 * c + k;
-                  p0 = at >= from && at < to ? p0 : 0.f;
-                  p1 = at + 1 >= from && at + 1 < to ? p1 : 0.f;
-                }
-                p[k / 2 & 1] = add2(p[k / 2 & 1], p2(p0, p1));
-              }
-            }
             tc_fence_before();
             arrive(L::kSFree + place);
+            auto add = [&](auto masked) {
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                uint4 w[8];
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                  if (k % 16 == 0) {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) w[u] = ld_shared16(col + 16u * (16 * c + k / 2 + u));
+                  }
+                  const uint4 x4 = w[k / 2 % 8];  // scales and -lse of two rows
+                  unsigned long long s = p2(__uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
+                  if constexpr (I8) s = fma2(s, ks2, zero2);
+                  float t0, t1;
+                  up2(fma2(s, p2(__uint_as_float(x4.x), __uint_as_float(x4.y)),
+                           p2(__uint_as_float(x4.z), __uint_as_float(x4.w))),
+                      t0, t1);
+                  float p0 = exp2_approx(t0), p1 = exp2_approx(t1);
+                  if constexpr (masked) {
+                    const int at = 64 * set + 32 * c + k;
+                    p0 = at >= from && at < to ? p0 : 0.f;
+                    p1 = at + 1 >= from && at + 1 < to ? p1 : 0.f;
+                  }
+                  p[k / 2 & 1] = add2(p[k / 2 & 1], p2(p0, p1));
+                }
+              }
+            };
+            if (edge) add(std::true_type());
+            else add(std::false_type());
             float s0, s1, s2, s3;
             up2(p[0], s0, s1);
             up2(p[1], s2, s3);
