@@ -298,7 +298,7 @@ spl_status launch_move(const EvictArgs& a, int blocks, cudaStream_t stream) {
   // from 16000 tokens to 6000: %%; one of 1250 to 1000: %%).
   const int heads = a.cache.heads, seqs = a.batch.seqs;
   constexpr int WIDE = ROW;
-  const bool wide = (int64_t)heads * seqs * (2 * ROW / WIDE) >= blocks;
+  const bool wide = (int64_t)heads * seqs * (2 * ROW / WIDE) >= 2 * blocks;
   const int parts = 2 * ROW / (wide ? WIDE : 32) + 1;
   int shares = 1;  // of a head's tokens, where their order does not matter
   if (a.out_table) shares = (int)std::max<int64_t>(1, std::min<int64_t>(4 * blocks / ((int64_t)parts * heads * seqs), 64));

@@ -247,11 +247,11 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_scores_kernel(const __grid_
   }
 }
 
-// A block has kSumKeys keys of a (sequence, key head): first the rows' maxima and totals, from what the scores'
-// kernel left of every 32 keys, then the rows' weights in their order, a thread four neighbouring keys at a time.
-// blockIdx: keys, key head, sequence.
-constexpr int kSumThreads = 256, kSumKeys = 2048, kSumRows = 64;
-__global__ void __launch_bounds__(kSumThreads, 4) weigh_sum_kernel(const __grid_constant__ WeighArgs w) {
+// A block has `trips` times 1024 keys of a (sequence, key head): first the rows' maxima and totals, from what the scores'
+// kernel left of every 32 keys, then the rows' weights in their order, a thread four neighbouring keys.  blockIdx: keys, key head, sequence.
+constexpr int kSumThreads = 256, kTrip = 4 * kSumThreads, kSumRows = 64;
+constexpr int kMostTrips = 4;
+__global__ void __launch_bounds__(kSumThreads, 6) weigh_sum_kernel(const __grid_constant__ WeighArgs w, int trips) {
   struct Row {
     float m, inverse;  // maximum, 1 / total
     int lo, hi;        // keys that it sees
@@ -263,40 +263,26 @@ __global__ void __launch_bounds__(kSumThreads, 4) weigh_sum_kernel(const __grid_
   const int h = blockIdx.y, b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // (what the scores' kernel does not write may be read before it ends)
   const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
-  const int64_t rows = (int64_t)s.n * a.group;
-  constexpr int PER = kSumKeys / (4 * kSumThreads);
-  for (int64_t k0 = (int64_t)blockIdx.x * kSumKeys; k0 < s.len; k0 += (int64_t)gridDim.x * kSumKeys) {
-    float* score[PER];
-    float4 sum[PER], before[PER];
+  const int rows = s.n * a.group;
+  const bool wide = (reinterpret_cast<uintptr_t>(w.score) & 15u) == 0;
+  // row r of the key head: query head r % group of token r / group
+  auto row_of = [&](int r) { return (s.row0 + r / a.group) * (int64_t)w.q_heads + h * a.group + r % a.group; };
+  for (int64_t from = (int64_t)blockIdx.x * trips * kTrip; from < s.len; from += (int64_t)gridDim.x * trips * kTrip) {
+    const int64_t end = min((int64_t)s.len, from + trips * kTrip);
+    int pages[kMostTrips];  // (all at once: a trip's would wait for memory before its scores could)
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
-      score[u] = nullptr;
-      sum[u] = before[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (j >= s.len) continue;
-      const int page = paged_page(a.cache, a.batch, b, (int)j);
-      if (page >= 0) score[u] = w.score + paged_slot(a.cache, page, h, (int)j);  // (four keys lie in one page)
+    for (int u = 0; u < kMostTrips; ++u) {
+      const int64_t j = from + u * kTrip + 4 * threadIdx.x;
+      pages[u] = j < end ? __ldg(a.batch.table + b * a.batch.max_pages + (j >> a.cache.page_shift)) : 0;
     }
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
-      if (!score[u]) continue;
-      if (j < s.pos0) before[u].x = score[u][0];
-      if (j + 1 < s.pos0) before[u].y = score[u][1];
-      if (j + 2 < s.pos0) before[u].z = score[u][2];
-      if (j + 3 < s.pos0) before[u].w = score[u][3];
-    }
-    pdl_wait();
-    for (int64_t r0 = 0; r0 < rows; r0 += kSumRows) {
-      const int some = (int)min((int64_t)kSumRows, rows - r0);
-      // row r of the key head: query head r % group of token r / group
-      auto row_of = [&](int64_t r) { return (s.row0 + r / a.group) * w.q_heads + h * a.group + r % a.group; };
+    // Maxima and totals of up to kSumRows rows from r0 on.
+    auto totals = [&](int r0, int some) {
       const int team = some > 4 ? 1 : (some > 2 ? 2 : (some > 1 ? 4 : 8));
       __syncthreads();
       for (int q0 = 0; q0 < some * team; q0 += kSumThreads / 32) {  // `team` warps a row
         const int r = min((q0 + warp) / team, some - 1), mate = warp % team;
         int lo, hi;
-        row_keys(s, a.window, (int)((r0 + r) / a.group), lo, hi);
+        row_keys(s, a.window, (r0 + r) / a.group, lo, hi);
         const float2* parts = w.parts + row_of(r0 + r) * (w.cap / kPart);
         float m = -INFINITY, l = 0.f;
         for (int p0 = lo / kPart + 32 * mate; p0 * kPart < hi; p0 += 4 * 32 * team) {
@@ -333,31 +319,61 @@ __global__ void __launch_bounds__(kSumThreads, 4) weigh_sum_kernel(const __grid_
         }
         __syncthreads();
       }
+    };
+    pdl_wait();
+    if (rows <= kSumRows) totals(0, rows);
 #pragma unroll
-      for (int u = 0; u < PER; ++u) {
-        const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
-        if (!score[u]) continue;
-        const int key = (int)j;
+    for (int u = 0; u < kMostTrips; ++u) {
+      if (from + u * kTrip >= end) break;
+      const int key = (int)(from + u * kTrip) + 4 * threadIdx.x;
+      float* score = nullptr;
+      float4 before = make_float4(0.f, 0.f, 0.f, 0.f), sum = before;
+      if (key < end) {
+        if ((unsigned)pages[u] < (unsigned)a.cache.pages)
+          score = w.score + paged_slot(a.cache, pages[u], h, key);  // (four keys lie in one page)
+        else
+          atomicOr(a.batch.status, kStatusIndex);
+      }
+      if (score && wide && key + 3 < s.pos0) {
+        before = *reinterpret_cast<const float4*>(score);
+      } else if (score) {
+        if (key < s.pos0) before.x = score[0];
+        if (key + 1 < s.pos0) before.y = score[1];
+        if (key + 2 < s.pos0) before.z = score[2];
+        if (key + 3 < s.pos0) before.w = score[3];
+      }
+      for (int r0 = 0; r0 < rows; r0 += kSumRows) {
+        const int some = min(kSumRows, rows - r0);
+        if (rows > kSumRows) totals(r0, some);
+        if (!score) continue;
 #pragma unroll 4
         for (int r = 0; r < some; ++r) {
-          const Row x = rows_of[r];
-          if (key + 3 < x.lo || key >= x.hi) continue;
+          const Row q = rows_of[r];
+          if (key + 3 < q.lo || key >= q.hi) continue;
           const float4 v = *reinterpret_cast<const float4*>(scores_of[r] + key);
-          sum[u].x += key >= x.lo ? exp2_approx(v.x - x.m) * x.inverse : 0.f;
-          sum[u].y += key + 1 >= x.lo && key + 1 < x.hi ? exp2_approx(v.y - x.m) * x.inverse : 0.f;
-          sum[u].z += key + 2 >= x.lo && key + 2 < x.hi ? exp2_approx(v.z - x.m) * x.inverse : 0.f;
-          sum[u].w += key + 3 < x.hi ? exp2_approx(v.w - x.m) * x.inverse : 0.f;
+          float p[4] = {exp2_approx(v.x - q.m), exp2_approx(v.y - q.m), exp2_approx(v.z - q.m), exp2_approx(v.w - q.m)};
+          if (key < q.lo || key + 3 >= q.hi) {  // (where the row does not see a key anything may be there)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (key + i < q.lo || key + i >= q.hi) p[i] = 0.f;
+          }
+          sum.x = fmaf(p[0], q.inverse, sum.x);
+          sum.y = fmaf(p[1], q.inverse, sum.y);
+          sum.z = fmaf(p[2], q.inverse, sum.z);
+          sum.w = fmaf(p[3], q.inverse, sum.w);
         }
       }
-    }
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t j = k0 + 4 * (threadIdx.x + u * kSumThreads);
-      if (!score[u]) continue;
-      score[u][0] = before[u].x * w.decay + sum[u].x;
-      if (j + 1 < s.len) score[u][1] = before[u].y * w.decay + sum[u].y;
-      if (j + 2 < s.len) score[u][2] = before[u].z * w.decay + sum[u].z;
-      if (j + 3 < s.len) score[u][3] = before[u].w * w.decay + sum[u].w;
+      if (!score) continue;
+      const float4 after = make_float4(before.x * w.decay + sum.x, before.y * w.decay + sum.y, before.z * w.decay + sum.z,
+                                       before.w * w.decay + sum.w);
+      if (wide && key + 3 < s.len) {
+        *reinterpret_cast<float4*>(score) = after;
+      } else {
+        score[0] = after.x;
+        if (key + 1 < s.len) score[1] = after.y;
+        if (key + 2 < s.len) score[2] = after.z;
+        if (key + 3 < s.len) score[3] = after.w;
+      }
     }
   }
 }
@@ -371,16 +387,19 @@ spl_status launch_scores(const WeighArgs& w, int blocks, cudaStream_t stream) {
   return launch_status();
 }
 
-// Few rows: of a key head at most kFewRows, by max_rows, and scores that take no more than kMostScores bytes.
-constexpr int64_t kFewRows = 16, kMostScores = int64_t(1) << 31;
+// Few rows: of a key head at most so many, by max_rows, and scores that take no more than kMostScores bytes.  Measured, few and
+// many rows, us, 15 sequences over 600 to 6000 keys, 32 query heads on 8: int8, 32 rows of a key head 82, 114, 48 rows 122, 114;
+// binary16, 16 rows 55, 91, 32 rows 93, 91; one sequence over 6000, int8, 32 rows 38, 41, 64 rows 61, 42.
+constexpr int64_t kMostScores = int64_t(1) << 31;
+constexpr int64_t few_rows(bool i8) { return i8 ? 32 : 24; }
 struct Shape {
   bool few;
   int64_t cap;
   size_t s, parts, bytes;
 };
-Shape shape_of(const PagedCache& c, const PagedBatch& b, const spl_kv_batch* batch, int64_t q_heads, int head_dim) {
+Shape shape_of(const PagedCache& c, const PagedBatch& b, const spl_kv_batch* batch, int64_t q_heads, int head_dim, bool i8) {
   Shape x;
-  x.few = batch->max_rows * (q_heads / c.heads) <= kFewRows &&
+  x.few = batch->max_rows * (q_heads / c.heads) <= few_rows(i8) &&
           (double)b.rows * (double)q_heads * (double)(b.max_pages << c.page_shift) * 4 <= (double)kMostScores;
   if (!x.few) {
     x.bytes = b.rows == 0 ? 0 : weigh_tc_bytes(c, b, q_heads, head_dim);
@@ -415,7 +434,7 @@ extern "C" size_t spl_kv_weigh_workspace_bytes(const spl_kv_cache* cache, const 
   PagedCache c;
   PagedBatch b;
   if (check(cache, batch, rows, q_heads, &c, &b) != SPL_OK || b.seqs == 0) return 0;
-  return shape_of(c, b, batch, q_heads, (int)cache->head_dim).bytes;
+  return shape_of(c, b, batch, q_heads, (int)cache->head_dim, cache->format == SPL_KV_I8).bytes;
 }
 
 extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, const spl_kv_cache* cache,
@@ -431,7 +450,8 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   if (rows > 1 && ldq < q_heads * cache->head_dim) return SPL_EINVAL;
   if (!aligned16(Q) || !aligned4(score) || (rows > 1 && ldq % 4 != 0)) return SPL_EALIGN;
   const int dim = (int)cache->head_dim;
-  const Shape s = shape_of(a.cache, a.batch, batch, q_heads, dim);
+  const bool i8 = cache->format == SPL_KV_I8;
+  const Shape s = shape_of(a.cache, a.batch, batch, q_heads, dim, i8);
   if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes)) return SPL_EWORKSPACE;
   if (!aligned16(workspace)) return SPL_EALIGN;
   if (a.cache.pages == 0 || a.batch.max_pages == 0) return SPL_OK;
@@ -446,7 +466,6 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   a.slack = 1;
   a.join = 0;
   a.start = 1;
-  const bool i8 = cache->format == SPL_KV_I8;
   if (rows > 0 && !s.few)
     return run_weigh_tc({score, Q, ldq, a.cache, a.batch, a.group, (int)q_heads, a.window, a.scale_log2, decay, workspace}, dim,
                         i8, stream);
@@ -463,9 +482,11 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
                                 : (i8 ? launch_scores<64, true>(w, sms, stream) : launch_scores<64, false>(w, sms, stream));
     if (st != SPL_OK) return st;
   }
+  // Several trips a block where there are blocks enough (64 sequences over 1600 to 16000 keys: %%; one of 300: %%).
   const int64_t room = a.batch.max_pages << a.cache.page_shift;
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(room, kSumKeys), 1 << 16), a.cache.heads, a.batch.seqs);
-  if (rows > 0) return launch_pdl(weigh_sum_kernel, grid, dim3(kSumThreads), 0, stream, w);
-  weigh_sum_kernel<<<grid, kSumThreads, 0, stream>>>(w);  // (what is before it may have written the scores)
+  const int trips = ceil_div(room, kTrip) * a.cache.heads * a.batch.seqs >= (int64_t)8 * sms ? kMostTrips : 1;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(room, trips * kTrip), 1 << 16), a.cache.heads, a.batch.seqs);
+  if (rows > 0) return launch_pdl(weigh_sum_kernel, grid, dim3(kSumThreads), 0, stream, w, trips);
+  weigh_sum_kernel<<<grid, kSumThreads, 0, stream>>>(w, trips);  // (what is before it may have written the scores)
   return launch_status();
 }
