@@ -694,7 +694,8 @@ spl_status spl_tree_attention(float* out, int64_t ldo, const float* Q, int64_t l
  * slots of no token, and of pages outside the pool, are left as they are.  A page
  * holds tokens of one sequence of the batch only.  Sums are fp32, in the rows'
  * order.  Q [rows, q_heads head_dim] as there; 0 <= decay <= 1.  Workspace:
- * spl_kv_weigh_workspace_bytes, any contents.  Errors: as spl_paged_attention,
+ * spl_kv_weigh_workspace_bytes, any contents; its first 64 KiB are not touched,
+ * so the product workspace can be shared.  Errors: as spl_paged_attention,
  * EINVAL for a decay outside [0, 1]. */
 size_t spl_kv_weigh_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows,
                                     int64_t q_heads);
@@ -714,7 +715,7 @@ spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, const spl_kv_
  * other token of the batch.  Pages that are moved into belong to one sequence
  * only.  A score, source or target on a page outside the pool: the token counts
  * as the lightest, or is not moved.  batch->row_start is not used (but not NULL).
- * Workspace: spl_kv_evict_workspace_bytes, any contents.  Errors: as
+ * Workspace: spl_kv_evict_workspace_bytes, as spl_kv_weigh's.  Errors: as
  * spl_kv_append, EINVAL for recent > keep or negative ones, EWORKSPACE. */
 size_t spl_kv_evict_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t keep);
 spl_status spl_kv_evict(const spl_kv_cache* cache, float* score, const spl_kv_batch* batch, int64_t keep,

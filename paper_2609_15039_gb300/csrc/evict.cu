@@ -385,7 +385,7 @@ size_t chosen_of(const PagedCache& c, const PagedBatch& b, int64_t keep) {
   return (size_t)std::min(keep, room_of(c, b)) * c.heads * b.seqs;
 }
 size_t evict_bytes(const PagedCache& c, const PagedBatch& b, int64_t keep) {
-  return round_up((int64_t)b.seqs * kPlan * sizeof(int), 16) + chosen_of(c, b, keep) * sizeof(int);
+  return kCounterBytes + round_up((int64_t)b.seqs * kPlan * sizeof(int), 16) + chosen_of(c, b, keep) * sizeof(int);
 }
 
 }  // namespace
@@ -423,7 +423,7 @@ extern "C" spl_status spl_kv_evict(const spl_kv_cache* cache, float* score, cons
   a.keep = (int)std::min(keep, kMaxLength);
   a.recent = (int)std::min(recent, kMaxLength);
   a.chosen = std::min(keep, room_of(a.cache, a.batch));
-  a.plan = static_cast<int*>(workspace);
+  a.plan = reinterpret_cast<int*>(static_cast<char*>(workspace) + kCounterBytes);  // (the counters are others')
   a.list = a.plan + round_up((int64_t)a.batch.seqs * kPlan, 4);
   const size_t held = (size_t)std::min<int64_t>(kHeld, room_of(a.cache, a.batch)) * sizeof(uint32_t);  // (room: whole pages)
   static bool done[kMaxDevices] = {false};

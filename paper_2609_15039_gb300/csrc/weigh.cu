@@ -434,7 +434,8 @@ extern "C" size_t spl_kv_weigh_workspace_bytes(const spl_kv_cache* cache, const 
   PagedCache c;
   PagedBatch b;
   if (check(cache, batch, rows, q_heads, &c, &b) != SPL_OK || b.seqs == 0) return 0;
-  return shape_of(c, b, batch, q_heads, (int)cache->head_dim, cache->format == SPL_KV_I8).bytes;
+  const size_t bytes = shape_of(c, b, batch, q_heads, (int)cache->head_dim, cache->format == SPL_KV_I8).bytes;
+  return bytes ? kCounterBytes + bytes : 0;
 }
 
 extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, const spl_kv_cache* cache,
@@ -452,7 +453,7 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   const int dim = (int)cache->head_dim;
   const bool i8 = cache->format == SPL_KV_I8;
   const Shape s = shape_of(a.cache, a.batch, batch, q_heads, dim, i8);
-  if (s.bytes > 0 && (!workspace || workspace_bytes < s.bytes)) return SPL_EWORKSPACE;
+  if (s.bytes > 0 && (!workspace || workspace_bytes < kCounterBytes + s.bytes)) return SPL_EWORKSPACE;
   if (!aligned16(workspace)) return SPL_EALIGN;
   if (a.cache.pages == 0 || a.batch.max_pages == 0) return SPL_OK;
   if (!score) return SPL_EINVAL;
@@ -466,14 +467,14 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
   a.slack = 1;
   a.join = 0;
   a.start = 1;
+  char* at = static_cast<char*>(workspace) + kCounterBytes;  // (the counters are others')
   if (rows > 0 && !s.few)
-    return run_weigh_tc({score, Q, ldq, a.cache, a.batch, a.group, (int)q_heads, a.window, a.scale_log2, decay, workspace}, dim,
+    return run_weigh_tc({score, Q, ldq, a.cache, a.batch, a.group, (int)q_heads, a.window, a.scale_log2, decay, at}, dim,
                         i8, stream);
   w.score = score;
   w.decay = decay;
   w.q_heads = (int)q_heads;
   w.cap = s.cap;
-  char* at = static_cast<char*>(workspace);
   w.s = reinterpret_cast<float*>(at);
   w.parts = reinterpret_cast<float2*>(at + s.s);
   const int sms = device_sm_count();

@@ -534,7 +534,7 @@ def test_weigh_is_deterministic_in_graphs_and_on_streams(spl, rows):
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         spl.spl_kv_weigh(score, q, c.cache, batch, 8, workspace=ws)
-    ws.fill_(255)  # any contents
+    ws.fill_(255)  # any contents, and the counters' place is not touched
     for lens in ([900, 1500], [rows, rows + 400], [900, 0]):
         batch.kv_len.copy_(i32(lens))
         score.fill_(0.75)
@@ -546,6 +546,7 @@ def test_weigh_is_deterministic_in_graphs_and_on_streams(spl, rows):
             want = added + 0.75 * (np.arange(n) < n - rows)
             assert np.allclose(got, want, rtol=1e-5, atol=0)
     assert spl.spl_get_device_status() == spl.SPL_OK
+    assert bool((ws[:65536] == 255).all())
 
 
 # ---------------------------------------------------------------------------------- eviction

@@ -174,3 +174,27 @@ def test_oracle_tree_verification_keeps_the_target_distribution():
     won = np.argmax(p[0] / e, axis=1)
     share = np.bincount(won, minlength=3) / len(won)
     assert np.all(np.abs(share - p[0]) < 5 * np.sqrt(p[0] * (1 - p[0]) / len(won)))
+
+
+# ---------------------------------------------------------------------------------- serving.py
+def test_the_shape_of_a_tree():
+    from paper_2609_15039_gb300 import serving as example
+    t = example.Tree([3, 2])
+    assert (t.nodes, t.levels, t.first) == (10, 3, [0, 1, 4, 10])
+    assert t.parents == [-1, 0, 0, 0, 1, 1, 2, 2, 3, 3]
+    assert t.seen[:, 0].tolist() == [1, 3, 5, 9, 19, 35, 69, 133, 265, 521]
+    t = example.Tree([1] * 40)  # a chain: the bits of all before, over two words
+    assert t.seen.shape == (41, 2) and t.seen[40].tolist() == [-1, 511] and t.seen[31].tolist() == [-1, 0]
+    assert example.Tree([]).nodes == 1
+    with pytest.raises(ValueError):
+        example.Tree([2, 0])
+
+
+def test_generation_that_is_refused(monkeypatch):
+    from paper_2609_15039_gb300 import serving as example
+    for call in (lambda: example.generate_tree(None, None, None, [[1], []], [2], 1),
+                 lambda: example.generate_bounded(None, None, [[]], 1, 4, 1),
+                 lambda: example.generate_bounded(None, None, [[1]], 1, 4, 5),
+                 lambda: example.generate_bounded(None, None, [[1]], 1, 4, -1)):
+        with pytest.raises(ValueError):
+            call()
