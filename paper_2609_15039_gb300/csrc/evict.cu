@@ -354,6 +354,7 @@ __device__ void move_path(const PathArgs& a, const PagedSeq& s, int b, int count
 template <int ROW>
 __global__ void __launch_bounds__(kPathThreads) keep_path_kernel(const PathArgs a) {
   constexpr int LANES = ROW / 16;
+  pdl_wait();
   const int b = blockIdx.y, heads = a.cache.heads;
   const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
   int count = __ldg(a.accepted + b);
@@ -459,10 +460,6 @@ extern "C" spl_status spl_kv_keep_path(const spl_kv_cache* cache, float* score, 
   const int row = (int)cache->head_dim * (i8 ? 1 : 2);
   const int64_t tasks = (int64_t)a.cache.heads * (2 * row / 16 + 3);
   const dim3 grid((unsigned)ceil_div(tasks, kPathThreads), a.batch.seqs);
-  auto launch = [&](auto kernel) {
-    kernel<<<grid, kPathThreads, 0, stream>>>(a);
-    return launch_status();
-  };
-  return row == 256 ? launch(keep_path_kernel<256>)
-                    : (row == 128 ? launch(keep_path_kernel<128>) : launch(keep_path_kernel<64>));
+  return launch_pdl(row == 256 ? keep_path_kernel<256> : (row == 128 ? keep_path_kernel<128> : keep_path_kernel<64>), grid,
+                    dim3(kPathThreads), 0, stream, a);
 }

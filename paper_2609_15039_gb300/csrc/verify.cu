@@ -16,6 +16,7 @@
 #include <climits>
 
 #include "paged.cuh"
+#include "ptx.cuh"
 
 namespace spl {
 namespace {
@@ -109,14 +110,38 @@ struct Trip {
   __device__ __forceinline__ void load_random(const float* e, int base, int n) { load(e, base, n, 1.0f); }
 };
 
-// The race over n entries of one row, from v0 on; q null: the weights are p's own.  `first`: e of the thread's first trip.
+// A trip of the race: the weights w against c, of the entries from `base` on, of n; the whole warp.
 // Quotients are approximated within 2^-21 first; only those that may be their warp's largest are rounded (a rounded
 // quotient of every entry took 64 sequences of 8 drafts over 151936 entries 45 us).
+template <bool VEC>
+__device__ __forceinline__ void race_trip(Best& best, const Trip<VEC>& w, const Trip<VEC>& c, int base, int n, bool& positive) {
+  using T = Trip<VEC>;
+  constexpr float kLeast = 0x1p-60f, kMost = 0x1p60f;  // of e, where the approximations hold
+  float top = 0.f, heaviest = 0.f, least = c.x[0], most = c.x[0];
+#pragma unroll
+  for (int i = 0; i < T::N; ++i) {
+    heaviest = fmaxf(heaviest, w.x[i]);
+    least = fminf(least, c.x[i]);
+    most = fmaxf(most, c.x[i]);
+    top = fmaxf(top, w.x[i] * rcp_approx(c.x[i]));
+  }
+  positive |= heaviest > 0.0f;
+  // The warp's largest; infinite where the approximations may not hold, and then all quotients are rounded.
+  const float shown = least >= kLeast && most <= kMost ? fmaxf(top, best.ratio) : INFINITY;
+  const float all = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(shown)));
+  const float bound = all >= 0x1p-60f && all <= 0x1p100f ? all * (1.0f - 0x1p-18f) : -1.0f;
+  if (!(top < bound)) {
+#pragma unroll
+    for (int i = 0; i < T::N; ++i)
+      if (!(w.x[i] * rcp_approx(c.x[i]) < bound) && T::at(base, i) < n) best.look(w.x[i], c.x[i], T::at(base, i));
+  }
+}
+
+// The race over n entries of one row, from v0 on; q null: the weights are p's own.  `first`: e of the thread's first trip.
 template <bool VEC>
 __device__ unsigned long long race_row(const float* p, const float* q, const float* e, int64_t v0, int n,
                                        const Trip<VEC>& first, bool& positive) {
   using T = Trip<VEC>;
-  constexpr float kLeast = 0x1p-60f, kMost = 0x1p60f;  // of e, where the approximations hold
   const int mine = (VEC ? 4 : 1) * threadIdx.x;
   p += v0, e += v0;
   if (q) q += v0;
@@ -135,24 +160,7 @@ __device__ unsigned long long race_row(const float* p, const float* q, const flo
 #pragma unroll
       for (int i = 0; i < T::N; ++i) w.x[i] = fmaxf(__fsub_rn(w.x[i], b.x[i]), 0.0f);
     }
-    float top = 0.f, heaviest = 0.f, least = c.x[0], most = c.x[0];
-#pragma unroll
-    for (int i = 0; i < T::N; ++i) {
-      heaviest = fmaxf(heaviest, w.x[i]);
-      least = fminf(least, c.x[i]);
-      most = fmaxf(most, c.x[i]);
-      top = fmaxf(top, w.x[i] * rcp_approx(c.x[i]));
-    }
-    positive |= heaviest > 0.0f;
-    // The warp's largest; infinite where the approximations may not hold, and then all quotients are rounded.
-    const float shown = least >= kLeast && most <= kMost ? fmaxf(top, best.ratio) : INFINITY;
-    const float all = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(shown)));
-    const float bound = all >= 0x1p-60f && all <= 0x1p100f ? all * (1.0f - 0x1p-18f) : -1.0f;
-    if (!(top < bound)) {
-#pragma unroll
-      for (int i = 0; i < T::N; ++i)
-        if (!(w.x[i] * rcp_approx(c.x[i]) < bound) && T::at(base, i) < n) best.look(w.x[i], c.x[i], T::at(base, i));
-    }
+    race_trip<VEC>(best, w, c, base, n, positive);
     w = w2, b = b2, c = c2;
   }
   return best.key(v0);
@@ -257,7 +265,6 @@ struct TreeArgs {
   unsigned int* status;
 };
 constexpr int kMostBlocks = 16;  // of a cluster
-constexpr int kHeldNodes = 2;
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -274,71 +281,136 @@ __device__ __forceinline__ void store_in_block(unsigned long long* at, uint32_t 
   asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(v) : "memory");
 }
 
+// Where rows begin at 16-byte boundaries a ninth warp copies the slice into a ring in shared memory, trip after trip, and of
+// the next level the exponentials, which do not wait for the outcome.  Every warp decides by itself where the walk goes on.
+constexpr int kWarps = kThreads / 32, kTreeThreads = kThreads + 32, kRing = 4;
+constexpr uint32_t kPart = Trip<true>::SPAN * sizeof(float), kStage = 2 * kPart;  // of p and of e
+constexpr int kHeldNodes = 4;  // a lane
+
 template <bool VEC>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) verify_tree_kernel(const TreeArgs a, int64_t per_split, int blocks) {
-  __shared__ unsigned long long keys[kThreads / 32], bests[2][kMostBlocks];  // (of two levels in turn)
-  __shared__ int s_child[2];
+__global__ void __launch_bounds__(kTreeThreads, kBlocksPerSm) verify_tree_kernel(const TreeArgs a, int64_t per_split, int blocks) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ unsigned long long bests[2][kMostBlocks][kWarps];  // (of two levels in turn)
+  __shared__ __align__(8) uint64_t s_bars[2 * kRing];
+  using T = Trip<VEC>;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b = blockIdx.x / blocks;
-  const uint32_t rank = cluster_rank();
+  const uint32_t rank = cluster_rank(), bars = smem_u32(s_bars);  // full, empty
   const int64_t row0 = min(max((int64_t)__ldg(a.row_start + b), (int64_t)0), a.rows);
   const int64_t row1 = min(max((int64_t)__ldg(a.row_start + b + 1), row0), a.rows);
   const int nodes = (int)(row1 - row0);
-  const int64_t v0 = min(a.vocab, rank * per_split), v1 = min(a.vocab, v0 + per_split);
-  if (threadIdx.x < 2) s_child[threadIdx.x] = INT_MAX;
-  const float* e = a.e + (int64_t)b * a.levels * a.lde;  // of the level
-  auto load_first = [&](Trip<VEC>& t, int64_t from) {
-    t.load_random(e + from, (VEC ? 4 : 1) * threadIdx.x, (int)max((int64_t)0, min(kMostEntries, v1 - from)));
-  };
-  Trip<VEC> first;
-  if (nodes > 0) load_first(first, v0);
-  // A thread's nodes, in its registers where they are few.
-  int parent[kHeldNodes], held[kHeldNodes];
+  const int64_t v0 = min(a.vocab, rank * per_split);
+  const int n = (int)min(a.vocab - v0, per_split), trips = (n + T::SPAN - 1) / T::SPAN;
+  if (VEC && threadIdx.x < 2 * kRing) mbar_init(bars + 8u * threadIdx.x, threadIdx.x < kRing ? 2 : kWarps);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  int parent[kHeldNodes], held[kHeldNodes];  // a lane's nodes, where they are few
 #pragma unroll
   for (int u = 0; u < kHeldNodes; ++u) {
-    const int i = 1 + (int)threadIdx.x + u * kThreads;
+    const int i = 1 + lane + 32 * u;
     parent[u] = i < nodes ? __ldg(a.parent + row0 + i) : -1;
     held[u] = i < nodes ? __ldg(a.x + row0 + i) : -1;
   }
   cluster_sync();  // every block has begun: its shared memory may be written
-  int at = 0, depth = 0, token = -1;
+  pdl_trigger();   // (spl_kv_keep_path may be launched: it waits for the outcome)
+  const float* e = a.e + (int64_t)b * a.levels * a.lde + v0;  // of the level
+  int at = 0, depth = 0, token = -1, it = 0, ahead = 0;  // trips of the levels before; of the next one's, those whose e is under way
+  bool late = false;
+  auto stage_of = [&](int i) { return smem_u32(ring) + (uint32_t)(i % kRing) * kStage; };
+  auto full = [&](int i) { return bars + 8u * (i % kRing); };
+  auto empty = [&](int i) { return bars + 8u * (kRing + i % kRing); };
+  auto bytes_of = [&](int t) { return (uint32_t)(min(T::SPAN, n - t * T::SPAN) & ~3) * 4u; };  // what can be copied
+  auto copy = [&](int i, int t, uint32_t part, const float* from, bool wait) {  // one thread
+    if (wait && i >= kRing && !mbar_wait(empty(i), (uint32_t)(i / kRing - 1) & 1u, kWaitNs, nullptr)) late = true;
+    mbar_expect_tx(full(i), bytes_of(t));
+    if (bytes_of(t)) bulk_load(stage_of(i) + part, from + (int64_t)t * T::SPAN, bytes_of(t), full(i), l2_evict_first());
+  };
   for (; nodes > 0; ++depth) {  // every block of the cluster makes every turn
-    const float* p = a.p + (row0 + at) * a.ldp;
-    unsigned long long key = 0;
-    bool positive = false;
-    for (int64_t from = v0; from < v1; from += kMostEntries) {
-      if (from > v0) load_first(first, from);
-      key = max(key, race_row<VEC>(p, nullptr, e, from, (int)min(kMostEntries, v1 - from), first, positive));
+    const float* p = a.p + (row0 + at) * a.ldp + v0;
+    if (warp == kWarps) {
+      if (VEC && lane == 0) {
+        for (int t = 0; t < trips; ++t) {
+          if (t >= ahead) copy(it + t, t, kPart, e, true);
+          copy(it + t, t, 0u, p, false);
+        }
+        ahead = 0;
+        for (; depth + 1 < a.levels && ahead < min(trips, kRing); ++ahead) copy(it + trips + ahead, ahead, kPart, e + a.lde, true);
+      }
+      __syncwarp();
+    } else {
+      Best best;
+      bool positive = false;
+      const int mine = (VEC ? 4 : 1) * threadIdx.x;
+      for (int t = 0; t < trips; ++t) {
+        const int base0 = t * T::SPAN, some = min(T::SPAN, n - base0);
+        T w, c;
+        if constexpr (VEC) {
+          if (!mbar_wait_soon(full(it + t), (uint32_t)((it + t) / kRing) & 1u, kWaitNs, nullptr)) late = true;
+          const float* from = reinterpret_cast<const float*>(ring + (it + t) % kRing * kStage);
+#pragma unroll
+          for (int i = 0; i < T::N; i += 4) {
+            const int v = T::at(mine, i);
+            if (v < (some & ~3)) {
+              const float4 x = *reinterpret_cast<const float4*>(from + v), y = *reinterpret_cast<const float4*>(from + T::SPAN + v);
+              w.x[i] = x.x, w.x[i + 1] = x.y, w.x[i + 2] = x.z, w.x[i + 3] = x.w;
+              c.x[i] = y.x, c.x[i + 1] = y.y, c.x[i + 2] = y.z, c.x[i + 3] = y.w;
+            } else {  // past the last, or one of the last three
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                w.x[i + k] = v + k < some ? p[base0 + v + k] : 0.f;
+                c.x[i + k] = v + k < some ? e[base0 + v + k] : 1.f;
+              }
+            }
+          }
+          __syncwarp();  // every lane has read the stage
+          if (lane == 0) mbar_arrive(empty(it + t));
+        } else {
+          w.load(p, base0 + mine, n, 0.f);
+          c.load_random(e, base0 + mine, n);
+        }
+        race_trip<VEC>(best, w, c, base0 + mine, n, positive);
+      }
+      unsigned long long key = best.key(v0);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, o);
+        key = other > key ? other : key;
+      }
+      if (lane < blocks) store_in_block(&bests[depth & 1][rank][warp], lane, key);
     }
+    it += trips;
     e += a.lde;
-    if (depth + 1 < a.levels) load_first(first, v0);  // the next level's first entries do not wait for the outcome
-    key = block_max(key, keys);
-    key = __shfl_sync(0xffffffffu, key, 0);
-    if (threadIdx.x < blocks) store_in_block(&bests[depth & 1][rank], threadIdx.x, key);
     cluster_sync();
-    for (int r = 0; r < blocks; ++r) key = r == 0 ? bests[depth & 1][0] : max(key, bests[depth & 1][r]);
+    unsigned long long key = 0;
+    for (int i = lane; i < blocks * kWarps; i += 32) key = max(key, bests[depth & 1][i / kWarps][i % kWarps]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, o);
+      key = other > key ? other : key;
+    }
     token = key == 0 ? -1 : (int)(0xffffffffu - (uint32_t)key);  // 0: no entry took part
     if (token < 0 || depth + 1 == a.levels) break;
     // The first child that holds it.
     int child = INT_MAX;
 #pragma unroll
     for (int u = 0; u < kHeldNodes; ++u) {
-      const int i = 1 + (int)threadIdx.x + u * kThreads;
+      const int i = 1 + lane + 32 * u;
       if (i < nodes && parent[u] == at && held[u] == token) child = min(child, i);
     }
-    for (int i = 1 + threadIdx.x + kHeldNodes * kThreads; i < nodes; i += kThreads)
+    for (int i = 1 + lane + 32 * kHeldNodes; i < nodes; i += 32)
       if (__ldg(a.parent + row0 + i) == at && __ldg(a.x + row0 + i) == token) child = min(child, i);
     child = __reduce_min_sync(0xffffffffu, child);
-    if ((threadIdx.x & 31) == 0 && child != INT_MAX) atomicMin(&s_child[depth & 1], child);
-    __syncthreads();
-    child = s_child[depth & 1];
-    if (threadIdx.x == 0) s_child[(depth + 1) & 1] = INT_MAX;
-    __syncthreads();
     if (child == INT_MAX) break;
     if (rank == 0 && threadIdx.x == 0) a.path[b * a.ldpath + depth] = child;
     at = child;
   }
+  if (warp == kWarps && lane == 0)  // nothing is on its way when the block leaves
+    for (int t = 0; t < ahead; ++t) {
+      mbar_arrive(full(it + t));
+      mbar_wait(full(it + t), (uint32_t)((it + t) / kRing) & 1u, kDrainNs, nullptr);
+    }
+  if (late) atomicOr(a.status, kStatusTimeout);
   if (rank == 0) {
-    for (int d = depth + threadIdx.x; d < a.levels; d += kThreads) a.path[b * a.ldpath + d] = -1;
+    for (int d = depth + threadIdx.x; d < a.levels; d += kTreeThreads) a.path[b * a.ldpath + d] = -1;
     if (threadIdx.x == 0) {
       a.accepted[b] = depth;
       a.token[b] = token;
@@ -368,22 +440,25 @@ extern "C" spl_status spl_verify_tree(int32_t* accepted, int32_t* path, int64_t 
   unsigned int* status = device_status_word();
   if (!status) return SPL_ECUDA;
   // A cluster of the blocks of one wave that a sequence's share has, each with at least a trip of its threads' loads.
-  const int64_t most = std::min(ceil_div(vocab, (int64_t)4 * kThreads), (int64_t)kBlocksPerSm * device_sm_count() / seqs);
+  const int64_t most = std::max(std::min(ceil_div(vocab, (int64_t)4 * kThreads), (int64_t)kBlocksPerSm * device_sm_count() / seqs),
+                                ceil_div(vocab, kMostEntries));  // (of a block at most so many: 32-bit indexes)
   int blocks = 1;
   while (blocks < kMostBlocks && 2 * blocks <= most) blocks *= 2;
   const int64_t per_split = round_up(ceil_div(vocab, blocks), 4);
   const bool vec = ldp % 4 == 0 && lde % 4 == 0 && aligned16(P) && aligned16(e);
   const TreeArgs a = {accepted, path, token, P, e, x, parent, row_start, ldp, lde, ldpath, vocab, rows, (int)levels, status};
-  auto launch = [&](auto kernel, bool(&done)[kMaxDevices]) {
+  auto launch = [&](auto kernel, uint32_t smem, bool(&sized)[kMaxDevices], bool(&wide)[kMaxDevices]) {
+    if (!allow_shared(reinterpret_cast<const void*>(kernel), smem, sized)) return SPL_ECUDA;
     int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) return SPL_ECUDA;
-    if (device >= kMaxDevices || !done[device]) {
+    if (cudaGetDevice(&device) != cudaSuccess || device >= kMaxDevices) return SPL_ECUDA;
+    if (!wide[device]) {
       if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SPL_ECUDA;
-      if (device < kMaxDevices) done[device] = true;
+      wide[device] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(blocks * seqs));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(kTreeThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -395,8 +470,9 @@ extern "C" spl_status spl_verify_tree(int32_t* accepted, int32_t* path, int64_t 
     note_launches(1);
     return err == cudaSuccess ? SPL_OK : SPL_ECUDA;
   };
-  static bool done[2][kMaxDevices] = {};
-  return vec ? launch(verify_tree_kernel<true>, done[0]) : launch(verify_tree_kernel<false>, done[1]);
+  static bool sized[2][kMaxDevices] = {}, wide[2][kMaxDevices] = {};
+  return vec ? launch(verify_tree_kernel<true>, kRing * kStage, sized[0], wide[0])
+             : launch(verify_tree_kernel<false>, 0, sized[1], wide[1]);
 }
 
 extern "C" size_t spl_verify_drafts_workspace_bytes(int64_t seqs) {

@@ -376,6 +376,7 @@ __global__ void __launch_bounds__(kSumThreads, 6) weigh_sum_kernel(const __grid_
       }
     }
   }
+  pdl_wait();  // (of a block without keys: this kernel may not end before the scores' one)
 }
 
 template <int D, bool I8>
@@ -398,7 +399,7 @@ struct Shape {
   size_t s, parts, bytes;
 };
 Shape shape_of(const PagedCache& c, const PagedBatch& b, const spl_kv_batch* batch, int64_t q_heads, int head_dim, bool i8) {
-  Shape x;
+  Shape x = {};
   x.few = batch->max_rows * (q_heads / c.heads) <= few_rows(i8) &&
           (double)b.rows * (double)q_heads * (double)(b.max_pages << c.page_shift) * 4 <= (double)kMostScores;
   if (!x.few) {

@@ -684,3 +684,122 @@ def test_a_step_over_a_bounded_cache(spl, fmt):
     keep = 32
     check_evict(c, score.clone(), keep, 8)
     assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+def test_one_workspace_for_all(spl):
+    """Attention, weights and eviction in turn on one workspace, with a product's and graphs': the same bits every time, and
+    the arrival counters stay zero."""
+    a = Case(spl, [(1, 900), (1, 1500)], (8, 2, 128), "f16", 64, seed=1)
+    b = many(Case(spl, [(130, 500), (60, 700)], (4, 2, 64), "i8", 16, seed=2))
+    for c in (a, b):
+        c.fill()
+    keep = 400
+    ws = spl.workspace(max(max(spl.spl_paged_attention_workspace_bytes(c.cache, c.batch(), c.hq),
+                               spl.spl_kv_weigh_workspace_bytes(c.cache, c.batch(), c.hq),
+                               spl.spl_kv_evict_workspace_bytes(c.cache, c.batch(), keep)) for c in (a, b)))
+    qs = [torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV) for c in (a, b)]
+    batches = [c.batch() for c in (a, b)]
+    outs = [torch.empty_like(q) for q in qs]
+    scores = [scores_for(c) for c in (a, b)]
+    lens = [i32([0, 0]) for _ in range(2)]
+
+    def step(i, c):
+        scores[i].fill_(0.5)
+        spl.spl_paged_attention(outs[i], qs[i], c.cache, batches[i], c.hq, workspace=ws)
+        spl.spl_kv_weigh(scores[i], qs[i], c.cache, batches[i], c.hq, workspace=ws)
+        return outs[i], scores[i]
+
+    want = []
+    for i, c in enumerate((a, b)):
+        want.append([t.clone() for t in step(i, c)])
+    graphs = []
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        for i, c in enumerate((a, b)):
+            step(i, c)
+    s.synchronize()
+    for i, c in enumerate((a, b)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            step(i, c)
+    for turn in range(3):
+        for i in (0, 1, 1, 0):
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i][0]) and torch.equal(raw(scores[i]), raw(want[i][1]))
+    for i, c in enumerate((a, b)):  # (moves the caches' tokens: last)
+        spl.spl_kv_evict(c.cache, scores[i], batches[i], keep, 16, lens[i], workspace=ws)
+        assert lens[i].tolist() == [keep, keep]
+    assert int(ws[:65536].count_nonzero()) == 0
+    assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+def test_offsets_past_32_bits(spl, fmt):
+    """Tokens on the last pages of a pool of more than 4 GB of keys: the bits of a small pool's."""
+    seqs, heads, page = [(20, 300), (1, 150), (40, 90)], (4, 2, 64), 256
+    small = Case(spl, seqs, heads, fmt, page, seed=21)
+    small.fill()
+    big = Case(spl, seqs, heads, fmt, page, seed=21)
+    pages = (9 << 28) // (2 * page * 64)  # 2.4e9 elements
+    big.cache = spl.KVCache.empty(pages, 2, 64, page, fmt)
+    big.table = np.where(big.table < small.cache.pages, big.table + pages - small.cache.pages, pages + 7).astype(np.int32)
+    big.fill()
+    last = slice(pages - small.cache.pages, pages)
+    g = np.random.default_rng(2)
+    masks = [masks_of(random_tree(g, r)) for r, _ in seqs]
+    score = torch.rand(tuple(small.cache.k.shape[:3]), device=DEV)
+    wide = torch.empty(tuple(big.cache.k.shape[:3]), device=DEV)
+    wide[last] = score
+    q = torch.as_tensor(small.q.reshape(small.rows, -1)).to(DEV)
+    for kernel in (few, many):
+        assert np.array_equal(attend_tree(kernel(small), masks, 2), attend_tree(kernel(big), masks, 2))
+        spl.spl_kv_weigh(score, q, small.cache, small.batch(), 4)
+        spl.spl_kv_weigh(wide, q, big.cache, big.batch(), 4)
+        assert torch.equal(raw(wide[last]), raw(score))
+    path, accepted, lens = i32([[1, 4, 9], [-1, -1, -1], [3, 7, 39]]), i32([3, 0, 3]), i32([0, 0, 0])
+    for c, sc in ((small, score), (big, wide)):
+        spl.spl_kv_keep_path(c.cache, c.batch(), path, accepted, score=sc)
+        spl.spl_kv_evict(c.cache, sc, c.batch(), 100, 10, lens)
+    used = sorted(set(int(p) for b, (_, n) in enumerate(seqs) for p in small.table[b, :-(-n // page)]))
+    for name in ("k", "v", "k_scale", "v_scale"):
+        x, y = getattr(small.cache, name), getattr(big.cache, name)
+        if x is not None:
+            assert torch.equal(raw(y[last][used]), raw(x[used])), name
+    assert torch.equal(raw(wide[last][used]), raw(score[used]))
+    assert spl.spl_get_device_status() == spl.SPL_OK
+    del big, wide
+    torch.cuda.empty_cache()
+
+
+def test_decisions_follow_their_stream(spl):
+    """Probabilities and trees made on a stream that is still busy, an eviction and a path behind them in a graph."""
+    p, x, parents, e = tree_draws(8, [12, 5], 5003, 5)
+    want = [serving.verify_tree(p[b], x[b], parents[b], e[b]) for b in range(2)]
+    c = Case(spl, [(12, 60), (5, 40)], (2, 2, 64), "f16", 16, seed=3)
+    c.fill()
+    before = c.cache.k.clone()
+    flat = lambda parts, t: torch.as_tensor(np.concatenate(parts).astype(t)).to(DEV)  # noqa: E731
+    P, E, X, up = flat(p, np.float32), torch.as_tensor(e.reshape(-1, 5003)).to(DEV), flat(x, np.int32), flat(parents, np.int32)
+    accepted, token, path = i32([0, 0]), i32([0, 0]), i32([[0] * 5] * 2)
+    batch, s = c.batch(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        late = P.clone()
+        spl.spl_verify_tree(accepted, path, token, late, X, up, E, batch.row_start)
+        spl.spl_kv_keep_path(c.cache, batch, path, accepted)
+    s.synchronize()
+    assert accepted.tolist() == [len(w) for w, _ in want] and token.tolist() == [t for _, t in want]
+    moved = c.cache.k.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        spl.spl_verify_tree(accepted, path, token, P, X, up, E, batch.row_start)
+        spl.spl_kv_keep_path(c.cache, batch, path, accepted)
+    for _ in range(2):
+        c.cache.k.copy_(before)
+        accepted.fill_(-3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(raw(c.cache.k), raw(moved)) and accepted.tolist() == [len(w) for w, _ in want]
+    assert spl.spl_get_device_status() == spl.SPL_OK
