@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const int e = fp16_row_exponent(top);
-    const float up = pow2f(e);
+    const float up = w.scale_log2 < 0.f ? -pow2f(e) : pow2f(e);  // the scale's sign goes into q
     uint32_t h0, l0, h1, l1;
     split_f16(v.x * up, v.y * up, h0, l0);
     split_f16(v.z * up, v.w * up, h1, l1);
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
     const int64_t row = (int64_t)(head / w.group) * a.total + token * w.group + head % w.group;
     reinterpret_cast<uint2*>(a.q_hi + row * D)[at] = make_uint2(h0, h1);
     reinterpret_cast<uint2*>(a.q_lo + row * D)[at] = make_uint2(l0, l1);
-    if (at == 0) a.rows[row].x = w.scale_log2 * pow2f(-e);
+    if (at == 0) a.rows[row].x = fabsf(w.scale_log2) * pow2f(-e);
   }
 }
 
@@ -476,10 +476,14 @@ struct Kernel {
         const int at = key0 + KEY_STEP * k;
         const uint32_t v[4] = {q[k].x ^ 0x80808080u, q[k].y ^ 0x80808080u, q[k].z ^ 0x80808080u, q[k].w ^ 0x80808080u};
         const uint32_t row = panel + at * 128;
-        st_shared16(row + ((c0 ^ (at & 7)) << 4), make_uint4(i8_pair(v[0], 0x4140u), i8_pair(v[0], 0x4342u),
-                                                             i8_pair(v[1], 0x4140u), i8_pair(v[1], 0x4342u)));
-        st_shared16(row + (((c0 + 1) ^ (at & 7)) << 4), make_uint4(i8_pair(v[2], 0x4140u), i8_pair(v[2], 0x4342u),
-                                                                   i8_pair(v[3], 0x4140u), i8_pair(v[3], 0x4342u)));
+        // (the upper panel's threads begin with their second chunk: the eight threads of a key then meet no bank twice)
+        const bool swap = part >= 4;
+        const uint32_t w0 = swap ? v[2] : v[0], w1 = swap ? v[3] : v[1], w2 = swap ? v[0] : v[2], w3 = swap ? v[1] : v[3];
+        const int first = swap ? c0 + 1 : c0;
+        st_shared16(row + ((first ^ (at & 7)) << 4), make_uint4(i8_pair(w0, 0x4140u), i8_pair(w0, 0x4342u),
+                                                                i8_pair(w1, 0x4140u), i8_pair(w1, 0x4342u)));
+        st_shared16(row + (((first ^ 1) ^ (at & 7)) << 4), make_uint4(i8_pair(w2, 0x4140u), i8_pair(w2, 0x4342u),
+                                                                      i8_pair(w3, 0x4140u), i8_pair(w3, 0x4342u)));
       }
       st_shared4(smem + L::SCALE + 4u * (held % kNotes * kTile + i), __float_as_uint(scale));
       if (lane == 0) st_shared4(smem + L::GONE + 16u * (held % kNotes) + 4u * (i >> 5), gone);
@@ -552,6 +556,17 @@ struct Kernel {
   }
 
   // ---------------------------------------------------------------- epilogue
+  static __device__ __forceinline__ void mul2(uint32_t& a, uint32_t& b, uint32_t x, uint32_t y) {
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tmul.rn.f32x2 p, p, q;\n\t"
+        "mov.b64 {%0, %1}, p;\n\t}"
+        : "+r"(a), "+r"(b)
+        : "r"(x), "r"(y));
+  }
+  static __device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+  }
   // The 128 scores of a thread's lane, 32 at a time, the load of some beside the work on those before.
   template <class Take>
   __device__ void over_chunks(uint32_t ts, Take take) const {
@@ -590,16 +605,14 @@ struct Kernel {
             const uint32_t note = smem + L::GONE + 16u * (key % kNotes);
             const uint4 gone = ld_shared16(note);
             const bool edge = j0 < y.all_lo || j0 + kTile > y.all_hi || (gone.x | gone.y | gone.z | gone.w) != 0;
+            const unsigned long long scale2 = p2(scale, scale);
             over_chunks(lanes + 128u * place, [&](int c, uint32_t (&r)[32]) {
-              float s[32];
-#pragma unroll
-              for (int k = 0; k < 32; ++k) s[k] = __uint_as_float(r[k]) * scale;
               if constexpr (I8) {
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) {
                   const uint4 w = ld_shared16(smem + L::SCALE + 4u * (key % kNotes * kTile + 32 * c + k));
-                  s[k] *= __uint_as_float(w.x), s[k + 1] *= __uint_as_float(w.y);
-                  s[k + 2] *= __uint_as_float(w.z), s[k + 3] *= __uint_as_float(w.w);
+                  mul2(r[k], r[k + 1], w.x, w.y);
+                  mul2(r[k + 2], r[k + 3], w.z, w.w);
                 }
               }
               if (edge) {
@@ -607,21 +620,36 @@ struct Kernel {
                 const int from = lo - j0 - 32 * c, to = hi - j0 - 32 * c;
 #pragma unroll
                 for (int k = 0; k < 32; ++k)
-                  if (k < from || k >= to || (g >> k & 1u)) s[k] = -INFINITY;
+                  if (k < from || k >= to || (g >> k & 1u)) r[k] = 0xff800000u;
               }
-              float top[4] = {s[0], s[1], s[2], s[3]};
+              float top[2] = {__uint_as_float(r[0]), __uint_as_float(r[1])};
 #pragma unroll
-              for (int k = 4; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], s[k]);
-              const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+              for (int k = 2; k < 32; k += 4) {
+                top[0] = max3(top[0], __uint_as_float(r[k]), __uint_as_float(r[k + 1]));
+                if (k + 3 < 32) top[1] = max3(top[1], __uint_as_float(r[k + 2]), __uint_as_float(r[k + 3]));
+              }
+              float t = fmaxf(top[0], top[1]);
+              t = t == -INFINITY ? t : t * scale;
               if (t > m) {
                 l *= exp2_approx(m - t);
                 m = t;
               }
-              const float base = m == -INFINITY ? 0.f : m;
-              float sum[4] = {0.f, 0.f, 0.f, 0.f};
+              const float base = m == -INFINITY ? 0.f : -m;
+              const unsigned long long base2 = p2(base, base);
+              unsigned long long sum[2] = {p2(0.f, 0.f), p2(0.f, 0.f)};
 #pragma unroll
-              for (int k = 0; k < 32; ++k) sum[k & 3] += exp2_approx(s[k] - base);
-              l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+              for (int k = 0; k < 32; k += 2) {
+                float t0, t1;
+                up2(fma2(p2(__uint_as_float(r[k]), __uint_as_float(r[k + 1])), scale2, base2), t0, t1);
+                if (edge) {  // (-inf times a scale of 0)
+                  t0 = r[k] == 0xff800000u ? -INFINITY : t0;
+                  t1 = r[k + 1] == 0xff800000u ? -INFINITY : t1;
+                }
+                sum[k / 2 & 1] = add2(sum[k / 2 & 1], p2(exp2_approx(t0), exp2_approx(t1)));
+              }
+              float s0, s1;
+              up2(add2(sum[0], sum[1]), s0, s1);
+              l += s0 + s1;
             });
             tc_fence_before();
             arrive(L::kSFree + place);

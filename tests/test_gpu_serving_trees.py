@@ -743,6 +743,7 @@ def test_offsets_past_32_bits(spl, fmt):
     big = Case(spl, seqs, heads, fmt, page, seed=21)
     pages = (9 << 28) // (2 * page * 64)  # 2.4e9 elements
     big.cache = spl.KVCache.empty(pages, 2, 64, page, fmt)
+    big.poison()
     big.table = np.where(big.table < small.cache.pages, big.table + pages - small.cache.pages, pages + 7).astype(np.int32)
     big.fill()
     last = slice(pages - small.cache.pages, pages)
