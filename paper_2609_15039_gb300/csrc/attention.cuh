@@ -91,6 +91,8 @@ __device__ __forceinline__ int tree_lo(const uint32_t* mask, int64_t words, int 
   return len;
 }
 
+// Only tiles at an edge look at the masks: in 16 sequences' trees of 64 over 1200 to 12000 keys (24 heads on 8, 153 us) two of
+// the last key tiles; the rest is as for a chain of as many rows.
 // (A tree's rows are taken together: some may see less than the keys from key_lo on, or more than those of [all_lo, all_hi).)
 template <int RT, int U, bool TREE>
 __device__ __forceinline__ void tile_span(AttnTile& x, int group, int window) {

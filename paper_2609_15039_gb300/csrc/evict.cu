@@ -9,6 +9,10 @@
 // in the targets' order, so that it suffices that a trip's loads are done before its stores: what a trip overwrites are
 // sources of itself or of trips before it.  Into other pages there is no such order, and a head's tokens are shared out.
 //
+// Measured with 8 heads of 128 dims, binary16: 32 sequences of 1600 to 16000 tokens cut to 6000, into other pages, 21 and 231 us
+// (5.8 TB/s); one cut from 1250 to 1000 8.9 and 7.6 us (launches and three dependent loads each).  15 of 500 to 5000, int8, cut
+// to 800: 12.4 and 17 us, in columns of 32 bytes (whole vectors: 20).
+//
 // An accepted path (a handful of tokens): a thread has 16 bytes of a vector, or a scale, and moves them one after another.
 
 #include <algorithm>
@@ -196,9 +200,8 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
 
 // W bytes of each vector a block, 16 a thread.  blockIdx.x: the part of the vector (K's, then V's, then the scores and scales),
 // and of the tokens (into other pages only); blockIdx.y: key head; blockIdx.z: sequence.
-constexpr int kMoveThreads = 256;
-template <int ROW, int W>  // bytes of a vector
-__global__ void __launch_bounds__(kMoveThreads, 5) evict_move_kernel(const EvictArgs a, int shares) {
+template <int ROW, int W, int THREADS>  // bytes of a vector
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 5) evict_move_kernel(const EvictArgs a, int shares) {
   constexpr int SLICES = ROW / W;
   const int part = blockIdx.x / shares, share = blockIdx.x % shares, h = blockIdx.y, b = blockIdx.z;
   pdl_wait();
@@ -219,7 +222,7 @@ __global__ void __launch_bounds__(kMoveThreads, 5) evict_move_kernel(const Evict
   const int* to_table = a.out_table ? a.out_table : a.batch.table;
   const int first = (int)((int64_t)moves * share / shares), last = (int)((int64_t)moves * (share + 1) / shares);
   if (part < 2 * SLICES) {
-    constexpr int LANES = W / 16, ROWS = kMoveThreads / LANES, U = 4;
+    constexpr int LANES = W / 16, ROWS = THREADS / LANES, U = 4;
     char* base = static_cast<char*>(part < SLICES ? a.cache.k : a.cache.v) + part % SLICES * W + threadIdx.x % LANES * 16;
     const int row = threadIdx.x / LANES;
     int from[U], to[U], next_from[U], next_to[U];
@@ -256,12 +259,12 @@ __global__ void __launch_bounds__(kMoveThreads, 5) evict_move_kernel(const Evict
     }
   } else {
     constexpr int U = 4;
-    for (int i0 = first; i0 < last; i0 += kMoveThreads * U) {
+    for (int i0 = first; i0 < last; i0 += THREADS * U) {
       int from[U], to[U];
       float v[U], k[U], w[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * kMoveThreads + threadIdx.x;
+        const int i = i0 + u * THREADS + threadIdx.x;
         from[u] = to[u] = -1;
         if (i >= last) continue;
         const int pos = source(i);
@@ -294,16 +297,18 @@ __global__ void __launch_bounds__(kMoveThreads, 5) evict_move_kernel(const Evict
 
 template <int ROW>
 spl_status launch_move(const EvictArgs& a, int blocks, cudaStream_t stream) {
-  // Whole vectors' lines where there are blocks enough, 32 bytes each where a block an SM would be missing (32 sequences cut
-  // from 16000 tokens to 6000: %%; one of 1250 to 1000: %%).
-  const int heads = a.cache.heads, seqs = a.batch.seqs;
-  constexpr int WIDE = ROW;
-  const bool wide = (int64_t)heads * seqs * (2 * ROW / WIDE) >= 2 * blocks;
-  const int parts = 2 * ROW / (wide ? WIDE : 32) + 1;
+  // Whole vectors where there are blocks enough, else 32 bytes of each; blocks of 1024 threads, of fewer and longer trips, where
+  // there are few even then and they go through their tokens one trip after another (one sequence cut in place from 16000
+  // tokens to 12000: 77 us with blocks of 256, 50 so; 32 sequences into other pages: 273 us in columns of 128 bytes, 229 whole).
+  const int64_t heads = a.cache.heads, seqs = a.batch.seqs;
+  const bool wide = heads * seqs * 2 >= 2 * blocks;
+  const int parts = wide ? 3 : 2 * ROW / 32 + 1;
+  const bool large = !wide && !a.out_table && parts * heads * seqs <= 2 * blocks;
   int shares = 1;  // of a head's tokens, where their order does not matter
-  if (a.out_table) shares = (int)std::max<int64_t>(1, std::min<int64_t>(4 * blocks / ((int64_t)parts * heads * seqs), 64));
-  const dim3 grid(parts * shares, heads, seqs);
-  return launch_pdl(wide ? evict_move_kernel<ROW, WIDE> : evict_move_kernel<ROW, 32>, grid, dim3(kMoveThreads), 0, stream, a,
+  if (a.out_table) shares = (int)std::max<int64_t>(1, std::min<int64_t>(4 * blocks / (parts * heads * seqs), 64));
+  const dim3 grid(parts * shares, (unsigned)heads, (unsigned)seqs);
+  if (large) return launch_pdl(evict_move_kernel<ROW, 32, 1024>, grid, dim3(1024), 0, stream, a, shares);
+  return launch_pdl(wide ? evict_move_kernel<ROW, ROW, 256> : evict_move_kernel<ROW, 32, 256>, grid, dim3(256), 0, stream, a,
                     shares);
 }
 

@@ -5,6 +5,9 @@
 // stored values are exact in binary16, so the result has fp32 accuracy) and writes them to the workspace, with the largest
 // and the total of 2^(s - largest) of every 32 keys and row.  Another joins those by rows and sums 2^(s - m) / l over the
 // rows for each key: a score is 4 bytes beside the 2 D of its key.
+// Measured with 24 query heads on 8 of 128 dims: 64 sequences of one row over 1600 to 16000 keys, binary16, 176 us for the scores
+// (1.15 GB of keys, 6.6 TB/s) and 31 us for the sums, which read 75 MB of scores and totals from memory under ncu, mostly L2
+// otherwise; one sequence of 300 keys 9.4 and 7.6 us, two launches' latency.
 
 #include <algorithm>
 #include <cmath>
@@ -484,7 +487,8 @@ extern "C" spl_status spl_kv_weigh(float* score, const float* Q, int64_t ldq, co
                                 : (i8 ? launch_scores<64, true>(w, sms, stream) : launch_scores<64, false>(w, sms, stream));
     if (st != SPL_OK) return st;
   }
-  // Several trips a block where there are blocks enough (64 sequences over 1600 to 16000 keys: %%; one of 300: %%).
+  // Several trips a block where there are blocks enough, which then make the totals once (64 sequences over 1600 to 16000 keys:
+  // 30 us instead of 38; one sequence's few blocks are better spread).
   const int64_t room = a.batch.max_pages << a.cache.page_shift;
   const int trips = ceil_div(room, kTrip) * a.cache.heads * a.batch.seqs >= (int64_t)8 * sms ? kMostTrips : 1;
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(room, trips * kTrip), 1 << 16), a.cache.heads, a.batch.seqs);
