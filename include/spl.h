@@ -692,8 +692,8 @@ spl_status spl_tree_attention(float* out, int64_t ldo, const float* Q, int64_t l
  * what their slots held does not count.  A row that sees a NaN or infinity makes
  * the scores of the keys that it sees NaN; one that sees nothing adds nothing;
  * slots of no token, and of pages outside the pool, are left as they are.  A page
- * holds tokens of one sequence of the batch only.  Sums are fp32, in the rows'
- * order.  Q [rows, q_heads head_dim] as there; 0 <= decay <= 1.  Workspace:
+ * holds tokens of one sequence of the batch only.  Sums are fp32, in an order that
+ * does not depend on timing.  Q [rows, q_heads head_dim] as there; 0 <= decay <= 1.  Workspace:
  * spl_kv_weigh_workspace_bytes, any contents; its first 64 KiB are not touched,
  * so the product workspace can be shared.  Errors: as spl_paged_attention,
  * EINVAL for a decay outside [0, 1]. */

@@ -804,3 +804,46 @@ def test_decisions_follow_their_stream(spl):
         torch.cuda.synchronize()
         assert torch.equal(raw(c.cache.k), raw(moved)) and accepted.tolist() == [len(w) for w, _ in want]
     assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+def test_rows_behind_the_last_sequence(spl, fmt):
+    """A padded batch: rows of no sequence, NaN in theirs, are left as they were and reach nobody."""
+    g = np.random.default_rng(3)
+    for kernel in (few, many):
+        c = kernel(Case(spl, [(9, 200), (40, 90), (0, 33)], (4, 2, 128), fmt, 16, seed=14))
+        c.fill()
+        masks = [masks_of(random_tree(g, r)) for r, _ in c.seqs]
+        want, score = attend_tree(c, masks, 2), check_weights(c)
+        extra, batch = 13, c.batch()
+        padded = spl.KVBatch(batch.row_start, batch.kv_len, batch.page_table, c.rows + extra, 1 if kernel is few else 1 << 24)
+        q = torch.full((c.rows + extra, 4 * 128), float("nan"), device=DEV)
+        q[:c.rows] = torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV)
+        seen = torch.full((c.rows + extra, 2), -1, dtype=torch.int32, device=DEV)
+        seen[:c.rows] = words_of(sum(masks, []), 2)
+        out = torch.full_like(q, 7.0)
+        spl.spl_tree_attention(out, q, c.cache, padded, seen, 4)
+        assert np.array_equal(out[:c.rows].cpu().numpy().reshape(want.shape), want) and bool((out[c.rows:] == 7.0).all())
+        again = scores_for(c, 0.75)
+        spl.spl_kv_weigh(again, q, c.cache, padded, 4)
+        assert torch.equal(raw(again), raw(score))
+        assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("kernel", [few, many], ids=["few", "many"])
+def test_weigh_as_many_sequences_as_there_may_be(spl, kernel):
+    g = np.random.default_rng(7)
+    seqs = [(int(r), int(r + n)) for r, n in zip(g.integers(0, 3, 4096), g.integers(0, 40, 4096))]
+    seqs[0] = seqs[-1] = (40, 300)
+    c = kernel(Case(spl, seqs, (4, 2, 64), "f16", 16, seed=7))
+    c.fill()
+    check_weights(c, decay=0.5)
+
+
+def test_evict_as_many_sequences_as_there_may_be(spl):
+    g = np.random.default_rng(8)
+    seqs = [(0, int(n)) for n in g.integers(0, 60, 4096)]
+    c = Case(spl, seqs, (2, 2, 64), "i8", 16, seed=8)
+    c.fill()
+    score = torch.as_tensor(g.random(tuple(c.cache.k.shape[:3])).astype(np.float32)).to(DEV)
+    check_evict(c, score, 20, 4, alias=True)
