@@ -51,6 +51,7 @@ constexpr int kPieces = 4;
 struct WeighPlan {
   int range, tiles;
   int64_t pieces[2];
+  unsigned long long taken[2];  // beyond every block's first
 };
 
 struct TcArgs {
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
     __syncthreads();
     if (threadIdx.x == 0)
       *a.plan = {chosen[0], chosen[1], {(int64_t)sums[chosen[0] - 1] * w.cache.heads,
-                                        (int64_t)sums[kMostRange + chosen[1] - 1] * w.cache.heads}};
+                                        (int64_t)sums[kMostRange + chosen[1] - 1] * w.cache.heads}, {0, 0}};
     // Each sequence's first piece: sums before it, a run of sequences a thread.
     const int per = (seqs + kPrepThreads - 1) / kPrepThreads, b0 = min(seqs, per * (int)threadIdx.x), b1 = min(seqs, b0 + per);
     auto count = [&](int b, int pass) {
@@ -243,8 +244,8 @@ struct Kernel {
   Piece* pieces;
 
   __device__ uint32_t bar(int i) const { return smem + L::BARS + 8u * i; }
-  __device__ bool wait(int i, uint32_t parity) const {
-    return __all_sync(0xffffffffu, mbar_wait_soon(bar(i), parity, kWaitNs, abort));
+  __device__ bool wait(int i, uint32_t parity, unsigned long long ns = kWaitNs) const {
+    return __all_sync(0xffffffffu, mbar_wait_soon(bar(i), parity, ns, abort));
   }
   __device__ void arrive(int i) const {  // one for the warp, after all its lanes' work
     __syncwarp();
@@ -301,8 +302,11 @@ struct Kernel {
   // The k-th piece of the block, by warp 1.
   __device__ bool hand_out(int k) const {
     const int lane = threadIdx.x & 31, seqs = a.w.batch.seqs, group = a.w.group;
-    if (k >= kPieces && !wait(L::kPieceFree + k % kPieces, (uint32_t)(k / kPieces - 1) & 1u)) return false;
-    const int64_t item = blockIdx.x + (int64_t)k * gridDim.x;
+    if (k >= kPieces && !wait(L::kPieceFree + k % kPieces, (uint32_t)(k / kPieces - 1) & 1u, kLoaderNs)) return false;
+    // The next that nobody has: pieces differ in size, and which block has one does not matter to any result.
+    unsigned long long taken = 0;
+    if (k > 0 && lane == 0) taken = atomicAdd(&a.plan->taken[SUM], 1ull);
+    const int64_t item = k == 0 ? (int64_t)blockIdx.x : (int64_t)gridDim.x + (int64_t)__shfl_sync(0xffffffffu, taken, 0);
     Piece x = {};
     x.last = 1;
     if (item < a.plan->pieces[SUM]) {
@@ -355,7 +359,9 @@ struct Kernel {
     const int page = paged_page(a.w.cache, a.w.batch, x.b, j);
     return page >= 0 ? page : kGone;
   }
-  // Warp 1.  The pieces are handed out kPieces ahead of its own walk over them.
+  // Warp 1.  In the second pass it begins while the first one's last blocks and the join are at work, for which the others wait
+  // without spinning: its own waits may last longer.
+  static constexpr unsigned long long kLoaderNs = SUM ? 20 * kWaitNs : kWaitNs;
   __device__ void loader() const {
     const int lane = threadIdx.x & 31, shift = a.w.cache.page_shift;
     const int box = min(kTile, 1 << shift), boxes = kTile / box;
@@ -374,7 +380,7 @@ struct Kernel {
         const Span y = span(x, rt);
         if (y.k0 >= y.k1) continue;
         const int q = tiles % kQStages;
-        if (tiles >= kQStages) ok = wait(L::kQEmpty + q, (uint32_t)(tiles / kQStages - 1) & 1u);
+        if (tiles >= kQStages) ok = wait(L::kQEmpty + q, (uint32_t)(tiles / kQStages - 1) & 1u, kLoaderNs);
         if (!ok) break;
         if (lane == 0) {
           const uint32_t to = smem + L::Q + (uint32_t)q * 2u * L::TILE;
@@ -398,7 +404,7 @@ struct Kernel {
         for (int kt = y.k0; ok && kt < y.k1; ++kt) {
           const int64_t next = look_up(kt + 1);
           const int stage = keys % L::STAGES;
-          if (keys >= L::STAGES) ok = wait(L::kKEmpty + stage, (uint32_t)(keys / L::STAGES - 1) & 1u);
+          if (keys >= L::STAGES) ok = wait(L::kKEmpty + stage, (uint32_t)(keys / L::STAGES - 1) & 1u, kLoaderNs);
           if (!ok) break;
           const unsigned gone = __ballot_sync(0xffffffffu, slot == kGone);
           if (lane < 4) {  // a bit a key
@@ -833,7 +839,8 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  pdl_wait();
+  // (the plan is from the launch before the last: the second pass's loader need not wait)
+  if (!SUM || warp != 1) pdl_wait();
   pdl_trigger();
   const Kernel<D, I8, SUM> k{a, map_hi, map_lo, map_k, smem, __shfl_sync(0xffffffffu, *tmem_slot, 0), abort,
                              reinterpret_cast<Piece*>(base + L::PIECES)};
@@ -861,30 +868,45 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
 // Between the passes, a thread a row: its lse, of rows that see nothing one that leaves nothing.
 constexpr int kJoinThreads = 256;
 __global__ void __launch_bounds__(kJoinThreads) weigh_join_rows_kernel(const __grid_constant__ TcArgs a) {
-  pdl_wait();
   pdl_trigger();
-  const int64_t row = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
-  if (row >= a.total * a.w.cache.heads) return;
-  const int64_t token = row % a.total / a.w.group;
-  int b = 0, end = a.w.batch.seqs;  // the last sequence that begins at or before the token
-  while (end - b > 1) {
-    const int mid = (b + end) >> 1;
-    if (__ldg(a.w.batch.row_start + mid) <= token) b = mid;
-    else end = mid;
-  }
-  const PagedSeq s = paged_seq(a.w.batch, a.w.cache.page_shift, b);
-  const int64_t i = token - s.row0;
+  const int64_t row0 = (int64_t)blockIdx.x * kJoinThreads + (threadIdx.x & ~31), row = row0 + (threadIdx.x & 31);
+  const int64_t all = a.total * a.w.cache.heads;
+  const int group = a.w.group;
+  // What the first pass does not write is looked up while it ends: the row's sequence and the keys that it sees.
   int lo = 0, hi = 0;
-  if (i >= 0 && i < s.n) row_keys(s, a.w.window, (int)i, lo, hi);
-  float m = -INFINITY, l = 0.f;
-  if (lo < hi) {
-    const int keys = a.plan->range * kTile;
-    for (int split = lo / keys; split <= (hi - 1) / keys; ++split) {
-      const float4 v = *reinterpret_cast<const float4*>(a.parts + (row * a.splits + split) * 2);
-      const float top = fmaxf(fmaxf(m, v.x), v.z), base = top == -INFINITY ? 0.f : top;
-      l = l * exp2_approx(m - base) + (v.y * exp2_approx(v.x - base) + v.w * exp2_approx(v.z - base));
-      m = top;
+  const int64_t first = quotient(min(row0, all - 1) % a.total, group);  // the warp's first token
+  int b = paged_find(a.w.batch.row_start, a.w.batch.seqs, first);
+  if (row < all) {
+    const int64_t token = quotient(row % a.total, group);
+    if (token < first || (b + 1 < a.w.batch.seqs && __ldg(a.w.batch.row_start + b + 1) <= token)) {  // not the first one's sequence
+      int end = a.w.batch.seqs;
+      for (b = token < first ? 0 : b; end - b > 1;) {
+        const int mid = (b + end) >> 1;
+        if (__ldg(a.w.batch.row_start + mid) <= token) b = mid;
+        else end = mid;
+      }
     }
+    const PagedSeq s = paged_seq(a.w.batch, a.w.cache.page_shift, b);
+    const int64_t i = token - s.row0;
+    if (i >= 0 && i < s.n) row_keys(s, a.w.window, (int)i, lo, hi);
+  }
+  const int keys = a.plan->range * kTile, end = lo < hi ? (hi - 1) / keys : -1;
+  pdl_wait();
+  if (row >= all) return;
+  float m = -INFINITY, l = 0.f;
+  const float4* parts = reinterpret_cast<const float4*>(a.parts) + row * a.splits;
+  for (int split = lo / keys; split <= end; split += 8) {
+    float4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = split + i <= end ? parts[split + i] : make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(v[i].x, v[i].z));
+    const float base = top == -INFINITY ? 0.f : top;
+    l *= exp2_approx(m - base);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l += v[i].y * exp2_approx(v[i].x - base) + v[i].w * exp2_approx(v[i].z - base);
+    m = top;
   }
   a.rows[row].y = l == 0.f ? INFINITY : m + log2f(l);
 }
