@@ -18,7 +18,7 @@
 // Bound by the tensor pipe: 16 instructions a tile of 128 dims, each 96 clocks, as both operands lie in shared memory.  Measured
 // with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 264 and 246 us (0.59 and 0.64 of the pipe's cycles, the
 // most at that rate is 0.67), 18 us before them and 8 between; int8 376 and 431 us, the widening and its stores beside the
-// products.  15 sequences of 32 rows over 600 to 6000 keys, int8: 43 and 54 us, of which some 13 each are a launch, the dependent
+// products.  15 sequences of 32 rows over 600 to 6000 keys, int8: 105 us in all, of which 10 to 13 a pass are a launch, the dependent
 // loads of the first piece and the first tile.
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its
 // copies and MMAs done.
