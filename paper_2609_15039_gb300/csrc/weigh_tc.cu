@@ -18,8 +18,11 @@
 // Bound by the tensor pipe: 16 instructions a tile of 128 dims, each 96 clocks, as both operands lie in shared memory.  Measured
 // with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 264 and 246 us (0.59 and 0.64 of the pipe's cycles, the
 // most at that rate is 0.67), 18 us before them and 8 between; int8 376 and 431 us, the widening and its stores beside the
-// products.  15 sequences of 32 rows over 600 to 6000 keys, int8: 105 us in all, of which 10 to 13 a pass are a launch, the dependent
+// products.  15 sequences of 32 rows over 600 to 6000 keys, int8: 107 us in all, of which 10 to 13 a pass are a launch, the dependent
 // loads of the first piece and the first tile.
+// A piece of the second pass has all rows of its keys, unless heads and key tiles are too few for all SMs: then it has one of
+// several parts of them, and the last to end adds the parts' sums up.  2048 rows of 14 heads on 2 of 64 dims over 12049 keys 354 ->
+// 251 us; 2048 rows of 32 heads on 8 over themselves 142 -> 126, 512 rows 46 -> 40.
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its
 // copies and MMAs done.
 
@@ -45,11 +48,13 @@ constexpr int kMostRange = 16;      // key tiles of a piece of the first pass
 constexpr int kNotes = 8;           // key tiles whose marks or scales have a place: the loader is at most 3 ahead of the
                                     // issuer, which is at most kS ahead of the epilogue
 constexpr int kPieces = 4;
+constexpr int kMostChunks = 16;     // parts of the rows that a piece of the second pass may have
+constexpr int kSumTiles = 2048;     // key tiles of all pieces together when it has a part
 
 // What the blocks go by, made on the device: key tiles of a piece of each pass, pieces of each, and behind it the first
 // pieces of the sequences, [seqs] for each pass.
 struct WeighPlan {
-  int range, tiles;
+  int range, tiles, chunks;  // and parts of the rows, of which a piece of the second has one
   int64_t pieces[2];
   unsigned long long taken[2];  // beyond every block's first
 };
@@ -60,6 +65,9 @@ struct TcArgs {
   float2* rows;           // [heads][total]: scale, lse
   float2* parts;          // [heads][total][splits][2]: maximum, total
   int splits;             // places of a row
+  // rows in parts: a piece's sums, [item][group][its key tile][key], and behind each range's first how many are there, [warp]
+  float* sums;
+  unsigned* arrived;
   int64_t total;
   WeighPlan* plan;
   int64_t* first[2];
@@ -71,6 +79,7 @@ struct alignas(16) Piece {
   int rt0, rt1;  // row tiles [rt0, rt1), of the first pass one
   int t0, t1;    // key tiles
   int split;     // the range's index among the sequence's
+                 // second pass: the piece's number where rows are in parts, else -1
   int last;      // no piece: the end
 };
 
@@ -83,14 +92,15 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seqs = w.batch.seqs;
   if (blockIdx.x == 0) {
     __shared__ unsigned long long sums[kMostRange + kMostTiles], scan[2][kPrepThreads];  // pieces of a head, by their length
-    __shared__ int key_tiles[kMaxSeqs], row_tiles[kMaxSeqs], longest, chosen[2];
-    if (threadIdx.x == 0) longest = 0;
+    __shared__ int key_tiles[kMaxSeqs], row_tiles[kMaxSeqs], longest, tallest, chosen[2], chunks;
+    if (threadIdx.x == 0) longest = tallest = 0;
     __syncthreads();
     for (int b = threadIdx.x; b < seqs; b += kPrepThreads) {
       const PagedSeq s = paged_seq(w.batch, w.cache.page_shift, b);
       key_tiles[b] = (s.len + kTile - 1) / kTile;
       row_tiles[b] = (s.n * w.group + kTile - 1) / kTile;
       atomicMax(&longest, key_tiles[b]);
+      atomicMax(&tallest, row_tiles[b]);
     }
     __syncthreads();
     for (int i = warp; i < kMostRange + kMostTiles; i += kPrepThreads / 32) {
@@ -104,26 +114,43 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
       if (lane == 0) sums[i] = sum;
     }
     __syncthreads();
-    if (threadIdx.x < 64) {  // the length that gives the fewest key tiles to any block; beginning a piece costs some too
-      const int pass = threadIdx.x >> 5, n = lane + 1, most = pass == 0 ? kMostRange : kMostTiles;
+    // The lengths that give the fewest key tiles to any block; beginning a piece or, in the second pass, a row tile costs some too.
+    if (warp == 0) {
       unsigned long long cost = ~0ull;
-      if (n <= most && (pass == 1 || (longest + n - 1) / n <= a.splits)) {
-        const unsigned long long pieces = sums[pass * kMostRange + lane] * w.cache.heads;
-        cost = (pieces + grid - 1) / grid * (n + (pass == 0 ? 2 : 1)) * 32 + (31 - lane);
+      const int n = lane + 1;
+      if (n <= kMostRange && (longest + n - 1) / n <= a.splits) {
+        const unsigned long long pieces = sums[lane] * w.cache.heads;
+        cost = (pieces + grid - 1) / grid * (n + 2) * 32 + (31 - lane);
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) cost = min(cost, __shfl_xor_sync(0xffffffffu, cost, o));
-      if (lane == 0) chosen[pass] = 32 - (int)(cost & 31);  // (of equal ones the longest)
+      if (lane == 0) chosen[0] = 32 - (int)(cost & 31);  // (of equal ones the longest)
+    } else if (warp == 1) {
+      // And where that leaves blocks without work, the rows in parts.
+      static_assert(kMostTiles == 8, "three bits");
+      unsigned long long cost = ~0ull;
+      const int n = lane % kMostTiles + 1;
+      const unsigned long long pieces = sums[kMostRange + n - 1] * w.cache.heads;
+      for (int c = 1 + lane / kMostTiles; c <= kMostChunks && c <= max(1, tallest); c += 32 / kMostTiles) {
+        if (c > 1 && pieces * c * n > kSumTiles) break;
+        // (a part's sums leave and come back: some 4 tiles' time)
+        const unsigned long long one = (unsigned long long)((tallest + c - 1) / c) * (n + 1) + (c > 1 ? 4 : 0);
+        cost = min(cost, ((pieces * c + grid - 1) / grid * one) * 256 + (c - 1) * 8 + (kMostTiles - n));
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) cost = min(cost, __shfl_xor_sync(0xffffffffu, cost, o));
+      if (lane == 0) chosen[1] = kMostTiles - (int)(cost % 8), chunks = (int)(cost / 8 % 32) + 1;
     }
     __syncthreads();
-    if (threadIdx.x == 0)
-      *a.plan = {chosen[0], chosen[1], {(int64_t)sums[chosen[0] - 1] * w.cache.heads,
-                                        (int64_t)sums[kMostRange + chosen[1] - 1] * w.cache.heads}, {0, 0}};
+    const int64_t items = (int64_t)sums[kMostRange + chosen[1] - 1] * w.cache.heads * chunks;
+    if (threadIdx.x == 0) *a.plan = {chosen[0], chosen[1], chunks, {(int64_t)sums[chosen[0] - 1] * w.cache.heads, items}, {0, 0}};
+    if (chunks > 1)
+      for (int i = threadIdx.x; i < 4 * (int)items; i += kPrepThreads) a.arrived[i] = 0u;
     // Each sequence's first piece: sums before it, a run of sequences a thread.
     const int per = (seqs + kPrepThreads - 1) / kPrepThreads, b0 = min(seqs, per * (int)threadIdx.x), b1 = min(seqs, b0 + per);
     auto count = [&](int b, int pass) {
       const uint32_t n = (uint32_t)chosen[pass];
-      return (unsigned long long)(((uint32_t)key_tiles[b] + n - 1u) / n) * (pass == 0 ? (uint32_t)row_tiles[b] : 1u) *
+      return (unsigned long long)(((uint32_t)key_tiles[b] + n - 1u) / n) * (uint32_t)(pass == 0 ? row_tiles[b] : chunks) *
              (unsigned)w.cache.heads;
     };
     for (int pass = 0; pass < 2; ++pass) {
@@ -324,19 +351,28 @@ struct Kernel {
       const int tiles = (s.len + kTile - 1) / kTile, rows = s.n * group, row_tiles = (rows + kTile - 1) / kTile;
       const int splits = (tiles + per - 1) / per;
       int64_t rest = item - first[lo];
-      const int64_t of_head = (int64_t)splits * (SUM ? 1 : row_tiles);
+      const int chunks = SUM ? a.plan->chunks : 1;
+      const int64_t of_head = (int64_t)splits * (SUM ? chunks : row_tiles);
       x.b = lo;
       x.h = (int)quotient(rest, of_head);
       rest -= x.h * of_head;
       x.row0 = s.row0, x.n = s.n, x.len = s.len, x.pos0 = s.pos0;
-      x.split = (int)(rest % splits);
-      x.t0 = x.split * per;
+      int split, chunk = 0;
+      if constexpr (SUM) {
+        split = (int)quotient(rest, chunks);
+        chunk = (int)(rest - (int64_t)split * chunks);
+        x.split = chunks > 1 ? (int)item : -1;
+      } else {
+        x.split = split = (int)(rest % splits);
+      }
+      x.t0 = split * per;
       x.t1 = min(tiles, x.t0 + per);
       if constexpr (SUM) {  // the tokens that may see a key of the range
         const int64_t i0 = max((int64_t)0, (int64_t)x.t0 * kTile - s.pos0);
         const int64_t i1 = a.w.window == INT32_MAX ? s.n : min((int64_t)s.n, (int64_t)x.t1 * kTile - s.pos0 + a.w.window);
-        x.rt0 = i0 < i1 ? (int)(i0 * group / kTile) : 0;
-        x.rt1 = i0 < i1 ? (int)((i1 * group + kTile - 1) / kTile) : 0;
+        const int64_t rt0 = i0 < i1 ? i0 * group / kTile : 0, rt1 = i0 < i1 ? (i1 * group + kTile - 1) / kTile : 0;
+        x.rt0 = chunks == 1 ? (int)rt0 : (int)(rt0 + (rt1 - rt0) * chunk / chunks);
+        x.rt1 = chunks == 1 ? (int)rt1 : (int)(rt0 + (rt1 - rt0) * (chunk + 1) / chunks);
       } else {
         x.rt0 = (int)quotient(rest, splits);
         x.rt1 = x.rt0 + 1;
@@ -591,6 +627,36 @@ struct Kernel {
       take(c, v[c & 1]);
     }
   }
+  // A part of the rows: the sums to the workspace, and of the warps that have sums of the same keys the last to arrive adds all
+  // up, in the parts' order whichever it is.
+  __device__ void join_parts(const Piece& x, int own, int set, const float (&sum)[kMostTiles],
+                             const int (&slot)[kMostTiles]) const {
+    const int lane = threadIdx.x & 31, per = a.plan->tiles * kTile, chunks = a.plan->chunks, first = x.split / chunks * chunks;
+    float* to = a.sums + ((int64_t)x.split * 2 + set) * per + own;
+#pragma unroll
+    for (int i = 0; i < kMostTiles; ++i)
+      if (i < x.t1 - x.t0) __stcg(to + i * kTile, sum[i]);
+    __threadfence();
+    __syncwarp();
+    unsigned there = 0;
+    if (lane == 0) there = atomicAdd(a.arrived + 4 * first + own / 32, 1u);
+    there = __shfl_sync(0xffffffffu, there, 0);
+    if ((int)there != 2 * chunks - 1) return;
+    __threadfence();
+    const float* from = a.sums + (int64_t)first * 2 * per + own;
+    float all[kMostTiles] = {}, before[kMostTiles];
+#pragma unroll
+    for (int i = 0; i < kMostTiles; ++i)
+      before[i] = slot[i] >= 0 && (x.t0 + i) * kTile + own < x.pos0 ? a.w.score[slot[i]] * a.w.decay : 0.f;
+#pragma unroll 2
+    for (int c = 0; c < 2 * chunks; ++c, from += per)
+#pragma unroll
+      for (int i = 0; i < kMostTiles; ++i)
+        if (i < x.t1 - x.t0) all[i] += __ldcg(from + i * kTile);
+#pragma unroll
+    for (int i = 0; i < kMostTiles; ++i)
+      if (slot[i] >= 0) a.w.score[slot[i]] = before[i] + all[i];
+  }
   __device__ void epilogue() const {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, set = (warp - 4) >> 2;
     const int own = 32 * (warp & 3) + lane;
@@ -771,6 +837,10 @@ struct Kernel {
             return true;
           },
           [&](const Piece& x) {
+            if (x.split >= 0) {
+              join_parts(x, own, set, sum, slot);
+              return true;
+            }
             // A piece at a time: neither group's barrier gets a phase ahead of its waiter.
             if (set == 1 && !wait(L::kFirst, (uint32_t)number & 1u)) return false;
             if (set == 0 && number > 0 && !wait(L::kSecond, (uint32_t)(number - 1) & 1u)) return false;
@@ -916,13 +986,14 @@ int splits_of(const PagedCache& c, const PagedBatch& b) {
   return (int)std::max<int64_t>(8, ceil_div(tiles, kMostRange));
 }
 struct Sizes {
-  size_t q, rows, parts, plan;
+  size_t q, rows, parts, plan, sums;
 };
 Sizes sizes_of(const PagedCache& c, const PagedBatch& b, int64_t q_heads, int head_dim) {
   const int64_t rows = b.rows * q_heads;
   return {(size_t)rows * head_dim * 2, (size_t)round_up(rows * sizeof(float2), 16),
           (size_t)rows * splits_of(c, b) * 2 * sizeof(float2),
-          (size_t)round_up(sizeof(WeighPlan) + (int64_t)b.seqs * 2 * sizeof(int64_t), 16)};
+          (size_t)round_up(sizeof(WeighPlan) + (int64_t)b.seqs * 2 * sizeof(int64_t), 16),
+          (size_t)kSumTiles * (2 * kTile * sizeof(float) + 4 * sizeof(unsigned))};
 }
 
 template <int D, bool I8, bool SUM>
@@ -956,7 +1027,7 @@ spl_status launch(const TcArgs& a, int blocks, cudaStream_t stream) {
 
 size_t weigh_tc_bytes(const PagedCache& c, const PagedBatch& b, int64_t q_heads, int head_dim) {
   const Sizes s = sizes_of(c, b, q_heads, head_dim);
-  return 2 * s.q + s.rows + s.parts + s.plan;
+  return 2 * s.q + s.rows + s.parts + s.plan + s.sums;
 }
 
 spl_status run_weigh_tc(const WeighCall& w, int head_dim, bool i8, cudaStream_t stream) {
@@ -969,6 +1040,8 @@ spl_status run_weigh_tc(const WeighCall& w, int head_dim, bool i8, cudaStream_t 
   a.parts = reinterpret_cast<float2*>(at + 2 * s.q);
   a.rows = reinterpret_cast<float2*>(at + 2 * s.q + s.parts);
   a.plan = reinterpret_cast<WeighPlan*>(at + 2 * s.q + s.parts + s.rows);
+  a.sums = reinterpret_cast<float*>(at + 2 * s.q + s.parts + s.rows + s.plan);
+  a.arrived = reinterpret_cast<unsigned*>(a.sums + (size_t)kSumTiles * 2 * kTile);
   a.first[0] = reinterpret_cast<int64_t*>(a.plan + 1);
   a.first[1] = a.first[0] + w.batch.seqs;
   a.splits = splits_of(w.cache, w.batch);

@@ -549,6 +549,59 @@ def test_weigh_is_deterministic_in_graphs_and_on_streams(spl, rows):
     assert bool((ws[:65536] == 255).all())
 
 
+# Few heads and many rows: the rows of a key are shared out, and the last of their parts to end adds all up.  Tolerance: a sum's
+# additions, one a part and half more, are no more than its rows.
+PARTS = {"one": [(1500, 1600)], "itself": [(700, 700)], "past": [(600, 3000)],
+         "ragged": [(700, 900), (0, 5), (1, 1300), (260, 260), (0, 0)]}
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("window", [0, 300])
+@pytest.mark.parametrize("heads", [(7, 1, 64), (14, 2, 64), (4, 1, 128), (1, 1, 128)], ids=str)
+@pytest.mark.parametrize("name", PARTS)
+def test_weigh_rows_in_parts(spl, name, heads, window, fmt):
+    c = many(Case(spl, PARTS[name], heads, fmt, 32, seed=len(name)))
+    c.fill()
+    check_weights(c, window=window, decay=0.5)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+def test_weigh_rows_in_parts_again(spl, fmt):
+    """The same bits whichever part ends last, over any contents of the workspace; two graphs on one workspace; a replayed call
+    after the lengths have changed, where a part may have no rows."""
+    c = many(Case(spl, [(900, 1000), (300, 2000)], (4, 1, 64), fmt, 32, seed=3))
+    c.fill()
+    first = check_weights(c)
+    q = torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV)
+    batch = c.batch()
+    ws = spl.workspace(spl.spl_kv_weigh_workspace_bytes(c.cache, batch, c.hq))
+    score = scores_for(c, 0.75)
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            spl.spl_kv_weigh(score, q, c.cache, batch, c.hq, workspace=ws)
+    for turn in range(20):
+        if turn % 5 == 0:
+            ws.fill_(255)
+        score.fill_(0.75)
+        graphs[turn % 2].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(raw(score), raw(first))
+    for lens in ([900, 300], [900, 0], [0, 300], [1000, 300]):
+        batch.kv_len.copy_(i32(lens))
+        score.fill_(0.75)
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        for b, (n, rows) in enumerate(zip(lens, (900, 300))):
+            own = c.q[c.start[b]:c.start[b + 1]]
+            k = c.stored("k", b)[:n]
+            added = serving.weights(own, k, n, 4, 64 ** -0.5) if n else np.zeros((1, 0))
+            kept = 0.75 * (np.arange(n) < n - rows)
+            tol = weight_tolerance(own, k, 64 ** -0.5, 4, rows * 4) * added + 2 * U * (kept + added) + 1e-30
+            assert np.all(np.abs(score_of(c, score, b)[:, :n] - (kept + added)) <= tol)
+    assert spl.spl_get_device_status() == spl.SPL_OK
+
+
 # ---------------------------------------------------------------------------------- eviction
 def check_evict(c, score, keep, recent, fresh=False, alias=False):
     """Against the definition, to the bit; scores [pages, heads, page] on the device."""
