@@ -15,18 +15,21 @@
 //   warps 4-11   two groups: maxima and totals (the key tiles in turn), or sums (half of a tile's rows each).
 //   warps 12-19  int8: two groups widen the key tiles to binary16 in turn.
 // Tensor memory: four places of S.
-// Bound by the tensor pipe: 16 instructions a tile of 128 dims, each 96 clocks, as both operands lie in shared memory.  Measured
-// with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 264 and 246 us (0.59 and 0.64 of the pipe's cycles, the
-// most at that rate is 0.67), 18 us before them and 8 between; int8 376 and 431 us, the widening and its stores beside the
-// products.  15 sequences of 32 rows over 600 to 6000 keys, int8: 107 us in all, of which 10 to 13 a pass are a launch, the dependent
-// loads of the first piece and the first tile.
+// Measured with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 235 us each, 19 us before them and 7 between;
+// int8 302 and 302.  Without the epilogues' arithmetic 211 to 227, with two instructions of a tile's 16 207 to 222, without both
+// 175: the key tiles' way here, of which three fit beside two tiles of q, is the longest of three that are nearly alike.  So the
+// epilogues pay for what they execute and read: both have code of their own for tiles of which all is seen, and in the second,
+// where a column's scale and lse go to every thread (4 wavefronts for 16 bytes), q's exponents are in steps so that a tile mostly
+// has one scale (15 sequences of 32 rows int8, second pass 54 -> 43 us).  These in all, over 600 to 6000 keys: 92 us, of which 10
+// to 13 a pass are a launch, the dependent loads of the first piece and the first tile.
 // A piece of the second pass has all rows of its keys, unless heads and key tiles are too few for all SMs: then it has one of
-// several parts of them, and the last to end adds the parts' sums up.  2048 rows of 14 heads on 2 of 64 dims over 12049 keys 354 ->
-// 251 us; 2048 rows of 32 heads on 8 over themselves 142 -> 126, 512 rows 46 -> 40.
+// several parts of them, and the last to end adds the parts' sums up: 2048 rows of 14 heads on 2 of 64 dims over 12049 keys 354 ->
+// 251 us (now 216); 2048 rows of 32 heads on 8 over themselves 142 -> 126 (now 122).
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its
 // copies and MMAs done.
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -62,7 +65,7 @@ struct WeighPlan {
 struct TcArgs {
   WeighCall w;
   uint16_t *q_hi, *q_lo;  // [heads][total][dim], total = rows group
-  float2* rows;           // [heads][total]: scale, lse
+  float2* rows;           // [heads][total]: scale, negative if the row may not be finite; lse
   float2* parts;          // [heads][total][splits][2]: maximum, total
   int splits;             // places of a row
   // rows in parts: a piece's sums, [item][group][its key tile][key], and behind each range's first how many are there, [warp]
@@ -195,10 +198,16 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
     const int head = there ? (int)(i % w.q_heads) : 0;
     const float4 v = there ? __ldcs(reinterpret_cast<const float4*>(w.q + token * w.ldq + (int64_t)head * D) + at)
                            : make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = fabsf(v.x) + fabsf(v.y) + (fabsf(v.z) + fabsf(v.w));
     float top = fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const int e = fp16_row_exponent(top);
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+    // (in steps of 12, so that rows of like size have the same and the second pass one scale for a tile; the largest is then in
+    // [2^3, 2^15), where the low half's smallest step, 2^-24, is still far below 2^-22 of it)
+    const int e = top > 0.f ? (fp16_row_exponent(top) - 8 + 132) / 12 * 12 - 132 + 8 : 8;
     const float up = w.scale_log2 < 0.f ? -pow2f(e) : pow2f(e);  // the scale's sign goes into q
     uint32_t h0, l0, h1, l1;
     split_f16(v.x * up, v.y * up, h0, l0);
@@ -207,7 +216,7 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
     const int64_t row = (int64_t)(head / w.group) * a.total + token * w.group + head % w.group;
     reinterpret_cast<uint2*>(a.q_hi + row * D)[at] = make_uint2(h0, h1);
     reinterpret_cast<uint2*>(a.q_lo + row * D)[at] = make_uint2(l0, l1);
-    if (at == 0) a.rows[row].x = fabsf(w.scale_log2) * pow2f(-e);
+    if (at == 0) a.rows[row].x = copysignf(w.scale_log2 * pow2f(-e), sum <= FLT_MAX ? 1.f : -1.f);
   }
 }
 
@@ -220,10 +229,12 @@ struct Layout {
   // second pass: the rows' scales and lse of each stage of q; int8: the keys' scales; first pass: marks of keys without a page
   static constexpr uint32_t COL = K + STAGES * TILE, SCALE = COL + kQStages * kTile * 8;
   static constexpr uint32_t GONE = SCALE + (I8 ? kNotes * kTile * 4 : 0);
-  static constexpr uint32_t BARS = GONE + kNotes * 16;
+  static constexpr uint32_t ONE = GONE + kNotes * 16, BARS = ONE + 16;
   enum { kKFull = 0, kKEmpty = 3, kQFull = 6, kQEmpty = 8, kSFull = 10, kSFree = 14, kPieceFull = 18, kPieceFree = 22, kDrain = 26,
          kColFull = 27, kColEmpty = 29, kFirst = 31, kSecond = 32, kBars = 34 };
-  static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece), SMEM = MISC + 16;
+  static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece);
+  // int8, second pass: the slots and old scores of the threads' keys, [group][2][key tile][key]
+  static constexpr uint32_t STASH = MISC + 16, SMEM = STASH + (I8 ? 2 * 2 * kMostTiles * kTile * 4 : 0);
   static_assert(PIECES % 16 == 0 && SMEM <= 232448, "227 KB of dynamic shared memory per block");
   static constexpr uint32_t IDESC = make_idesc(0, 128, 128);
 };
@@ -257,6 +268,11 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
 }
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint32_t ld_shared4(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
 }
 __device__ __forceinline__ void st_shared4(uint32_t addr, uint32_t v) {
   asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
@@ -473,7 +489,8 @@ struct Kernel {
         mbar_wait(bar(L::kKFull + t % L::STAGES), (uint32_t)(t / L::STAGES) & 1u, kDrainNs, nullptr);
     }
   }
-  // Warp 2, second pass: scales and -lse of a tile's rows, in pairs; of rows that are not there an lse that leaves nothing.
+  // Warp 2, second pass: scales and -lse of a tile's rows, of rows that are not there an lse that leaves nothing; and the scale,
+  // if all have the same and nothing else in the products is not finite, else -1.
   __device__ void columns() const {
     const int lane = threadIdx.x & 31;
     const bool ok = walk(
@@ -482,13 +499,27 @@ struct Kernel {
           const int q = tile % kQStages;
           if (tile >= kQStages && !wait(L::kColEmpty + q, (uint32_t)(tile / kQStages - 1) & 1u)) return false;
           const float2* rows = a.rows + (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0;
+          const float one = fabsf(rows[0].x);
+          const int64_t left = a.total * a.w.cache.heads - (rows - a.rows);
+          float2 v[4];
+          bool fast = true;
 #pragma unroll
-          for (int i = lane; i < kTile / 2; i += 32) {
-            const float2 none = make_float2(0.f, INFINITY);
-            const float2 v = 2 * i < y.rows ? rows[2 * i] : none, u = 2 * i + 1 < y.rows ? rows[2 * i + 1] : none;
-            st_shared16(smem + L::COL + 16u * (q * (kTile / 2) + i),
-                        make_uint4(__float_as_uint(v.x), __float_as_uint(u.x), __float_as_uint(-v.y), __float_as_uint(-u.y)));
+          for (int i = 0; i < 4; ++i) {  // (rows behind the tile's own are in its products all the same)
+            v[i] = 4 * lane + i < left ? rows[4 * lane + i] : make_float2(0.f, INFINITY);
+            if (4 * lane + i < y.rows) {
+              v[i].x = fabsf(v[i].x);
+              fast = fast && v[i].x == one;
+            } else {
+              fast = fast && __float_as_int(v[i].x) >= 0;
+              v[i] = make_float2(0.f, INFINITY);
+            }
           }
+          const uint32_t to = smem + L::COL + 1024u * q + 16u * lane;
+          st_shared16(to, make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[1].x), __float_as_uint(v[2].x), __float_as_uint(v[3].x)));
+          st_shared16(to + 512u, make_uint4(__float_as_uint(-v[0].y), __float_as_uint(-v[1].y), __float_as_uint(-v[2].y),
+                                            __float_as_uint(-v[3].y)));
+          fast = __all_sync(0xffffffffu, fast);
+          if (lane == 0) st_shared4(smem + L::ONE + 4u * q, __float_as_uint(fast ? one : -1.f));
           arrive(L::kColFull + q);
           return true;
         },
@@ -620,17 +651,35 @@ struct Kernel {
   __device__ void over_chunks(uint32_t ts, Take take) const {
     uint32_t v[2][32];
     tmem_ld_32x32_begin(ts, v[0]);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      tmem_ld_wait(v[c & 1]);
-      if (c < 3) tmem_ld_32x32_begin(ts + 32u * (c + 1), v[(c + 1) & 1]);
-      take(c, v[c & 1]);
+#pragma unroll 1
+    for (int c = 0; c < 4; c += 2) {
+      tmem_ld_wait(v[0]);
+      tmem_ld_32x32_begin(ts + 32u * (c + 1), v[1]);
+      take(c, v[0]);
+      tmem_ld_wait(v[1]);
+      if (c == 0) tmem_ld_32x32_begin(ts + 64u, v[0]);
+      take(c + 1, v[1]);
     }
+  }
+  // The slots of the thread's key of each of the piece's key tiles, -1 where there is none.
+  __device__ void slots_of(const Piece& x, int own, int (&slot)[kMostTiles]) const {
+    const int* table = a.w.batch.table + x.b * a.w.batch.max_pages;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kMostTiles; ++i) {  // (the pages first, so that the loads run side by side)
+      const int kt = x.t0 + i, j = kt * kTile + own;
+      slot[i] = kt < x.t1 && j < x.len ? __ldg(table + (j >> a.w.cache.page_shift)) : -1;
+      bad |= kt < x.t1 && j < x.len && (unsigned)slot[i] >= (unsigned)a.w.cache.pages;
+    }
+    if (bad) atomicOr(a.w.batch.status, kStatusIndex);
+#pragma unroll
+    for (int i = 0; i < kMostTiles; ++i)
+      slot[i] = (unsigned)slot[i] < (unsigned)a.w.cache.pages ? (int)paged_slot(a.w.cache, slot[i], x.h, (x.t0 + i) * kTile + own)
+                                                               : -1;
   }
   // A part of the rows: the sums to the workspace, and of the warps that have sums of the same keys the last to arrive adds all
   // up, in the parts' order whichever it is.
-  __device__ void join_parts(const Piece& x, int own, int set, const float (&sum)[kMostTiles],
-                             const int (&slot)[kMostTiles]) const {
+  __device__ void join_parts(const Piece& x, int own, int set, const float (&sum)[kMostTiles]) const {
     const int lane = threadIdx.x & 31, per = a.plan->tiles * kTile, chunks = a.plan->chunks, first = x.split / chunks * chunks;
     float* to = a.sums + ((int64_t)x.split * 2 + set) * per + own;
 #pragma unroll
@@ -645,6 +694,8 @@ struct Kernel {
     __threadfence();
     const float* from = a.sums + (int64_t)first * 2 * per + own;
     float all[kMostTiles] = {}, before[kMostTiles];
+    int slot[kMostTiles];
+    slots_of(x, own, slot);
 #pragma unroll
     for (int i = 0; i < kMostTiles; ++i)
       before[i] = slot[i] >= 0 && (x.t0 + i) * kTile + own < x.pos0 ? a.w.score[slot[i]] * a.w.decay : 0.f;
@@ -668,9 +719,10 @@ struct Kernel {
       ok = walk(
           nothing,
           [&](const Piece& x, const Span& y, int) {
-            m = -INFINITY, l = 0.f, scale = 0.f, lo = hi = 0;
+            m = -INFINITY, l = 0.f, scale = FLT_MIN, lo = hi = 0;
             if (own < y.rows) {
-              scale = a.rows[(int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0 + own].x;
+              // (not 0, by which -inf would not stay)
+              scale = fmaxf(fabsf(a.rows[(int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0 + own].x), FLT_MIN);
               row_keys({x.row0, x.n, x.len, x.pos0}, a.w.window, (y.r0 + own) / a.w.group, lo, hi);
             }
             return true;
@@ -706,8 +758,7 @@ struct Kernel {
                 top[0] = max3(top[0], __uint_as_float(r[k]), __uint_as_float(r[k + 1]));
                 if (k + 3 < 32) top[1] = max3(top[1], __uint_as_float(r[k + 2]), __uint_as_float(r[k + 3]));
               }
-              float t = fmaxf(top[0], top[1]);
-              t = t == -INFINITY ? t : t * scale;
+              const float t = fmaxf(top[0], top[1]) * scale;
               if (t > m) {
                 l *= exp2_approx(m - t);
                 m = t;
@@ -719,10 +770,6 @@ struct Kernel {
               for (int k = 0; k < 32; k += 2) {
                 float t0, t1;
                 up2(fma2(p2(__uint_as_float(r[k]), __uint_as_float(r[k + 1])), scale2, base2), t0, t1);
-                if (edge) {  // (-inf times a scale of 0)
-                  t0 = r[k] == 0xff800000u ? -INFINITY : t0;
-                  t1 = r[k + 1] == 0xff800000u ? -INFINITY : t1;
-                }
                 sum[k / 2 & 1] = add2(sum[k / 2 & 1], p2(exp2_approx(t0), exp2_approx(t1)));
               }
               float s0, s1;
@@ -746,23 +793,23 @@ struct Kernel {
       float sum[kMostTiles], before[kMostTiles];
       int slot[kMostTiles];  // of the thread's key of each, -1 where there is none
       int number = 0;        // of pieces
+      // (int8: not in registers meanwhile)
+      const uint32_t stash = smem + L::STASH + 4u * (2 * kMostTiles * kTile * set + own);
       ok = walk(
           [&](const Piece& x) {
-            const int* table = a.w.batch.table + x.b * a.w.batch.max_pages;
-            bool bad = false;
 #pragma unroll
-            for (int i = 0; i < kMostTiles; ++i) {  // (the pages first, so that the loads run side by side)
-              const int kt = x.t0 + i, j = kt * kTile + own;
-              sum[i] = 0.f;
-              slot[i] = kt < x.t1 && j < x.len ? __ldg(table + (j >> a.w.cache.page_shift)) : -1;
-              bad |= kt < x.t1 && j < x.len && (unsigned)slot[i] >= (unsigned)a.w.cache.pages;
-            }
-            if (bad) atomicOr(a.w.batch.status, kStatusIndex);
+            for (int i = 0; i < kMostTiles; ++i) sum[i] = 0.f;
+            if (x.split >= 0) return true;
+            slots_of(x, own, slot);
 #pragma unroll
-            for (int i = 0; i < kMostTiles; ++i) {
-              const int j = (x.t0 + i) * kTile + own;
-              slot[i] = (unsigned)slot[i] < (unsigned)a.w.cache.pages ? (int)paged_slot(a.w.cache, slot[i], x.h, j) : -1;
-              before[i] = set == 0 && slot[i] >= 0 && j < x.pos0 ? a.w.score[slot[i]] : 0.f;
+            for (int i = 0; i < kMostTiles; ++i)
+              before[i] = set == 0 && slot[i] >= 0 && (x.t0 + i) * kTile + own < x.pos0 ? a.w.score[slot[i]] : 0.f;
+            if constexpr (I8) {
+#pragma unroll
+              for (int i = 0; i < kMostTiles; ++i) {
+                st_shared4(stash + 4u * kTile * i, (uint32_t)slot[i]);
+                st_shared4(stash + 4u * kTile * (kMostTiles + i), __float_as_uint(before[i]));
+              }
             }
             return true;
           },
@@ -773,9 +820,11 @@ struct Kernel {
             const int place = key % kS, j0 = kt * kTile, which = kt - x.t0;
             if (!wait(L::kSFull + place, (uint32_t)(key / kS) & 1u)) return false;
             tc_fence_after();
-            const bool edge = j0 < y.all_lo || j0 + kTile > y.all_hi || y.rows < kTile;
+            float one;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(one) : "r"(smem + L::ONE + 4u * (tile % kQStages)));
+            const bool general = j0 < y.all_lo || j0 + kTile > y.all_hi || one < 0.f;
             int from = 0, to = kTile;  // columns that see the thread's key
-            if (edge) {
+            if (general) {
               const int64_t i0 = max((int64_t)0, (int64_t)j0 + own - x.pos0);
               const int64_t i1 =
                   a.w.window == INT32_MAX ? x.n : min((int64_t)x.n, (int64_t)j0 + own - x.pos0 + a.w.window);
@@ -785,8 +834,7 @@ struct Kernel {
             float ks = 1.f;
             if constexpr (I8)
               asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(smem + L::SCALE + 4u * (key % kNotes * kTile + own)));
-            const unsigned long long ks2 = p2(ks, ks), zero2 = p2(-0.f, -0.f);
-            const uint32_t col = smem + L::COL + 16u * (tile % kQStages * (kTile / 2)) + 512u * set;
+            const uint32_t col = smem + L::COL + 1024u * (tile % kQStages) + 256u * set;
             unsigned long long p[2] = {p2(0.f, 0.f), p2(0.f, 0.f)};
             uint32_t v[2][32];
             tmem_ld_32x32_begin(lanes + 128u * place + 64u * set, v[0]);
@@ -795,34 +843,42 @@ struct Kernel {
             tmem_ld_wait(v[1]);
             tc_fence_before();
             arrive(L::kSFree + place);
-            auto add = [&](auto masked) {
+            // Any rows, any scales; or all rows (what is not there has an infinite lse) and one scale, where the lse are all that is
+            // read: the same bits.
+            auto add = [&](auto any) {
+              const float both = any ? ks : ks * one;
+              const unsigned long long ks2 = p2(both, both), zero2 = p2(-0.f, -0.f);
 #pragma unroll
               for (int c = 0; c < 2; ++c) {
-                uint4 w[8];
 #pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                  if (k % 16 == 0) {
+                for (int k = 0; k < 32; k += 4) {
+                  const uint4 e4 = ld_shared16(col + 512u + 128u * c + 4u * k);  // -lse of four rows
+                  uint4 x4;
+                  if constexpr (any) x4 = ld_shared16(col + 128u * c + 4u * k);
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) w[u] = ld_shared16(col + 16u * (16 * c + k / 2 + u));
+                  for (int u = 0; u < 4; u += 2) {
+                    const unsigned long long s = p2(__uint_as_float(v[c][k + u]), __uint_as_float(v[c][k + u + 1]));
+                    const unsigned long long e2 = u == 0 ? p2(__uint_as_float(e4.x), __uint_as_float(e4.y))
+                                                         : p2(__uint_as_float(e4.z), __uint_as_float(e4.w));
+                    unsigned long long by = ks2;
+                    if constexpr (any) {
+                      by = u == 0 ? p2(__uint_as_float(x4.x), __uint_as_float(x4.y)) : p2(__uint_as_float(x4.z), __uint_as_float(x4.w));
+                      if constexpr (I8) by = fma2(ks2, by, zero2);
+                    }
+                    float t0, t1;
+                    up2(fma2(s, by, e2), t0, t1);
+                    float p0 = exp2_approx(t0), p1 = exp2_approx(t1);
+                    if constexpr (any) {
+                      const int at = 64 * set + 32 * c + k + u;
+                      p0 = at >= from && at < to ? p0 : 0.f;
+                      p1 = at + 1 >= from && at + 1 < to ? p1 : 0.f;
+                    }
+                    p[u / 2] = add2(p[u / 2], p2(p0, p1));
                   }
-                  const uint4 x4 = w[k / 2 % 8];  // scales and -lse of two rows
-                  unsigned long long s = p2(__uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
-                  if constexpr (I8) s = fma2(s, ks2, zero2);
-                  float t0, t1;
-                  up2(fma2(s, p2(__uint_as_float(x4.x), __uint_as_float(x4.y)),
-                           p2(__uint_as_float(x4.z), __uint_as_float(x4.w))),
-                      t0, t1);
-                  float p0 = exp2_approx(t0), p1 = exp2_approx(t1);
-                  if constexpr (masked) {
-                    const int at = 64 * set + 32 * c + k;
-                    p0 = at >= from && at < to ? p0 : 0.f;
-                    p1 = at + 1 >= from && at + 1 < to ? p1 : 0.f;
-                  }
-                  p[k / 2 & 1] = add2(p[k / 2 & 1], p2(p0, p1));
                 }
               }
             };
-            if (edge) add(std::true_type());
+            if (general) add(std::true_type());
             else add(std::false_type());
             float s0, s1, s2, s3;
             up2(p[0], s0, s1);
@@ -838,8 +894,15 @@ struct Kernel {
           },
           [&](const Piece& x) {
             if (x.split >= 0) {
-              join_parts(x, own, set, sum, slot);
+              join_parts(x, own, set, sum);
               return true;
+            }
+            if constexpr (I8) {
+#pragma unroll
+              for (int i = 0; i < kMostTiles; ++i) {
+                slot[i] = (int)ld_shared4(stash + 4u * kTile * i);
+                before[i] = __uint_as_float(ld_shared4(stash + 4u * kTile * (kMostTiles + i)));
+              }
             }
             // A piece at a time: neither group's barrier gets a phase ahead of its waiter.
             if (set == 1 && !wait(L::kFirst, (uint32_t)number & 1u)) return false;
