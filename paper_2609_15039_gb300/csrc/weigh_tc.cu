@@ -15,8 +15,8 @@
 //   warps 4-11   two groups: maxima and totals (the key tiles in turn), or sums (half of a tile's rows each).
 //   warps 12-19  int8: two groups widen the key tiles to binary16 in turn.
 // Tensor memory: four places of S.
-// Measured with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 235 us each, 19 us before them and 7 between;
-// int8 302 and 302.  Without the epilogues' arithmetic 211 to 227, with two instructions of a tile's 16 207 to 222, without both
+// Measured with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 229 and 236 us, 19 us before them and 7
+// between; int8 307 and 303.  Without the epilogues' arithmetic 211 to 227, with two instructions of a tile's 16 207 to 222, without both
 // 175: the key tiles' way here, of which three fit beside two tiles of q, is the longest of three that are nearly alike.  So the
 // epilogues pay for what they execute and read: both have code of their own for tiles of which all is seen, and in the second,
 // where a column's scale and lse go to every thread (4 wavefronts for 16 bytes), q's exponents are in steps so that a tile mostly
@@ -48,8 +48,6 @@ constexpr int kThreads = 32 * (4 + kEpilogue), kThreadsI8 = kThreads + 32 * 8;
 constexpr int kQStages = 2, kS = 4;
 constexpr int kMostTiles = 8;       // key tiles of a piece of the second pass (a thread has every other one's sum)
 constexpr int kMostRange = 16;      // key tiles of a piece of the first pass
-constexpr int kNotes = 8;           // key tiles whose marks or scales have a place: the loader is at most 3 ahead of the
-                                    // issuer, which is at most kS ahead of the epilogue
 constexpr int kPieces = 4;
 constexpr int kMostChunks = 16;     // parts of the rows that a piece of the second pass may have
 constexpr int kSumTiles = 2048;     // key tiles of all pieces together when it has a part
@@ -223,15 +221,19 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
 // ---------------------------------------------------------------- the passes
 template <int D, bool I8>
 struct Layout {
-  static constexpr int PANELS = D / 64, STAGES = I8 ? 2 : 3;
+  static constexpr int PANELS = D / 64, STAGES = D == 64 ? (I8 ? 4 : 6) : (I8 ? 2 : 3);
+  // key tiles whose marks or scales have a place: the loader is at most STAGES ahead of the issuer, which is at most kS ahead of
+  // the epilogue
+  static constexpr int NOTES = D == 64 ? 16 : 8;
+  static_assert(NOTES > STAGES + kS, "and one that is being written");
   static constexpr uint32_t PANEL = 128 * 128, TILE = PANELS * PANEL;
   static constexpr uint32_t Q = 0, K = kQStages * 2 * TILE;  // stages of [q_hi, q_lo]; of K
   // second pass: the rows' scales and lse of each stage of q; int8: the keys' scales; first pass: marks of keys without a page
   static constexpr uint32_t COL = K + STAGES * TILE, SCALE = COL + kQStages * kTile * 8;
-  static constexpr uint32_t GONE = SCALE + (I8 ? kNotes * kTile * 4 : 0);
-  static constexpr uint32_t ONE = GONE + kNotes * 16, BARS = ONE + 16;
-  enum { kKFull = 0, kKEmpty = 3, kQFull = 6, kQEmpty = 8, kSFull = 10, kSFree = 14, kPieceFull = 18, kPieceFree = 22, kDrain = 26,
-         kColFull = 27, kColEmpty = 29, kFirst = 31, kSecond = 32, kBars = 34 };
+  static constexpr uint32_t GONE = SCALE + (I8 ? NOTES * kTile * 4 : 0);
+  static constexpr uint32_t ONE = GONE + NOTES * 16, BARS = ONE + 16;
+  enum { kQFull = 0, kQEmpty = 2, kSFull = 4, kSFree = 8, kPieceFull = 12, kPieceFree = 16, kColFull = 20, kColEmpty = 22,
+         kFirst = 24, kSecond = 25, kDrain = 26, kKFull = 27, kKEmpty = kKFull + STAGES, kBars = (kKEmpty + STAGES + 1) / 2 * 2 };
   static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece);
   // int8, second pass: the slots and old scores of the threads' keys, [group][2][key tile][key]
   static constexpr uint32_t STASH = MISC + 16, SMEM = STASH + (I8 ? 2 * 2 * kMostTiles * kTile * 4 : 0);
@@ -463,7 +465,7 @@ struct Kernel {
             uint32_t word = 0;
             for (int i = 0; i < 32; i += 16)
               if (gone >> ((32 * lane + i) / box) & 1u) word |= 0xffffu << i;
-            st_shared4(smem + L::GONE + 16u * (keys % kNotes) + 4u * lane, word);
+            st_shared4(smem + L::GONE + 16u * (keys % L::NOTES) + 4u * lane, word);
           }
           __syncwarp();
           if (lane == 0) mbar_expect_tx(bar(L::kKFull + stage), L::TILE);
@@ -515,7 +517,8 @@ struct Kernel {
             }
           }
           const uint32_t to = smem + L::COL + 1024u * q + 16u * lane;
-          st_shared16(to, make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[1].x), __float_as_uint(v[2].x), __float_as_uint(v[3].x)));
+          st_shared16(to, make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[1].x), __float_as_uint(v[2].x),
+                                     __float_as_uint(v[3].x)));
           st_shared16(to + 512u, make_uint4(__float_as_uint(-v[0].y), __float_as_uint(-v[1].y), __float_as_uint(-v[2].y),
                                             __float_as_uint(-v[3].y)));
           fast = __all_sync(0xffffffffu, fast);
@@ -564,8 +567,8 @@ struct Kernel {
         st_shared16(row + (((first ^ 1) ^ (at & 7)) << 4), make_uint4(i8_pair(w2, 0x4140u), i8_pair(w2, 0x4342u),
                                                                       i8_pair(w3, 0x4140u), i8_pair(w3, 0x4342u)));
       }
-      st_shared4(smem + L::SCALE + 4u * (held % kNotes * kTile + i), __float_as_uint(scale));
-      if (lane == 0) st_shared4(smem + L::GONE + 16u * (held % kNotes) + 4u * (i >> 5), gone);
+      st_shared4(smem + L::SCALE + 4u * (held % L::NOTES * kTile + i), __float_as_uint(scale));
+      if (lane == 0) st_shared4(smem + L::GONE + 16u * (held % L::NOTES) + 4u * (i >> 5), gone);
       fence_proxy_async_smem();
       arrive(L::kKFull + stage);
       held = -1;
@@ -605,8 +608,14 @@ struct Kernel {
         [&](const Piece&, const Span&, int tile) { return wait(L::kQFull + tile % kQStages, (uint32_t)(tile / kQStages) & 1u); },
         [&](const Piece&, const Span&, int, int key, int tile) {
           const int stage = key % L::STAGES, place = key % kS;
-          if (!wait(L::kKFull + stage, (uint32_t)(key / L::STAGES) & 1u)) return false;
-          if (key >= kS && !wait(L::kSFree + place, (uint32_t)(key / kS - 1) & 1u)) return false;
+          const uint32_t k_parity = (uint32_t)(key / L::STAGES) & 1u, s_parity = (uint32_t)(key / kS - 1) & 1u;
+          // (both asked at once: mostly neither is waited for, and the answers are what takes time)
+          const bool there = mbar_try(bar(L::kKFull + stage), k_parity);
+          const bool free = key < kS || mbar_try(bar(L::kSFree + place), s_parity);
+          if (!__all_sync(0xffffffffu, there && free)) {
+            if (!wait(L::kKFull + stage, k_parity)) return false;
+            if (key >= kS && !wait(L::kSFree + place, s_parity)) return false;
+          }
           tc_fence_after();
           const uint32_t q = sdesc_lo(smem + L::Q + (uint32_t)__shfl_sync(0xffffffffu, tile % kQStages, 0) * 2u * L::TILE);
           const uint32_t kd = sdesc_lo(smem + L::K + (uint32_t)__shfl_sync(0xffffffffu, stage, 0) * L::TILE);
@@ -619,9 +628,12 @@ struct Kernel {
             const uint32_t qi = q + off + (i < D / 16 ? L::TILE >> 4 : 0u), ki = kd + off;
             mma_ss(d, SUM ? ki : qi, SUM ? qi : ki, kSdescHi128, L::IDESC, i > 0 ? 1u : 0u, leader);
           }
-          commit(L::kKEmpty + stage);
-          if (leader) mbar_arrive(bar(L::kSFull + place));
-          commit(L::kSFull + place);
+          if (leader) {
+            mma_commit(bar(L::kKEmpty + stage));
+            mbar_arrive(bar(L::kSFull + place));
+            mma_commit(bar(L::kSFull + place));
+          }
+          __syncwarp();
           return true;
         },
         [&](const Piece&, const Span&, int tile) {
@@ -732,7 +744,7 @@ struct Kernel {
             const int place = key % kS, j0 = kt * kTile;
             if (!wait(L::kSFull + place, (uint32_t)(key / kS) & 1u)) return false;
             tc_fence_after();
-            const uint32_t note = smem + L::GONE + 16u * (key % kNotes);
+            const uint32_t note = smem + L::GONE + 16u * (key % L::NOTES);
             const uint4 gone = ld_shared16(note);
             const bool edge = j0 < y.all_lo || j0 + kTile > y.all_hi || (gone.x | gone.y | gone.z | gone.w) != 0;
             const unsigned long long scale2 = p2(scale, scale);
@@ -740,7 +752,7 @@ struct Kernel {
               if constexpr (I8) {
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) {
-                  const uint4 w = ld_shared16(smem + L::SCALE + 4u * (key % kNotes * kTile + 32 * c + k));
+                  const uint4 w = ld_shared16(smem + L::SCALE + 4u * (key % L::NOTES * kTile + 32 * c + k));
                   mul2(r[k], r[k + 1], w.x, w.y);
                   mul2(r[k + 2], r[k + 3], w.z, w.w);
                 }
@@ -833,7 +845,7 @@ struct Kernel {
             }
             float ks = 1.f;
             if constexpr (I8)
-              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(smem + L::SCALE + 4u * (key % kNotes * kTile + own)));
+              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(smem + L::SCALE + 4u * (key % L::NOTES * kTile + own)));
             const uint32_t col = smem + L::COL + 1024u * (tile % kQStages) + 256u * set;
             unsigned long long p[2] = {p2(0.f, 0.f), p2(0.f, 0.f)};
             uint32_t v[2][32];
@@ -843,8 +855,8 @@ struct Kernel {
             tmem_ld_wait(v[1]);
             tc_fence_before();
             arrive(L::kSFree + place);
-            // Any rows, any scales; or all rows (what is not there has an infinite lse) and one scale, where the lse are all that is
-            // read: the same bits.
+            // Any rows, any scales; or all rows (what is not there has an infinite lse) and one scale, where the lse are all that
+            // is read: the same bits.
             auto add = [&](auto any) {
               const float both = any ? ks : ks * one;
               const unsigned long long ks2 = p2(both, both), zero2 = p2(-0.f, -0.f);
@@ -862,7 +874,8 @@ struct Kernel {
                                                          : p2(__uint_as_float(e4.z), __uint_as_float(e4.w));
                     unsigned long long by = ks2;
                     if constexpr (any) {
-                      by = u == 0 ? p2(__uint_as_float(x4.x), __uint_as_float(x4.y)) : p2(__uint_as_float(x4.z), __uint_as_float(x4.w));
+                      by = u == 0 ? p2(__uint_as_float(x4.x), __uint_as_float(x4.y))
+                                  : p2(__uint_as_float(x4.z), __uint_as_float(x4.w));
                       if constexpr (I8) by = fma2(ks2, by, zero2);
                     }
                     float t0, t1;

@@ -549,6 +549,39 @@ def test_weigh_is_deterministic_in_graphs_and_on_streams(spl, rows):
     assert bool((ws[:65536] == 255).all())
 
 
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("scale", [None, 0.0, -0.25, 3.0], ids=str)
+@pytest.mark.parametrize("heads", [(8, 2, 128), (7, 1, 64)], ids=str)
+@KERNELS
+def test_weigh_rows_of_any_size(spl, kernel, heads, scale, fmt):
+    """Rows that differ by powers of two, by far, or are zero: each keeps its own precision."""
+    c = kernel(Case(spl, [(200, 600), (40, 40), (33, 500)], heads, fmt, 32, seed=8))
+    c.fill()
+    g = np.random.default_rng(9)
+    for b, sizes in enumerate(([0, -1, -6, -12, -13, -40], [0], [-200, -2])):
+        rows = slice(c.start[b], c.start[b + 1])
+        c.q[rows] = np.ldexp(c.q[rows], g.choice(sizes, size=c.q[rows].shape[:2])[..., None])
+        c.q[rows][g.random(c.q[rows].shape[:2]) < 0.05] = 0.0
+    check_weights(c, scale=scale, decay=0.5)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), 3e38], ids=str)
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@KERNELS
+def test_weigh_rows_of_other_sequences(spl, kernel, fmt, value):
+    """What the rows next to a sequence's are does not reach it, to the bit."""
+    c = kernel(Case(spl, [(100, 700), (150, 300), (40, 900)], (4, 2, 64), fmt, 32, seed=10))
+    c.fill()
+    want = [score_of(c, check_weights(c), b) for b in (0, 2)]
+    q = torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV)
+    q[c.start[1]:c.start[2]] = value
+    score = scores_for(c, 0.75)
+    spl.spl_kv_weigh(score, q, c.cache, c.batch(), c.hq)
+    for b, was in zip((0, 2), want):
+        assert np.array_equal(score_of(c, score, b), was)
+    assert spl.spl_get_device_status() == spl.SPL_OK
+
+
 # Few heads and many rows: the rows of a key are shared out, and the last of their parts to end adds all up.  Tolerance: a sum's
 # additions, one a part and half more, are no more than its rows.
 PARTS = {"one": [(1500, 1600)], "itself": [(700, 700)], "past": [(600, 3000)],
