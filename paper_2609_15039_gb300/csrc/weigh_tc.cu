@@ -221,11 +221,13 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
 // ---------------------------------------------------------------- the passes
 template <int D, bool I8>
 struct Layout {
-  static constexpr int PANELS = D / 64, STAGES = D == 64 ? (I8 ? 4 : 6) : (I8 ? 2 : 3);
+  static constexpr int PANELS = D / 64, STAGES = D == 64 ? 4 : (I8 ? 2 : 3);
   // key tiles whose marks or scales have a place: the loader is at most STAGES ahead of the issuer, which is at most kS ahead of
   // the epilogue
   static constexpr int NOTES = D == 64 ? 16 : 8;
   static_assert(NOTES > STAGES + kS, "and one that is being written");
+  // A tile's products are done, and its stage free, when its scores are there: the next on that place is not before it is used again.
+  static_assert(STAGES <= kS, "one phase to wait for");
   static constexpr uint32_t PANEL = 128 * 128, TILE = PANELS * PANEL;
   static constexpr uint32_t Q = 0, K = kQStages * 2 * TILE;  // stages of [q_hi, q_lo]; of K
   // second pass: the rows' scales and lse of each stage of q; int8: the keys' scales; first pass: marks of keys without a page
@@ -233,7 +235,7 @@ struct Layout {
   static constexpr uint32_t GONE = SCALE + (I8 ? NOTES * kTile * 4 : 0);
   static constexpr uint32_t ONE = GONE + NOTES * 16, BARS = ONE + 16;
   enum { kQFull = 0, kQEmpty = 2, kSFull = 4, kSFree = 8, kPieceFull = 12, kPieceFree = 16, kColFull = 20, kColEmpty = 22,
-         kFirst = 24, kSecond = 25, kDrain = 26, kKFull = 27, kKEmpty = kKFull + STAGES, kBars = (kKEmpty + STAGES + 1) / 2 * 2 };
+         kFirst = 24, kSecond = 25, kDrain = 26, kKFull = 27, kBars = (kKFull + STAGES + 1) / 2 * 2 };
   static constexpr uint32_t PIECES = BARS + 8 * kBars, MISC = PIECES + kPieces * sizeof(Piece);
   // int8, second pass: the slots and old scores of the threads' keys, [group][2][key tile][key]
   static constexpr uint32_t STASH = MISC + 16, SMEM = STASH + (I8 ? 2 * 2 * kMostTiles * kTile * 4 : 0);
@@ -291,6 +293,11 @@ struct Kernel {
   __device__ uint32_t bar(int i) const { return smem + L::BARS + 8u * i; }
   __device__ bool wait(int i, uint32_t parity, unsigned long long ns = kWaitNs) const {
     return __all_sync(0xffffffffu, mbar_wait_soon(bar(i), parity, ns, abort));
+  }
+  // Whether the stage of key tile `key` may be written, whose last was the one STAGES before.
+  __device__ bool stage_free(int key, unsigned long long ns = kWaitNs) const {
+    const int last = key - L::STAGES;
+    return last < 0 || wait(L::kSFull + last % kS, (uint32_t)(last / kS) & 1u, ns);
   }
   __device__ void arrive(int i) const {  // one for the warp, after all its lanes' work
     __syncwarp();
@@ -458,7 +465,7 @@ struct Kernel {
         for (int kt = y.k0; ok && kt < y.k1; ++kt) {
           const int64_t next = look_up(kt + 1);
           const int stage = keys % L::STAGES;
-          if (keys >= L::STAGES) ok = wait(L::kKEmpty + stage, (uint32_t)(keys / L::STAGES - 1) & 1u, kLoaderNs);
+          ok = stage_free(keys, kLoaderNs);
           if (!ok) break;
           const unsigned gone = __ballot_sync(0xffffffffu, slot == kGone);
           if (lane < 4) {  // a bit a key
@@ -551,7 +558,7 @@ struct Kernel {
     auto finish = [&]() {
       if (held < 0) return true;
       const int stage = held % L::STAGES;
-      if (held >= L::STAGES && !wait(L::kKEmpty + stage, (uint32_t)(held / L::STAGES - 1) & 1u)) return false;
+      if (!stage_free(held)) return false;
       const uint32_t panel = smem + L::K + (uint32_t)stage * L::TILE + (uint32_t)(part >> 2) * L::PANEL;
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
@@ -629,7 +636,6 @@ struct Kernel {
             mma_ss(d, SUM ? ki : qi, SUM ? qi : ki, kSdescHi128, L::IDESC, i > 0 ? 1u : 0u, leader);
           }
           if (leader) {
-            mma_commit(bar(L::kKEmpty + stage));
             mbar_arrive(bar(L::kSFull + place));
             mma_commit(bar(L::kSFull + place));
           }
@@ -956,7 +962,6 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
     auto init = [&](int i, int count) { mbar_init(smem + L::BARS + 8u * i, count); };
     for (int s = 0; s < L::STAGES; ++s) {
       init(L::kKFull + s, I8 ? 4 : 1);
-      init(L::kKEmpty + s, 1);
     }
     for (int s = 0; s < kQStages; ++s) {
       init(L::kQFull + s, 1);
