@@ -15,16 +15,18 @@
 //   warps 4-11   two groups: maxima and totals (the key tiles in turn), or sums (half of a tile's rows each).
 //   warps 12-19  int8: two groups widen the key tiles to binary16 in turn.
 // Tensor memory: four places of S.
-// Measured with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 229 and 236 us, 19 us before them and 7
-// between; int8 307 and 303.  Without the epilogues' arithmetic 211 to 227, with two instructions of a tile's 16 207 to 222, without both
-// 175: the key tiles' way here, of which three fit beside two tiles of q, is the longest of three that are nearly alike.  So the
-// epilogues pay for what they execute and read: both have code of their own for tiles of which all is seen, and in the second,
-// where a column's scale and lse go to every thread (4 wavefronts for 16 bytes), q's exponents are in steps so that a tile mostly
-// has one scale (15 sequences of 32 rows int8, second pass 54 -> 43 us).  These in all, over 600 to 6000 keys: 92 us, of which 10
-// to 13 a pass are a launch, the dependent loads of the first piece and the first tile.
+// Measured with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 222 and 232 us, 19 us before them and 7
+// between; int8 303 and 303.  What sets the pace is the issuing warp: a tile's 16 products are 1024 clocks of the tensor pipe (0.71
+// and 0.68 of the time), but of its 1320 it spends 680 in handing them over, 200 in a commit and an arrival, 150 in asking for the
+// operands and the place, the rest between tiles, and the pipe runs dry.  So it asks at once and commits once: a key tile's stage is
+// free when its scores are there.  The epilogues come next: without the products, 207 and 222 us.  They pay for what they execute
+// and read, so tiles of which all is seen have code of their own, and in the second pass, where a column's scale and lse go to
+// every thread (4 wavefronts for 16 bytes), q's exponents are in steps, for a tile mostly to have one scale (15 sequences of 32
+// rows int8, second pass 54 -> 43 us).  These in all, over 600 to 6000 keys: 92 us, of which 10 to 13 a pass are a launch, the
+// dependent loads of the first piece and the first tile.
 // A piece of the second pass has all rows of its keys, unless heads and key tiles are too few for all SMs: then it has one of
-// several parts of them, and the last to end adds the parts' sums up: 2048 rows of 14 heads on 2 of 64 dims over 12049 keys 354 ->
-// 251 us (now 216); 2048 rows of 32 heads on 8 over themselves 142 -> 126 (now 122).
+// several parts of them, and the last to end adds the parts' sums up: 2048 rows of 14 heads on 2 of 64 dims over 12049 keys
+// 354 -> 251 us (now 210); 2048 rows of 32 heads on 8 over themselves 142 -> 126 (now 118).
 // Every wait is bounded; on expiry the status word is raised and the block leaves with its
 // copies and MMAs done.
 
@@ -226,7 +228,8 @@ struct Layout {
   // the epilogue
   static constexpr int NOTES = D == 64 ? 16 : 8;
   static_assert(NOTES > STAGES + kS, "and one that is being written");
-  // A tile's products are done, and its stage free, when its scores are there: the next on that place is not before it is used again.
+  // A tile's products are done, and its stage free, when its scores are there; their place's next phase is not before the stage is
+  // used again.
   static_assert(STAGES <= kS, "one phase to wait for");
   static constexpr uint32_t PANEL = 128 * 128, TILE = PANELS * PANEL;
   static constexpr uint32_t Q = 0, K = kQStages * 2 * TILE;  // stages of [q_hi, q_lo]; of K
