@@ -392,10 +392,12 @@ spl_status launch_scores(const WeighArgs& w, int blocks, cudaStream_t stream) {
 }
 
 // Few rows: of a key head at most so many, by max_rows, and scores that take no more than kMostScores bytes.  Measured, few and
-// many rows, us, 15 sequences over 600 to 6000 keys, 32 query heads on 8: int8, 32 rows of a key head 82, 114, 48 rows 122, 114;
-// binary16, 16 rows 55, 91, 32 rows 93, 91; one sequence over 6000, int8, 32 rows 38, 41, 64 rows 61, 42.
+// many rows, us.  15 sequences over 600 to 6000 keys, 32 query heads on 8: int8, 16 rows of a key head 52, 91, 24 rows 72, 92, 32
+// rows 90, 90; binary16, 8 rows 41, 76, 16 rows 62, 76, 24 rows 91, 77.  64 sequences over 1600 to 16000, 24 on 8: int8, 12 rows
+// 327, 611, 18 rows 477, 612; binary16, 6 rows 252, 470, 12 rows 486, 471, 18 rows 716, 472.  Two sequences over up to 6000: int8,
+// 24 rows 40, 40; binary16, 8 rows 25, 30, 16 rows 32, 31.
 constexpr int64_t kMostScores = int64_t(1) << 31;
-constexpr int64_t few_rows(bool i8) { return i8 ? 32 : 24; }
+constexpr int64_t few_rows(bool i8) { return i8 ? 24 : 12; }
 struct Shape {
   bool few;
   int64_t cap;
