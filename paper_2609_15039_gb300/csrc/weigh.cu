@@ -241,7 +241,9 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_scores_kernel(const __grid_
       for (int c = 0; c < 8; ++c) sum += exp2_approx(s[c] - base);
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      if (!mine) continue;
+      // (A tile whose rows see nothing has a unit all the same, which may lie behind the row's places; nobody reads what no row
+      // sees.)
+      if (!mine || j0 >= x.key_hi) continue;
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         *reinterpret_cast<float2*>(s_row + j0 + 8 * c + 2 * t) = make_float2(s[2 * c], s[2 * c + 1]);

@@ -1,0 +1,71 @@
+"""Attention weights at the edges of their contract: lengths past the page table."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving
+from test_gpu_serving import DEV, U, Case, i32
+from test_gpu_serving_trees import KERNELS, score_of, scores_for, weight_tolerance
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def spl():
+    from paper_2609_15039_gb300 import spl as binding
+    assert torch.cuda.is_available(), "GPU tests need CUDA"
+    binding.lib()
+    return binding
+
+
+def queries(c):
+    return torch.as_tensor(c.q.reshape(c.rows, -1)).to(DEV)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("page", [64, 256])
+@pytest.mark.parametrize("over", [0, 2])
+@pytest.mark.parametrize("past", [50, 700])
+@pytest.mark.parametrize("window", [0, 1, 100])
+@KERNELS
+def test_weigh_lengths_past_a_table_of_whole_tiles(spl, kernel, window, past, over, page, fmt):
+    """A length past the table whose room is a whole number of tiles of keys: its rows see what is there, or nothing; the other
+    sequences' scores keep their bits, and nothing is written behind the workspace."""
+    room = 512
+    c = kernel(Case(spl, [(3, room), (2, 300), (3, room)], (4, 2, 64), fmt, page, seed=past))
+    c.table = np.ascontiguousarray(c.table[:, :room // page])
+    c.fill()
+    batch, q = c.batch(), queries(c)
+    size = spl.spl_kv_weigh_workspace_bytes(c.cache, batch, c.hq)
+    memory = torch.full((size + 65536,), 0xa5, dtype=torch.uint8, device=DEV)
+
+    def weigh(lens):
+        batch.kv_len.copy_(i32(lens))
+        score = scores_for(c, 0.75)
+        spl.spl_kv_weigh(score, q, c.cache, batch, c.hq, window=window, workspace=memory[:size])
+        torch.cuda.synchronize()
+        assert bool((memory[size:] == 0xa5).all())
+        return score
+
+    lens = [n for _, n in c.seqs]
+    clean = weigh(lens)
+    assert spl.spl_get_device_status() == spl.SPL_OK
+    lens[over] = room + past
+    score = weigh(lens)
+    assert spl.spl_get_device_status() == spl.SPL_EINVAL
+    for b in {0, 1, 2} - {over}:
+        assert np.array_equal(score_of(c, score, b), score_of(c, clean, b))
+    rows, k = c.q[c.start[over]:c.start[over + 1]], c.stored("k", over)
+    added = np.zeros((c.hk, room))
+    for i in range(3):
+        lo, hi = serving.visible(room + past - 3 + i, room, window)
+        if lo < hi:
+            added[:, lo:hi] += serving.weights(rows[i:i + 1], k[lo:hi], hi - lo, 2, 0.125)
+    err = np.abs(score_of(c, score, over) - (0.75 + added))  # (all of them are before the rows)
+    assert np.all(err <= weight_tolerance(rows, k, 0.125, 2, 6) * added + 2 * U * (0.75 + added))
+    used = np.zeros(tuple(score.shape), dtype=bool)
+    for b, (_, n) in enumerate(c.seqs):
+        j = np.arange(n)
+        used[c.table[b, j // page], :, j % page] = True
+    assert np.all(score.cpu().numpy()[~used] == 0.75)
