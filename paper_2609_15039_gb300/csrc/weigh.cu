@@ -356,11 +356,14 @@ __global__ void __launch_bounds__(kSumThreads, 6) weigh_sum_kernel(const __grid_
           const Row q = rows_of[r];
           if (key + 3 < q.lo || key >= q.hi) continue;
           const float4 v = *reinterpret_cast<const float4*>(scores_of[r] + key);
-          float p[4] = {exp2_approx(v.x - q.m), exp2_approx(v.y - q.m), exp2_approx(v.z - q.m), exp2_approx(v.w - q.m)};
-          if (key < q.lo || key + 3 >= q.hi) {  // (where the row does not see a key anything may be there)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (key + i < q.lo || key + i >= q.hi) p[i] = 0.f;
+          const float p[4] = {exp2_approx(v.x - q.m), exp2_approx(v.y - q.m), exp2_approx(v.z - q.m), exp2_approx(v.w - q.m)};
+          if (key < q.lo || key + 3 >= q.hi) {
+            // Where the row does not see a key anything may be there, and its total may be NaN: what is added is chosen, not p.
+            if (key >= q.lo) sum.x = fmaf(p[0], q.inverse, sum.x);
+            if (key + 1 >= q.lo && key + 1 < q.hi) sum.y = fmaf(p[1], q.inverse, sum.y);
+            if (key + 2 >= q.lo && key + 2 < q.hi) sum.z = fmaf(p[2], q.inverse, sum.z);
+            if (key + 3 < q.hi) sum.w = fmaf(p[3], q.inverse, sum.w);
+            continue;
           }
           sum.x = fmaf(p[0], q.inverse, sum.x);
           sum.y = fmaf(p[1], q.inverse, sum.y);

@@ -1,4 +1,4 @@
-"""Attention weights at the edges of their contract: lengths past the page table."""
+"""Attention weights at the edges of their contract: lengths past the page table, rows that are not finite."""
 
 import numpy as np
 import pytest
@@ -69,3 +69,40 @@ def test_weigh_lengths_past_a_table_of_whole_tiles(spl, kernel, window, past, ov
         j = np.arange(n)
         used[c.table[b, j // page], :, j % page] = True
     assert np.all(score.cpu().numpy()[~used] == 0.75)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")], ids=str)
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("length", [200, 201, 202, 203])
+@pytest.mark.parametrize("window", [1, 2, 63, 64])
+@KERNELS
+def test_weigh_a_nan_row_leaves_what_is_before_its_window(spl, kernel, window, length, fmt, value):
+    c = kernel(Case(spl, [(1, length)], (4, 2, 64), fmt, 16, seed=window))
+    c.fill()
+    c.q[0, 2, 3] = value
+    score = scores_for(c, 0.75)
+    spl.spl_kv_weigh(score, queries(c), c.cache, c.batch(), c.hq, window=window)
+    got = score_of(c, score, 0)
+    assert np.all(got[:, :length - window] == 0.75)
+    assert np.isfinite(got[0]).all() and np.isnan(got[1, length - window:]).all()
+    assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")], ids=str)
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("context", [100, 101, 102, 103])
+@KERNELS
+def test_weigh_a_nan_row_leaves_what_is_behind_it(spl, kernel, context, fmt, value):
+    """The tokens that only later rows see, in the same four keys or not, get their weights."""
+    c = kernel(Case(spl, [(9, context + 9)], (4, 2, 64), fmt, 16, seed=context))
+    c.fill()
+    c.q[1, 2, 3] = value
+    score = scores_for(c, 0.75)
+    spl.spl_kv_weigh(score, queries(c), c.cache, c.batch(), c.hq)
+    got = score_of(c, score, 0)
+    assert np.isfinite(got[0]).all() and np.isnan(got[1, :context + 2]).all()
+    k = c.stored("k", 0)
+    added = serving.weights(c.q[2:], k, context + 9, 2, 0.125)[1, context + 2:]
+    err = np.abs(got[1, context + 2:] - added)  # (new tokens: they start from 0)
+    assert np.all(err <= weight_tolerance(c.q[2:], k, 0.125, 2, 18) * added + 2 * U * added)
+    assert spl.spl_get_device_status() == spl.SPL_OK
