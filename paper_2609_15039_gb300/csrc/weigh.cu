@@ -213,12 +213,16 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_scores_kernel(const __grid_
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        s[2 * c] = (acc[c][0] + acc[c][2]) * row_scale;
-        s[2 * c + 1] = (acc[c][1] + acc[c][3]) * row_scale;
+        // An infinity of a key, which both halves of q may make one of the same sign, is a NaN of the score: x - x is NaN there,
+        // and 0 else.  (Finite ones are at most 2^39.)
+        const float a0 = acc[c][0] + acc[c][2], a1 = acc[c][1] + acc[c][3];
         if constexpr (I8) {
           const float2 sc = *reinterpret_cast<const float2*>(at + F::SCALE + 4 * (k0 + 8 * c + 2 * t));
-          s[2 * c] *= sc.x;
-          s[2 * c + 1] *= sc.y;
+          s[2 * c] = fmaf(a0 * row_scale, sc.x, sc.x - sc.x);
+          s[2 * c + 1] = fmaf(a1 * row_scale, sc.y, sc.y - sc.y);
+        } else {
+          s[2 * c] = fmaf(a0, row_scale, a0 - a0);
+          s[2 * c + 1] = fmaf(a1, row_scale, a1 - a1);
         }
       }
       __syncwarp();  // every lane has read the stage

@@ -12,6 +12,7 @@
 //   warp 0       MMA issuer.
 //   warp 1       hands out the block's pieces of work and loads tiles of q and (binary16) of K, by TMA, a box a page.
 //   warp 2       second pass: the rows' scales and lse.
+//   warp 3       first pass, binary16: looks for keys that are not finite.
 //   warps 4-11   two groups: maxima and totals (the key tiles in turn), or sums (half of a tile's rows each).
 //   warps 12-19  int8: two groups widen the key tiles to binary16 in turn.
 // Tensor memory: four places of S.
@@ -65,7 +66,7 @@ struct WeighPlan {
 struct TcArgs {
   WeighCall w;
   uint16_t *q_hi, *q_lo;  // [heads][total][dim], total = rows group
-  float2* rows;           // [heads][total]: scale, negative if the row may not be finite; lse
+  float2* rows;           // [heads][total]: scale, NaN of a row that is not finite; lse, before it NaN if a key that it sees is not
   float2* parts;          // [heads][total][splits][2]: maximum, total
   int splits;             // places of a row
   // rows in parts: a piece's sums, [item][group][its key tile][key], and behind each range's first how many are there, [warp]
@@ -196,8 +197,8 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
     const bool there = i < all;
     const int64_t token = there ? i / w.q_heads : 0;
     const int head = there ? (int)(i % w.q_heads) : 0;
-    const float4 v = there ? __ldcs(reinterpret_cast<const float4*>(w.q + token * w.ldq + (int64_t)head * D) + at)
-                           : make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 v = there ? __ldcs(reinterpret_cast<const float4*>(w.q + token * w.ldq + (int64_t)head * D) + at)
+                     : make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = fabsf(v.x) + fabsf(v.y) + (fabsf(v.z) + fabsf(v.w));
     float top = fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
 #pragma unroll
@@ -205,6 +206,9 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       sum += __shfl_xor_sync(0xffffffffu, sum, o);
     }
+    // A row that is not finite is zeros in the products, which then are finite wherever the key is, and NaN by its scale.
+    const bool finite = top <= FLT_MAX && sum == sum;
+    if (!finite) v = make_float4(0.f, 0.f, 0.f, 0.f), top = 0.f;
     // (in steps of 12, so that rows of like size have the same and the second pass one scale for a tile; the largest is then in
     // [2^3, 2^15), where the low half's smallest step, 2^-24, is still far below 2^-22 of it)
     const int e = top > 0.f ? (fp16_row_exponent(top) - 8 + 132) / 12 * 12 - 132 + 8 : 8;
@@ -216,7 +220,7 @@ __global__ void __launch_bounds__(kPrepThreads) weigh_prepare_kernel(const __gri
     const int64_t row = (int64_t)(head / w.group) * a.total + token * w.group + head % w.group;
     reinterpret_cast<uint2*>(a.q_hi + row * D)[at] = make_uint2(h0, h1);
     reinterpret_cast<uint2*>(a.q_lo + row * D)[at] = make_uint2(l0, l1);
-    if (at == 0) a.rows[row].x = copysignf(w.scale_log2 * pow2f(-e), sum <= FLT_MAX ? 1.f : -1.f);
+    if (at == 0) a.rows[row] = make_float2(finite ? fabsf(w.scale_log2) * pow2f(-e) : NAN, 0.f);
   }
 }
 
@@ -502,7 +506,7 @@ struct Kernel {
     }
   }
   // Warp 2, second pass: scales and -lse of a tile's rows, of rows that are not there an lse that leaves nothing; and the scale,
-  // if all have the same and nothing else in the products is not finite, else -1.
+  // if all have the same, else -1.
   __device__ void columns() const {
     const int lane = threadIdx.x & 31;
     const bool ok = walk(
@@ -511,20 +515,14 @@ struct Kernel {
           const int q = tile % kQStages;
           if (tile >= kQStages && !wait(L::kColEmpty + q, (uint32_t)(tile / kQStages - 1) & 1u)) return false;
           const float2* rows = a.rows + (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0;
-          const float one = fabsf(rows[0].x);
-          const int64_t left = a.total * a.w.cache.heads - (rows - a.rows);
+          const float one = rows[0].x;
           float2 v[4];
           bool fast = true;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {  // (rows behind the tile's own are in its products all the same)
-            v[i] = 4 * lane + i < left ? rows[4 * lane + i] : make_float2(0.f, INFINITY);
-            if (4 * lane + i < y.rows) {
-              v[i].x = fabsf(v[i].x);
-              fast = fast && v[i].x == one;
-            } else {
-              fast = fast && __float_as_int(v[i].x) >= 0;
-              v[i] = make_float2(0.f, INFINITY);
-            }
+          for (int i = 0; i < 4; ++i) {  // (rows behind the tile's own are in its products all the same, finite ones)
+            const bool there = 4 * lane + i < y.rows;
+            v[i] = there ? rows[4 * lane + i] : make_float2(0.f, INFINITY);
+            fast = fast && (!there || v[i].x == one);
           }
           const uint32_t to = smem + L::COL + 1024u * q + 16u * lane;
           st_shared16(to, make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[1].x), __float_as_uint(v[2].x),
@@ -598,6 +596,7 @@ struct Kernel {
             q[k] = slot >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + (int64_t)slot * D) + part) : make_uint4(0u, 0u, 0u, 0u);
           }
           scale = own >= 0 ? __ldg(a.w.cache.k_scale + own) : 0.f;
+          scale += scale - scale;  // an infinite one is NaN: its scores might be -inf, which is no weight
           gone = __ballot_sync(0xffffffffu, own == kGone);
           held = key;
           return true;
@@ -653,6 +652,42 @@ struct Kernel {
     if (!ok && leader) give_up();
     commit(L::kDrain);  // every MMA done before tensor and shared memory are given back
     mbar_wait(bar(L::kDrain), 0u, kDrainNs, nullptr);
+  }
+
+  // Warp 3, first pass, binary16: an infinity of a key may be one of the same sign in both halves' products, and a score of -inf
+  // would be a weight of 0, not NaN.  But then all rows' scores of the key are infinities or NaN (others are at most 2^39), so one
+  // warp's 32 rows are enough, and a sum of each.  Of tiles of which the rows see all; the others' are looked at one by one above
+  // their masks.  (Done by the epilogue's warps, for all keys or a quarter each: 486 to 490 us instead of 478 for the 2048 rows.)
+  __device__ void infinities() const {
+    const int lane = threadIdx.x & 31;
+    const bool ok = walk(
+        nothing, nothing,
+        [&](const Piece& x, const Span& y, int kt, int key, int) {
+          const int place = key % kS, j0 = kt * kTile;
+          if (!wait(L::kSFull + place, (uint32_t)(key / kS) & 1u)) return false;
+          tc_fence_after();
+          const uint4 gone = ld_shared16(smem + L::GONE + 16u * (key % L::NOTES));
+          const bool edge = j0 < y.all_lo || j0 + kTile > y.all_hi || (gone.x | gone.y | gone.z | gone.w) != 0;
+          unsigned long long sum[2] = {p2(0.f, 0.f), p2(0.f, 0.f)};
+          if (!edge) {
+            over_chunks(tmem + (96u << 16) + 128u * place, [&](int, uint32_t (&r)[32]) {
+#pragma unroll
+              for (int k = 0; k < 32; k += 2)
+                sum[k / 2 & 1] = add2(sum[k / 2 & 1], p2(__uint_as_float(r[k]), __uint_as_float(r[k + 1])));
+            });
+          }
+          tc_fence_before();
+          arrive(L::kSFree + place);
+          float s0, s1;
+          up2(add2(sum[0], sum[1]), s0, s1);
+          if (__any_sync(0xffffffffu, !(fabsf(s0 + s1) <= FLT_MAX))) {
+            float2* rows = a.rows + (int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0;
+            for (int i = lane; i < y.rows; i += 32) rows[i].y = NAN;
+          }
+          return true;
+        },
+        nothing, nothing);
+    if (!ok && lane == 0) give_up();
   }
 
   // ---------------------------------------------------------------- epilogue
@@ -742,8 +777,8 @@ struct Kernel {
           [&](const Piece& x, const Span& y, int) {
             m = -INFINITY, l = 0.f, scale = FLT_MIN, lo = hi = 0;
             if (own < y.rows) {
-              // (not 0, by which -inf would not stay)
-              scale = fmaxf(fabsf(a.rows[(int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0 + own].x), FLT_MIN);
+              scale = a.rows[(int64_t)x.h * a.total + (int64_t)x.row0 * a.w.group + y.r0 + own].x;
+              if (scale < FLT_MIN) scale = FLT_MIN;  // (not 0, by which -inf would not stay)
               row_keys({x.row0, x.n, x.len, x.pos0}, a.w.window, (y.r0 + own) / a.w.group, lo, hi);
             }
             return true;
@@ -770,8 +805,10 @@ struct Kernel {
                 const uint32_t g = c == 0 ? gone.x : (c == 1 ? gone.y : (c == 2 ? gone.z : gone.w));
                 const int from = lo - j0 - 32 * c, to = hi - j0 - 32 * c;
 #pragma unroll
-                for (int k = 0; k < 32; ++k)
+                for (int k = 0; k < 32; ++k) {  // (-inf: see infinities())
+                  if (!I8 && r[k] == 0xff800000u) r[k] = 0x7fc00000u;
                   if (k < from || k >= to || (g >> k & 1u)) r[k] = 0xff800000u;
+                }
               }
               float top[2] = {__uint_as_float(r[0]), __uint_as_float(r[1])};
 #pragma unroll
@@ -974,10 +1011,10 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
     }
     for (int s = 0; s < kS; ++s) {
       init(L::kSFull + s, 2);  // the products, and the issuer for what it has seen of the key tile's notes
-      init(L::kSFree + s, SUM ? kEpilogue : kEpilogue / 2);
+      init(L::kSFree + s, SUM ? kEpilogue : kEpilogue / 2 + (I8 ? 0 : 1));
     }
-    // issuer, loader, epilogue and, where they work, warp 2 and the widening warps
-    const int readers = 2 + kEpilogue + (SUM ? 1 : 0) + (I8 ? 8 : 0);
+    // issuer, loader, epilogue and, where they work, warp 2 or 3 and the widening warps
+    const int readers = 2 + kEpilogue + (SUM || !I8 ? 1 : 0) + (I8 ? 8 : 0);
     for (int s = 0; s < kPieces; ++s) {
       init(L::kPieceFull + s, 1);
       init(L::kPieceFree + s, readers);
@@ -1004,6 +1041,7 @@ weigh_tc_kernel(const __grid_constant__ TcArgs a, const __grid_constant__ CUtens
     if (warp == 0) k.issuer();
     else if (warp == 1) k.loader();
     else if (SUM && warp == 2) k.columns();
+    else if (!SUM && !I8 && warp == 3) k.infinities();
   } else if (warp < 4 + kEpilogue) {
     if constexpr (I8) asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
     k.epilogue();
@@ -1047,7 +1085,7 @@ __global__ void __launch_bounds__(kJoinThreads) weigh_join_rows_kernel(const __g
   const int keys = a.plan->range * kTile, end = lo < hi ? (hi - 1) / keys : -1;
   pdl_wait();
   if (row >= all) return;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = a.rows[row].y;
   const float4* parts = reinterpret_cast<const float4*>(a.parts) + row * a.splits;
   for (int split = lo / keys; split <= end; split += 8) {
     float4 v[8];

@@ -1,4 +1,4 @@
-"""Attention weights at the edges of their contract: lengths past the page table, rows that are not finite."""
+"""Attention weights at the edges of their contract: lengths past the page table, rows and keys that are not finite."""
 
 import numpy as np
 import pytest
@@ -105,4 +105,67 @@ def test_weigh_a_nan_row_leaves_what_is_behind_it(spl, kernel, context, fmt, val
     added = serving.weights(c.q[2:], k, context + 9, 2, 0.125)[1, context + 2:]
     err = np.abs(got[1, context + 2:] - added)  # (new tokens: they start from 0)
     assert np.all(err <= weight_tolerance(c.q[2:], k, 0.125, 2, 18) * added + 2 * U * added)
+    assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf")], ids=str)
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("at", [5, 131, 290])
+@pytest.mark.parametrize("window", [0, 40, 300])
+@KERNELS
+def test_weigh_infinite_keys(spl, kernel, window, at, fmt, value):
+    """A stored infinity (of an 8-bit vector: its scale), whichever way the halves of a query row point: the rows that see it give
+    NaN to what they see, in its head alone; those that do not are as without it, to the bit."""
+    seqs = [(1, 300 + b) for b in range(24)]
+    c = kernel(Case(spl, seqs, (4, 2, 64), fmt, 16, seed=at))
+    c.fill()
+    clean = scores_for(c, 0.75)
+    spl.spl_kv_weigh(clean, queries(c), c.cache, c.batch(), c.hq, window=window)
+    for b in range(0, len(seqs), 2):  # (every other sequence)
+        page, place = int(c.table[b, at // 16]), at % 16
+        if fmt == "f16":
+            c.cache.k[page, 1, place, b % 64] = value
+        else:
+            c.cache.k_scale[page, 1, place] = value
+    score = scores_for(c, 0.75)
+    spl.spl_kv_weigh(score, queries(c), c.cache, c.batch(), c.hq, window=window)
+    for b, (_, n) in enumerate(seqs):
+        got, was = score_of(c, score, b), score_of(c, clean, b)
+        lo = max(0, n - window) if window else 0
+        assert np.array_equal(got[0], was[0])
+        if b % 2 == 0 and at >= lo:
+            assert np.array_equal(got[1, :lo], was[1, :lo]) and np.isnan(got[1, lo:]).all()
+        else:
+            assert np.array_equal(got[1], was[1])
+    assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf")], ids=str)
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("at", [20, 400, 610])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 2, 128)], ids=str)
+@KERNELS
+def test_weigh_infinite_keys_of_many_rows(spl, kernel, heads, at, fmt, value):
+    """The rows that see the key give NaN to all that they see: without a window the last one's is everything, with one what the
+    others see stays, to the bit, and so do other sequences and heads."""
+    c = kernel(Case(spl, [(200, 700), (150, 300)], heads, fmt, 32, seed=at))
+    c.fill()
+    clean = [scores_for(c, 0.75) for _ in range(2)]
+    score = [scores_for(c, 0.75) for _ in range(2)]
+    for s, window in zip(clean, (0, 100)):
+        spl.spl_kv_weigh(s, queries(c), c.cache, c.batch(), c.hq, window=window)
+    page, place = int(c.table[0, at // 32]), at % 32
+    if fmt == "f16":
+        c.cache.k[page, 1, place, 7] = value
+    else:
+        c.cache.k_scale[page, 1, place] = value
+    for s, window in zip(score, (0, 100)):
+        spl.spl_kv_weigh(s, queries(c), c.cache, c.batch(), c.hq, window=window)
+    # rows from max(at, 500) on see it, those up to at + 99 with the window
+    first, last = max(at, 500), min(699, at + 99)
+    for s, was, lo, hi in zip(score, clean, (0, first - 99 if first <= last else 700), (700, last + 1)):
+        got, want = score_of(c, s, 0), score_of(c, was, 0)
+        assert np.array_equal(score_of(c, s, 1), score_of(c, was, 1)) and np.array_equal(got[0], want[0])
+        assert np.isnan(got[1, lo:hi]).all() and np.array_equal(got[1, :lo], want[1, :lo])
+        assert lo > hi or np.array_equal(got[1, hi:], want[1, hi:])
     assert spl.spl_get_device_status() == spl.SPL_OK
