@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 5) evict_move_ker
   const int want = a.keep - a.recent;
   const bool over = before > a.keep;  // (else all of them move, to the same positions elsewhere)
   const int* list = a.list + ((int64_t)b * a.cache.heads + h) * a.chosen;
-  auto source = [&](int i) { return !over ? i : (i < want ? __ldg(list + i) : before - a.keep + i); };
+  // (a plain load: the kernel before, beside which this one began, wrote it, and __ldg is for what nobody writes meanwhile)
+  auto source = [&](int i) { return !over ? i : (i < want ? list[i] : before - a.keep + i); };
   auto slot_of = [&](const int* table, int pos) -> int {  // (a pool has fewer than 2^31)
     const int page = __ldg(table + b * a.batch.max_pages + (pos >> a.cache.page_shift));
     if ((unsigned)page >= (unsigned)a.cache.pages) {
@@ -336,7 +337,7 @@ __device__ void move_path(const PathArgs& a, const PagedSeq& s, int b, int count
     for (int i = 0; i < kPathBatch; ++i) {
       to[i] = nullptr;
       if (i0 + i >= count) continue;
-      const int node = __ldg(path + i0 + i);
+      const int node = path[i0 + i];  // (plain loads of what the kernel before may have written beside this one's start)
       if (node <= last || node >= s.n) {  // not a path: what follows stays where it is
         atomicOr(a.batch.status, kStatusIndex);
         count = i0 + i;
@@ -345,7 +346,7 @@ __device__ void move_path(const PathArgs& a, const PagedSeq& s, int b, int count
       last = node;
       const int from = s.pos0 + node, place = s.pos0 + 1 + i0 + i;
       if (from == place || place < 0 || from >= s.len) continue;  // (rows without a place in the table)
-      const int p0 = paged_page(a.cache, a.batch, b, from), p1 = paged_page(a.cache, a.batch, b, place);
+      const int p0 = paged_page<true>(a.cache, a.batch, b, from), p1 = paged_page<true>(a.cache, a.batch, b, place);
       if (p0 < 0 || p1 < 0) continue;
       v[i] = *at(p0, from);
       to[i] = at(p1, place);
@@ -361,8 +362,8 @@ __global__ void __launch_bounds__(kPathThreads) keep_path_kernel(const PathArgs 
   constexpr int LANES = ROW / 16;
   pdl_wait();
   const int b = blockIdx.y, heads = a.cache.heads;
-  const PagedSeq s = paged_seq(a.batch, a.cache.page_shift, b);
-  int count = __ldg(a.accepted + b);
+  const PagedSeq s = paged_seq<true>(a.batch, a.cache.page_shift, b);
+  int count = a.accepted[b];
   if (count < 0 || count > a.levels) {
     atomicOr(a.batch.status, kStatusIndex);
     count = 0;

@@ -33,15 +33,23 @@ struct PagedBatch {
 struct PagedSeq {
   int row0, n, len, pos0;
 };
+// LATE: by plain loads, for a kernel that may begin before the one ahead of it has written the batch's arrays: __ldg is for
+// what nobody writes while the kernel lives, and may be moved above the wait for that one.
+template <bool LATE>
+__device__ __forceinline__ int paged_load(const int* p) {
+  if constexpr (LATE) return *p;
+  else return __ldg(p);
+}
+template <bool LATE = false>
 __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& batch, int page_shift, int b) {
   PagedSeq s;
-  const int64_t a = __ldg(batch.row_start + b), e = __ldg(batch.row_start + b + 1);
+  const int64_t a = paged_load<LATE>(batch.row_start + b), e = paged_load<LATE>(batch.row_start + b + 1);
   const int64_t row0 = a < 0 ? 0 : (a > batch.rows ? batch.rows : a);
   const int64_t end = e < row0 ? row0 : (e > batch.rows ? batch.rows : e);
   s.row0 = (int)row0;
   s.n = (int)(end - row0);
   const int64_t room = batch.max_pages << page_shift;
-  const int said = __ldg(batch.kv_len + b), len = said < 0 ? 0 : said;
+  const int said = paged_load<LATE>(batch.kv_len + b), len = said < 0 ? 0 : said;
   s.len = len > room ? (int)room : len;
   s.pos0 = len - s.n;
   if (s.len != said) atomicOr(batch.status, kStatusIndex);
@@ -49,8 +57,9 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& batch, int page_
 }
 
 // The page of position pos (inside the table) of sequence b, or -1 (and the status bit) for an id outside the pool.
+template <bool LATE = false>
 __device__ __forceinline__ int paged_page(const PagedCache& cache, const PagedBatch& batch, int b, int pos) {
-  const int page = __ldg(batch.table + b * batch.max_pages + (pos >> cache.page_shift));
+  const int page = paged_load<LATE>(batch.table + b * batch.max_pages + (pos >> cache.page_shift));
   if ((unsigned)page < (unsigned)cache.pages) return page;
   atomicOr(batch.status, kStatusIndex);
   return -1;

@@ -22,3 +22,22 @@ def test_every_drain_arrival_is_waited_for():
         assert len(re.findall(r"mma_commit(?:_pair)?\(drain_bar\)", text)) == len(
             re.findall(r"mbar_wait\(drain_bar", text)), name
     assert found == 4
+
+
+def test_what_an_overlapping_kernel_writes_is_not_read_as_read_only():
+    """A kernel that begins beside the one before it reads what that one writes by plain loads: the read-only path is for what
+    nobody writes while the kernel lives, and its loads may be moved above the wait."""
+    for name, kernels, written in (
+            ("evict.cu", ("evict_move_kernel", "keep_path_kernel", "move_path"), r"(?:a\.)?(?:list|plan|path|accepted)\b"),
+            ("weigh.cu", ("weigh_sum_kernel",), r"(?:w\.)?(?:parts|s)\b|scores_of"),
+            ("weigh_tc.cu", ("struct Kernel", "weigh_join_rows_kernel"), r"(?:a\.)?(?:rows|parts|sums|plan|first|arrived)\b"),
+            ("attention_tc.cu", ("attention_join_kernel",), r"(?:a\.)?(?:slots|divided|counters)\b")):
+        with open(os.path.join(CSRC, name)) as f:
+            text = re.sub(r"//[^\n]*", "", f.read())
+        for kernel in kernels:
+            assert kernel in text, kernel
+        assert not re.findall(r"__ldg\(\s*(?:reinterpret_cast<[^>]*>\()?\s*(?:" + written + ")", text), name
+    with open(os.path.join(CSRC, "evict.cu")) as f:
+        path = re.search(r"void move_path\(.*?\n}\n.*?void __launch_bounds__\(kPathThreads\) keep_path_kernel\(.*?\n}\n", f.read(), re.S).group(0)
+    # (it may begin beside any kernel that writes the lengths or the table)
+    assert not re.findall(r"__ldg|paged_(?:seq|page)\(", path)
