@@ -72,6 +72,7 @@ __device__ __forceinline__ uint32_t tree_keys(const uint32_t* mask, int64_t word
 __device__ __forceinline__ int tree_lo(const uint32_t* mask, int64_t words, int window, int pos0, int len) {
   if (window == INT32_MAX) return 0;
   const int first = max(0, pos0);  // the first key among the rows
+  if (pos0 >= len) return max(0, len - window);  // (a length past the table: the rows stand behind what it has)
   const int64_t some = min(words, ((int64_t)len - pos0 + 31) >> 5);
   int64_t count = 0;
   for (int64_t w = (first - (int64_t)pos0) >> 5; w < some; ++w)

@@ -1,12 +1,12 @@
-"""Attention weights at the edges of their contract: lengths past the page table, rows and keys that are not finite."""
+"""Attention weights and trees at the edges of their contracts: lengths past the page table, rows and keys that are not finite."""
 
 import numpy as np
 import pytest
 import torch
 
 from oracle import serving
-from test_gpu_serving import DEV, U, Case, i32
-from test_gpu_serving_trees import KERNELS, score_of, scores_for, weight_tolerance
+from test_gpu_serving import DEV, U, Case, i32, many, tolerance
+from test_gpu_serving_trees import KERNELS, attend_tree, masks_of, random_tree, score_of, scores_for, weight_tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -169,3 +169,28 @@ def test_weigh_infinite_keys_of_many_rows(spl, kernel, heads, at, fmt, value):
         assert np.isnan(got[1, lo:hi]).all() and np.array_equal(got[1, :lo], want[1, :lo])
         assert lo > hi or np.array_equal(got[1, hi:], want[1, hi:])
     assert spl.spl_get_device_status() == spl.SPL_OK
+
+
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("past", [0, 3, 5, 40, 400])
+@pytest.mark.parametrize("window", [1, 5, 40, 63, 64, 100])
+def test_tree_attention_windows_of_lengths_past_the_table(spl, window, past, fmt):
+    """A window takes the last keys that a row sees, which end with the table where the length does not."""
+    g = np.random.default_rng(past)
+    room = 64
+    for kernel in (lambda c: c, many):
+        c = kernel(Case(spl, [(5, room), (3, 40)], (4, 2, 64), fmt, 16, seed=window))
+        c.table = np.ascontiguousarray(c.table[:, :room // 16])
+        c.fill()
+        masks = [masks_of(random_tree(g, r)) for r, _ in c.seqs]
+        batch = c.batch()
+        c.batch = lambda all_rows=False, batch=batch: batch
+        batch.kv_len.copy_(i32([room + past, 40]))
+        got = attend_tree(c, masks, 1, window=window)
+        assert spl.spl_get_device_status() == (spl.SPL_EINVAL if past else spl.SPL_OK)
+        for b, context in enumerate((room + past - 5, 37)):
+            q, k, v = c.q[c.start[b]:c.start[b + 1]], c.stored("k", b), c.stored("v", b)
+            ref, mass = serving.tree_attention(q, k, v, masks[b], context, 2, 0.125, window)
+            tol = tolerance(q, k, 0.125, len(k), 2, mass) + 2.0 ** -32 * len(k) * np.max(np.abs(v))
+            err = np.abs(got[c.start[b]:c.start[b + 1]].astype(np.float64) - ref)
+            assert np.all(err <= tol), f"sequence {b}: worst err/tol {np.max(err / tol):.3g}"
