@@ -135,7 +135,9 @@ class CachedDecoder:
 
     def forward(self, tokens, batch, seen=None, weigh=False):
         """Logits [rows, vocab] of the batch's new tokens (int64 [rows]), which join the caches.  seen: the rows form trees,
-        with these masks; weigh: the attention weight that they give the stored tokens is added to ``scores``."""
+        with these masks; weigh: the attention weight that they give the stored tokens is added to ``scores`` (not of trees)."""
+        if weigh and seen is not None:
+            raise ValueError("forward: a tree's rows are not weighed (spl_kv_weigh has no masks)")
         if weigh and self.scores is None:
             self.scores = [torch.zeros(c.k.shape[:3], device=c.k.device) for c in self.caches]
         norm = lambda t: t * torch.rsqrt(t.square().mean(-1, keepdim=True) + 1e-6)  # noqa: E731

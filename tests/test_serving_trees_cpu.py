@@ -198,3 +198,9 @@ def test_generation_that_is_refused(monkeypatch):
                  lambda: example.generate_bounded(None, None, [[1]], 1, 4, -1)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_a_trees_rows_are_not_weighed():
+    from paper_2609_15039_gb300 import serving as example
+    with pytest.raises(ValueError, match="tree"):
+        example.CachedDecoder.forward(None, None, None, seen=1, weigh=True)
