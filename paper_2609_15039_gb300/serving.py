@@ -95,6 +95,19 @@ class Tree:
         return self.seen[:self.first[level]].repeat(seqs, 1).cuda()
 
 
+def slots(batch, cache):
+    """(page, place) of the batch's new tokens, of those that have one."""
+    ends, table = batch.row_start.long(), batch.page_table.long()
+    rows = ends[1:] - ends[:-1]
+    seq = torch.repeat_interleave(torch.arange(len(rows), device=rows.device), rows)
+    pos = torch.arange(len(seq), device=seq.device) - ends[seq] + (batch.kv_len.long() - rows)[seq]
+    there = (pos >= 0) & (pos < table.shape[1] * cache.page_size)
+    seq, pos = seq[there], pos[there]
+    page = table[seq, pos // cache.page_size]
+    there = (page >= 0) & (page < cache.pages)
+    return page[there], (pos % cache.page_size)[there]
+
+
 class CachedDecoder:
     """Decoder layers (attention and MLP, residual, RMS-normalised inputs) with one paged cache each."""
 
@@ -135,11 +148,16 @@ class CachedDecoder:
 
     def forward(self, tokens, batch, seen=None, weigh=False):
         """Logits [rows, vocab] of the batch's new tokens (int64 [rows]), which join the caches.  seen: the rows form trees,
-        with these masks; weigh: the attention weight that they give the stored tokens is added to ``scores`` (not of trees)."""
+        with these masks; weigh: the attention weight that they give the stored tokens is added to ``scores`` (not of trees).  Without it,
+        new tokens have none yet."""
         if weigh and seen is not None:
             raise ValueError("forward: a tree's rows are not weighed (spl_kv_weigh has no masks)")
         if weigh and self.scores is None:
             self.scores = [torch.zeros(c.k.shape[:3], device=c.k.device) for c in self.caches]
+        if not weigh and self.scores is not None:  # (spl_kv_weigh lets new tokens start from 0)
+            page, place = slots(batch, self.caches[0])
+            for score in self.scores:
+                score[page, :, place] = 0.0
         norm = lambda t: t * torch.rsqrt(t.square().mean(-1, keepdim=True) + 1e-6)  # noqa: E731
         x = self.embedding[tokens]
         for i, (layer, cache) in enumerate(zip(self.layers, self.caches)):

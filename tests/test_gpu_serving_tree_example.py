@@ -101,3 +101,25 @@ def test_the_command(serving, capsys, more, said):
     assert serving.main(["--sequences", "3", "--layers", "2", "--rounds", "20", "--prompt", "33", "--eps", "4"] + more) == 0
     line = capsys.readouterr().out
     assert "status SPL_OK" in line and said in line
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_tokens_that_are_not_weighed_start_from_nothing(serving, tree):
+    """What their slots' last owners gathered is not theirs: a step after them weighs them as if they had been new to the pool."""
+    got = []
+    for stale in (0.0, 1000.0):
+        target, _, pages = serving.synthetic(2, seqs=2, max_len=320)
+        target.scores = [torch.full(tuple(c.k.shape[:3]), stale, device="cuda") for c in target.caches]
+        g = np.random.default_rng(1)
+        draw = lambda n: torch.as_tensor(g.integers(0, 1024, n)).cuda()  # noqa: E731
+        target.forward(draw(193), pages.grow([63, 130]), weigh=True)
+        target.forward(draw(20), pages.grow([10, 10]), serving.Tree([1] * 9).rows(10, 2) if tree else None)
+        target.forward(draw(2), pages.grow([1, 1]), weigh=True)
+        j = torch.tensor([(int(pages.table[b, i // 64]), i % 64) for b in range(2) for i in range(pages.lens[b])]).cuda()
+        got.append([score[j[:, 0], :, j[:, 1]] for score in target.scores])
+        # every row that is weighed gives a weight of 1 a query head
+        for score in got[-1]:
+            assert abs(score.double().sum().item() - 8 * 195) < 1e-3 * 8 * 195
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    from paper_2609_15039_gb300 import spl
+    assert spl.spl_get_device_status() == spl.SPL_OK

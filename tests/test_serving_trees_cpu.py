@@ -204,3 +204,17 @@ def test_a_trees_rows_are_not_weighed():
     from paper_2609_15039_gb300 import serving as example
     with pytest.raises(ValueError, match="tree"):
         example.CachedDecoder.forward(None, None, None, seen=1, weigh=True)
+
+
+def test_the_slots_of_new_tokens():
+    """By sequences without rows, rows before the first position or past the table, and pages outside the pool."""
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2609_15039_gb300 import serving as example
+    batch = SimpleNamespace(row_start=torch.tensor([0, 3, 3, 5, 9, 11]), kv_len=torch.tensor([18, 7, 1, 34, 17]),
+                            page_table=torch.tensor([[4, 2], [0, 0], [1, 0], [3, 5], [0, 6]]))
+    page, place = example.slots(batch, SimpleNamespace(page_size=16, pages=6))
+    assert page.tolist() == [4, 2, 2] + [1] + [5, 5] + [0]
+    assert place.tolist() == [15, 0, 1] + [0] + [14, 15] + [15]
