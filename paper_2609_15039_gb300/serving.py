@@ -336,6 +336,8 @@ def main(argv=None):
     p.add_argument("--tree", type=lambda v: [int(b) for b in v.split(",")], help="children of a node, level by level")
     p.add_argument("--keep", type=int, default=0, help="tokens of a sequence that the cache is cut to (without drafts)")
     a = p.parse_args(argv)
+    if a.keep and a.tree:
+        p.error("--keep is without drafts: no --tree")
     most = Tree(a.tree).nodes if a.tree else a.drafts + 1
     room = a.prompt + most * (a.rounds + 1)
     target, draft, pages = synthetic(a.layers, seqs=a.sequences, max_len=room, eps=a.eps)

@@ -218,3 +218,14 @@ def test_the_slots_of_new_tokens():
     page, place = example.slots(batch, SimpleNamespace(page_size=16, pages=6))
     assert page.tolist() == [4, 2, 2] + [1] + [5, 5] + [0]
     assert place.tolist() == [15, 0, 1] + [0] + [14, 15] + [15]
+
+
+def test_a_bound_and_a_tree_are_not_one_command(monkeypatch, capsys):
+    from paper_2609_15039_gb300 import serving as example
+
+    def begun(*a, **k):
+        raise AssertionError("the command began")
+    monkeypatch.setattr(example, "synthetic", begun)
+    with pytest.raises(SystemExit) as end:
+        example.main(["--keep", "40", "--tree", "3,2"])
+    assert end.value.code == 2 and "--tree" in capsys.readouterr().err
