@@ -620,7 +620,8 @@ constexpr int64_t kFewUnits = 1600;
 Shape shape_of(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t q_heads) {
   const int d = (int)cache->head_dim, sms = device_sm_count();
   Shape s;
-  const int64_t tiles = ceil_div(std::max<int64_t>(batch->max_rows, 1) * (q_heads / cache->kv_heads), kRT);
+  const int64_t rows = std::min<int64_t>(std::max<int64_t>(batch->max_rows, 1), INT32_MAX);  // (it may be any number)
+  const int64_t tiles = ceil_div(rows * (q_heads / cache->kv_heads), kRT);
   const int64_t units = cache->pages == 0 ? 0 : ceil_div(batch->max_pages * cache->page_size, 64);
   const int most = cache->format == SPL_KV_I8 ? 3 : d == 64 ? 2 : 1;
   s.few = tiles <= most || (double)tiles * (double)units * (double)(batch->seqs * cache->kv_heads) <= kFewUnits;

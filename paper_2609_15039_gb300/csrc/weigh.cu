@@ -414,7 +414,7 @@ struct Shape {
 };
 Shape shape_of(const PagedCache& c, const PagedBatch& b, const spl_kv_batch* batch, int64_t q_heads, int head_dim, bool i8) {
   Shape x = {};
-  x.few = batch->max_rows * (q_heads / c.heads) <= few_rows(i8) &&
+  x.few = batch->max_rows <= few_rows(i8) / (q_heads / c.heads) &&  // (max_rows may be any number)
           (double)b.rows * (double)q_heads * (double)(b.max_pages << c.page_shift) * 4 <= (double)kMostScores;
   if (!x.few) {
     x.bytes = b.rows == 0 ? 0 : weigh_tc_bytes(c, b, q_heads, head_dim);

@@ -229,3 +229,16 @@ def test_a_bound_and_a_tree_are_not_one_command(monkeypatch, capsys):
     with pytest.raises(SystemExit) as end:
         example.main(["--keep", "40", "--tree", "3,2"])
     assert end.value.code == 2 and "--tree" in capsys.readouterr().err
+
+
+def test_a_bound_on_the_rows_that_bounds_nothing(spl, base):  # noqa: F811
+    """max_rows may be any number that is enough: the largest chooses the kernels of many rows like any other large one."""
+    L = spl.lib()
+    for group in (1, 2, 3, 1024):
+        for size in (L.spl_kv_weigh_workspace_bytes, L.spl_paged_attention_workspace_bytes):
+            for d in (64, 128):
+                # (a table wide enough for the choice of kernel to go by the rows)
+                c = ctypes.byref(cache_of(spl, base, head_dim=d, pages=1 << 16))
+                need = [size(c, ctypes.byref(batch_of(spl, base, max_rows=most, max_pages=1 << 16)), 30, 2 * group)
+                        for most in (1 << 24, 1 << 61, (1 << 63) - 1)]
+                assert need[0] > 0 and need[1:] == need[:1] * 2, (group, d, need)
