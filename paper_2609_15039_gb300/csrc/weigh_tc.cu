@@ -575,7 +575,8 @@ struct Kernel {
         st_shared16(row + (((first ^ 1) ^ (at & 7)) << 4), make_uint4(i8_pair(w2, 0x4140u), i8_pair(w2, 0x4342u),
                                                                       i8_pair(w3, 0x4140u), i8_pair(w3, 0x4342u)));
       }
-      st_shared4(smem + L::SCALE + 4u * (held % L::NOTES * kTile + i), __float_as_uint(scale));
+      // (an infinite scale is NaN: its scores might be -inf, which is no weight)
+      st_shared4(smem + L::SCALE + 4u * (held % L::NOTES * kTile + i), __float_as_uint(scale + (scale - scale)));
       if (lane == 0) st_shared4(smem + L::GONE + 16u * (held % L::NOTES) + 4u * (i >> 5), gone);
       fence_proxy_async_smem();
       arrive(L::kKFull + stage);
@@ -596,7 +597,6 @@ struct Kernel {
             q[k] = slot >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + (int64_t)slot * D) + part) : make_uint4(0u, 0u, 0u, 0u);
           }
           scale = own >= 0 ? __ldg(a.w.cache.k_scale + own) : 0.f;
-          scale += scale - scale;  // an infinite one is NaN: its scores might be -inf, which is no weight
           gone = __ballot_sync(0xffffffffu, own == kGone);
           held = key;
           return true;
