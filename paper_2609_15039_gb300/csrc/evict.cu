@@ -328,33 +328,50 @@ constexpr int kPathThreads = 256, kPathBatch = 4;
 // lies at or behind its place, so moving them in order overwrites no later one's source.
 template <class T, class At>
 __device__ void move_path(const PathArgs& a, const PagedSeq& s, int b, int count, At at) {
-  const int* path = a.path + b * a.ldpath;
+  // Plain loads, of what kernels before may have written beside this one's start; a batch's side by side.
+  const int *path = a.path + b * a.ldpath, *table = a.batch.table + b * a.batch.max_pages;
+  const int shift = a.cache.page_shift, pages = a.cache.pages;
   int last = 0;  // the node before
+  bool bad = false;
   for (int i0 = 0; i0 < count; i0 += kPathBatch) {
+    int node[kPathBatch], place[kPathBatch], from_page[kPathBatch], to_page[kPathBatch];
+#pragma unroll
+    for (int i = 0; i < kPathBatch; ++i) node[i] = i0 + i < count ? path[i0 + i] : 0;
+#pragma unroll
+    for (int i = 0; i < kPathBatch; ++i) {
+      place[i] = -1;
+      if (i0 + i >= count) continue;
+      if (node[i] <= last || node[i] >= s.n) {  // not a path: what follows stays where it is
+        bad = true;
+        count = i0 + i;
+        continue;
+      }
+      last = node[i];
+      if (node[i] != 1 + i0 + i && s.pos0 + node[i] < s.len) place[i] = s.pos0 + 1 + i0 + i;  // (or no place in the table, or -1)
+    }
+#pragma unroll
+    for (int i = 0; i < kPathBatch; ++i) {
+      from_page[i] = place[i] >= 0 ? table[(s.pos0 + node[i]) >> shift] : 0;
+      to_page[i] = place[i] >= 0 ? table[place[i] >> shift] : 0;
+    }
     T v[kPathBatch] = {};
     T* to[kPathBatch];
 #pragma unroll
     for (int i = 0; i < kPathBatch; ++i) {
       to[i] = nullptr;
-      if (i0 + i >= count) continue;
-      const int node = path[i0 + i];  // (plain loads of what the kernel before may have written beside this one's start)
-      if (node <= last || node >= s.n) {  // not a path: what follows stays where it is
-        atomicOr(a.batch.status, kStatusIndex);
-        count = i0 + i;
+      if (place[i] < 0) continue;
+      if ((unsigned)from_page[i] >= (unsigned)pages || (unsigned)to_page[i] >= (unsigned)pages) {
+        bad = true;
         continue;
       }
-      last = node;
-      const int from = s.pos0 + node, place = s.pos0 + 1 + i0 + i;
-      if (from == place || place < 0 || from >= s.len) continue;  // (rows without a place in the table)
-      const int p0 = paged_page<true>(a.cache, a.batch, b, from), p1 = paged_page<true>(a.cache, a.batch, b, place);
-      if (p0 < 0 || p1 < 0) continue;
-      v[i] = *at(p0, from);
-      to[i] = at(p1, place);
+      v[i] = *at(from_page[i], s.pos0 + node[i]);
+      to[i] = at(to_page[i], place[i]);
     }
 #pragma unroll
     for (int i = 0; i < kPathBatch; ++i)
       if (to[i]) *to[i] = v[i];
   }
+  if (bad) atomicOr(a.batch.status, kStatusIndex);
 }
 
 template <int ROW>
@@ -362,8 +379,8 @@ __global__ void __launch_bounds__(kPathThreads) keep_path_kernel(const PathArgs 
   constexpr int LANES = ROW / 16;
   pdl_wait();
   const int b = blockIdx.y, heads = a.cache.heads;
-  const PagedSeq s = paged_seq<true>(a.batch, a.cache.page_shift, b);
   int count = a.accepted[b];
+  const PagedSeq s = paged_seq<true>(a.batch, a.cache.page_shift, b);
   if (count < 0 || count > a.levels) {
     atomicOr(a.batch.status, kStatusIndex);
     count = 0;

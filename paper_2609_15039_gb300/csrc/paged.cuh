@@ -57,9 +57,8 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& batch, int page_
 }
 
 // The page of position pos (inside the table) of sequence b, or -1 (and the status bit) for an id outside the pool.
-template <bool LATE = false>
 __device__ __forceinline__ int paged_page(const PagedCache& cache, const PagedBatch& batch, int b, int pos) {
-  const int page = paged_load<LATE>(batch.table + b * batch.max_pages + (pos >> cache.page_shift));
+  const int page = __ldg(batch.table + b * batch.max_pages + (pos >> cache.page_shift));
   if ((unsigned)page < (unsigned)cache.pages) return page;
   atomicOr(batch.status, kStatusIndex);
   return -1;
