@@ -194,3 +194,25 @@ def test_tree_attention_windows_of_lengths_past_the_table(spl, window, past, fmt
             tol = tolerance(q, k, 0.125, len(k), 2, mass) + 2.0 ** -32 * len(k) * np.max(np.abs(v))
             err = np.abs(got[c.start[b]:c.start[b + 1]].astype(np.float64) - ref)
             assert np.all(err <= tol), f"sequence {b}: worst err/tol {np.max(err / tol):.3g}"
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")], ids=str)
+@pytest.mark.parametrize("fmt", ["f16", "i8"])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 2, 128)], ids=str)
+@KERNELS
+def test_weigh_a_nan_row_among_many(spl, kernel, heads, fmt, value):
+    """Over several ranges of keys and tiles of rows: what the row does not see is as without it, to the bit."""
+    c = kernel(Case(spl, [(40, 90), (300, 5000), (0, 300)], heads, fmt, 64, seed=1))
+    c.fill()
+    clean = scores_for(c, 0.75)
+    spl.spl_kv_weigh(clean, queries(c), c.cache, c.batch(), c.hq, window=700, decay=0.5)
+    c.q[40 + 100, c.hq // 2, 5] = value
+    score = scores_for(c, 0.75)
+    spl.spl_kv_weigh(score, queries(c), c.cache, c.batch(), c.hq, window=700, decay=0.5)
+    lo, hi = serving.visible(4800, 5000, 700)
+    for b in (0, 2):
+        assert np.array_equal(score_of(c, score, b), score_of(c, clean, b))
+    got, want = score_of(c, score, 1), score_of(c, clean, 1)
+    assert np.isnan(got[1, lo:hi]).all() and np.array_equal(got[0], want[0])
+    assert np.array_equal(got[1, :lo], want[1, :lo]) and np.array_equal(got[1, hi:], want[1, hi:])
+    assert spl.spl_get_device_status() == spl.SPL_OK
