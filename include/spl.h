@@ -649,7 +649,9 @@ spl_status spl_kv_read(float* K, float* V, const spl_kv_cache* cache, const spl_
  *   out = sum_j softmax_j(scale q . k_j) v_j,
  * and zeros if it sees none; rows of no sequence are left as they are.  What a
  * row does not see (stale slots, later tokens) does not reach it, NaN or not; of
- * one that sees a NaN or infinity the outputs concerned, or all, are NaN.
+ * one that sees a NaN or infinity the outputs concerned, or all, are NaN (an
+ * infinity in a stored key, which spl_kv_append writes none of, may count as a
+ * score of -inf instead, a probability of 0).
  * fp32 accuracy from the stored values: query rows and probabilities enter the
  * tensor cores as two binary16 terms (hi + lo, scaled by powers of two; a
  * probability far below its row's largest keeps an absolute 2^-33 of it, over I8
@@ -689,13 +691,18 @@ spl_status spl_tree_attention(float* out, int64_t ldo, const float* Q, int64_t l
  *   score_j <- decay score_j + sum of softmax_j(scale q . k)
  * over the batch's rows and the key head's query heads, softmax and window as in
  * spl_paged_attention.  The rows' own tokens (append them first) start from 0:
- * what their slots held does not count.  A row that sees a NaN or infinity makes
- * the scores of the keys that it sees NaN; one that sees nothing adds nothing;
+ * what their slots held does not count.  A row that is not finite, or sees a key
+ * that is not, makes the scores of the keys that it sees NaN, and of no others;
+ * one that sees nothing adds nothing;
  * slots of no token, and of pages outside the pool, are left as they are.  A page
  * holds tokens of one sequence of the batch only.  Sums are fp32, in an order that
- * does not depend on timing.  Q [rows, q_heads head_dim] as there; 0 <= decay <= 1.  Workspace:
+ * does not depend on timing.  Q [rows, q_heads head_dim] as there; 0 <= decay <= 1.
+ * The rows are a chain's: a tree's masks are not known here.  Workspace:
  * spl_kv_weigh_workspace_bytes, any contents; its first 64 KiB are not touched,
- * so the product workspace can be shared.  Errors: as spl_paged_attention,
+ * so the product workspace can be shared.  It goes by the page table's width, not
+ * by lengths: some 4 bytes a row, query head and token (256 at least; past 2 GiB
+ * the kernels of many rows take the call), or for many rows 4 bytes a value of Q
+ * and 16 a row, query head and 2048 tokens (128 at least).  Errors: as spl_paged_attention,
  * EINVAL for a decay outside [0, 1]. */
 size_t spl_kv_weigh_workspace_bytes(const spl_kv_cache* cache, const spl_kv_batch* batch, int64_t rows,
                                     int64_t q_heads);

@@ -4,8 +4,8 @@
 // keep - recent with the largest scores, the earliest of equal ones; they keep their order and go to the positions 0 ..
 // keep - 1.  Two launches.  The first chooses: the scores become whole numbers that order as they do, the smallest that
 // stays is found digit by digit (8 bits a round, a histogram in shared memory), and the positions that stay are written
-// down in order, strip after strip, by a prefix sum.  The second moves, bound by HBM: a block has some columns of K or of V
-// (32 or 128 bytes of every vector) of one head.  In place a target lies at or before its source, and a block's trips are
+// down in order, strip after strip, by a prefix sum.  The second moves, bound by HBM: a block has K's or V's vectors of one
+// head, or 32 bytes of each.  In place a target lies at or before its source, and a block's trips are
 // in the targets' order, so that it suffices that a trip's loads are done before its stores: what a trip overwrites are
 // sources of itself or of trips before it.  Into other pages there is no such order, and a head's tokens are shared out.
 //

@@ -404,7 +404,9 @@ spl_status launch_scores(const WeighArgs& w, int blocks, cudaStream_t stream) {
 // many rows, us.  15 sequences over 600 to 6000 keys, 32 query heads on 8: int8, 16 rows of a key head 52, 91, 24 rows 72, 92, 32
 // rows 90, 90; binary16, 8 rows 41, 76, 16 rows 62, 76, 24 rows 91, 77.  64 sequences over 1600 to 16000, 24 on 8: int8, 12 rows
 // 327, 611, 18 rows 477, 612; binary16, 6 rows 252, 470, 12 rows 486, 471, 18 rows 716, 472.  Two sequences over up to 6000: int8,
-// 24 rows 40, 40; binary16, 8 rows 25, 30, 16 rows 32, 31.
+// 24 rows 40, 40; binary16, 8 rows 25, 30, 16 rows 32, 31.  One limit a format, by the rows alone: what the keys and the number of
+// sequences would ask for differs from it by up to 23% (15 sequences of 16 rows binary16) on one side and 3% (64 of 12) on the other.
+// And the scores' places go by the page table's width: many sequences of a row with a wide table leave for the kernels of many.
 constexpr int64_t kMostScores = int64_t(1) << 31;
 constexpr int64_t few_rows(bool i8) { return i8 ? 24 : 12; }
 struct Shape {

@@ -16,8 +16,8 @@
 //   warps 4-11   two groups: maxima and totals (the key tiles in turn), or sums (half of a tile's rows each).
 //   warps 12-19  int8: two groups widen the key tiles to binary16 in turn.
 // Tensor memory: four places of S.
-// Measured with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 222 and 232 us, 19 us before them and 7
-// between; int8 303 and 303.  What sets the pace is the issuing warp: a tile's 16 products are 1024 clocks of the tensor pipe (0.71
+// Measured with 32 query heads on 8, 2048 rows over 12049 keys, binary16: passes of 222 to 229 and 232 to 237 us, 19 us before
+// them and 7 between; int8 303 and 303.  What sets the pace is the issuing warp: a tile's 16 products are 1024 clocks of the tensor pipe (0.71
 // and 0.68 of the time), but of its 1320 it spends 680 in handing them over, 200 in a commit and an arrival, 150 in asking for the
 // operands and the place, the rest between tiles, and the pipe runs dry.  So it asks at once and commits once: a key tile's stage is
 // free when its scores are there.  The epilogues come next: without the products, 207 and 222 us.  They pay for what they execute
@@ -49,7 +49,7 @@ constexpr int kTile = 128;          // rows and keys
 constexpr int kEpilogue = 8;        // warps
 constexpr int kThreads = 32 * (4 + kEpilogue), kThreadsI8 = kThreads + 32 * 8;
 constexpr int kQStages = 2, kS = 4;
-constexpr int kMostTiles = 8;       // key tiles of a piece of the second pass (a thread has every other one's sum)
+constexpr int kMostTiles = 8;       // key tiles of a piece of the second pass (a thread has a sum of each)
 constexpr int kMostRange = 16;      // key tiles of a piece of the first pass
 constexpr int kPieces = 4;
 constexpr int kMostChunks = 16;     // parts of the rows that a piece of the second pass may have
